@@ -226,10 +226,54 @@ pearl_status pearl_kv_unpack(const pearl_kv_shape* shape, const pearl_seq_desc* 
                              const void* buf, void* k_pool, void* v_pool, void* stream);
 
 /*
+ * KV cache in MX blocks: 4 or 8 bits an element instead of 16, so a decode step reads 3.76 or 1.94
+ * times fewer bytes (paper, section 4.3, Eq. 1: the KV-cache read is a sequence's marginal decode
+ * cost) and a GPU holds as many times more context.  32 neighbouring channels of one token and kv-head
+ * share a power-of-two scale 2^(s - 127), s one byte (255: all 32 elements are NaN); elements are E2M1 (0,
+ * 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) or E4M3 (up to 448, NaN for codes 0x7f and 0xff).
+ *   Quantisation of 32 values x: s is the least with max|x| <= 1.75 * 2^emax * 2^(s - 127) (emax = 2
+ *   for E2M1, 8 for E4M3), at least 1, and an element is x * 2^(127 - s) rounded to nearest, ties to
+ *   the even code, zeros keeping their sign; magnitudes above 6 in E2M1 become 6.  If an x is NaN or
+ *   infinite, s is 255 and the codes are 0.  A value read back is code * 2^(s - 127) in bf16, exact (values
+ *   under 2^-133 are rounded); quantising what was read back gives the same values.
+ *   cache: uint8 [num_pages][num_kv_heads][pearl_mx_block_bytes(head_dim, format)], 16-byte aligned.  A
+ *   block holds the 16 tokens of one page and kv-head, nb = head_dim / 32:
+ *     K codes, 16 rows: slot's channels in order (E2M1: two to a byte, the even channel in the low bits);
+ *     V codes, units of 16 bytes, each one pair of neighbouring channels (2i, 2i+1) of 16 (E2M1) or 8
+ *       (E4M3) tokens in order: a token's two codes side by side (one byte, or two); units ordered
+ *       (tokens 0-7 before 8-15 in E4M3, i);
+ *     K scales [slot % 4][nb][slot / 4], V scales [nb][slot].
+ *   Any bytes are valid contents of slots that no attended position owns.
+ */
+typedef enum { PEARL_MXFP4 = 4, PEARL_MXFP8 = 8 } pearl_mx_format;
+
+/* Bytes of one (page, kv-head) block; 0 for an unsupported head_dim or format. */
+size_t pearl_mx_block_bytes(int head_dim, pearl_mx_format format);
+
+/*
+ * pearl_kv_append into a cache of MX blocks: the rows k_new / v_new of the new tokens are quantised
+ * as above and written to their slots.  No other byte of the cache changes.  Rows whose page id
+ * is outside [0, num_pages) or whose logical page is beyond bt_stride are skipped.
+ *   k_new, v_new: bf16 [total_q][num_kv_heads][head_dim] (read); cache: written.
+ */
+pearl_status pearl_kv_append_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, pearl_mx_format format,
+                                const void* k_new, const void* v_new, void* cache, void* stream);
+
+/*
+ * pearl_kv_pack out of a cache of MX blocks: the token ranges' rows, read back as bf16.  The buffer
+ * can be unpacked into bf16 pools (pearl_kv_unpack), or appended to another cache of MX blocks of
+ * the same format (pearl_kv_append_mx of its two halves), which then holds the same values.
+ *   cache: read; buf: bf16 [2][total_q][num_kv_heads][head_dim], K rows, then V rows (written).
+ * Rows of a page id outside [0, num_pages) are zeros.
+ */
+pearl_status pearl_kv_pack_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, pearl_mx_format format,
+                              const void* cache, void* buf, void* stream);
+
+/*
  * Timing hook for benchmarks and profilers (not part of the computation).  While a pair is set,
  * every library call made on the calling thread records `before` on its stream immediately
  * before launching its main kernel (the attention kernel for the three attention calls, the
- * page-copy kernel for pearl_kv_append, pearl_kv_pack and pearl_kv_unpack) and `after`
+ * page-copy kernel for pearl_kv_append, pearl_kv_pack, pearl_kv_unpack and their _mx forms) and `after`
  * immediately after it.  The handles are
  * hipEvent_t values created and owned by the caller; pass NULL, NULL to clear.  The pair stays
  * set until changed, so a caller timing several calls sets a fresh pair before each one.

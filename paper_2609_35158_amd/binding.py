@@ -17,6 +17,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libpearl_attn.so")
 
 PEARL_OK = 0
+PAGE_SIZE = 16                                      # tokens per page
 _lib = None
 
 
@@ -43,7 +44,8 @@ EXPORTED = ("pearl_abi_version", "pearl_status_str", "pearl_last_error", "pearl_
             "pearl_attn_workspace_bytes", "pearl_attn_prefill_append", "pearl_attn_decode",
             "pearl_attn_mixed", "pearl_kv_pack", "pearl_kv_unpack", "pearl_set_kernel_events",
             "pearl_hbm_copy", "pearl_hbm_read", "pearl_hbm_read_nt", "pearl_hbm_fill", "pearl_attn_decode_static",
-            "pearl_attn_decode_static_max_bytes", "pearl_attn_decode_append")
+            "pearl_attn_decode_static_max_bytes", "pearl_attn_decode_append", "pearl_mx_block_bytes",
+            "pearl_kv_append_mx", "pearl_kv_pack_mx")
 
 
 def load(path: str = LIB_PATH):
@@ -89,6 +91,14 @@ def load(path: str = LIB_PATH):
                                              ctypes.c_void_p]
     lib.pearl_attn_decode_static_max_bytes.restype = ctypes.c_size_t
     lib.pearl_attn_decode_static_max_bytes.argtypes = []
+    lib.pearl_mx_block_bytes.restype = ctypes.c_size_t
+    lib.pearl_mx_block_bytes.argtypes = [ctypes.c_int, ctypes.c_int]
+    lib.pearl_kv_append_mx.restype = ctypes.c_int
+    lib.pearl_kv_append_mx.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_void_p]
+    lib.pearl_kv_pack_mx.restype = ctypes.c_int
+    lib.pearl_kv_pack_mx.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                     ctypes.c_void_p]
     lib.pearl_set_kernel_events.restype = None
     lib.pearl_set_kernel_events.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
     # measurement tooling (include/pearl_bench.h)
@@ -361,6 +371,84 @@ def mixed(q, k_pool, v_pool, block_table, ctx_lens, cu_q_lens, max_q_len, max_kv
     """Colocated prefill chunks and decodes in one attention launch (pearl_attn_mixed)."""
     return _attention("pearl_attn_mixed", q, k_pool, v_pool, block_table, ctx_lens, cu_q_lens,
                       max_q_len, max_kv_len, scale, return_lse, out, lse, workspace)
+
+
+# ------------------------------------------------------------------------------------------------
+# KV cache in MX blocks (4 or 8 bits an element)
+# ------------------------------------------------------------------------------------------------
+
+MXFP4, MXFP8 = 4, 8
+_MX_BLOCKS = {}                                     # block bytes -> (head_dim, format)
+
+
+def mx_block_bytes(head_dim: int, fmt: int) -> int:
+    """Bytes of the block of one (page, kv-head) in a cache of MX blocks (pearl_mx_block_bytes)."""
+    n = int(load().pearl_mx_block_bytes(int(head_dim), int(fmt)))
+    if n == 0:
+        raise PearlError(2, "pearl_mx_block_bytes", last_error())
+    return n
+
+
+def mx_cache(num_pages: int, num_kv_heads: int, head_dim: int, fmt: int, device="cuda") -> torch.Tensor:
+    """A cache of MX blocks, zeroed: uint8 [num_pages][num_kv_heads][mx_block_bytes(head_dim, fmt)], fmt
+    MXFP4 or MXFP8.  head_dim and format follow from the block's size, so the calls below take the
+    cache alone."""
+    return torch.zeros((num_pages, num_kv_heads, mx_block_bytes(head_dim, fmt)), dtype=torch.uint8, device=device)
+
+
+def _mx_shape(num_q_heads: Optional[int], cache: torch.Tensor) -> Tuple[KvShape, int]:
+    """Shape (num_q_heads None: as many as kv-heads, for calls that have no queries) and format."""
+    _need(cache, "cache", torch.uint8)
+    if not _MX_BLOCKS:
+        _MX_BLOCKS.update({mx_block_bytes(d, f): (d, f) for d in (64, 128) for f in (MXFP4, MXFP8)})
+    if cache.dim() != 3 or cache.shape[2] not in _MX_BLOCKS:
+        raise ValueError("cache must be [num_pages][num_kv_heads][mx_block_bytes(head_dim, fmt)]")
+    n, hkv, block = cache.shape
+    d, fmt = _MX_BLOCKS[block]
+    return KvShape(int(hkv if num_q_heads is None else num_q_heads), int(hkv), d, PAGE_SIZE, int(n)), fmt
+
+
+def _on_current_device(cache: torch.Tensor, *tensors: Optional[torch.Tensor]) -> None:
+    """The library launches on the current device: every tensor of a call has to be there."""
+    dev = torch.cuda.current_device()
+    for t in (cache,) + tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError("tensors must be on the current device (cuda:%d), got %s" % (dev, t.device))
+
+
+def kv_append_mx(k_new: torch.Tensor, v_new: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor,
+                 ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor], max_q_len: int, max_kv_len: int) -> None:
+    """Quantise new K/V rows bf16 [total_q][H_kv][d] into their slots of a cache of MX blocks
+    (pearl_kv_append_mx)."""
+    for t, n in ((k_new, "k_new"), (v_new, "v_new")):
+        _need(t, n, torch.bfloat16)
+    shape, fmt = _mx_shape(None, cache)
+    if k_new.dim() != 3 or tuple(k_new.shape[1:]) != (shape.num_kv_heads, shape.head_dim) or v_new.shape != k_new.shape:
+        raise ValueError("k_new and v_new must be [total_q][%d][%d]" % (shape.num_kv_heads, shape.head_dim))
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, int(k_new.shape[0]), max_q_len, max_kv_len)
+    _on_current_device(cache, k_new, v_new, block_table, ctx_lens, cu_q_lens)
+    st = load().pearl_kv_append_mx(ctypes.byref(shape), ctypes.byref(desc), fmt, k_new.data_ptr(), v_new.data_ptr(),
+                                   cache.data_ptr(), _stream())
+    _check(st, "pearl_kv_append_mx")
+
+
+def kv_pack_mx(cache: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+               cu_q_lens: Optional[torch.Tensor], total: int, max_q_len: int, max_kv_len: int,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Read token ranges [ctx_lens[b], ctx_lens[b] + n_b) of every sequence back out of a cache of MX
+    blocks, as bf16 [2][total][H_kv][d] (pearl_kv_pack_mx)."""
+    shape, fmt = _mx_shape(None, cache)
+    want = (2, int(total), shape.num_kv_heads, shape.head_dim)
+    if out is None:
+        out = torch.empty(want, dtype=torch.bfloat16, device=cache.device)
+    _need(out, "out", torch.bfloat16)
+    if tuple(out.shape) != want:
+        raise ValueError("out must have shape %s" % (want,))
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len)
+    _on_current_device(cache, block_table, ctx_lens, cu_q_lens, out)
+    st = load().pearl_kv_pack_mx(ctypes.byref(shape), ctypes.byref(desc), fmt, cache.data_ptr(), out.data_ptr(), _stream())
+    _check(st, "pearl_kv_pack_mx")
+    return out
 
 
 # ------------------------------------------------------------------------------------------------

@@ -93,6 +93,12 @@ pearl_status check_seqs(const pearl_seq_desc* q, bool need_q_lens) {
   return PEARL_OK;
 }
 
+pearl_status check_format(pearl_mx_format f) {
+  if (f != PEARL_MXFP4 && f != PEARL_MXFP8)
+    return fail(PEARL_ERR_UNSUPPORTED, "cache format %d is neither PEARL_MXFP4 nor PEARL_MXFP8", (int)f);
+  return PEARL_OK;
+}
+
 struct Plan {
   PlanParams p;
   WsLayout lay;
@@ -414,6 +420,76 @@ pearl_status pearl_kv_unpack(const pearl_kv_shape* shape, const pearl_seq_desc* 
     return pearl_kv_append(shape, seqs, k_rows, v_rows, k_pool, v_pool, stream);
   } catch (...) {
     return fail(PEARL_ERR_HIP, "unexpected exception in pearl_kv_unpack");
+  }
+}
+
+size_t pearl_mx_block_bytes(int head_dim, pearl_mx_format format) {
+  g_err[0] = 0;
+  if (check_format(format) != PEARL_OK) return 0;
+  if (head_dim != 64 && head_dim != 128) {
+    set_err("head_dim %d not in {64,128}", head_dim);
+    return 0;
+  }
+  return 2 * (size_t)kPage * (head_dim * (int)format / 8 + head_dim / 32);
+}
+
+pearl_status pearl_kv_append_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, pearl_mx_format format,
+                                const void* k_new, const void* v_new, void* cache, void* stream) {
+  try {
+    g_err[0] = 0;
+    pearl_status st = check_shape(shape);
+    if (st != PEARL_OK) return st;
+    st = check_format(format);
+    if (st != PEARL_OK) return st;
+    st = check_seqs(seqs, false);
+    if (st != PEARL_OK) return st;
+    if (seqs->total_q == 0) return PEARL_OK;
+    if (!k_new || !v_new || !cache) return fail(PEARL_ERR_INVALID_ARG, "k_new, v_new and cache must be non-NULL");
+    if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(cache))
+      return fail(PEARL_ERR_INVALID_ARG, "k_new, v_new and cache must be 16-byte aligned");
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    hipError_t e = record_before(hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+    e = launch_kv_append_mx((int)format, static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new),
+                            static_cast<uint8_t*>(cache), seqs->block_table, seqs->bt_stride, seqs->ctx_lens,
+                            seqs->cu_q_lens, seqs->batch, seqs->max_q_len, shape->num_kv_heads, shape->head_dim,
+                            shape->num_pages, seqs->total_q, hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "kv_append_mx launch: %s", hipGetErrorString(e));
+    e = record_after(hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+    return PEARL_OK;
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_kv_append_mx");
+  }
+}
+
+pearl_status pearl_kv_pack_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, pearl_mx_format format,
+                              const void* cache, void* buf, void* stream) {
+  try {
+    g_err[0] = 0;
+    pearl_status st = check_shape(shape);
+    if (st != PEARL_OK) return st;
+    st = check_format(format);
+    if (st != PEARL_OK) return st;
+    st = check_seqs(seqs, false);
+    if (st != PEARL_OK) return st;
+    if (seqs->total_q == 0) return PEARL_OK;
+    if (!cache || !buf) return fail(PEARL_ERR_INVALID_ARG, "cache and buf must be non-NULL");
+    if (!aligned16(cache) || !aligned16(buf)) return fail(PEARL_ERR_INVALID_ARG, "cache and buf must be 16-byte aligned");
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    uint16_t* k_rows = static_cast<uint16_t*>(buf);
+    uint16_t* v_rows = k_rows + (size_t)seqs->total_q * shape->num_kv_heads * shape->head_dim;
+    hipError_t e = record_before(hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+    e = launch_kv_pack_mx((int)format, static_cast<const uint8_t*>(cache), k_rows, v_rows, seqs->block_table,
+                          seqs->bt_stride, seqs->ctx_lens, seqs->cu_q_lens, seqs->batch, seqs->max_q_len,
+                          shape->num_kv_heads, shape->head_dim, shape->num_pages, seqs->total_q, hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "kv_pack_mx launch: %s", hipGetErrorString(e));
+    e = record_after(hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+    return PEARL_OK;
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_kv_pack_mx");
   }
 }
 

@@ -1,0 +1,271 @@
+// gfx950 kernels that write K/V rows into a cache of MX blocks and read them back: kv_append_mx (the
+// append of a turn's new tokens; paper, Background: the context grows by each turn's tokens) and
+// kv_pack_mx (the token ranges of a transfer between workers; section 4.3, Eq. 3).
+//
+// Quantisation of a block of 32 channels: with amax its largest magnitude, s is the least scale that
+// keeps amax <= 1.75 * 2^emax * 2^(s - 127) (emax = 2 at 4 bits, 8 at 8), at least 1, and every element is
+// x 2^(127 - s) rounded to nearest, ties to even.  At 8 bits 1.75 * 2^8 = 448 is the largest element, so
+// none is clipped.  At 4 bits the largest is 6, and amax of 6 to 7 units becomes 6: at most a unit off,
+// half the step from 4 to 6, as everywhere else on that step.  (Root mean square error over the signal's, 32 normal numbers a
+// block: bound 6 0.1154, 7 0.1119, 8 0.1150; Laplace 0.132, 0.124, 0.127.)  1.75 is read off amax's bf16
+// bits, and scaling by a power of two is exact, so the bytes are a function of the bf16 inputs alone.
+// Reading back and quantising again gives the same values: the block's largest element is over 3.5
+// units at 4 bits, hence s again, and at 8 bits s may drop by one where every element is twice as many units.
+// A block holding a NaN or an infinity gets scale 255 and codes 0: all its elements read as NaN.
+//
+// A workgroup of D threads takes one (page, kv-head).  K: a thread quantises 8 channels of a
+// token, four threads share a block (a maximum over a quad).  V: a thread takes one channel pair for 8 tokens and
+// 16 neighbouring threads are a block, so the transposed unit is complete in the thread's registers.
+// Bound by HBM: bf16 rows one way (512 bytes a token and kv-head at D = 128), MX blocks the other (136 or 264).
+
+#include "mx_format.h"
+
+namespace pearl {
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+template <int kCtrl> __device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
+  const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false);
+  return x > y ? x : y;
+}
+constexpr int kQuadXor1 = 0xB1, kQuadXor2 = 0x4E, kRowRor = 0x120;
+
+// The larger magnitude of a dword's two bf16, as bits: NaN and infinity are the largest.
+__device__ __forceinline__ uint32_t mag2(uint32_t w) {
+  const uint32_t a = w & 0x7fffu, b = (w >> 16) & 0x7fffu;
+  return a > b ? a : b;
+}
+
+// The scale byte of a block whose largest magnitude has these bf16 bits.
+template <int kBits> __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
+  const int e = (int)(amax >> 7), s = e - (kBits == 4 ? 2 : 8) + ((amax & 127u) > 96u);
+  return e == 255 ? 255u : (uint32_t)(s < 1 ? 1 : s);
+}
+
+// Two bf16 as codes: a byte (4 bits) or 16 bits (8 bits).
+template <int kBits> __device__ __forceinline__ uint32_t mx_down(uint32_t w, float scale) {
+  if constexpr (kBits == 4) {
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, w), scale, 0) & 0xffu;
+  } else {
+    const s16x2 r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, __builtin_bit_cast(bf16x2, w), scale, false);
+    return (uint32_t)(uint16_t)r[0];
+  }
+}
+
+// The (page, kv-head) of a workgroup: its slots [s0, s1) hold the rows row0 .. of this call.
+struct PageRows {
+  int s0, s1, page;                                 // s0 >= s1: nothing to do
+  size_t row0;
+};
+
+__device__ __forceinline__ PageRows page_rows(int item, const int32_t* bt, int bt_stride, const int32_t* ctx_lens,
+                                              const int32_t* cu, int pages_per_seq, int total_q) {
+  const int b = item / pages_per_seq, rel = item - b * pages_per_seq;
+  const int q_start = cu ? cu[b] : b;
+  const int ctx = ctx_lens[b];
+  const int q_len = min(cu ? cu[b + 1] - q_start : 1, total_q - q_start);
+  if (q_len <= 0 || q_start < 0 || ctx < 0) return PageRows{0, 0, -1, 0};
+  const int lp = ctx / kPage + rel;
+  const long long first = max((long long)ctx, (long long)lp * kPage);
+  const long long end = min((long long)ctx + q_len, ((long long)lp + 1) * kPage);
+  if (first >= end || lp >= bt_stride) return PageRows{0, 0, -1, 0};
+  return PageRows{(int)(first - (long long)lp * kPage), (int)(end - (long long)lp * kPage),
+                  bt[(size_t)b * bt_stride + lp], (size_t)(q_start + first - ctx)};
+}
+
+}  // namespace
+
+// blockIdx.x = (b * pages_per_seq + rel) * num_kv_heads + h.  Rows of a page id outside [0, num_pages) are skipped.
+template <int D, int kBits>
+__global__ __launch_bounds__(D) void kv_append_mx_kernel(
+    const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new, uint8_t* __restrict__ cache,
+    const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
+    const int32_t* __restrict__ cu, int pages_per_seq, int num_kv_heads, int num_pages, int total_q) {
+  using MX = MxBlock<D, kBits>;
+  constexpr int kRowThreads = D / 8, kRowsAtOnce = D / kRowThreads, kIters = kPage / kRowsAtOnce;   // 8 rows, 2 turns
+  const int item = blockIdx.x / num_kv_heads, h = blockIdx.x - item * num_kv_heads;
+  const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, pages_per_seq, total_q);
+  if (p.s0 >= p.s1 || p.page < 0 || p.page >= num_pages) return;
+  const int tid = threadIdx.x;
+  uint8_t* const blk = cache + ((size_t)p.page * num_kv_heads + h) * MX::kBytes;
+  auto row = [&](const uint16_t* rows, int slot) {  // slot in [s0, s1)
+    return rows + ((p.row0 + (slot - p.s0)) * num_kv_heads + h) * D;
+  };
+  // all loads first: K 16 bytes of rows tid / kRowThreads + {0, 8}, V 4 bytes of 8 tokens
+  const int kr = tid / kRowThreads, kc = tid % kRowThreads;
+  u32x4 k[kIters];
+#pragma unroll
+  for (int i = 0; i < kIters; ++i) {
+    const int slot = kr + i * kRowsAtOnce;
+    k[i] = slot >= p.s0 && slot < p.s1 ? *reinterpret_cast<const u32x4*>(row(k_new, slot) + 8 * kc) : u32x4{0u, 0u, 0u, 0u};
+  }
+  const int pair = tid % (D / 2), half = tid / (D / 2);
+  uint32_t v[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    const int slot = 8 * half + t;
+    v[t] = slot >= p.s0 && slot < p.s1 ? *reinterpret_cast<const uint32_t*>(row(v_new, slot) + 2 * pair) : 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < kIters; ++i) {
+    const int slot = kr + i * kRowsAtOnce;
+    uint32_t m = max(max(mag2(k[i][0]), mag2(k[i][1])), max(mag2(k[i][2]), mag2(k[i][3])));
+    m = dpp_max<kQuadXor2>(dpp_max<kQuadXor1>(m));
+    const uint32_t s = scale_byte<kBits>(m);
+    const float f = mx_scale(s);
+    uint32_t c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = s == 255u ? 0u : mx_down<kBits>(k[i][j], f);
+    if (slot >= p.s0 && slot < p.s1) {
+      if constexpr (kBits == 4)
+        *reinterpret_cast<uint32_t*>(blk + slot * MX::kRow + 4 * kc) = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+      else
+        *reinterpret_cast<u32x2*>(blk + slot * MX::kRow + 8 * kc) = u32x2{c[0] | c[1] << 16, c[2] | c[3] << 16};
+      if ((kc & 3) == 0) blk[MX::k_scale(slot, kc >> 2)] = (uint8_t)s;
+    }
+  }
+  uint32_t c[8], s[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    uint32_t m = mag2(v[t]);
+    m = dpp_max<kRowRor + 8>(m);
+    m = dpp_max<kRowRor + 4>(m);
+    m = dpp_max<kRowRor + 2>(m);
+    m = dpp_max<kRowRor + 1>(m);
+    s[t] = scale_byte<kBits>(m);
+    c[t] = s[t] == 255u ? 0u : mx_down<kBits>(v[t], mx_scale(s[t]));
+  }
+  const int lo = p.s0 - 8 * half, hi = p.s1 - 8 * half;       // this thread's tokens are lo <= t < hi
+  if (lo >= 8 || hi <= 0) return;
+  const bool scales = (pair & 15) == 0;
+  uint8_t* const vc = blk + MX::v_code(8 * half, pair);
+  uint8_t* const vs = blk + MX::v_scale(8 * half, pair >> 4);
+  if (lo <= 0 && hi >= 8) {
+    if constexpr (kBits == 4)
+      *reinterpret_cast<u32x2*>(vc) = u32x2{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24};
+    else
+      *reinterpret_cast<u32x4*>(vc) = u32x4{c[0] | c[1] << 16, c[2] | c[3] << 16, c[4] | c[5] << 16, c[6] | c[7] << 16};
+    if (scales)
+      *reinterpret_cast<u32x2*>(vs) = u32x2{s[0] | s[1] << 8 | s[2] << 16 | s[3] << 24, s[4] | s[5] << 8 | s[6] << 16 | s[7] << 24};
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      if (t < lo || t >= hi) continue;
+      if constexpr (kBits == 4) vc[t] = (uint8_t)c[t];
+      else reinterpret_cast<uint16_t*>(vc)[t] = (uint16_t)c[t];
+      if (scales) vs[t] = (uint8_t)s[t];
+    }
+  }
+}
+
+// The rows of the same token ranges, as bf16: zeros for a page id outside [0, num_pages).
+template <int D, int kBits>
+__global__ __launch_bounds__(D) void kv_pack_mx_kernel(
+    const uint8_t* __restrict__ cache, uint16_t* __restrict__ k_rows, uint16_t* __restrict__ v_rows,
+    const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
+    const int32_t* __restrict__ cu, int pages_per_seq, int num_kv_heads, int num_pages, int total_q) {
+  using MX = MxBlock<D, kBits>;
+  constexpr int kRowThreads = D / 8, kRowsAtOnce = D / kRowThreads, kIters = kPage / kRowsAtOnce;
+  const int item = blockIdx.x / num_kv_heads, h = blockIdx.x - item * num_kv_heads;
+  const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, pages_per_seq, total_q);
+  if (p.s0 >= p.s1) return;
+  const bool ok = p.page >= 0 && p.page < num_pages;
+  const int tid = threadIdx.x;
+  const uint8_t* const blk = cache + ((size_t)(ok ? p.page : 0) * num_kv_heads + h) * MX::kBytes;
+  auto row = [&](uint16_t* rows, int slot) {
+    return rows + ((p.row0 + (slot - p.s0)) * num_kv_heads + h) * D;
+  };
+  const int kr = tid / kRowThreads, kc = tid % kRowThreads;
+  u32x2 k[kIters];
+  uint32_t ks[kIters];
+#pragma unroll
+  for (int i = 0; i < kIters; ++i) {
+    const int slot = kr + i * kRowsAtOnce;
+    if constexpr (kBits == 4) k[i] = u32x2{*reinterpret_cast<const uint32_t*>(blk + slot * MX::kRow + 4 * kc), 0u};
+    else k[i] = *reinterpret_cast<const u32x2*>(blk + slot * MX::kRow + 8 * kc);
+    ks[i] = blk[MX::k_scale(slot, kc >> 2)];
+  }
+  const int pair = tid % (D / 2), half = tid / (D / 2);
+  const uint8_t* const vc = blk + MX::v_code(8 * half, pair);
+  u32x4 v;
+  if constexpr (kBits == 4) {
+    const u32x2 w = *reinterpret_cast<const u32x2*>(vc);
+    v = u32x4{w[0], w[1], 0u, 0u};
+  } else {
+    v = *reinterpret_cast<const u32x4*>(vc);
+  }
+  const u32x2 vs = *reinterpret_cast<const u32x2*>(blk + MX::v_scale(8 * half, pair >> 4));
+#pragma unroll
+  for (int i = 0; i < kIters; ++i) {
+    const int slot = kr + i * kRowsAtOnce;
+    const float f = mx_scale(ks[i]);
+    u32x4 x;
+    if constexpr (kBits == 4)
+      x = u32x4{mx_up<4, 0>(k[i][0], f), mx_up<4, 1>(k[i][0], f), mx_up<4, 2>(k[i][0], f), mx_up<4, 3>(k[i][0], f)};
+    else
+      x = u32x4{mx_up<8, 0>(k[i][0], f), mx_up<8, 1>(k[i][0], f), mx_up<8, 0>(k[i][1], f), mx_up<8, 1>(k[i][1], f)};
+    if (slot >= p.s0 && slot < p.s1)
+      *reinterpret_cast<u32x4*>(row(k_rows, slot) + 8 * kc) = ok ? x : u32x4{0u, 0u, 0u, 0u};
+  }
+  auto token = [&](auto t_c) {                      // token 8 half + t: 4 bytes a thread, a row together
+    constexpr int t = decltype(t_c)::value;
+    const int slot = 8 * half + t;
+    if (slot < p.s0 || slot >= p.s1) return;
+    const float f = mx_scale_of<t % 4>(vs[t / 4]);
+    const uint32_t x = kBits == 4 ? mx_up<kBits, t % 4>(v[t / 4], f) : mx_up<kBits, t % 2>(v[t / 2], f);
+    *reinterpret_cast<uint32_t*>(row(v_rows, slot) + 2 * pair) = ok ? x : 0u;
+  };
+  token(std::integral_constant<int, 0>{});
+  token(std::integral_constant<int, 1>{});
+  token(std::integral_constant<int, 2>{});
+  token(std::integral_constant<int, 3>{});
+  token(std::integral_constant<int, 4>{});
+  token(std::integral_constant<int, 5>{});
+  token(std::integral_constant<int, 6>{});
+  token(std::integral_constant<int, 7>{});
+}
+
+namespace {
+// Workgroups of a launch over the token ranges, or -1 if they pass the grid's limit: a range of n tokens
+// starting anywhere touches at most ceil((n + 15) / 16) pages.
+int64_t page_items(int batch, int max_q_len, int num_kv_heads, int* pages_per_seq) {
+  *pages_per_seq = (max_q_len + 2 * kPage - 2) / kPage;
+  const int64_t blocks = (int64_t)batch * *pages_per_seq * num_kv_heads;
+  return blocks > INT32_MAX ? -1 : blocks;
+}
+}  // namespace
+
+hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* v_new, uint8_t* cache,
+                               const int32_t* block_table, int bt_stride, const int32_t* ctx_lens,
+                               const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
+                               int num_pages, int total_q, hipStream_t stream) {
+  if (max_q_len <= 0 || batch <= 0 || total_q <= 0) return hipSuccess;
+  int pages = 0;
+  const int64_t blocks = page_items(batch, max_q_len, num_kv_heads, &pages);
+  if (blocks < 0) return hipErrorInvalidValue;
+  auto kernel = head_dim == 64 ? (bits == 4 ? kv_append_mx_kernel<64, 4> : kv_append_mx_kernel<64, 8>)
+                               : (bits == 4 ? kv_append_mx_kernel<128, 4> : kv_append_mx_kernel<128, 8>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(head_dim), 0, stream, k_new, v_new, cache, block_table,
+                     bt_stride, ctx_lens, cu_q_lens, pages, num_kv_heads, num_pages, total_q);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_pack_mx(int bits, const uint8_t* cache, uint16_t* k_rows, uint16_t* v_rows,
+                             const int32_t* block_table, int bt_stride, const int32_t* ctx_lens,
+                             const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
+                             int num_pages, int total_q, hipStream_t stream) {
+  if (max_q_len <= 0 || batch <= 0 || total_q <= 0) return hipSuccess;
+  int pages = 0;
+  const int64_t blocks = page_items(batch, max_q_len, num_kv_heads, &pages);
+  if (blocks < 0) return hipErrorInvalidValue;
+  auto kernel = head_dim == 64 ? (bits == 4 ? kv_pack_mx_kernel<64, 4> : kv_pack_mx_kernel<64, 8>)
+                               : (bits == 4 ? kv_pack_mx_kernel<128, 4> : kv_pack_mx_kernel<128, 8>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(head_dim), 0, stream, cache, k_rows, v_rows, block_table,
+                     bt_stride, ctx_lens, cu_q_lens, pages, num_kv_heads, num_pages, total_q);
+  return hipGetLastError();
+}
+
+}  // namespace pearl
