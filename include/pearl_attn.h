@@ -270,6 +270,23 @@ pearl_status pearl_kv_pack_mx(const pearl_kv_shape* shape, const pearl_seq_desc*
                               const void* cache, void* buf, void* stream);
 
 /*
+ * pearl_attn_decode over a cache of MX blocks, and with its append: the values that the cache stands for
+ * take the place of k_j and v_j (keys and values enter the products exactly, weights in 16 bits).
+ * pearl_attn_decode_append_mx is pearl_kv_append_mx of this step's rows followed by
+ * pearl_attn_decode_mx, with the same results bit for bit, in as many launches as the decode alone.
+ *   workspace: as for the other attention calls, of pearl_attn_workspace_bytes(shape, seqs).
+ * Sequences are taken in groups of 1024 in order; where a length violates the host bounds, the attention
+ * of its group writes nothing (an append still takes place).
+ */
+pearl_status pearl_attn_decode_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, pearl_mx_format format,
+                                  const void* q, const void* cache, float softmax_scale, void* out, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+pearl_status pearl_attn_decode_append_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs,
+                                         pearl_mx_format format, const void* q, const void* k_new, const void* v_new,
+                                         void* cache, float softmax_scale, void* out, float* lse, void* workspace,
+                                         size_t workspace_bytes, void* stream);
+
+/*
  * Timing hook for benchmarks and profilers (not part of the computation).  While a pair is set,
  * every library call made on the calling thread records `before` on its stream immediately
  * before launching its main kernel (the attention kernel for the three attention calls, the

@@ -34,7 +34,7 @@ def mx_quantise(bits: np.ndarray, fmt: int) -> Tuple[np.ndarray, np.ndarray]:
     """bf16 bit patterns [..., d] -> (codes uint8 [..., d], scales uint8 [..., d / 32])."""
     e_max, _, _, most = _ELEMENT[fmt]
     x = bf16_bits_to_f64(bits)
-    x = x.reshape(x.shape[:-1] + (-1, 32))
+    x = x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
     bad = ~np.isfinite(x).all(-1)
     x = np.where(bad[..., None], 0.0, x)
     top = np.abs(x).max(-1)
@@ -51,12 +51,12 @@ def mx_quantise(bits: np.ndarray, fmt: int) -> Tuple[np.ndarray, np.ndarray]:
     code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)
     code = code | (np.signbit(y).astype(np.int64) << (fmt - 1))
     code[bad] = 0
-    return (code.reshape(code.shape[:-2] + (-1,)).astype(np.uint8), np.where(bad, 255, s).astype(np.uint8))
+    return (code.reshape(bits.shape).astype(np.uint8), np.where(bad, 255, s).astype(np.uint8))
 
 
 def mx_values(codes: np.ndarray, scales: np.ndarray, fmt: int) -> np.ndarray:
     """float64 values of codes [..., d] under scales [..., d / 32]."""
-    v = mx_element_values(fmt)[codes].reshape(codes.shape[:-1] + (-1, 32))
+    v = mx_element_values(fmt)[codes].reshape(codes.shape[:-1] + (codes.shape[-1] // 32, 32))
     s = scales.astype(np.int64)[..., None]
     return np.where(s == 255, np.nan, np.ldexp(v, s - 127)).reshape(codes.shape)
 
@@ -84,7 +84,7 @@ def _pack_codes(codes: np.ndarray, fmt: int) -> np.ndarray:
 
 
 def _unpack_codes(b: np.ndarray, fmt: int) -> np.ndarray:
-    return b if fmt == 8 else np.stack([b & 15, b >> 4], -1).reshape(b.shape[:-1] + (-1,))
+    return b if fmt == 8 else np.stack([b & 15, b >> 4], -1).reshape(b.shape[:-1] + (2 * b.shape[-1],))
 
 
 def mx_append(cache: np.ndarray, fmt: int, k_new: np.ndarray, v_new: np.ndarray, block_table: np.ndarray,

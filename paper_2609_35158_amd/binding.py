@@ -45,7 +45,7 @@ EXPORTED = ("pearl_abi_version", "pearl_status_str", "pearl_last_error", "pearl_
             "pearl_attn_mixed", "pearl_kv_pack", "pearl_kv_unpack", "pearl_set_kernel_events",
             "pearl_hbm_copy", "pearl_hbm_read", "pearl_hbm_read_nt", "pearl_hbm_fill", "pearl_attn_decode_static",
             "pearl_attn_decode_static_max_bytes", "pearl_attn_decode_append", "pearl_mx_block_bytes",
-            "pearl_kv_append_mx", "pearl_kv_pack_mx")
+            "pearl_kv_append_mx", "pearl_kv_pack_mx", "pearl_attn_decode_mx", "pearl_attn_decode_append_mx")
 
 
 def load(path: str = LIB_PATH):
@@ -99,6 +99,15 @@ def load(path: str = LIB_PATH):
     lib.pearl_kv_pack_mx.restype = ctypes.c_int
     lib.pearl_kv_pack_mx.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                      ctypes.c_void_p]
+    lib.pearl_attn_decode_mx.restype = ctypes.c_int
+    lib.pearl_attn_decode_mx.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                         ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                         ctypes.c_size_t, ctypes.c_void_p]
+    lib.pearl_attn_decode_append_mx.restype = ctypes.c_int
+    lib.pearl_attn_decode_append_mx.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p,
+                                                ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_float,
+                                                ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                                ctypes.c_void_p]
     lib.pearl_set_kernel_events.restype = None
     lib.pearl_set_kernel_events.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
     # measurement tooling (include/pearl_bench.h)
@@ -449,6 +458,72 @@ def kv_pack_mx(cache: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.T
     st = load().pearl_kv_pack_mx(ctypes.byref(shape), ctypes.byref(desc), fmt, cache.data_ptr(), out.data_ptr(), _stream())
     _check(st, "pearl_kv_pack_mx")
     return out
+
+
+def workspace_bytes_mx(num_q_heads: int, cache: torch.Tensor, desc: SeqDesc) -> int:
+    """Bytes of workspace that the attention calls over this cache need (pearl_attn_workspace_bytes)."""
+    shape, _ = _mx_shape(num_q_heads, cache)
+    n = load().pearl_attn_workspace_bytes(ctypes.byref(shape), ctypes.byref(desc))
+    if n == 0:
+        raise PearlError(1, "pearl_attn_workspace_bytes", last_error())
+    return int(n)
+
+
+def _attention_mx(fname: str, q: torch.Tensor, new, cache: torch.Tensor, block_table: torch.Tensor,
+                  ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor], max_q_len: int, max_kv_len: int,
+                  scale: Optional[float], return_lse: bool, out: Optional[torch.Tensor], lse: Optional[torch.Tensor],
+                  workspace: Optional[torch.Tensor]):
+    _need(q, "q", torch.bfloat16)
+    if q.dim() != 3:
+        raise ValueError("q must be [total_q][num_q_heads][head_dim]")
+    total_q, H_q, d = q.shape
+    shape, fmt = _mx_shape(H_q, cache)
+    if d != shape.head_dim:
+        raise ValueError("q has head_dim %d, the cache %d" % (d, shape.head_dim))
+    for t, n in zip(new, ("k_new", "v_new")):
+        _need(t, n, torch.bfloat16)
+        if tuple(t.shape) != (total_q, shape.num_kv_heads, d):
+            raise ValueError("k_new and v_new must be [batch][num_kv_heads][head_dim]")
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, total_q, max_q_len, max_kv_len)
+    if out is None:
+        out = torch.empty_like(q)
+    _need(out, "out", torch.bfloat16)
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if return_lse and lse is None:
+        lse = torch.empty((total_q, H_q), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _need(lse, "lse", torch.float32)
+        if tuple(lse.shape) != (total_q, H_q):
+            raise ValueError("lse must be [total_q][num_q_heads]")
+    if workspace is None:
+        workspace = torch.empty(workspace_bytes_mx(H_q, cache, desc), dtype=torch.uint8, device=q.device)
+    else:
+        _need(workspace, "workspace", torch.uint8)   # the library checks its size
+    _on_current_device(cache, q, *new, block_table, ctx_lens, cu_q_lens, out, lse, workspace)
+    if scale is None:
+        scale = 1.0 / float(d) ** 0.5
+    st = getattr(load(), fname)(ctypes.byref(shape), ctypes.byref(desc), fmt, q.data_ptr(),
+                                *[t.data_ptr() for t in new], cache.data_ptr(), float(scale), out.data_ptr(),
+                                _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, fname)
+    return (out, lse) if lse is not None else out
+
+
+def decode_mx(q, cache, block_table, ctx_lens, max_kv_len, scale=None, return_lse=False, out=None, lse=None,
+              workspace=None):
+    """Single-token decode over a cache of MX blocks (pearl_attn_decode_mx); q is [batch][H_q][d]."""
+    return _attention_mx("pearl_attn_decode_mx", q, (), cache, block_table, ctx_lens, None, 1, max_kv_len, scale,
+                         return_lse, out, lse, workspace)
+
+
+def decode_append_mx(q, k_new, v_new, cache, block_table, ctx_lens, max_kv_len, scale=None, return_lse=False, out=None,
+                     lse=None, workspace=None):
+    """One decode step with its append over a cache of MX blocks (pearl_attn_decode_append_mx): k_new / v_new
+    [batch][H_kv][d] are quantised into position ctx_lens[b] of every sequence, which then attends over
+    ctx_lens[b] + 1 keys."""
+    return _attention_mx("pearl_attn_decode_append_mx", q, (k_new, v_new), cache, block_table, ctx_lens, None, 1,
+                         max_kv_len, scale, return_lse, out, lse, workspace)
 
 
 # ------------------------------------------------------------------------------------------------

@@ -99,6 +99,21 @@ pearl_status check_format(pearl_mx_format f) {
   return PEARL_OK;
 }
 
+// The pointers and sizes of an attention call over a cache of MX blocks.
+pearl_status check_mx_pointers(const pearl_kv_shape* s, const pearl_seq_desc* q, const void* qp, const void* cache,
+                               const void* out, const float* lse, float scale, const void* ws) {
+  if (!qp || !cache || !out) return fail(PEARL_ERR_INVALID_ARG, "q, cache and out must be non-NULL");
+  if (!ws) return fail(PEARL_ERR_WORKSPACE, "workspace is NULL");
+  if (!aligned16(qp) || !aligned16(cache) || !aligned16(out))
+    return fail(PEARL_ERR_INVALID_ARG, "q, cache and out must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) return fail(PEARL_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (lse && (reinterpret_cast<uintptr_t>(lse) & 3) != 0) return fail(PEARL_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(PEARL_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+  if ((int64_t)q->total_q * s->num_q_heads * s->head_dim > INT32_MAX * int64_t(8))
+    return fail(PEARL_ERR_UNSUPPORTED, "q/out too large");
+  return PEARL_OK;
+}
+
 struct Plan {
   PlanParams p;
   WsLayout lay;
@@ -133,6 +148,48 @@ Plan make_plan(const pearl_kv_shape* s, const pearl_seq_desc* q, int mode) {
   p.pre_jobs_cap = may_split ? pl.lay.pre_jobs_cap : 0;
   p.mixed_grid = mode == kModeMixed ? attention_grid(s->head_dim, 3) : 0;
   return pl;
+}
+
+// The kernels' arguments with the pools and the fused append left out.
+AttnArgs attn_args(const pearl_kv_shape* s, const pearl_seq_desc* q, const Plan& pl, const void* qp, float scale,
+                   void* out, float* lse, void* ws) {
+  char* w = static_cast<char*>(ws);
+  AttnArgs a = {};
+  a.q = static_cast<const uint16_t*>(qp);
+  a.block_table = q->block_table;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.ws_hdr = reinterpret_cast<int32_t*>(w + pl.lay.hdr);
+  a.seqinfo = reinterpret_cast<const SeqInfo*>(w + pl.lay.seqinfo);
+  a.split_base = reinterpret_cast<const int32_t*>(w + pl.lay.split_base);
+  a.entries = reinterpret_cast<const int2*>(w + pl.lay.entries);
+  a.part_o = reinterpret_cast<float*>(w + pl.lay.part_o);
+  a.part_ml = reinterpret_cast<float*>(w + pl.lay.part_ml);
+  a.pre_jobs = reinterpret_cast<const int4*>(w + pl.lay.pre_jobs);
+  a.part_pre_o = reinterpret_cast<float*>(w + pl.lay.part_pre_o);
+  a.part_pre_ml = reinterpret_cast<float*>(w + pl.lay.part_pre_ml);
+  a.split_cnt = reinterpret_cast<int32_t*>(w + pl.lay.split_cnt);
+  a.bt_stride = q->bt_stride;
+  a.num_pages = s->num_pages;
+  a.num_q_heads = s->num_q_heads;
+  a.num_kv_heads = s->num_kv_heads;
+  a.group = pl.p.group;
+  a.tokens_per_tile = pl.p.tokens_per_tile;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  return a;
+}
+
+// With PEARL_DEBUG=1: waits for the call and reports what its kernels refused.
+pearl_status debug_check(const char* w, const Plan& pl, hipStream_t hs) {
+  if (!debug_mode()) return PEARL_OK;
+  hipError_t e = hipStreamSynchronize(hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "PEARL_DEBUG sync: %s", hipGetErrorString(e));
+  int32_t flag = 0;
+  e = hipMemcpy(&flag, w + pl.lay.hdr + 4 * kHdrError, sizeof(flag), hipMemcpyDeviceToHost);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "PEARL_DEBUG readback: %s", hipGetErrorString(e));
+  if (flag == 1) return fail(PEARL_ERR_INVALID_ARG, "device lengths violate the host bounds (total_q/max_q_len/max_kv_len/bt_stride) or decode q_len != 1; nothing was computed");
+  if (flag != 0) return fail(PEARL_ERR_INVALID_ARG, "work list exceeded its capacity; nothing was computed");
+  return PEARL_OK;
 }
 
 // static_ws: use the library's static per-device workspace (pearl_attn_decode_static) instead of
@@ -198,34 +255,13 @@ pearl_status run_attention(int mode, const pearl_kv_shape* s, const pearl_seq_de
     e = launch_plan(pl.p, q->ctx_lens, q->cu_q_lens, ws, pl.lay, hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "plan launch: %s", hipGetErrorString(e));
   }
-  AttnArgs a;
-  a.q = static_cast<const uint16_t*>(qp);
+  AttnArgs a = attn_args(s, q, pl, qp, scale, out, lse, ws);
   a.k_pool = static_cast<const uint16_t*>(k_pool);
   a.v_pool = static_cast<const uint16_t*>(v_pool);
-  a.block_table = q->block_table;
-  a.out = static_cast<uint16_t*>(out);
-  a.lse = lse;
-  a.ws_hdr = reinterpret_cast<int32_t*>(w + pl.lay.hdr);
-  a.seqinfo = reinterpret_cast<const SeqInfo*>(w + pl.lay.seqinfo);
-  a.split_base = reinterpret_cast<const int32_t*>(w + pl.lay.split_base);
-  a.entries = reinterpret_cast<const int2*>(w + pl.lay.entries);
-  a.part_o = reinterpret_cast<float*>(w + pl.lay.part_o);
-  a.part_ml = reinterpret_cast<float*>(w + pl.lay.part_ml);
-  a.pre_jobs = reinterpret_cast<const int4*>(w + pl.lay.pre_jobs);
-  a.part_pre_o = reinterpret_cast<float*>(w + pl.lay.part_pre_o);
-  a.part_pre_ml = reinterpret_cast<float*>(w + pl.lay.part_pre_ml);
-  a.split_cnt = reinterpret_cast<int32_t*>(w + pl.lay.split_cnt);
   a.k_new = dec_in_kernel ? static_cast<const uint16_t*>(k_new) : nullptr;
   a.v_new = dec_in_kernel ? static_cast<const uint16_t*>(v_new) : nullptr;
   a.k_pool_w = static_cast<uint16_t*>(const_cast<void*>(k_pool));
   a.v_pool_w = static_cast<uint16_t*>(const_cast<void*>(v_pool));
-  a.bt_stride = q->bt_stride;
-  a.num_pages = s->num_pages;
-  a.num_q_heads = s->num_q_heads;
-  a.num_kv_heads = s->num_kv_heads;
-  a.group = pl.p.group;
-  a.tokens_per_tile = pl.p.tokens_per_tile;
-  a.scale_log2 = scale * 1.4426950408889634f;
   const int64_t max_items = (pl.lay.max_pre + pl.lay.max_dec) * s->num_kv_heads;
   DecPlanArgs d;
   d.ctx_lens = q->ctx_lens;
@@ -256,16 +292,66 @@ pearl_status run_attention(int mode, const pearl_kv_shape* s, const pearl_seq_de
     e = launch_merge_prefill(a, s->head_dim, pl.p.pre_jobs_cap, hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "prefill merge launch: %s", hipGetErrorString(e));
   }
-  if (debug_mode()) {
-    e = hipStreamSynchronize(hs);
-    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "PEARL_DEBUG sync: %s", hipGetErrorString(e));
-    int32_t flag = 0;
-    e = hipMemcpy(&flag, w + pl.lay.hdr + 4 * kHdrError, sizeof(flag), hipMemcpyDeviceToHost);
-    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "PEARL_DEBUG readback: %s", hipGetErrorString(e));
-    if (flag == 1) return fail(PEARL_ERR_INVALID_ARG, "device lengths violate the host bounds (total_q/max_q_len/max_kv_len/bt_stride) or decode q_len != 1; nothing was computed");
-    if (flag != 0) return fail(PEARL_ERR_INVALID_ARG, "work list exceeded its capacity; nothing was computed");
+  return debug_check(w, pl, hs);
+}
+
+// Decode (k_new / v_new: with its append) over a cache of MX blocks, in groups of up to kDecPlanMaxSeqs
+// sequences, each two launches: what clears the counters, with the append if there is one, and the decode.
+pearl_status run_decode_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pearl_mx_format format, const void* qp,
+                           const void* k_new, const void* v_new, const void* cache, float scale, void* out, float* lse,
+                           void* ws, size_t ws_bytes, void* stream) {
+  pearl_status st = check_shape(s);
+  if (st != PEARL_OK) return st;
+  st = check_format(format);
+  if (st != PEARL_OK) return st;
+  st = check_seqs(q, false);
+  if (st != PEARL_OK) return st;
+  if (q->cu_q_lens) return fail(PEARL_ERR_INVALID_ARG, "decode requires cu_q_lens == NULL (one token per sequence)");
+  st = check_mx_pointers(s, q, qp, cache, out, lse, scale, ws);
+  if (st != PEARL_OK) return st;
+  if (k_new && (!aligned16(k_new) || !aligned16(v_new)))
+    return fail(PEARL_ERR_INVALID_ARG, "k_new and v_new must be 16-byte aligned");
+  const Plan pl = make_plan(s, q, kModeDecode);
+  if (pl.lay.max_dec * (int64_t)s->num_kv_heads > INT32_MAX)
+    return fail(PEARL_ERR_UNSUPPORTED, "partial slots (%lld x %d kv-heads) exceed int32", (long long)pl.lay.max_dec, s->num_kv_heads);
+  if (ws_bytes < pl.lay.total)
+    return fail(PEARL_ERR_WORKSPACE, "workspace_bytes %zu < required %zu", ws_bytes, pl.lay.total);
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const int bits = (int)format, grid = decode_mx_grid(s->head_dim, bits);
+  const AttnArgs whole = attn_args(s, q, pl, qp, scale, out, lse, ws);
+  for (int b0 = 0; b0 < q->batch; b0 += kDecPlanMaxSeqs) {
+    AttnArgs a = whole;
+    const size_t rows = (size_t)b0 * s->num_q_heads;
+    a.q += rows * s->head_dim;
+    a.out += rows * s->head_dim;
+    if (a.lse) a.lse += rows;
+    a.block_table += (size_t)b0 * q->bt_stride;
+    DecPlanArgs d = {};
+    d.ctx_lens = q->ctx_lens + b0;
+    d.batch = std::min(q->batch - b0, kDecPlanMaxSeqs);
+    d.max_kv_len = q->max_kv_len;
+    d.max_dec = (int)pl.lay.max_dec;
+    set_decode_runs(d, s->num_kv_heads, grid);
+    ZeroWords zero = decode_zero_words(a, d);
+    if (b0 > 0) zero.hdr = nullptr;                 // an earlier group's error flag stays
+    hipError_t e;
+    if (k_new) {
+      const size_t at = (size_t)b0 * s->num_kv_heads * s->head_dim;
+      e = launch_kv_append_mx(bits, static_cast<const uint16_t*>(k_new) + at, static_cast<const uint16_t*>(v_new) + at,
+                              static_cast<uint8_t*>(const_cast<void*>(cache)), a.block_table, q->bt_stride, d.ctx_lens,
+                              nullptr, d.batch, 1, s->num_kv_heads, s->head_dim, s->num_pages, d.batch, zero, hs);
+    } else {
+      e = launch_zero_words(zero, hs);
+    }
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "decode prologue launch: %s", hipGetErrorString(e));
+    e = record_before(hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+    e = launch_decode_mx(a, d, static_cast<const uint8_t*>(cache), s->head_dim, bits, hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "decode launch: %s", hipGetErrorString(e));
+    e = record_after(hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
   }
-  return PEARL_OK;
+  return debug_check(static_cast<const char*>(ws), pl, hs);
 }
 
 }  // namespace
@@ -453,7 +539,7 @@ pearl_status pearl_kv_append_mx(const pearl_kv_shape* shape, const pearl_seq_des
     e = launch_kv_append_mx((int)format, static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new),
                             static_cast<uint8_t*>(cache), seqs->block_table, seqs->bt_stride, seqs->ctx_lens,
                             seqs->cu_q_lens, seqs->batch, seqs->max_q_len, shape->num_kv_heads, shape->head_dim,
-                            shape->num_pages, seqs->total_q, hs);
+                            shape->num_pages, seqs->total_q, ZeroWords{nullptr, nullptr, 0}, hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "kv_append_mx launch: %s", hipGetErrorString(e));
     e = record_after(hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
@@ -490,6 +576,32 @@ pearl_status pearl_kv_pack_mx(const pearl_kv_shape* shape, const pearl_seq_desc*
     return PEARL_OK;
   } catch (...) {
     return fail(PEARL_ERR_HIP, "unexpected exception in pearl_kv_pack_mx");
+  }
+}
+
+pearl_status pearl_attn_decode_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, pearl_mx_format format,
+                                  const void* q, const void* cache, float softmax_scale, void* out, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  try {
+    g_err[0] = 0;
+    return run_decode_mx(shape, seqs, format, q, nullptr, nullptr, cache, softmax_scale, out, lse, workspace,
+                         workspace_bytes, stream);
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_attn_decode_mx");
+  }
+}
+
+pearl_status pearl_attn_decode_append_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs,
+                                         pearl_mx_format format, const void* q, const void* k_new, const void* v_new,
+                                         void* cache, float softmax_scale, void* out, float* lse, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
+  try {
+    g_err[0] = 0;
+    if (!k_new || !v_new) return fail(PEARL_ERR_INVALID_ARG, "k_new and v_new must be non-NULL");
+    return run_decode_mx(shape, seqs, format, q, k_new, v_new, cache, softmax_scale, out, lse, workspace,
+                         workspace_bytes, stream);
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_attn_decode_append_mx");
   }
 }
 

@@ -79,13 +79,19 @@ __device__ __forceinline__ PageRows page_rows(int item, const int32_t* bt, int b
 }  // namespace
 
 // blockIdx.x = (b * pages_per_seq + rel) * num_kv_heads + h.  Rows of a page id outside [0, num_pages) are skipped.
+// The first workgroup also clears `zero` (a decode step's append and its decode are then two launches, as decode
+// alone).
 template <int D, int kBits>
 __global__ __launch_bounds__(D) void kv_append_mx_kernel(
     const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new, uint8_t* __restrict__ cache,
     const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
-    const int32_t* __restrict__ cu, int pages_per_seq, int num_kv_heads, int num_pages, int total_q) {
+    const int32_t* __restrict__ cu, int pages_per_seq, int num_kv_heads, int num_pages, int total_q, ZeroWords zero) {
   using MX = MxBlock<D, kBits>;
   constexpr int kRowThreads = D / 8, kRowsAtOnce = D / kRowThreads, kIters = kPage / kRowsAtOnce;   // 8 rows, 2 turns
+  if (blockIdx.x == 0) {
+    if (zero.hdr && threadIdx.x < kHdrWords) zero.hdr[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < zero.n_cnt; i += D) zero.cnt[i] = 0;
+  }
   const int item = blockIdx.x / num_kv_heads, h = blockIdx.x - item * num_kv_heads;
   const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, pages_per_seq, total_q);
   if (p.s0 >= p.s1 || p.page < 0 || p.page >= num_pages) return;
@@ -241,7 +247,7 @@ int64_t page_items(int batch, int max_q_len, int num_kv_heads, int* pages_per_se
 hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* v_new, uint8_t* cache,
                                const int32_t* block_table, int bt_stride, const int32_t* ctx_lens,
                                const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
-                               int num_pages, int total_q, hipStream_t stream) {
+                               int num_pages, int total_q, const ZeroWords& zero, hipStream_t stream) {
   if (max_q_len <= 0 || batch <= 0 || total_q <= 0) return hipSuccess;
   int pages = 0;
   const int64_t blocks = page_items(batch, max_q_len, num_kv_heads, &pages);
@@ -249,7 +255,7 @@ hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* 
   auto kernel = head_dim == 64 ? (bits == 4 ? kv_append_mx_kernel<64, 4> : kv_append_mx_kernel<64, 8>)
                                : (bits == 4 ? kv_append_mx_kernel<128, 4> : kv_append_mx_kernel<128, 8>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(head_dim), 0, stream, k_new, v_new, cache, block_table,
-                     bt_stride, ctx_lens, cu_q_lens, pages, num_kv_heads, num_pages, total_q);
+                     bt_stride, ctx_lens, cu_q_lens, pages, num_kv_heads, num_pages, total_q, zero);
   return hipGetLastError();
 }
 

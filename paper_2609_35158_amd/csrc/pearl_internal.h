@@ -1,5 +1,5 @@
 // Internal interface between the C-ABI host layer (api.cpp) and the gfx950 kernels
-// (attn_kernels.hip, kv_pages.hip, kv_mx.hip).  Not installed; callers use include/pearl_attn.h.
+// (attn_kernels.hip, decode_mx.hip, kv_pages.hip, kv_mx.hip).  Not installed; callers use include/pearl_attn.h.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -46,15 +46,8 @@ constexpr int kNumXcd = 8;
 // Decode batches of up to this many sequences are planned inside the attention kernel (in LDS);
 // larger ones go through plan_kernel.
 constexpr int kDecPlanMaxSeqs = 1024;
-// Such a launch cuts each kv-head's list of pages into runs of at least kDecMinPages pages;
-// several kv-heads share a workgroup if kDecPieceCost times the pieces of the longest sequence are
-// at most the pages of a wave's share (DecShares).
-constexpr int kDecMinPages = 16;
-constexpr int kDecPieceCost = 8;
 // With more kv-heads than resident workgroups, runs for about this many rounds of them.
 constexpr int kDecRounds = 4;
-// The runs hold whole sequences if that makes none longer than an equal run by more than this.
-constexpr int kDecWholePages = 28;
 
 enum Mode : int { kModePrefill = 0, kModeDecode = 1, kModeMixed = 2 };
 
@@ -186,11 +179,17 @@ hipError_t launch_kv_pack(const uint16_t* k_pool, const uint16_t* v_pool, uint16
                           const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
                           int num_pages, int total_q, hipStream_t stream);
 
-// The same for a cache of MX blocks; bits: 4 or 8 an element.
+// The same for a cache of MX blocks; bits: 4 or 8 an element.  zero: words that the launch also clears (the
+// decode that follows it needs them cleared).
+struct ZeroWords {
+  int32_t* hdr;                                     // kHdrWords, or null
+  int32_t* cnt;
+  int n_cnt;
+};
 hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* v_new, uint8_t* cache,
                                const int32_t* block_table, int bt_stride, const int32_t* ctx_lens,
                                const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
-                               int num_pages, int total_q, hipStream_t stream);
+                               int num_pages, int total_q, const ZeroWords& zero, hipStream_t stream);
 
 hipError_t launch_kv_pack_mx(int bits, const uint8_t* cache, uint16_t* k_rows, uint16_t* v_rows,
                              const int32_t* block_table, int bt_stride, const int32_t* ctx_lens,
@@ -211,8 +210,16 @@ hipError_t launch_merge(const AttnArgs& a, int head_dim, int batch, hipStream_t 
 int decode_grid(int head_dim);
 // Sets d's run counts and grid for so many resident workgroups, from d.batch and d.max_dec.
 void set_decode_runs(DecPlanArgs& d, int num_kv_heads, int grid);
+// What a decode launch needs cleared.
+ZeroWords decode_zero_words(const AttnArgs& a, const DecPlanArgs& d);
+hipError_t launch_zero_words(const ZeroWords& zero, hipStream_t stream);
 hipError_t launch_decode_prologue(const AttnArgs& a, const DecPlanArgs& d, hipStream_t stream);
 hipError_t launch_decode(const AttnArgs& a, const DecPlanArgs& d, int head_dim, hipStream_t stream);
+
+// Decode over a cache of MX blocks, cut as the one above.
+int decode_mx_grid(int head_dim, int bits);
+hipError_t launch_decode_mx(const AttnArgs& a, const DecPlanArgs& d, const uint8_t* cache, int head_dim, int bits,
+                            hipStream_t stream);
 
 // Merge of split prefill tiles; jobs_cap bounds the device-side job count.
 hipError_t launch_merge_prefill(const AttnArgs& a, int head_dim, int64_t jobs_cap, hipStream_t stream);
