@@ -287,6 +287,17 @@ pearl_status pearl_attn_decode_append_mx(const pearl_kv_shape* shape, const pear
                                          size_t workspace_bytes, void* stream);
 
 /*
+ * pearl_attn_prefill_append over a cache of MX blocks, which must already hold the new tokens (call
+ * pearl_kv_append_mx first, on the same stream): every new token attends to its context and causally
+ * to the new ones, all as the values that the cache stands for.  Weights enter the products in bf16.  A
+ * colocated batch can take this call too: a sequence with one new token is a tile of one row.
+ */
+pearl_status pearl_attn_prefill_append_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs,
+                                          pearl_mx_format format, const void* q, const void* cache,
+                                          float softmax_scale, void* out, float* lse, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+/*
  * Timing hook for benchmarks and profilers (not part of the computation).  While a pair is set,
  * every library call made on the calling thread records `before` on its stream immediately
  * before launching its main kernel (the attention kernel for the three attention calls, the

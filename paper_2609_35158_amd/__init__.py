@@ -6,9 +6,9 @@ The Python layer only marshals arguments (see ``binding``); it has no compute fa
 from .binding import (  # noqa: F401
     LIB_PATH, MXFP4, MXFP8, PearlError, abi_version, decode, decode_append, decode_append_mx, decode_mx, kv_append,
     kv_append_mx, kv_pack, kv_pack_mx, kv_unpack, last_error, load, mixed, mx_block_bytes, mx_cache, prefill_append,
-    workspace_bytes, workspace_bytes_mx,
+    prefill_append_mx, workspace_bytes, workspace_bytes_mx,
 )
 
 __all__ = ["kv_append", "kv_pack", "kv_unpack", "prefill_append", "decode", "decode_append", "mixed", "workspace_bytes",
            "mx_cache", "mx_block_bytes", "MXFP4", "MXFP8", "kv_append_mx", "kv_pack_mx", "decode_mx",
-           "decode_append_mx", "workspace_bytes_mx", "abi_version", "last_error", "load", "PearlError", "LIB_PATH"]
+           "decode_append_mx", "prefill_append_mx", "workspace_bytes_mx", "abi_version", "last_error", "load", "PearlError", "LIB_PATH"]

@@ -45,7 +45,8 @@ EXPORTED = ("pearl_abi_version", "pearl_status_str", "pearl_last_error", "pearl_
             "pearl_attn_mixed", "pearl_kv_pack", "pearl_kv_unpack", "pearl_set_kernel_events",
             "pearl_hbm_copy", "pearl_hbm_read", "pearl_hbm_read_nt", "pearl_hbm_fill", "pearl_attn_decode_static",
             "pearl_attn_decode_static_max_bytes", "pearl_attn_decode_append", "pearl_mx_block_bytes",
-            "pearl_kv_append_mx", "pearl_kv_pack_mx", "pearl_attn_decode_mx", "pearl_attn_decode_append_mx")
+            "pearl_kv_append_mx", "pearl_kv_pack_mx", "pearl_attn_decode_mx", "pearl_attn_decode_append_mx",
+            "pearl_attn_prefill_append_mx")
 
 
 def load(path: str = LIB_PATH):
@@ -99,10 +100,11 @@ def load(path: str = LIB_PATH):
     lib.pearl_kv_pack_mx.restype = ctypes.c_int
     lib.pearl_kv_pack_mx.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                      ctypes.c_void_p]
-    lib.pearl_attn_decode_mx.restype = ctypes.c_int
-    lib.pearl_attn_decode_mx.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
-                                         ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
-                                         ctypes.c_size_t, ctypes.c_void_p]
+    for name in ("pearl_attn_decode_mx", "pearl_attn_prefill_append_mx"):
+        f = getattr(lib, name)
+        f.restype = ctypes.c_int
+        f.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_float,
+                      ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
     lib.pearl_attn_decode_append_mx.restype = ctypes.c_int
     lib.pearl_attn_decode_append_mx.argtypes = [P(KvShape), P(SeqDesc), ctypes.c_int, ctypes.c_void_p,
                                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_float,
@@ -523,6 +525,14 @@ def decode_append_mx(q, k_new, v_new, cache, block_table, ctx_lens, max_kv_len, 
     [batch][H_kv][d] are quantised into position ctx_lens[b] of every sequence, which then attends over
     ctx_lens[b] + 1 keys."""
     return _attention_mx("pearl_attn_decode_append_mx", q, (k_new, v_new), cache, block_table, ctx_lens, None, 1,
+                         max_kv_len, scale, return_lse, out, lse, workspace)
+
+
+def prefill_append_mx(q, cache, block_table, ctx_lens, cu_q_lens, max_q_len, max_kv_len, scale=None, return_lse=False,
+                      out=None, lse=None, workspace=None):
+    """Causal prefill-append attention over a cache of MX blocks that holds the new tokens
+    (pearl_attn_prefill_append_mx)."""
+    return _attention_mx("pearl_attn_prefill_append_mx", q, (), cache, block_table, ctx_lens, cu_q_lens, max_q_len,
                          max_kv_len, scale, return_lse, out, lse, workspace)
 
 

@@ -318,7 +318,8 @@ pearl_status run_decode_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pea
     return fail(PEARL_ERR_WORKSPACE, "workspace_bytes %zu < required %zu", ws_bytes, pl.lay.total);
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
   const int bits = (int)format, grid = decode_mx_grid(s->head_dim, bits);
-  const AttnArgs whole = attn_args(s, q, pl, qp, scale, out, lse, ws);
+  AttnArgs whole = attn_args(s, q, pl, qp, scale, out, lse, ws);
+  whole.cache = static_cast<const uint8_t*>(cache);
   for (int b0 = 0; b0 < q->batch; b0 += kDecPlanMaxSeqs) {
     AttnArgs a = whole;
     const size_t rows = (size_t)b0 * s->num_q_heads;
@@ -346,10 +347,46 @@ pearl_status run_decode_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pea
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "decode prologue launch: %s", hipGetErrorString(e));
     e = record_before(hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
-    e = launch_decode_mx(a, d, static_cast<const uint8_t*>(cache), s->head_dim, bits, hs);
+    e = launch_decode_mx(a, d, s->head_dim, bits, hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "decode launch: %s", hipGetErrorString(e));
     e = record_after(hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+  }
+  return debug_check(static_cast<const char*>(ws), pl, hs);
+}
+
+pearl_status run_prefill_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pearl_mx_format format, const void* qp,
+                            const void* cache, float scale, void* out, float* lse, void* ws, size_t ws_bytes,
+                            void* stream) {
+  pearl_status st = check_shape(s);
+  if (st != PEARL_OK) return st;
+  st = check_format(format);
+  if (st != PEARL_OK) return st;
+  st = check_seqs(q, false);
+  if (st != PEARL_OK) return st;
+  st = check_mx_pointers(s, q, qp, cache, out, lse, scale, ws);
+  if (st != PEARL_OK) return st;
+  const Plan pl = make_plan(s, q, kModePrefill);
+  if ((pl.lay.max_pre + pl.lay.max_dec) * (int64_t)s->num_kv_heads > INT32_MAX)
+    return fail(PEARL_ERR_UNSUPPORTED, "work list bound (%lld entries x %d kv-heads) exceeds int32",
+                (long long)(pl.lay.max_pre + pl.lay.max_dec), s->num_kv_heads);
+  if (ws_bytes < pl.lay.total)
+    return fail(PEARL_ERR_WORKSPACE, "workspace_bytes %zu < required %zu", ws_bytes, pl.lay.total);
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  hipError_t e = launch_plan(pl.p, q->ctx_lens, q->cu_q_lens, ws, pl.lay, hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "plan launch: %s", hipGetErrorString(e));
+  AttnArgs a = attn_args(s, q, pl, qp, scale, out, lse, ws);
+  a.cache = static_cast<const uint8_t*>(cache);
+  e = record_before(hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+  e = launch_prefill_mx(a, s->head_dim, (int)format, (pl.lay.max_pre + pl.lay.max_dec) * s->num_kv_heads,
+                        (int)pl.lay.max_pre, hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "attention launch: %s", hipGetErrorString(e));
+  e = record_after(hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+  if (pl.p.pre_jobs_cap > 0) {
+    e = launch_merge_prefill(a, s->head_dim, pl.p.pre_jobs_cap, hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "prefill merge launch: %s", hipGetErrorString(e));
   }
   return debug_check(static_cast<const char*>(ws), pl, hs);
 }
@@ -588,6 +625,18 @@ pearl_status pearl_attn_decode_mx(const pearl_kv_shape* shape, const pearl_seq_d
                          workspace_bytes, stream);
   } catch (...) {
     return fail(PEARL_ERR_HIP, "unexpected exception in pearl_attn_decode_mx");
+  }
+}
+
+pearl_status pearl_attn_prefill_append_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs,
+                                          pearl_mx_format format, const void* q, const void* cache,
+                                          float softmax_scale, void* out, float* lse, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+  try {
+    g_err[0] = 0;
+    return run_prefill_mx(shape, seqs, format, q, cache, softmax_scale, out, lse, workspace, workspace_bytes, stream);
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_attn_prefill_append_mx");
   }
 }
 

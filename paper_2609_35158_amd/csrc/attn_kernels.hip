@@ -27,6 +27,7 @@
 
 #include "attn_device.h"
 #include "decode_shares.h"
+#include "mx_format.h"
 
 #include <math.h>
 
@@ -580,6 +581,86 @@ template <int D, int KEYS = kKeysPerStage> struct DmaTile {
   }
 };
 
+// A wave's half page (8 tokens) of a K and of a V stage in MX blocks, as loaded, and its bf16 rows in DmaTile's
+// layout.
+template <int D, int kBits> struct MxStage {
+  using MX = MxBlock<D, kBits>;
+  using DT = DmaTile<D>;
+  static constexpr int KW = D * kBits / 256;        // dwords of D / 8 channels of a token row
+  static constexpr int VT = D / 16;                 // tokens of a lane's channel pair
+  static constexpr int VW = VT * kBits / 16;        // dwords of them
+  uint32_t k[KW], ks, v[VW], vs[VT / 4];
+  int k_at, ks_at, v_at, vs_at;                     // this lane's places in a block
+  __device__ __forceinline__ MxStage(int lane, int w) {
+    const int half = 8 * (w & 1), row = half + lane / 8, piece = lane % 8;
+    k_at = row * MX::kRow + piece * (MX::kRow / 8);
+    ks_at = MX::k_scale(row, piece * (D / 8) / 32);
+    const int pair = lane % (D / 2), slot = half + lane / (D / 2) * VT;
+    v_at = MX::v_code(slot, pair);
+    vs_at = MX::v_scale(slot, pair / 16);
+  }
+  template <int N> __device__ static __forceinline__ void load_words(uint32_t* x, const uint8_t* p) {
+    if constexpr (N == 1) {
+      x[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (N == 2) {
+      const u32x2 y = *reinterpret_cast<const u32x2*>(p);
+      x[0] = y[0];
+      x[1] = y[1];
+    } else {
+      const u32x4 y = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = y[i];
+    }
+  }
+  __device__ __forceinline__ void load_k(const uint8_t* blk) {
+    load_words<KW>(k, blk + k_at);
+    ks = blk[ks_at];
+  }
+  __device__ __forceinline__ void load_v(const uint8_t* blk) {
+    load_words<VW>(v, blk + v_at);
+    load_words<VT / 4>(vs, blk + vs_at);
+  }
+  // K: D / 64 chunks of 8 channels of token row 8 w + lane / 8
+  __device__ __forceinline__ void store_k(char* dst, int w) const {
+    const int lane = threadIdx.x & 63, r = 8 * w + lane / 8, c0 = lane % 8 * (D / 64);
+    const float f = mx_scale(ks);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      u32x4 x;
+      if constexpr (kBits == 4)
+        x = u32x4{mx_up<4, 0>(k[c], f), mx_up<4, 1>(k[c], f), mx_up<4, 2>(k[c], f), mx_up<4, 3>(k[c], f)};
+      else
+        x = u32x4{mx_up<8, 0>(k[2 * c], f), mx_up<8, 1>(k[2 * c], f), mx_up<8, 0>(k[2 * c + 1], f), mx_up<8, 1>(k[2 * c + 1], f)};
+      *reinterpret_cast<u32x4*>(dst + r * DT::RB + (((c0 + c) ^ DT::swz(r)) << 4)) = x;
+    }
+  }
+  // V: a dword (a channel pair of one token) at a time, a wave's lanes a whole row; of this wave's 8 tokens only
+  // the first `left` count, the others become zeros
+  __device__ __forceinline__ void store_v(char* dst, int w, int left) const {
+    const int lane = threadIdx.x & 63, pair = lane % (D / 2), t0 = lane / (D / 2) * VT;
+    auto put = [&](auto t_c) {
+      constexpr int t = decltype(t_c)::value;
+      if constexpr (t < VT) {
+        const int r = 8 * w + t0 + t;
+        const float f = mx_scale_of<t % 4>(vs[t / 4]);
+        uint32_t x;
+        if constexpr (kBits == 4) x = mx_up<4, t % 4>(v[t / 4], f);
+        else x = mx_up<8, t % 2>(v[t / 2], f);
+        if (left < 8) x = t0 + t < left ? x : 0u;
+        *reinterpret_cast<uint32_t*>(dst + r * DT::RB + (((pair >> 2) ^ DT::swz(r)) << 4) + (pair & 3) * 4) = x;
+      }
+    };
+    put(std::integral_constant<int, 0>{});
+    put(std::integral_constant<int, 1>{});
+    put(std::integral_constant<int, 2>{});
+    put(std::integral_constant<int, 3>{});
+    put(std::integral_constant<int, 4>{});
+    put(std::integral_constant<int, 5>{});
+    put(std::integral_constant<int, 6>{});
+    put(std::integral_constant<int, 7>{});
+  }
+};
+
 // ------------------------------------------------------------------------------------------------
 // Prefill-append work item: one (sequence, kv-head g, q-tile).  The tile holds 256 q-rows =
 // tokens_per_tile tokens x G heads of the group (row rho -> token rho / G, head rho % G), so every
@@ -614,8 +695,13 @@ template <int D, int KEYS = kKeysPerStage> struct DmaTile {
 // Before the barrier that ends phase 2j-1 every wave waits for its own copies of K(j) and V(j-1)
 // (the copies issued since stay in flight).
 // ------------------------------------------------------------------------------------------------
+//
+// Over a cache of MX blocks (kBits 4 or 8 an element; 0: bf16 pools) only the way of a stage into its buffers
+// differs: a wave loads its 8 tokens' codes and scales of K(j+3) and V(j+2) into registers in its softmax phase of
+// pair j, after it has turned those it loaded a pair before, K(j+2) and V(j+1), into bf16 (exactly) and
+// stored them in the same buffers.  Everything from the buffers on is the same.
 // at_end: called by every thread when the stages are done, before the epilogue.
-template <int D, typename AtEnd>
+template <int D, int kBits, typename AtEnd>
 __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int code, int g, char* kb0, char* vb0, AtEnd at_end) {
   constexpr int KB = D / 16;                        // 16-wide k blocks of the QK product
   constexpr int MB = D / 32;                        // 32-wide dim blocks of the PV product
@@ -675,7 +761,7 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
   const int gi = lane >> 4, jl = lane & 15;
   const int krow = 4 * (gi >> 1) + (jl >> 2);
   const int dcol = 16 * (gi & 1) + 4 * (jl & 3);
-  int koff[KB], voff[2][MB], goff[DT::NDMA];
+  int koff[KB], voff[2][MB], goff[DT::NDMA];        // goff: bf16 pools only
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) koff[kb] = (lane & 31) * RB + (((2 * kb + half) ^ DT::swz(lane & 15)) << 4);
 #pragma unroll
@@ -715,8 +801,17 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
     }
   };
 
+  // MX blocks: this wave's 8 tokens of a K and a V stage as loaded, and their way into the buffers.  K: 8 lanes
+  // a token row, D / 8 channels each.  V: a channel pair a lane, for D / 16 tokens.
+  static_assert(kBits == 0 || DT::RPW == 8, "a wave's tokens of a stage are half a page");
+  MxStage<D, kBits == 0 ? 4 : kBits> raw(lane, w);
+  auto mx_block = [&](int entry) {
+    return a.cache + ((size_t)clamp_page(entry, a.num_pages) * H_kv + g) * MxStage<D, kBits == 0 ? 4 : kBits>::MX::kBytes;
+  };
+  auto mx_store_v = [&](int j, char* dst) { raw.store_v(dst, w, kv_needed - ((step_begin + j) * SK + DT::RPW * w)); };
+
   // block-table entries of the next copies: pid_k for K rows, pid_v for V rows (pid_n: the K
-  // rows after those, read ahead by group B)
+  // rows after those, read ahead by group B).  MX blocks: of the next loads, of stages j + 3 and j + 2.
   int pid_v = 1 < n ? page_of(1) : 0, pid_k = 2 < n ? page_of(2) : 0, pid_n = 0;
 
   f32x16 s[NST];                                    // S^T of the stage between its M and V phases
@@ -858,6 +953,10 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
   // the barrier without the release fence of __syncthreads (which would drain every copy)
   constexpr int P = DT::NDMA;                       // DMA instructions per tensor and stage
   auto end_phase = [&](int t) {
+    if constexpr (kBits != 0) {                     // the compiler waits for its loads itself, where it uses them
+      __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      return;
+    }
     if ((t & 1) == 0) {
       const int i = t >> 1;
       if (i + 2 < n) __builtin_amdgcn_s_waitcnt(PEARL_VMCNT(P));   // K(i + 2) stays in flight
@@ -873,17 +972,50 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
   // reads' counter and complete out of order, so one in flight during an M phase would make
   // every operand wait drain the counter, and one used right away would stall the phase for a
   // memory round trip.  The end-of-phase drain completes them.
-  {
-    const int p0 = page_of(0);
-    dma(0, false, p0, kbuf(0));
-    dma(0, true, p0, vbuf(0));
-  }
-  if (1 < n) dma(1, false, pid_v, kbuf(1));
+  if constexpr (kBits == 0) {
+    {
+      const int p0 = page_of(0);
+      dma(0, false, p0, kbuf(0));
+      dma(0, true, p0, vbuf(0));
+    }
+    if (1 < n) dma(1, false, pid_v, kbuf(1));
 #pragma unroll
-  for (int i = 0; i < DT::NDMA; ++i)
-    lds_dma16_untracked(zero_src, vbuf(2) + (DT::RPW * w + DT::RPI * i) * RB);
-  __builtin_amdgcn_s_waitcnt(PEARL_VMCNT(0));       // Q loads and the first copies (also this item's)
-  __asm__ volatile("s_barrier" ::: "memory");
+    for (int i = 0; i < DT::NDMA; ++i)
+      lds_dma16_untracked(zero_src, vbuf(2) + (DT::RPW * w + DT::RPI * i) * RB);
+    __builtin_amdgcn_s_waitcnt(PEARL_VMCNT(0));     // Q loads and the first copies (also this item's)
+    __asm__ volatile("s_barrier" ::: "memory");
+  } else {
+    const uint8_t* b0 = mx_block(page_of(0));
+    raw.load_k(b0);
+    raw.load_v(b0);
+    raw.store_k(kbuf(0), w);
+    mx_store_v(0, vbuf(0));
+    if (1 < n) {
+      raw.load_k(mx_block(pid_v));
+      raw.store_k(kbuf(1), w);
+      raw.load_v(mx_block(pid_v));                  // pair 0: K(2), V(1)
+    }
+    if (2 < n) raw.load_k(mx_block(pid_k));
+#pragma unroll
+    for (int i = 0; i < DT::BYTES / (kThreads * 16); ++i)
+      *reinterpret_cast<u32x4*>(vbuf(2) + (i * kThreads + threadIdx.x) * 16) = u32x4{0u, 0u, 0u, 0u};
+    pid_v = pid_k;
+    if (3 < n) pid_k = page_of(3);
+    __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+  // MX blocks, in the softmax phase of pair j (R = j % 3): what was loaded for the pair goes into the buffers, the
+  // next pair's loads go out.
+  auto mx_pair = [&](auto r_c, int j) {
+    constexpr int R = decltype(r_c)::value;
+    if (j + 1 < n) mx_store_v(j + 1, vbuf((R + 1) % 3));
+    if (j + 2 < n) {
+      raw.store_k(kbuf((R + 2) % 3), w);
+      raw.load_v(mx_block(pid_v));
+    }
+    if (j + 3 < n) raw.load_k(mx_block(pid_k));
+    pid_v = pid_k;
+    if (j + 4 < n) pid_k = page_of(j + 4);
+  };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
   using I2 = std::integral_constant<int, 2>;
@@ -897,12 +1029,17 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
     auto step = [&](auto r_c, int j, auto first_c) {
       constexpr int R = decltype(r_c)::value;
       phase_m(r_c, !decltype(first_c)::value);
-      copy_k(r_c, j);
+      if constexpr (kBits == 0) copy_k(r_c, j);
       end_phase(2 * j);
-      copy_v(r_c, j);
-      pid_v = pid_k;
-      if (j + 3 < n) pid_k = page_of(j + 3);
-      phase_v(j);
+      if constexpr (kBits == 0) {
+        copy_v(r_c, j);
+        pid_v = pid_k;
+        if (j + 3 < n) pid_k = page_of(j + 3);
+        phase_v(j);
+      } else {
+        phase_v(j);
+        mx_pair(r_c, j);
+      }
       prefetch(std::integral_constant<int, (R + 1) % 3>{});
       end_phase(2 * j + 1);
     };
@@ -929,22 +1066,35 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
       pid_k = pid_n;
     };
     auto step = [&](auto r_c, int j) {
-      copy_k(r_c, j);
-      if (j + 3 < n) pid_n = page_of(j + 3);
-      phase_v(j - 1);
+      if constexpr (kBits == 0) {
+        copy_k(r_c, j);
+        if (j + 3 < n) pid_n = page_of(j + 3);
+        phase_v(j - 1);
+      } else {
+        phase_v(j - 1);
+        mx_pair(r_c, j);
+      }
       prefetch(r_c);
       end_phase(2 * j);
       phase_m(r_c, true);
-      copy_v(r_c, j);
-      pair_done();
+      if constexpr (kBits == 0) {
+        copy_v(r_c, j);
+        pair_done();
+      }
       end_phase(2 * j + 1);
     };
-    copy_k(I0{}, 0);
-    if (3 < n) pid_n = page_of(3);
+    if constexpr (kBits == 0) {
+      copy_k(I0{}, 0);
+      if (3 < n) pid_n = page_of(3);
+    } else {
+      mx_pair(I0{}, 0);
+    }
     end_phase(0);
     phase_m(I0{}, false);
-    copy_v(I0{}, 0);
-    pair_done();
+    if constexpr (kBits == 0) {
+      copy_v(I0{}, 0);
+      pair_done();
+    }
     end_phase(1);
     int j = 1;
     for (; j + 3 <= n + 1; j += 3) {
@@ -1362,14 +1512,16 @@ __device__ __forceinline__ void decode_split(const AttnArgs& a, const DecItem& i
 // through atomic counters (the next item is claimed as the current one ends); prefill tiles
 // come first (largest work), decode splits fill the tail.
 // ------------------------------------------------------------------------------------------------
-// kKinds: 1 = prefill tiles only, 2 = decode splits only, 3 = both (mixed batches).
+// kKinds: 1 = prefill tiles only, 2 = decode splits only, 3 = both (mixed batches).  kBits: bits of an element
+// in a cache of MX blocks (prefill only), 0 for the bf16 pools.
 template <int D, int kKinds> struct KernelCfg {
   static constexpr int NW = kWaves;
   static constexpr int NT = NW * 64;
 };
 
-template <int D, int kKinds>
+template <int D, int kKinds, int kBits = 0>
 __global__ __launch_bounds__((KernelCfg<D, kKinds>::NT)) void attn_kernel(AttnArgs a, int max_pre) {
+  static_assert(kBits == 0 || kKinds == 1, "MX blocks: prefill only");
   constexpr int NW = KernelCfg<D, kKinds>::NW;
   __shared__ __attribute__((aligned(16))) char smem[Lds<D, NW, kKinds>::bytes];
   // the two stages of the decode pipeline are separate objects so the LDS reads of one are
@@ -1475,13 +1627,13 @@ __global__ __launch_bounds__((KernelCfg<D, kKinds>::NT)) void attn_kernel(AttnAr
         static_assert(NW == kWaves, "prefill tiles use 8 waves");
         const int2 en = a.entries[e];
         if constexpr (kKinds == 1) {
-          prefill_tile_pp<D>(a, en.x, en.y, g, pk, pv, send_claim);
+          prefill_tile_pp<D, kBits>(a, en.x, en.y, g, pk, pv, send_claim);
         } else {
           // the mixed kernel's prefill stage buffers share its LDS region with the decode stages (a
           // workgroup runs one item at a time, and items are separated by a drained barrier)
           constexpr int B = DmaTile<D>::BYTES;
           static_assert(6 * B <= Lds<D, NW, kKinds>::bytes, "stage buffers fit the shared region");
-          prefill_tile_pp<D>(a, en.x, en.y, g, smem, smem + 3 * B, send_claim);
+          prefill_tile_pp<D, 0>(a, en.x, en.y, g, smem, smem + 3 * B, send_claim);
         }
       }
     } else {
@@ -1890,14 +2042,15 @@ struct DevCache {
   int num_cu = 0;
   int occ[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};   // [D == 128][kinds]
   int occ_dec[2] = {0, 0};                        // decode_kernel, [D == 128]
+  int occ_mx[2][2] = {{0, 0}, {0, 0}};            // prefill over MX blocks, [D == 128][8 bits]
   void* scratch = nullptr;                        // device address of this device's scratch array
   hipError_t scratch_err = hipSuccess;
 };
 
-template <int D, int K>
+template <int D, int K, int kBits = 0>
 int occupancy_of() {
   int o = 1;
-  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&o, attn_kernel<D, K>, KernelCfg<D, K>::NT, 0) != hipSuccess || o < 1) o = 1;
+  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&o, attn_kernel<D, K, kBits>, KernelCfg<D, K>::NT, 0) != hipSuccess || o < 1) o = 1;
   return o;
 }
 
@@ -1914,6 +2067,8 @@ void fill_cache(DevCache& c, int dev) {
   if (hipGetDeviceProperties(&prop, dev) == hipSuccess && prop.multiProcessorCount > 0) ncu = prop.multiProcessorCount;
   c.occ[0][1] = occupancy_of<64, 1>(); c.occ[0][2] = occupancy_of<64, 2>(); c.occ[0][3] = occupancy_of<64, 3>();
   c.occ[1][1] = occupancy_of<128, 1>(); c.occ[1][2] = occupancy_of<128, 2>(); c.occ[1][3] = occupancy_of<128, 3>();
+  c.occ_mx[0][0] = occupancy_of<64, 1, 4>(); c.occ_mx[0][1] = occupancy_of<64, 1, 8>();
+  c.occ_mx[1][0] = occupancy_of<128, 1, 4>(); c.occ_mx[1][1] = occupancy_of<128, 1, 8>();
   c.occ_dec[0] = occupancy_of_dec<64>(); c.occ_dec[1] = occupancy_of_dec<128>();
   c.num_cu = ncu;
   void* p = nullptr;
@@ -1988,6 +2143,16 @@ hipError_t launch_attention(const AttnArgs& a, int head_dim, int kinds, int64_t 
     else if (kinds == 2) hipLaunchKernelGGL((attn_kernel<128, 2>), g, dim3(KernelCfg<128, 2>::NT), 0, stream, a, max_pre);
     else hipLaunchKernelGGL((attn_kernel<128, 3>), g, dim3(KernelCfg<128, 3>::NT), 0, stream, a, max_pre);
   }
+  return hipGetLastError();
+}
+
+hipError_t launch_prefill_mx(const AttnArgs& a, int head_dim, int bits, int64_t max_items, int max_pre, hipStream_t stream) {
+  if (max_items <= 0) return hipSuccess;
+  const DevCache& c = dev_cache();
+  const int64_t grid = std::min<int64_t>((int64_t)c.num_cu * c.occ_mx[head_dim == 128][bits == 8], max_items);
+  auto kernel = head_dim == 64 ? (bits == 4 ? attn_kernel<64, 1, 4> : attn_kernel<64, 1, 8>)
+                               : (bits == 4 ? attn_kernel<128, 1, 4> : attn_kernel<128, 1, 8>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(KernelCfg<128, 1>::NT), 0, stream, a, max_pre);
   return hipGetLastError();
 }
 

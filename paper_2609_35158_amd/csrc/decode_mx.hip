@@ -232,7 +232,7 @@ __device__ __forceinline__ void consume(Unit<D, kBits>& u, const bf16x8* qop, f3
 }  // namespace
 
 template <int D, int kBits>
-__global__ __launch_bounds__(kThreads, 2) void decode_mx_kernel(AttnArgs a, DecPlanArgs d, const uint8_t* cache) {
+__global__ __launch_bounds__(kThreads, 2) void decode_mx_kernel(AttnArgs a, DecPlanArgs d) {
   using MX = MxBlock<D, kBits>;
   using U = Unit<D, kBits>;
   constexpr int KB = D / 32, TP = U::TP;
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mx_kernel(AttnArgs a, DecP
     const ConstI32Ptr bt = (ConstI32Ptr)a.block_table;
     const Lane<D, kBits> at(lane);
     const size_t page_bytes = (size_t)H * MX::kBytes;
-    const uint8_t* const heads = cache + (size_t)g * MX::kBytes;
+    const uint8_t* const heads = a.cache + (size_t)g * MX::kBytes;
     struct Ids { int x[kUnitPages]; };
     // a unit: up to four pages of the cursor's sequence; `left` pages of the share from its first page on
     auto pages_of = [&](const PageCursor& c, int left) { return min(min(kUnitPages, c.np - c.p), left); };
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mx_kernel(AttnArgs a, DecP
 // host launchers
 // ------------------------------------------------------------------------------------------------
 namespace {
-typedef void (*DecodeMx)(AttnArgs, DecPlanArgs, const uint8_t*);
+typedef void (*DecodeMx)(AttnArgs, DecPlanArgs);
 DecodeMx decode_mx_of(int head_dim, int bits) {
   return head_dim == 64 ? (bits == 4 ? decode_mx_kernel<64, 4> : decode_mx_kernel<64, 8>)
                         : (bits == 4 ? decode_mx_kernel<128, 4> : decode_mx_kernel<128, 8>);
@@ -439,9 +439,8 @@ int decode_mx_grid(int head_dim, int bits) {
   return device_num_cu() * occ;
 }
 
-hipError_t launch_decode_mx(const AttnArgs& a, const DecPlanArgs& d, const uint8_t* cache, int head_dim, int bits,
-                            hipStream_t stream) {
-  hipLaunchKernelGGL(decode_mx_of(head_dim, bits), dim3((unsigned)d.grid), dim3(kThreads), 0, stream, a, d, cache);
+hipError_t launch_decode_mx(const AttnArgs& a, const DecPlanArgs& d, int head_dim, int bits, hipStream_t stream) {
+  hipLaunchKernelGGL(decode_mx_of(head_dim, bits), dim3((unsigned)d.grid), dim3(kThreads), 0, stream, a, d);
   return hipGetLastError();
 }
 

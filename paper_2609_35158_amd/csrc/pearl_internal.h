@@ -110,6 +110,7 @@ struct AttnArgs {
   const uint16_t* q;
   const uint16_t* k_pool;
   const uint16_t* v_pool;
+  const uint8_t* cache;      // calls on MX blocks: in place of the pools
   const int32_t* block_table;
   uint16_t* out;
   float* lse;                // may be null
@@ -203,6 +204,9 @@ hipError_t launch_plan(const PlanParams& p, const int32_t* ctx_lens, const int32
 hipError_t launch_attention(const AttnArgs& a, int head_dim, int kinds, int64_t max_items, int max_pre,
                             hipStream_t stream);
 
+// Prefill tiles over a cache of MX blocks.
+hipError_t launch_prefill_mx(const AttnArgs& a, int head_dim, int bits, int64_t max_items, int max_pre, hipStream_t stream);
+
 hipError_t launch_merge(const AttnArgs& a, int head_dim, int batch, hipStream_t stream);
 
 // Decode planned in-kernel (batch <= kDecPlanMaxSeqs): the zeroing prologue, then the kernel.
@@ -218,8 +222,7 @@ hipError_t launch_decode(const AttnArgs& a, const DecPlanArgs& d, int head_dim, 
 
 // Decode over a cache of MX blocks, cut as the one above.
 int decode_mx_grid(int head_dim, int bits);
-hipError_t launch_decode_mx(const AttnArgs& a, const DecPlanArgs& d, const uint8_t* cache, int head_dim, int bits,
-                            hipStream_t stream);
+hipError_t launch_decode_mx(const AttnArgs& a, const DecPlanArgs& d, int head_dim, int bits, hipStream_t stream);
 
 // Merge of split prefill tiles; jobs_cap bounds the device-side job count.
 hipError_t launch_merge_prefill(const AttnArgs& a, int head_dim, int64_t jobs_cap, hipStream_t stream);

@@ -9,7 +9,7 @@ import torch
 import oracle
 import paper_2609_35158_amd as pa
 from paper_2609_35158_amd import binding as bd
-from test_abi import FAKE, INVALID, UNSUPPORTED, desc, shape
+from test_abi import FAKE, INVALID, UNSUPPORTED, WORKSPACE, desc, shape
 
 FORMATS = (pa.MXFP4, pa.MXFP8)
 
@@ -155,3 +155,45 @@ def test_binding_checks_tensors_before_the_library():
         pa.kv_pack_mx(cache, bt, ctx, None, 3, 1, 1)
     with pytest.raises(TypeError, match="cache"):
         pa.kv_pack_mx(cache.float(), bt, ctx, None, 3, 1, 1)
+
+
+ATTENTION = ("pearl_attn_decode_mx", "pearl_attn_decode_append_mx", "pearl_attn_prefill_append_mx")
+
+
+@pytest.mark.parametrize("fn", ATTENTION)
+def test_attention_refusals(fn):
+    f = getattr(pa.load(), fn)
+    prefill, append = fn == ATTENTION[2], fn == ATTENTION[1]
+
+    def call(s, d, fmt=4, q=FAKE, k=FAKE, v=FAKE, cache=FAKE, scale=0.1, out=FAKE, lse=None, ws=FAKE, wsb=1 << 30):
+        st = f(None if s is None else ctypes.byref(s), None if d is None else ctypes.byref(d), fmt, q,
+               *((k, v) if append else ()), cache, scale, out, lse, ws, wsb, None)
+        return st, pa.last_error()
+
+    ok = dict(cu=FAKE, total=9, max_q=5) if prefill else {}
+    assert call(None, desc(**ok))[0] == INVALID
+    assert call(shape(), None)[0] == INVALID
+    for fmt in (0, 3, 9):
+        st, msg = call(shape(), desc(**ok), fmt=fmt)
+        assert st == UNSUPPORTED and "format" in msg
+    for s in (shape(d=80), shape(ps=8), shape(hq=24), shape(hq=128, hkv=8)):
+        assert call(s, desc(**ok))[0] == UNSUPPORTED
+    assert call(shape(hkv=5), desc(**ok))[0] == INVALID
+    for bad in (dict(batch=0), dict(stride=0), dict(stride=10, max_kv=1000)):
+        assert call(shape(), desc(**dict(ok, **bad)))[0] == INVALID
+    for name in ("q", "cache", "out") + (("k", "v") if append else ()):
+        assert call(shape(), desc(**ok), **{name: None})[0] == INVALID
+        st, msg = call(shape(), desc(**ok), **{name: FAKE + 8})
+        assert st == INVALID and "aligned" in msg, name
+    assert call(shape(), desc(**ok), lse=FAKE + 2)[0] == INVALID
+    assert call(shape(), desc(**ok), ws=None)[0] == WORKSPACE
+    assert call(shape(), desc(**ok), ws=FAKE + 16)[0] == WORKSPACE
+    st, msg = call(shape(), desc(**ok), wsb=100)
+    assert st == WORKSPACE and "100" in msg
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert call(shape(), desc(**ok), scale=scale)[0] == INVALID
+    if not prefill:
+        st, msg = call(shape(), desc(cu=FAKE))
+        assert st == INVALID and "cu_q_lens" in msg
+        assert call(shape(), desc(total=5))[0] == INVALID
+    assert call(shape(), desc(batch=1, stride=(1 << 21) + 1, max_kv=(1 << 25) + 1, **({} if not prefill else dict(cu=FAKE, total=1))))[0] == UNSUPPORTED
