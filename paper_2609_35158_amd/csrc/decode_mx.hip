@@ -3,24 +3,25 @@
 // sequence is what a decode step costs).
 //
 // The launch is cut as decode_kernel's (decode_shares.h): every wave streams an equal run of the batch's
-// pages, whatever the lengths.  A wave takes four pages (64 keys) of a sequence at a time:
+// pages, whatever the lengths.  A wave takes a unit of kPages pages of a sequence at a time:
 //   S^T (keys x heads)   = K . Q^T      16x16x32 MFMA, A = K rows, B = the group's queries
-//   O^T (dims x heads)  += V^T . P^T    16x16x32 MFMA, A = V^T, B = the weights
-// and holds no tile in LDS: the cache's layout gives each lane its operands in 16-byte loads.
-//   * Lane l loads, of K tile t (t = 0..3), the row of page (l % 16) / 4, slot 4 t + l % 4, channels of k group
-//     l / 16, and of V the channel pairs 16 p + l % 16 (p = 0 .. D/32 - 1) of page l / 16, all its 16 tokens.
-//   * So tile t's S^T holds in lane l, rows 4 (l / 16) + i, the scores of page l / 16, slots 4 t + i: the 16
-//     slots of the page whose V that lane holds.  The weights are P.V's B operand as they are.
-//   * Elements are turned into bf16 by the conversion instructions, which apply the scale: exact.  K pairs are
-//     neighbouring channels under one scale and are operands at once; V pairs are two channels of one
-//     token, and one byte permute per two tokens sorts them by channel.
-// The products have 16 columns for at most 8 heads.  Columns 0..7 and 8..15 hold the same queries, and the weights
-// enter P.V in two bf16 parts, the upper 8 significant bits in one half of the columns and the rest in the
-// other; their outputs are added when the pair is done.  Weights to 16 bits cost no product more.
-// The running maximum may lag the true one by 8 (log2 units), as in the prefill kernel, so most steps find no maximum.
-//
-// What bounds it: the loads of four pages are sent before the four pages before them are computed, so
-// 8 waves hold about 70 KB (4 bits) in flight per compute unit.
+//   O^T (pairs x heads) += V^T . P^T    16x16x32 MFMA, A = channel pairs of V, B = the weights
+// A unit travels by LDS-DMA, block by block as it lies in memory (1 KiB an instruction), into the wave's two
+// buffers; the next unit's copies are in flight while one is attended.
+//   * Lane group g = l / 16 of the products holds the unit's tokens TG g .. TG g + TG - 1 (TG = 4 kPages).
+//     Row 4 g + i of K tile t is token 4 t + i of group g, so the scores of tile t come out, in the lanes of
+//     group g, as those of the tokens whose V those lanes hold: the weights are P.V's operand as they are.
+//   * Elements are turned into bf16 by the conversion instructions, which apply the scale: exact.  A K
+//     conversion gives two neighbouring channels, an operand's dword.  A V conversion gives the two
+//     channels of a pair for one token, and goes into the product as it is, as two contraction indices (token, even)
+//     and (token, odd): the products have 16 columns for at most 8 heads, so columns 0..7 hold the weights
+//     at the even indices and columns 8..15 at the odd ones (zeros at the others), and give the even and
+//     the odd channels.  (Sorted by channel first, with a byte permute per two tokens, the conversion of V
+//     took 192 instructions a unit instead of 128.)
+// Weights enter P.V in two bf16 parts, the nearest bf16 and the rest, in a product each: 16 bits of a weight.  One
+// part alone is 2-6% faster (64 sequences of 2K-16K tokens 122.4 us, with both 125.9) but off by up to 2^-9 a
+// weight, as much as rounding the outputs to bf16 is.
+// The running maximum may lag the true one by 8 (log2 units), as in the prefill kernel: most units look for none.
 
 #include "decode_shares.h"
 #include "mx_format.h"
@@ -33,214 +34,237 @@ namespace pearl {
 
 namespace {
 
-constexpr int kUnitPages = 4;                       // pages of a step
-
 struct MxCut {                                      // 2176 bytes of K and V a page and kv-head at 4 bits, d = 128
   static constexpr int kMinPages = 32, kPieceCost = 8, kWholePages = 56;
 };
 
-// Four pages' codes and scales as a lane holds them.
+// A unit: kPages pages of one (sequence, kv-head) and how they lie in a wave's buffer.
 template <int D, int kBits> struct Unit {
-  static constexpr int KW = D * kBits / 128;        // dwords of a K row and lane
+  using MX = MxBlock<D, kBits>;
+  static constexpr int kPages = D == 128 && kBits == 8 ? 2 : 4;
+  static constexpr int TG = 4 * kPages;             // tokens of a lane group
+  static constexpr int KB = D / 32;                 // 32-channel steps of the Q.K product
   static constexpr int TP = D / 32;                 // groups of 16 channel pairs
-  static constexpr int VW = kBits;                  // dwords of a channel pair's 16 tokens
-  static constexpr int KS = D == 128 && kBits == 8 ? 2 : 1;   // blocks of a lane's K channels
-  uint32_t k[4][KW];
-  uint32_t v[TP][VW];
-  u32x4 vs[TP];
-  uint32_t ks[KS];
+  static constexpr int kCopies = 2 * MX::kCodes / 1024;   // 1 KiB copies of a page's codes
+  static constexpr int kPageBytes = 2 * MX::kCodes + 16;  // 16 bytes apart mod 256: K rows of 4 pages on other banks
+  static constexpr int kScaleBytes = MX::kBytes - 2 * MX::kCodes;
+  static constexpr int kScales = kPages * kPageBytes;     // offset of the pages' scales
+  static constexpr int kBytes = kScales + kPages * kScaleBytes;
+  static constexpr int kLoads = kPages * kCopies + 1;     // copy instructions of a unit
+  static_assert(kCopies >= 1 && kCopies * 1024 == 2 * MX::kCodes && kPages * kScaleBytes <= 1024, "copies");
 };
 
-// The first channel of k-step ks of a lane's k group: 16-byte pieces of a row, in the order they are loaded.
+// The first channel of k-step ks of a lane group: 16-byte pieces of a row where a group holds more.
 template <int D, int kBits> __device__ __forceinline__ int k_channel(int group, int ks) {
   if constexpr (D == 128 && kBits == 8) return 64 * (ks >> 1) + 16 * group + 8 * (ks & 1);
   else return D / 4 * group + 8 * ks;
 }
 
-template <int N> __device__ __forceinline__ void load_words(uint32_t* dst, const uint8_t* src) {
-  if constexpr (N == 2) {
-    const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(src));
-    dst[0] = x[0];
-    dst[1] = x[1];
+// 1 KiB from base + 16 lane (+ 1024 i) to LDS at lds + 16 lane (+ 1024 i), i < N: as lds_dma16 in the bf16 kernels.
+template <int N> __device__ __forceinline__ void copy_codes(const uint8_t* base, int lane16, unsigned lds) {
+  unsigned saved;
+  if constexpr (N == 1)
+    __asm__ volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+                     "global_load_lds_dwordx4 %3, %2 nt\n\t"
+                     "s_mov_b32 m0, %0"
+                     : "=&s"(saved) : "s"(lds), "s"(base), "v"(lane16) : "memory");
+  else if constexpr (N == 2)
+    __asm__ volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+                     "global_load_lds_dwordx4 %3, %2 nt\n\t"
+                     "global_load_lds_dwordx4 %3, %2 offset:1024 nt\n\t"
+                     "s_mov_b32 m0, %0"
+                     : "=&s"(saved) : "s"(lds), "s"(base), "v"(lane16) : "memory");
+  else
+    __asm__ volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+                     "global_load_lds_dwordx4 %3, %2 nt\n\t"
+                     "global_load_lds_dwordx4 %3, %2 offset:1024 nt\n\t"
+                     "global_load_lds_dwordx4 %3, %2 offset:2048 nt\n\t"
+                     "global_load_lds_dwordx4 %3, %2 offset:3072 nt\n\t"
+                     "s_mov_b32 m0, %0"
+                     : "=&s"(saved) : "s"(lds), "s"(base), "v"(lane16) : "memory");
+}
+__device__ __forceinline__ void copy_scales(const uint8_t* at, unsigned lds) {   // 16 bytes a lane from its own address
+  unsigned saved;
+  __asm__ volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                   "global_load_lds_dwordx4 %1, off nt\n\t"
+                   "s_mov_b32 m0, %0"
+                   : "=&s"(saved) : "v"(at), "s"(lds) : "memory");
+}
+
+template <int N> __device__ __forceinline__ void lds_words(uint32_t* x, const char* p) {
+  if constexpr (N == 1) {
+    x[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (N == 2) {
+    const u32x2 y = *reinterpret_cast<const u32x2*>(p);
+    x[0] = y[0];
+    x[1] = y[1];
   } else {
-    const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dst[i] = x[i];
+    for (int i = 0; i < N; i += 4) {
+      const u32x4 y = *reinterpret_cast<const u32x4*>(p + 4 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i + j] = y[j];
+    }
   }
 }
 
-template <int D, int kBits> struct Lane {           // a lane's offsets in a block
-  using MX = MxBlock<D, kBits>;
-  using U = Unit<D, kBits>;
-  int k, ks, v;
-  __device__ __forceinline__ explicit Lane(int lane) {
-    const int m = lane & 15, group = lane >> 4;
-    k = (m & 3) * MX::kRow + (U::KW >= 4 ? 16 : 8) * group;
-    const int blk = D == 128 && kBits == 4 ? group : group >> 1;
-    ks = MX::kKScales + ((m & 3) * MX::kBlocks + blk) * 4;
-    v = MX::kVCodes + m * 16;
-  }
-  // kb: the block of this lane's K page, vb: of its V page
-  __device__ __forceinline__ void load(U& u, const uint8_t* kb, const uint8_t* vb) const {
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int c = 0; c < (U::KW + 3) / 4; ++c) load_words<U::KW == 2 ? 2 : 4>(&u.k[t][4 * c], kb + k + 4 * t * MX::kRow + 64 * c);
-#pragma unroll
-    for (int c = 0; c < U::KS; ++c) u.ks[c] = *reinterpret_cast<const uint32_t*>(kb + ks + 8 * c);
-#pragma unroll
-    for (int p = 0; p < U::TP; ++p) u.vs[p] = *reinterpret_cast<const u32x4*>(vb + MX::kVScales + 16 * p);
-#pragma unroll
-    for (int p = 0; p < U::TP; ++p)
-#pragma unroll
-      for (int h = 0; h < U::VW / 4; ++h) load_words<4>(&u.v[p][4 * h], vb + v + (h * (D / 2) + 16 * p) * 16);
-  }
-};
-
-template <int kBits, int kFirst> __device__ __forceinline__ bf16x8 eight_up(const uint32_t* w, float f) {
+template <int kBits> __device__ __forceinline__ bf16x8 eight_up(const uint32_t* w, float f) {
   if constexpr (kBits == 4)
     return as_bf16x8(u32x4{mx_up<4, 0>(w[0], f), mx_up<4, 1>(w[0], f), mx_up<4, 2>(w[0], f), mx_up<4, 3>(w[0], f)});
   else
     return as_bf16x8(u32x4{mx_up<8, 0>(w[0], f), mx_up<8, 1>(w[0], f), mx_up<8, 0>(w[1], f), mx_up<8, 1>(w[1], f)});
 }
 
-// Channel pairs of token s (0..15) of a lane's unit, as two bf16.
-template <int kBits, int s> __device__ __forceinline__ uint32_t v_pair(const uint32_t* w, const u32x4& scales) {
-  const float f = mx_scale_of<s % 4>(scales[s / 4]);
-  if constexpr (kBits == 4) return mx_up<4, s % 4>(w[s / 4], f);
-  else return mx_up<8, s % 2>(w[s / 2], f);
+// x in bf16 in both halves of a dword.
+__device__ __forceinline__ uint32_t twice_bf16(float x) {
+  const bf16x2 y = {(__bf16)x, (__bf16)x};
+  return __builtin_bit_cast(uint32_t, y);
 }
 
-// Attends the heads to one unit.  lim: the slots of page l / 16 that this sequence attends to (16 unless kTail).
-template <int D, int kBits, bool kTail>
-__device__ __forceinline__ void consume(Unit<D, kBits>& u, const bf16x8* qop, f32x4 (*oacc)[2], float& m_run, float& l_run,
-                                        float c, int lim, uint32_t part_hi, uint32_t part_lo) {
+// A lane's places in a buffer, and the products of a unit.
+template <int D, int kBits> struct Attend {
+  using MX = MxBlock<D, kBits>;
   using U = Unit<D, kBits>;
-  constexpr int KB = D / 32;
-  f32x4 s[4];
-  auto tile = [&](auto t_c) {
-    constexpr int t = decltype(t_c)::value;
-    s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  static constexpr int TG = U::TG, NT = U::kPages;  // NT: tiles of 16 keys
+  static constexpr int kPieces = D * kBits / 8 >= 128 ? 2 : 1;   // of a lane's K row: 16 bytes (8 at 64 x 4)
+  static constexpr int KW = D * kBits / 128;        // dwords of it
+  static constexpr int VW = TG * kBits / 16;        // dwords of a channel pair's tokens
+  int k, ks, v, vs;
+  int k_shift;                                      // of the scale word: tile t's byte becomes byte t
+  __device__ __forceinline__ explicit Attend(int lane) {
+    const int row = lane & 15, group = lane >> 4;
+    const int tok = row / 4 * TG + (row & 3);       // of tile 0; tile t is 4 t further, on the same page
+    k = tok / kPage * U::kPageBytes + tok % kPage * MX::kRow + group * (KW >= 4 ? 16 : 8);
+    const int blk = D == 128 && kBits == 4 ? group : group >> 1;   // of piece 0; piece 1 is two blocks on
+    ks = U::kScales + tok / kPage * U::kScaleBytes + ((tok & 3) * MX::kBlocks + blk) * 4;
+    k_shift = tok % kPage / 4 * 8;
+    const int vt = group * TG;
+    v = vt / kPage * U::kPageBytes + MX::v_code(vt % kPage, row);
+    vs = U::kScales + vt / kPage * U::kScaleBytes + MX::kVScales - 2 * MX::kCodes + vt % kPage;
+  }
+
+  // Attends the heads to the unit in buf.  lim: how many of this lane group's tokens count (TG unless kTail).
+  template <bool kTail>
+  __device__ __forceinline__ void unit(const char* buf, const bf16x8* qop, f32x4* oacc, float& m_run, float& l_run, float c,
+                                       int lim, uint32_t half) const {
+    f32x4 s[NT];
+    uint32_t scale[kPieces];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const float f = mx_scale_of<t>(u.ks[U::KS == 2 ? kb / 2 : 0]);
-      s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_up<kBits, 0>(&u.k[t][kb * kBits / 4], f), qop[kb], s[t], 0, 0, 0);
+    for (int p = 0; p < kPieces; ++p) {
+      lds_words<1>(&scale[p], buf + ks + 8 * p);
+      if constexpr (TG < 16) scale[p] >>= k_shift;
     }
-  };
-  tile(std::integral_constant<int, 0>{});
-  tile(std::integral_constant<int, 1>{});
-  tile(std::integral_constant<int, 2>{});
-  tile(std::integral_constant<int, 3>{});
-  if constexpr (kTail) {
-    // keys past the end: scores by a select, so stray bits never leak, and V codes and scales to zero
+    auto tile = [&](auto t_c) {
+      constexpr int t = decltype(t_c)::value;
+      if constexpr (t < NT) {
+        uint32_t w[KW];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+        for (int p = 0; p < kPieces; ++p) lds_words<KW / kPieces>(&w[p * (KW / kPieces)], buf + k + 4 * t * MX::kRow + 64 * p);
+        s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[t][i] = 4 * t + i < lim ? s[t][i] : -INFINITY;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const int left = min(max(lim - 4 * w, 0), 4);                        // tokens 4 w .. that count
-      const uint32_t mask = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
-#pragma unroll
-      for (int p = 0; p < U::TP; ++p) {
-        u.vs[p][w] &= mask;
-        if constexpr (kBits == 4) {
-          u.v[p][w] &= mask;
-        } else {
-          u.v[p][2 * w] &= left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
-          u.v[p][2 * w + 1] &= left == 4 ? 0xffffffffu : left == 3 ? 0xffffu : 0u;
+        for (int kb = 0; kb < U::KB; ++kb) {
+          const float f = mx_scale_of<t>(scale[kPieces == 2 ? kb / 2 : 0]);
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_up<kBits>(&w[kb * kBits / 4], f), qop[kb], s[t], 0, 0, 0);
         }
       }
+    };
+    tile(std::integral_constant<int, 0>{});
+    tile(std::integral_constant<int, 1>{});
+    tile(std::integral_constant<int, 2>{});
+    tile(std::integral_constant<int, 3>{});
+    if constexpr (kTail) {                          // keys past the end: by a select, so stray bits never leak
+#pragma unroll
+      for (int j = 0; j < TG; ++j) s[j / 4][j % 4] = j < lim ? s[j / 4][j % 4] : -INFINITY;
     }
-  }
-  float p[16];
-  auto weights = [&](float m) {
-    float a = 0.f, b = 0.f;
+    float p[TG];
+    auto weights = [&](float m) {
+      float a = 0.f, b = 0.f;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[4 * t + i] = fexp2(__builtin_fmaf(s[t][i], c, -m));
-        if (i & 1) b += p[4 * t + i]; else a += p[4 * t + i];
+      for (int j = 0; j < TG; ++j) {
+        p[j] = fexp2(__builtin_fmaf(s[j / 4][j % 4], c, -m));
+        if (j & 1) b += p[j]; else a += p[j];
       }
-    return a + b;
-  };
-  constexpr float kMaxSum = 256.0f;                 // bounds every weight by 2^8
-  float sum = weights(m_run);
-  if (__ballot(!(sum <= kMaxSum))) {                // the first unit (m = -inf), or scores far above m
-    float mx = s[0][0];
+      return a + b;
+    };
+    constexpr float kMaxSum = 256.0f;               // bounds every weight by 2^8
+    float sum = weights(m_run);
+    if (__ballot(!(sum <= kMaxSum))) {              // the first unit (m = -inf), or scores far above m
+      float mx = s[0][0];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+      for (int j = 1; j < TG; ++j) mx = fmaxf(mx, s[j / 4][j % 4]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = xor32_max(mx);
+      const bool grow = mx * c > m_run;
+      const float m_new = grow ? mx * c : m_run;
+      const float alpha = grow ? fexp2(m_run - m_new) : 1.0f;
+      sum = weights(m_new);
+      l_run *= alpha;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = xor32_max(mx);
-    const bool grow = mx * c > m_run;
-    const float m_new = grow ? mx * c : m_run;
-    const float alpha = grow ? fexp2(m_run - m_new) : 1.0f;
-    sum = weights(m_new);
-    l_run *= alpha;
+      for (int q = 0; q < U::TP; ++q) oacc[q] *= alpha;
+      m_run = m_new;
+    }
+    l_run += sum;
+    uint32_t pop[TG], rest[TG];                     // the weight's parts at this column's half of each index pair
+#pragma unroll
+    for (int j = 0; j < TG; ++j) {
+      const uint32_t both = twice_bf16(p[j]);
+      pop[j] = both & half;
+      rest[j] = twice_bf16(p[j] - __builtin_bit_cast(float, both & 0xffff0000u)) & half;
+    }
 #pragma unroll
     for (int q = 0; q < U::TP; ++q) {
-      oacc[q][0] *= alpha;
-      oacc[q][1] *= alpha;
-    }
-    m_run = m_new;
-  }
-  l_run += sum;
-  // this column's part of the weights: the upper 16 bits of each, or the rest, which is never 0 unless the
-  // weight is, so that an infinite value stays infinite
-  bf16x8 pop[2];
-#pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const uint32_t w = __builtin_bit_cast(uint32_t, p[j]);
-    const float y = __builtin_bit_cast(float, w & part_hi) - __builtin_bit_cast(float, w & part_lo);
-    pop[j / 8][j % 8] = (__bf16)fmaxf(y, fminf(p[j], 0x1p-100f));
-  }
-  auto group = [&](auto p_c) {
-    constexpr int q = decltype(p_c)::value;
-    uint32_t x[16];
-    auto token = [&](auto s_c) { x[decltype(s_c)::value] = v_pair<kBits, decltype(s_c)::value>(u.v[q], u.vs[q]); };
-    token(std::integral_constant<int, 0>{}); token(std::integral_constant<int, 1>{});
-    token(std::integral_constant<int, 2>{}); token(std::integral_constant<int, 3>{});
-    token(std::integral_constant<int, 4>{}); token(std::integral_constant<int, 5>{});
-    token(std::integral_constant<int, 6>{}); token(std::integral_constant<int, 7>{});
-    token(std::integral_constant<int, 8>{}); token(std::integral_constant<int, 9>{});
-    token(std::integral_constant<int, 10>{}); token(std::integral_constant<int, 11>{});
-    token(std::integral_constant<int, 12>{}); token(std::integral_constant<int, 13>{});
-    token(std::integral_constant<int, 14>{}); token(std::integral_constant<int, 15>{});
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      u32x4 even, odd;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        even[j] = __builtin_amdgcn_perm(x[8 * h + 2 * j + 1], x[8 * h + 2 * j], 0x05040100u);
-        odd[j] = __builtin_amdgcn_perm(x[8 * h + 2 * j + 1], x[8 * h + 2 * j], 0x07060302u);
+      uint32_t w[VW], sc[TG / 4];
+      if constexpr (VW <= 4) {
+        lds_words<VW>(w, buf + v + 256 * q);
+      } else {                                      // two units: tokens 0-7 and 8-15
+        lds_words<4>(w, buf + v + 256 * q);
+        lds_words<4>(w + 4, buf + v + 256 * q + D / 2 * 16);
       }
-      oacc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), pop[h], oacc[q][0], 0, 0, 0);
-      oacc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), pop[h], oacc[q][1], 0, 0, 0);
+      lds_words<TG / 4>(sc, buf + vs + kPage * q);
+      if constexpr (kTail) {                        // codes and scales past the end become zeros (0 times NaN is NaN)
+#pragma unroll
+        for (int x = 0; x < TG / 4; ++x) {
+          const int left = min(max(lim - 4 * x, 0), 4);
+          const uint32_t mask = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
+          sc[x] &= mask;
+          if constexpr (kBits == 4) {
+            w[x] &= mask;
+          } else {
+            w[2 * x] &= left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
+            w[2 * x + 1] &= left == 4 ? 0xffffffffu : left == 3 ? 0xffffu : 0u;
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < TG / 4; ++u) {
+        const float f0 = mx_scale_of<0>(sc[u]), f1 = mx_scale_of<1>(sc[u]), f2 = mx_scale_of<2>(sc[u]), f3 = mx_scale_of<3>(sc[u]);
+        u32x4 x;
+        if constexpr (kBits == 4) x = u32x4{mx_up<4, 0>(w[u], f0), mx_up<4, 1>(w[u], f1), mx_up<4, 2>(w[u], f2), mx_up<4, 3>(w[u], f3)};
+        else x = u32x4{mx_up<8, 0>(w[2 * u], f0), mx_up<8, 1>(w[2 * u], f1), mx_up<8, 0>(w[2 * u + 1], f2), mx_up<8, 1>(w[2 * u + 1], f3)};
+        oacc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            as_bf16x8(x), as_bf16x8(u32x4{pop[4 * u], pop[4 * u + 1], pop[4 * u + 2], pop[4 * u + 3]}), oacc[q], 0, 0, 0);
+        oacc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            as_bf16x8(x), as_bf16x8(u32x4{rest[4 * u], rest[4 * u + 1], rest[4 * u + 2], rest[4 * u + 3]}), oacc[q], 0, 0, 0);
+      }
     }
-  };
-  group(std::integral_constant<int, 0>{});
-  group(std::integral_constant<int, 1>{});
-  if constexpr (U::TP == 4) {
-    group(std::integral_constant<int, 2>{});
-    group(std::integral_constant<int, 3>{});
   }
-}
+};
 
 }  // namespace
 
 template <int D, int kBits>
-__global__ __launch_bounds__(kThreads, 2) void decode_mx_kernel(AttnArgs a, DecPlanArgs d) {
+__global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_kernel(AttnArgs a, DecPlanArgs d) {
   using MX = MxBlock<D, kBits>;
   using U = Unit<D, kBits>;
-  constexpr int KB = D / 32, TP = U::TP;
-  __shared__ __attribute__((aligned(16))) ShareEnd<D> stage[kWaves];
+  constexpr int KB = U::KB, TP = U::TP, kPages = U::kPages;
+  // a wave's two buffers, and at its share's end its partials
+  constexpr int kStage = 2 * U::kBytes > (int)sizeof(ShareEnd<D>) ? 2 * U::kBytes : (int)sizeof(ShareEnd<D>);
+  static_assert(kStage % 16 == 0, "stages stay aligned");
+  __shared__ __attribute__((aligned(16))) char stage[kWaves * kStage];
   __shared__ DecPlanLds P;
   __shared__ FinishLds F;
   const int lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6);
-  const int group = lane >> 4, col = lane & 15, hh = col & 7;
+  const int group = lane >> 4, col = lane & 15, hh = col & 7, odd = col >> 3;
   const int G = a.group, H = a.num_kv_heads, H_q = a.num_q_heads, B = d.batch;
 
   int most;
@@ -253,63 +277,48 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mx_kernel(AttnArgs a, DecP
   DecRun r;
   if (!decode_run(a, d, P, most, total_pages, sh, r)) return;
   const int g = r.g0 + r.j_w;
-  const bool head_ok = col < G && r.j_w >= r.dup;
+  const bool head_ok = hh < G && r.j_w >= r.dup;
   const int pages_seen = r.j_w < r.dup ? 1 : a.num_pages;
-  const uint32_t part_hi = col < 8 ? 0xffff0000u : 0xffffffffu, part_lo = col < 8 ? 0u : 0xffff0000u;
+  const uint32_t half = odd ? 0xffff0000u : 0x0000ffffu;
 
-  f32x4 oacc[TP][2];
+  f32x4 oacc[TP];
   float m_run = -INFINITY, l_run = 0.f;
   int first_b = -1;                                 // the pair whose end this share holds without its start
+  float m_first = 0.f, l_first = 0.f;
+  f32x4 o_first[TP];
   bool whole = false;                               // the current pair started inside this share
   PageCursor cur{-1, 0, 1, 1};
-  ShareEnd<D>& E = stage[w];
-
-  // The two parts' outputs added, every lane group's sums: the state of a pair that ends or is cut here.
-  auto close = [&]() {
 #pragma unroll
-    for (int p = 0; p < TP; ++p)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = oacc[p][e][i];            // (a bit cast of the element itself takes element 0)
-          const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x128, 0xf, 0xf, false);   // row_ror:8
-          oacc[p][e][i] = x + __builtin_bit_cast(float, y);
-        }
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
-  };
-  auto leave = [&](int which) {                     // lane: head col, dims 32 p + 8 group ..
-    if (!head_ok) return;
-#pragma unroll
-    for (int p = 0; p < TP; ++p) {
-      float* o = &E.o[which][col][32 * p + 8 * group];
-      *reinterpret_cast<f32x4*>(o) = f32x4{oacc[p][0][0], oacc[p][1][0], oacc[p][0][1], oacc[p][1][1]};
-      *reinterpret_cast<f32x4*>(o + 4) = f32x4{oacc[p][0][2], oacc[p][1][2], oacc[p][0][3], oacc[p][1][3]};
-    }
-    if (group == 0) { E.ml[which][col][0] = m_run; E.ml[which][col][1] = l_run; }
-  };
+  for (int p = 0; p < TP; ++p) oacc[p] = o_first[p] = f32x4{0.f, 0.f, 0.f, 0.f};
+  char* const st = stage + w * kStage;
 
   if (r.n > 0) {
     const ConstI32Ptr bt = (ConstI32Ptr)a.block_table;
-    const Lane<D, kBits> at(lane);
+    const Attend<D, kBits> at(lane);
     const size_t page_bytes = (size_t)H * MX::kBytes;
     const uint8_t* const heads = a.cache + (size_t)g * MX::kBytes;
-    struct Ids { int x[kUnitPages]; };
-    // a unit: up to four pages of the cursor's sequence; `left` pages of the share from its first page on
-    auto pages_of = [&](const PageCursor& c, int left) { return min(min(kUnitPages, c.np - c.p), left); };
-    auto ids_of = [&](const PageCursor& c, int np) {
+    struct Ids { int x[kPages]; };
+    // a unit: up to kPages pages of the cursor's sequence; `left` pages of the share from its first page on
+    auto pages_of = [&](const PageCursor& c, int left) { return min(min(kPages, c.np - c.p), left); };
+    auto ids_of = [&](const PageCursor& c, int np) {   // pages past the unit's last one repeat it
       Ids id;
 #pragma unroll
-      for (int i = 0; i < kUnitPages; ++i)
+      for (int i = 0; i < kPages; ++i)
         id.x[i] = clamp_page(bt[(size_t)c.b * a.bt_stride + c.p + min(i, np - 1)], pages_seen);
       return id;
     };
-    auto send = [&](U& u, const Ids& id) {
-      const int pk = col >> 2;
-      const int ik = pk < 2 ? (pk == 0 ? id.x[0] : id.x[1]) : (pk == 2 ? id.x[2] : id.x[3]);
-      const int iv = group < 2 ? (group == 0 ? id.x[0] : id.x[1]) : (group == 2 ? id.x[2] : id.x[3]);
-      at.load(u, heads + (size_t)ik * page_bytes, heads + (size_t)iv * page_bytes);
+    const int lane16 = lane * 16;
+    constexpr int SC = U::kScaleBytes / 16;         // lanes of a page's scales
+    auto send = [&](int buf, const Ids& id) {
+      const unsigned lds = (unsigned)(uintptr_t)((LDS_AS const char*)st) + buf;
+#pragma unroll
+      for (int i = 0; i < kPages; ++i)
+        copy_codes<U::kCopies>(heads + (size_t)id.x[i] * page_bytes, lane16, uni(lds + i * U::kPageBytes));
+      int mine = id.x[0];
+#pragma unroll
+      for (int i = 1; i < kPages; ++i) mine = lane / SC == i ? id.x[i] : mine;
+      if (lane < kPages * SC)
+        copy_scales(heads + (size_t)mine * page_bytes + 2 * MX::kCodes + lane % SC * 16, uni(lds + U::kScales));
     };
     auto send_q = [&](u32x4* q, const PageCursor& c) {
       const uint16_t* row = a.q + ((size_t)c.b * H_q + g * G + min(hh, G - 1)) * D;
@@ -324,69 +333,73 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mx_kernel(AttnArgs a, DecP
       c.np = uni(P.pre[c.b + 1]) - uni(P.pre[c.b]);
       c.kv = (c.np - 1) * kPage + uni(P.tail[c.b]) + 1;
     };
-    U ua, ub;
     u32x4 q_next[KB];
     bf16x8 qop[KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) qop[kb] = zero_bf16x8();
     cur = locate(P, r.t0, B);
     int left = r.n, np_cur = pages_of(cur, left);
     Ids id = ids_of(cur, np_cur);
     send_q(q_next, cur);
-    send(ua, id);
+    send(0, id);
     bool fresh = true;                              // the unit is the first of its pair in this share
     PageCursor nxt = cur;
     step_past(nxt, np_cur);
     int np_nxt = pages_of(nxt, left - np_cur);
     if (left > np_cur) id = ids_of(nxt, np_nxt);
-    // one unit: the next one's loads go out, then it is attended
-    auto unit = [&](U& now, U& next) {
+    int buf = 0;
+    for (;;) {
       if (fresh) {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          qop[kb] = hh < G ? as_bf16x8(q_next[kb]) : zero_bf16x8();
-        }
+        for (int kb = 0; kb < KB; ++kb) qop[kb] = hh < G ? as_bf16x8(q_next[kb]) : zero_bf16x8();
 #pragma unroll
-        for (int p = 0; p < TP; ++p) oacc[p][0] = oacc[p][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < TP; ++p) oacc[p] = f32x4{0.f, 0.f, 0.f, 0.f};
         m_run = -INFINITY;
         l_run = 0.f;
         whole = cur.p == 0;
       }
+      // the next unit's copies go out (its buffer's last reads are complete), then this one's are waited for
       const bool more = left > np_cur;
       PageCursor nn = nxt;
       int np_nn = 0;
       if (more) {
         if (nxt.p == 0) send_q(q_next, nxt);
-        send(next, id);
+        __builtin_amdgcn_s_waitcnt(PEARL_LGKMCNT0);
+        send(buf ^ U::kBytes, id);
         step_past(nn, np_nxt);
         np_nn = pages_of(nn, left - np_cur - np_nxt);
         if (left > np_cur + np_nxt) id = ids_of(nn, np_nn);
-      }
-      if (np_cur == kUnitPages && (cur.p + kUnitPages) * kPage <= cur.kv) {
-        consume<D, kBits, false>(now, qop, oacc, m_run, l_run, a.scale_log2, kPage, part_hi, part_lo);
+        __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(U::kLoads) : "memory");
       } else {
-        const int lim = group < np_cur ? cur.kv - (cur.p + group) * kPage : 0;
-        consume<D, kBits, true>(now, qop, oacc, m_run, l_run, a.scale_log2, lim, part_hi, part_lo);
+        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
+      if (np_cur == kPages && (cur.p + kPages) * kPage <= cur.kv)
+        at.template unit<false>(st + buf, qop, oacc, m_run, l_run, a.scale_log2, U::TG, half);
+      else
+        at.template unit<true>(st + buf, qop, oacc, m_run, l_run, a.scale_log2,
+                               min(cur.kv - cur.p * kPage, np_cur * kPage) - group * U::TG, half);
       const bool ends_here = cur.p + np_cur == cur.np;
       if (ends_here) {
-        close();
+        l_run += __shfl_xor(l_run, 16);
+        l_run += __shfl_xor(l_run, 32);
         if (whole) {
-          if (head_ok) {
-            const size_t row = (size_t)cur.b * H_q + g * G + col;
-            const float inv = 1.0f / l_run;
+          const size_t row = (size_t)cur.b * H_q + g * G + hh;
+          const float inv = 1.0f / l_run;
 #pragma unroll
-            for (int p = 0; p < TP; ++p) {
-              u32x4 x;
+          for (int p = 0; p < TP; ++p) {
+            u32x4 x;
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                x[i] = (uint32_t)bf16_bits(oacc[p][0][i] * inv) | ((uint32_t)bf16_bits(oacc[p][1][i] * inv) << 16);
-              *reinterpret_cast<u32x4*>(a.out + row * D + 32 * p + 8 * group) = x;
+            for (int i = 0; i < 4; ++i) {           // the odd channels from the lane 8 columns on
+              const float mine = oacc[p][i] * inv;  // (a bit cast of the element itself takes element 0)
+              const int other = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, mine), 0x128, 0xf, 0xf, false);   // row_ror:8
+              x[i] = (uint32_t)bf16_bits(mine) | ((uint32_t)bf16_bits(__builtin_bit_cast(float, other)) << 16);
             }
-            if (group == 0 && a.lse) a.lse[row] = (m_run + flog2(l_run)) * kLn2;
+            if (head_ok && !odd) *reinterpret_cast<u32x4*>(a.out + row * D + 32 * p + 8 * group) = x;
           }
+          if (head_ok && lane < 8 && a.lse) a.lse[row] = (m_run + flog2(l_run)) * kLn2;
         } else {                                    // only the first pair can have started earlier
-          leave(0);
+#pragma unroll
+          for (int p = 0; p < TP; ++p) o_first[p] = oacc[p];
+          m_first = m_run;
+          l_first = l_run;
           first_b = cur.b;
         }
       }
@@ -394,26 +407,34 @@ __global__ __launch_bounds__(kThreads, 2) void decode_mx_kernel(AttnArgs a, DecP
       left -= np_cur;
       if (!more) {
         if (ends_here) cur.b = -1;                  // the share ends with the pair's end
-        return;
+        break;
       }
       cur = nxt;
       np_cur = np_nxt;
       nxt = nn;
       np_nxt = np_nn;
-    };
-    for (;;) {
-      unit(ua, ub);
-      if (left == 0) break;
-      unit(ub, ua);
-      if (left == 0) break;
+      buf ^= U::kBytes;
     }
     if (cur.b >= 0) {
-      close();
-      leave(1);
+      l_run += __shfl_xor(l_run, 16);
+      l_run += __shfl_xor(l_run, 32);
     }
   }
-  finish_shares<D>(a, d, P, sh, r, reinterpret_cast<const char*>(stage), (int)sizeof(ShareEnd<D>),
-                   SharePairs{first_b, cur.b, !whole, r.n > 0}, F);
+
+  // the waves' partials, merged per pair through LDS
+  ShareEnd<D>& E = *reinterpret_cast<ShareEnd<D>*>(st);
+  auto leave = [&](int which, const f32x4* o, float m, float l) {
+#pragma unroll
+    for (int p = 0; p < TP; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) E.o[which][hh][32 * p + 8 * group + 2 * i + odd] = o[p][i];
+    if (lane < 8) { E.ml[which][hh][0] = m; E.ml[which][hh][1] = l; }
+  };
+  if (head_ok) {
+    if (first_b >= 0) leave(0, o_first, m_first, l_first);
+    if (cur.b >= 0) leave(1, oacc, m_run, l_run);
+  }
+  finish_shares<D>(a, d, P, sh, r, stage, kStage, SharePairs{first_b, cur.b, !whole, r.n > 0}, F);
 }
 
 // ------------------------------------------------------------------------------------------------
