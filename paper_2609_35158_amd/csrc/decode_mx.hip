@@ -147,31 +147,44 @@ template <int D, int kBits> struct Attend {
   template <bool kTail>
   __device__ __forceinline__ void unit(const char* buf, const bf16x8* qop, f32x4* oacc, float& m_run, float& l_run, float c,
                                        int lim, uint32_t half) const {
-    f32x4 s[NT];
-    uint32_t scale[kPieces];
+    // All of the unit's operands are read before the first is used, so that one LDS latency passes and not one a
+    // tile (the barrier keeps the compiler from moving each read to its use).
+    uint32_t scale[kPieces], kw[NT][KW], vw[U::TP][VW], vsc[U::TP][TG / 4];
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) {
-      lds_words<1>(&scale[p], buf + ks + 8 * p);
-      if constexpr (TG < 16) scale[p] >>= k_shift;
+    for (int p = 0; p < kPieces; ++p) lds_words<1>(&scale[p], buf + ks + 8 * p);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) lds_words<KW / kPieces>(&kw[t][p * (KW / kPieces)], buf + k + 4 * t * MX::kRow + 64 * p);
+#pragma unroll
+    for (int q = 0; q < U::TP; ++q) {
+      lds_words<TG / 4>(vsc[q], buf + vs + kPage * q);
+#pragma unroll
+      for (int x = 0; x < VW; x += 4)               // (8 words: tokens 0-7 and 8-15, a unit each)
+        lds_words<VW < 4 ? VW : 4>(&vw[q][x], buf + v + 256 * q + x / 4 * (D / 2 * 16));
     }
-    auto tile = [&](auto t_c) {
-      constexpr int t = decltype(t_c)::value;
-      if constexpr (t < NT) {
-        uint32_t w[KW];
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 s[NT];
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) lds_words<KW / kPieces>(&w[p * (KW / kPieces)], buf + k + 4 * t * MX::kRow + 64 * p);
-        s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (TG < 16) {
 #pragma unroll
-        for (int kb = 0; kb < U::KB; ++kb) {
+      for (int p = 0; p < kPieces; ++p) scale[p] >>= k_shift;
+    }
+#pragma unroll
+    for (int kb = 0; kb < U::KB; ++kb) {            // the tiles in turn: no product waits for the one before it
+      auto tile = [&](auto t_c) {
+        constexpr int t = decltype(t_c)::value;
+        if constexpr (t < NT) {
           const float f = mx_scale_of<t>(scale[kPieces == 2 ? kb / 2 : 0]);
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_up<kBits>(&w[kb * kBits / 4], f), qop[kb], s[t], 0, 0, 0);
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_up<kBits>(&kw[t][kb * kBits / 4], f), qop[kb], s[t], 0, 0, 0);
         }
-      }
-    };
-    tile(std::integral_constant<int, 0>{});
-    tile(std::integral_constant<int, 1>{});
-    tile(std::integral_constant<int, 2>{});
-    tile(std::integral_constant<int, 3>{});
+      };
+      tile(std::integral_constant<int, 0>{});
+      tile(std::integral_constant<int, 1>{});
+      tile(std::integral_constant<int, 2>{});
+      tile(std::integral_constant<int, 3>{});
+    }
     if constexpr (kTail) {                          // keys past the end: by a select, so stray bits never leak
 #pragma unroll
       for (int j = 0; j < TG; ++j) s[j / 4][j % 4] = j < lim ? s[j / 4][j % 4] : -INFINITY;
@@ -211,41 +224,44 @@ template <int D, int kBits> struct Attend {
       pop[j] = both & half;
       rest[j] = twice_bf16(p[j] - __builtin_bit_cast(float, both & 0xffff0000u)) & half;
     }
+    if constexpr (kTail) {                          // codes and scales past the end become zeros (0 times NaN is NaN)
 #pragma unroll
-    for (int q = 0; q < U::TP; ++q) {
-      uint32_t w[VW], sc[TG / 4];
-      if constexpr (VW <= 4) {
-        lds_words<VW>(w, buf + v + 256 * q);
-      } else {                                      // two units: tokens 0-7 and 8-15
-        lds_words<4>(w, buf + v + 256 * q);
-        lds_words<4>(w + 4, buf + v + 256 * q + D / 2 * 16);
-      }
-      lds_words<TG / 4>(sc, buf + vs + kPage * q);
-      if constexpr (kTail) {                        // codes and scales past the end become zeros (0 times NaN is NaN)
+      for (int x = 0; x < TG / 4; ++x) {
+        const int left = min(max(lim - 4 * x, 0), 4);
+        const uint32_t mask = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
 #pragma unroll
-        for (int x = 0; x < TG / 4; ++x) {
-          const int left = min(max(lim - 4 * x, 0), 4);
-          const uint32_t mask = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
-          sc[x] &= mask;
+        for (int q = 0; q < U::TP; ++q) {
+          vsc[q][x] &= mask;
           if constexpr (kBits == 4) {
-            w[x] &= mask;
+            vw[q][x] &= mask;
           } else {
-            w[2 * x] &= left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
-            w[2 * x + 1] &= left == 4 ? 0xffffffffu : left == 3 ? 0xffffu : 0u;
+            vw[q][2 * x] &= left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
+            vw[q][2 * x + 1] &= left == 4 ? 0xffffffffu : left == 3 ? 0xffffu : 0u;
           }
         }
       }
+    }
 #pragma unroll
-      for (int u = 0; u < TG / 4; ++u) {
-        const float f0 = mx_scale_of<0>(sc[u]), f1 = mx_scale_of<1>(sc[u]), f2 = mx_scale_of<2>(sc[u]), f3 = mx_scale_of<3>(sc[u]);
-        u32x4 x;
-        if constexpr (kBits == 4) x = u32x4{mx_up<4, 0>(w[u], f0), mx_up<4, 1>(w[u], f1), mx_up<4, 2>(w[u], f2), mx_up<4, 3>(w[u], f3)};
-        else x = u32x4{mx_up<8, 0>(w[2 * u], f0), mx_up<8, 1>(w[2 * u], f1), mx_up<8, 0>(w[2 * u + 1], f2), mx_up<8, 1>(w[2 * u + 1], f3)};
+    for (int u = 0; u < TG / 4; ++u) {
+      bf16x8 x[U::TP];
+#pragma unroll
+      for (int q = 0; q < U::TP; ++q) {
+        const uint32_t w = vsc[q][u];
+        const float f0 = mx_scale_of<0>(w), f1 = mx_scale_of<1>(w), f2 = mx_scale_of<2>(w), f3 = mx_scale_of<3>(w);
+        if constexpr (kBits == 4) {
+          const uint32_t y = vw[q][u];
+          x[q] = as_bf16x8(u32x4{mx_up<4, 0>(y, f0), mx_up<4, 1>(y, f1), mx_up<4, 2>(y, f2), mx_up<4, 3>(y, f3)});
+        } else {
+          const uint32_t y = vw[q][2 * u], z = vw[q][2 * u + 1];
+          x[q] = as_bf16x8(u32x4{mx_up<8, 0>(y, f0), mx_up<8, 1>(y, f1), mx_up<8, 0>(z, f2), mx_up<8, 1>(z, f3)});
+        }
         oacc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            as_bf16x8(x), as_bf16x8(u32x4{pop[4 * u], pop[4 * u + 1], pop[4 * u + 2], pop[4 * u + 3]}), oacc[q], 0, 0, 0);
-        oacc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            as_bf16x8(x), as_bf16x8(u32x4{rest[4 * u], rest[4 * u + 1], rest[4 * u + 2], rest[4 * u + 3]}), oacc[q], 0, 0, 0);
+            x[q], as_bf16x8(u32x4{pop[4 * u], pop[4 * u + 1], pop[4 * u + 2], pop[4 * u + 3]}), oacc[q], 0, 0, 0);
       }
+#pragma unroll
+      for (int q = 0; q < U::TP; ++q)
+        oacc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            x[q], as_bf16x8(u32x4{rest[4 * u], rest[4 * u + 1], rest[4 * u + 2], rest[4 * u + 3]}), oacc[q], 0, 0, 0);
     }
   }
 };
