@@ -50,7 +50,6 @@ template <int D, int kBits> struct Unit {
   static constexpr int kScaleBytes = MX::kBytes - 2 * MX::kCodes;
   static constexpr int kScales = kPages * kPageBytes;     // offset of the pages' scales
   static constexpr int kBytes = kScales + kPages * kScaleBytes;
-  static constexpr int kLoads = kPages * kCopies + 1;     // copy instructions of a unit
   static_assert(kCopies >= 1 && kCopies * 1024 == 2 * MX::kCodes && kPages * kScaleBytes <= 1024, "copies");
 };
 
@@ -279,6 +278,7 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
   __shared__ __attribute__((aligned(16))) char stage[kWaves * kStage];
   __shared__ DecPlanLds P;
   __shared__ FinishLds F;
+  __shared__ int to_go[kWaves];
   const int lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6);
   const int group = lane >> 4, col = lane & 15, hh = col & 7, odd = col >> 3;
   const int G = a.group, H = a.num_kv_heads, H_q = a.num_q_heads, B = d.batch;
@@ -325,15 +325,26 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     };
     const int lane16 = lane * 16;
     constexpr int SC = U::kScaleBytes / 16;         // lanes of a page's scales
-    auto send = [&](int buf, const Ids& id) {
+    // np pages' copies, np * kCopies + 1 instructions; what a buffer holds in place of the others is masked
+    auto send = [&](int buf, Ids id, int np) {
       const unsigned lds = (unsigned)(uintptr_t)((LDS_AS const char*)st) + buf;
-#pragma unroll
-      for (int i = 0; i < kPages; ++i)
-        copy_codes<U::kCopies>(heads + (size_t)id.x[i] * page_bytes, lane16, uni(lds + i * U::kPageBytes));
+      auto page = [&](auto i_c) {
+        constexpr int i = decltype(i_c)::value;
+        if constexpr (i < kPages) {
+          if (i < np) copy_codes<U::kCopies>(heads + (size_t)id.x[i] * page_bytes, lane16, uni(lds + i * U::kPageBytes));
+        }
+      };
+      page(std::integral_constant<int, 0>{});
+      page(std::integral_constant<int, 1>{});
+      page(std::integral_constant<int, 2>{});
+      page(std::integral_constant<int, 3>{});
       int mine = id.x[0];
-#pragma unroll
-      for (int i = 1; i < kPages; ++i) mine = lane / SC == i ? id.x[i] : mine;
-      if (lane < kPages * SC)
+      if (lane >= SC) mine = id.x[1];
+      if constexpr (kPages == 4) {
+        if (lane >= 2 * SC) mine = id.x[2];
+        if (lane >= 3 * SC) mine = id.x[3];
+      }
+      if (lane < np * SC)
         copy_scales(heads + (size_t)mine * page_bytes + 2 * MX::kCodes + lane % SC * 16, uni(lds + U::kScales));
     };
     auto send_q = [&](u32x4* q, const PageCursor& c) {
@@ -355,7 +366,7 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     int left = r.n, np_cur = pages_of(cur, left);
     Ids id = ids_of(cur, np_cur);
     send_q(q_next, cur);
-    send(0, id);
+    send(0, id, np_cur);
     bool fresh = true;                              // the unit is the first of its pair in this share
     PageCursor nxt = cur;
     step_past(nxt, np_cur);
@@ -363,6 +374,11 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     if (left > np_cur) id = ids_of(nxt, np_nxt);
     int buf = 0;
     for (;;) {
+      // A SIMD's two waves (w and w ^ 4) keep pace: the one with more left issues first (without it 64 sequences of
+      // 2K-16K tokens took 124 us in 4 bits, so 120).
+      if (lane == 0) *(volatile int*)&to_go[w] = left;
+      if (uni(*(volatile int*)&to_go[w ^ 4]) < left) __builtin_amdgcn_s_setprio(1);
+      else __builtin_amdgcn_s_setprio(0);
       if (fresh) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) qop[kb] = hh < G ? as_bf16x8(q_next[kb]) : zero_bf16x8();
@@ -379,11 +395,15 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
       if (more) {
         if (nxt.p == 0) send_q(q_next, nxt);
         __builtin_amdgcn_s_waitcnt(PEARL_LGKMCNT0);
-        send(buf ^ U::kBytes, id);
+        send(buf ^ U::kBytes, id, np_nxt);
         step_past(nn, np_nxt);
         np_nn = pages_of(nn, left - np_cur - np_nxt);
         if (left > np_cur + np_nxt) id = ids_of(nn, np_nn);
-        __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(U::kLoads) : "memory");
+        constexpr int C = U::kCopies;
+        if (np_nxt == kPages) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(kPages * C + 1) : "memory");
+        else if (np_nxt == 1) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(C + 1) : "memory");
+        else if (np_nxt == 2) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C + 1) : "memory");
+        else __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * C + 1) : "memory");
       } else {
         __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
