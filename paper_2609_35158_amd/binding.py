@@ -8,6 +8,7 @@ fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Tuple
 
@@ -184,16 +185,16 @@ def make_shape(num_q_heads: int, k_pool: torch.Tensor) -> KvShape:
 
 
 def make_desc(block_table: torch.Tensor, ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor],
-              total_q: int, max_q_len: int, max_kv_len: int) -> SeqDesc:
-    _need(block_table, "block_table", torch.int32)
-    _need(ctx_lens, "ctx_lens", torch.int32)
+              total_q: int, max_q_len: int, max_kv_len: int, need=_need) -> SeqDesc:
+    need(block_table, "block_table", torch.int32)
+    need(ctx_lens, "ctx_lens", torch.int32)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [batch][bt_stride]")
     batch = int(ctx_lens.shape[0])
     if block_table.shape[0] != batch:
         raise ValueError("block_table rows (%d) != batch (%d)" % (block_table.shape[0], batch))
     if cu_q_lens is not None:
-        _need(cu_q_lens, "cu_q_lens", torch.int32)
+        need(cu_q_lens, "cu_q_lens", torch.int32)
         if cu_q_lens.shape[0] != batch + 1:
             raise ValueError("cu_q_lens must have batch+1 entries")
     return SeqDesc(block_table.data_ptr(), int(block_table.shape[1]), ctx_lens.data_ptr(),
@@ -407,39 +408,53 @@ def mx_cache(num_pages: int, num_kv_heads: int, head_dim: int, fmt: int, device=
     return torch.zeros((num_pages, num_kv_heads, mx_block_bytes(head_dim, fmt)), dtype=torch.uint8, device=device)
 
 
-def _mx_shape(num_q_heads: Optional[int], cache: torch.Tensor) -> Tuple[KvShape, int]:
-    """Shape (num_q_heads None: as many as kv-heads, for calls that have no queries) and format."""
-    _need(cache, "cache", torch.uint8)
+@functools.lru_cache(maxsize=256)
+def _mx_geometry(num_q_heads: int, cache_shape: Tuple[int, int, int]):
+    """(KvShape, format, a reference to the shape for the library) of a cache [num_pages][H_kv][block]."""
     if not _MX_BLOCKS:
         _MX_BLOCKS.update({mx_block_bytes(d, f): (d, f) for d in (64, 128) for f in (MXFP4, MXFP8)})
-    if cache.dim() != 3 or cache.shape[2] not in _MX_BLOCKS:
+    if len(cache_shape) != 3 or cache_shape[2] not in _MX_BLOCKS:
         raise ValueError("cache must be [num_pages][num_kv_heads][mx_block_bytes(head_dim, fmt)]")
-    n, hkv, block = cache.shape
-    d, fmt = _MX_BLOCKS[block]
-    return KvShape(int(hkv if num_q_heads is None else num_q_heads), int(hkv), d, PAGE_SIZE, int(n)), fmt
+    d, fmt = _MX_BLOCKS[cache_shape[2]]
+    shape = KvShape(num_q_heads or cache_shape[1], cache_shape[1], d, PAGE_SIZE, cache_shape[0])
+    return shape, fmt, ctypes.byref(shape)
 
 
-def _on_current_device(cache: torch.Tensor, *tensors: Optional[torch.Tensor]) -> None:
-    """The library launches on the current device: every tensor of a call has to be there."""
-    dev = torch.cuda.current_device()
-    for t in (cache,) + tensors:
-        if t is not None and t.device.index != dev:
-            raise ValueError("tensors must be on the current device (cuda:%d), got %s" % (dev, t.device))
+class _MxCall:
+    """What the calls on a cache of MX blocks have in common: its geometry (num_q_heads None: as many as kv-heads,
+    for calls that have no queries), and that every tensor is on the current device, where the library launches."""
+
+    def __init__(self, cache: torch.Tensor, num_q_heads: Optional[int] = None):
+        _need(cache, "cache", torch.uint8)
+        self.shape, self.fmt, self.ref = _mx_geometry(num_q_heads, tuple(cache.shape))
+        self.dev = cache.get_device()
+        if self.dev != torch.cuda.current_device():
+            raise ValueError("cache is on cuda:%d, the current device is cuda:%d" % (self.dev, torch.cuda.current_device()))
+
+    def need(self, t: torch.Tensor, name: str, dtype: torch.dtype) -> None:
+        if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.get_device() == self.dev and t.is_contiguous()):
+            _need(t, name, dtype)
+            raise ValueError("%s must be on the cache's device (cuda:%d), got %s" % (name, self.dev, t.device))
+
+    def stream(self) -> int:
+        return _stream() if _raw_stream is None else _raw_stream(self.dev)
 
 
 def kv_append_mx(k_new: torch.Tensor, v_new: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor,
                  ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor], max_q_len: int, max_kv_len: int) -> None:
     """Quantise new K/V rows bf16 [total_q][H_kv][d] into their slots of a cache of MX blocks
     (pearl_kv_append_mx)."""
-    for t, n in ((k_new, "k_new"), (v_new, "v_new")):
-        _need(t, n, torch.bfloat16)
-    shape, fmt = _mx_shape(None, cache)
-    if k_new.dim() != 3 or tuple(k_new.shape[1:]) != (shape.num_kv_heads, shape.head_dim) or v_new.shape != k_new.shape:
-        raise ValueError("k_new and v_new must be [total_q][%d][%d]" % (shape.num_kv_heads, shape.head_dim))
-    desc = make_desc(block_table, ctx_lens, cu_q_lens, int(k_new.shape[0]), max_q_len, max_kv_len)
-    _on_current_device(cache, k_new, v_new, block_table, ctx_lens, cu_q_lens)
-    st = load().pearl_kv_append_mx(ctypes.byref(shape), ctypes.byref(desc), fmt, k_new.data_ptr(), v_new.data_ptr(),
-                                   cache.data_ptr(), _stream())
+    if getattr(k_new, "dtype", None) != torch.bfloat16:
+        _need(k_new, "k_new", torch.bfloat16)
+    c = _MxCall(cache)
+    c.need(k_new, "k_new", torch.bfloat16)
+    c.need(v_new, "v_new", torch.bfloat16)
+    total = k_new.shape[0]
+    if k_new.shape != (total, c.shape.num_kv_heads, c.shape.head_dim) or v_new.shape != k_new.shape:
+        raise ValueError("k_new and v_new must be [total_q][%d][%d]" % (c.shape.num_kv_heads, c.shape.head_dim))
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, c.need)
+    st = load().pearl_kv_append_mx(c.ref, ctypes.byref(desc), c.fmt, k_new.data_ptr(), v_new.data_ptr(),
+                                   cache.data_ptr(), c.stream())
     _check(st, "pearl_kv_append_mx")
 
 
@@ -448,24 +463,24 @@ def kv_pack_mx(cache: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.T
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Read token ranges [ctx_lens[b], ctx_lens[b] + n_b) of every sequence back out of a cache of MX
     blocks, as bf16 [2][total][H_kv][d] (pearl_kv_pack_mx)."""
-    shape, fmt = _mx_shape(None, cache)
-    want = (2, int(total), shape.num_kv_heads, shape.head_dim)
+    c = _MxCall(cache)
+    want = (2, int(total), c.shape.num_kv_heads, c.shape.head_dim)
     if out is None:
         out = torch.empty(want, dtype=torch.bfloat16, device=cache.device)
-    _need(out, "out", torch.bfloat16)
-    if tuple(out.shape) != want:
-        raise ValueError("out must have shape %s" % (want,))
-    desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len)
-    _on_current_device(cache, block_table, ctx_lens, cu_q_lens, out)
-    st = load().pearl_kv_pack_mx(ctypes.byref(shape), ctypes.byref(desc), fmt, cache.data_ptr(), out.data_ptr(), _stream())
+    else:
+        c.need(out, "out", torch.bfloat16)
+        if out.shape != want:
+            raise ValueError("out must have shape %s" % (want,))
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, c.need)
+    st = load().pearl_kv_pack_mx(c.ref, ctypes.byref(desc), c.fmt, cache.data_ptr(), out.data_ptr(), c.stream())
     _check(st, "pearl_kv_pack_mx")
     return out
 
 
 def workspace_bytes_mx(num_q_heads: int, cache: torch.Tensor, desc: SeqDesc) -> int:
     """Bytes of workspace that the attention calls over this cache need (pearl_attn_workspace_bytes)."""
-    shape, _ = _mx_shape(num_q_heads, cache)
-    n = load().pearl_attn_workspace_bytes(ctypes.byref(shape), ctypes.byref(desc))
+    _need(cache, "cache", torch.uint8)
+    n = load().pearl_attn_workspace_bytes(_mx_geometry(int(num_q_heads), tuple(cache.shape))[2], ctypes.byref(desc))
     if n == 0:
         raise PearlError(1, "pearl_attn_workspace_bytes", last_error())
     return int(n)
@@ -479,35 +494,36 @@ def _attention_mx(fname: str, q: torch.Tensor, new, cache: torch.Tensor, block_t
     if q.dim() != 3:
         raise ValueError("q must be [total_q][num_q_heads][head_dim]")
     total_q, H_q, d = q.shape
-    shape, fmt = _mx_shape(H_q, cache)
-    if d != shape.head_dim:
-        raise ValueError("q has head_dim %d, the cache %d" % (d, shape.head_dim))
+    c = _MxCall(cache, H_q)
+    c.need(q, "q", torch.bfloat16)
+    if d != c.shape.head_dim:
+        raise ValueError("q has head_dim %d, the cache %d" % (d, c.shape.head_dim))
     for t, n in zip(new, ("k_new", "v_new")):
-        _need(t, n, torch.bfloat16)
-        if tuple(t.shape) != (total_q, shape.num_kv_heads, d):
+        c.need(t, n, torch.bfloat16)
+        if t.shape != (total_q, c.shape.num_kv_heads, d):
             raise ValueError("k_new and v_new must be [batch][num_kv_heads][head_dim]")
-    desc = make_desc(block_table, ctx_lens, cu_q_lens, total_q, max_q_len, max_kv_len)
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, total_q, max_q_len, max_kv_len, c.need)
     if out is None:
         out = torch.empty_like(q)
-    _need(out, "out", torch.bfloat16)
-    if out.shape != q.shape:
-        raise ValueError("out must have q's shape")
-    if return_lse and lse is None:
-        lse = torch.empty((total_q, H_q), dtype=torch.float32, device=q.device)
+    else:
+        c.need(out, "out", torch.bfloat16)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
     if lse is not None:
-        _need(lse, "lse", torch.float32)
-        if tuple(lse.shape) != (total_q, H_q):
+        c.need(lse, "lse", torch.float32)
+        if lse.shape != (total_q, H_q):
             raise ValueError("lse must be [total_q][num_q_heads]")
+    elif return_lse:
+        lse = torch.empty((total_q, H_q), dtype=torch.float32, device=q.device)
     if workspace is None:
         workspace = torch.empty(workspace_bytes_mx(H_q, cache, desc), dtype=torch.uint8, device=q.device)
     else:
-        _need(workspace, "workspace", torch.uint8)   # the library checks its size
-    _on_current_device(cache, q, *new, block_table, ctx_lens, cu_q_lens, out, lse, workspace)
+        c.need(workspace, "workspace", torch.uint8)  # the library checks its size
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
-    st = getattr(load(), fname)(ctypes.byref(shape), ctypes.byref(desc), fmt, q.data_ptr(),
-                                *[t.data_ptr() for t in new], cache.data_ptr(), float(scale), out.data_ptr(),
-                                _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream())
+    st = getattr(load(), fname)(c.ref, ctypes.byref(desc), c.fmt, q.data_ptr(), *[t.data_ptr() for t in new],
+                                cache.data_ptr(), float(scale), out.data_ptr(), _ptr(lse), workspace.data_ptr(),
+                                workspace.numel(), c.stream())
     _check(st, fname)
     return (out, lse) if lse is not None else out
 

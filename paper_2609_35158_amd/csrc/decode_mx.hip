@@ -41,7 +41,11 @@ struct MxCut {                                      // 2176 bytes of K and V a p
 // A unit: kPages pages of one (sequence, kv-head) and how they lie in a wave's buffer.
 template <int D, int kBits> struct Unit {
   using MX = MxBlock<D, kBits>;
-  static constexpr int kPages = D == 128 && kBits == 8 ? 2 : 4;
+  // Two buffers of 8 waves in LDS: 4 pages at D = 128 and 4 bits, 2 at 8 bits.  At D = 64 and 4 bits 2 pages leave room for
+  // a second workgroup (us a call with 4 pages and with 2, 8 kv-heads: 100 sequences of 300-3000 tokens 33.9 and 30.8, 16
+  // of 2K-30K 40.5 and 38.8); at 8 bits that loses more at large batches (256 of 200-3000: 79.4 and 83.8) than it gains at
+  // small ones (40 of 300-6000: 32.0 and 31.2).
+  static constexpr int kPages = D * kBits == 512 ? 4 : 2;
   static constexpr int TG = 4 * kPages;             // tokens of a lane group
   static constexpr int KB = D / 32;                 // 32-channel steps of the Q.K product
   static constexpr int TP = D / 32;                 // groups of 16 channel pairs
