@@ -581,25 +581,58 @@ template <int D, int KEYS = kKeysPerStage> struct DmaTile {
   }
 };
 
-// A wave's half page (8 tokens) of a K and of a V stage in MX blocks, as loaded, and its bf16 rows in DmaTile's
-// layout.
-template <int D, int kBits> struct MxStage {
+// A prefill stage in MX blocks.  K's codes and scales come into LDS as they are (MxKTile) and each wave turns its
+// operands into bf16 as it reads them: 4 (8 bits: 2) times fewer LDS reads than of a bf16 tile, which the reads of the
+// products bound, for conversions that the vector ALU does beside the MFMAs.  V, whose operands are transposed,
+// becomes a bf16 tile (MxV).
+template <int D, int kBits> struct MxKTile {
+  using MX = MxBlock<D, kBits>;
+  static constexpr int kPages = kKeysPerStage / kPage;
+  static constexpr int kScales = kPage * MX::kBlocks;       // bytes of a page's K scales
+  static constexpr int kBytes = kPages * (MX::kCodes + kScales);
+  static constexpr int PR = MX::kRow / 16;                  // 16-byte pieces of a row
+  static constexpr int NP = PR / 2;                         // a lane's, of D / 2 channels
+  // Piece q of row r sits in place q ^ swz(r), so that the 16 rows that a quarter of a wave reads lie in 16
+  // different 16-byte groups of the banks.
+  __device__ static __forceinline__ int swz(int r) { return r / (16 / PR) % PR; }
+  int k_off, v_off;                                         // of a lane's 16 bytes in a page's codes
+  __device__ __forceinline__ explicit MxKTile(int lane) {
+    k_off = lane / PR % kPage * MX::kRow + ((lane % PR) ^ swz(lane / PR)) * 16;
+    v_off = lane * 16;
+  }
+  // This wave's copies of a K stage (page w of it, waves 0-3) or of a V stage (waves 4-7): kCopies instructions.
+  // blk: the block of page w % 4; to: a K tile or a raw V buffer
+  static constexpr int kInstr = MX::kCodes > 1024 ? 2 : 1, kCopies = kInstr + 1;
+  __device__ __forceinline__ void send(const uint8_t* blk, int lane, int w, char* to) const {
+    const int page = w & 3, is_v = w >> 2;
+    const char* codes = reinterpret_cast<const char*>(blk) + (is_v ? MX::kVCodes : 0);
+    const int first = is_v ? v_off : k_off;
+    const int off[2] = {first, is_v ? first : first ^ 64};   // K rows 8 further (8 pieces a row): swz's bit 2
+    if (MX::kCodes >= 1024 || lane < MX::kCodes / 16) lds_dma16_rows<kInstr>(codes, off, to + page * MX::kCodes);
+    const char* scales = reinterpret_cast<const char*>(blk) + (is_v ? MX::kVScales : MX::kKScales);
+    if (lane < kScales / 16) lds_dma16_rows<1>(scales, &v_off, to + kPages * MX::kCodes + page * kScales);
+  }
+};
+
+// This wave's 8 tokens of a V stage: a channel pair a lane, for D / 16 tokens.
+template <int D, int kBits> struct MxV {
   using MX = MxBlock<D, kBits>;
   using DT = DmaTile<D>;
-  static constexpr int KW = D * kBits / 256;        // dwords of D / 8 channels of a token row
   static constexpr int VT = D / 16;                 // tokens of a lane's channel pair
   static constexpr int VW = VT * kBits / 16;        // dwords of them
-  uint32_t k[KW], ks, v[VW], vs[VT / 4];
-  int k_at, ks_at, v_at, vs_at;                     // this lane's places in a block
-  __device__ __forceinline__ MxStage(int lane, int w) {
-    const int half = 8 * (w & 1), row = half + lane / 8, piece = lane % 8;
-    k_at = row * MX::kRow + piece * (MX::kRow / 8);
-    ks_at = MX::k_scale(row, piece * (D / 8) / 32);
-    const int pair = lane % (D / 2), slot = half + lane / (D / 2) * VT;
-    v_at = MX::v_code(slot, pair);
-    vs_at = MX::v_scale(slot, pair / 16);
+  static constexpr int kPages = kKeysPerStage / kPage;
+  static constexpr int kScales = kPage * MX::kBlocks;       // bytes of a page's V scales
+  static constexpr int kRawBytes = kPages * (MX::kCodes + kScales);
+  uint32_t v[VW], vs[VT / 4];
+  int v_at, vs_at;                                  // this lane's places in a raw buffer
+  int v_to;                                         // and in a tile
+  __device__ __forceinline__ MxV(int lane, int w) {
+    const int pair = lane % (D / 2), slot = 8 * (w & 1) + lane / (D / 2) * VT, first = 8 * w + lane / (D / 2) * VT;
+    v_at = (w >> 1) * MX::kCodes + MX::v_code(slot, pair) - MX::kVCodes;
+    vs_at = kPages * MX::kCodes + (w >> 1) * kScales + MX::v_scale(slot, pair / 16) - MX::kVScales;
+    v_to = first * DT::RB + (((pair >> 2) ^ DT::swz(first)) << 4) + (pair & 3) * 4;
   }
-  template <int N> __device__ static __forceinline__ void load_words(uint32_t* x, const uint8_t* p) {
+  template <int N> __device__ static __forceinline__ void words(uint32_t* x, const char* p) {
     if constexpr (N == 1) {
       x[0] = *reinterpret_cast<const uint32_t*>(p);
     } else if constexpr (N == 2) {
@@ -612,42 +645,24 @@ template <int D, int kBits> struct MxStage {
       for (int i = 0; i < 4; ++i) x[i] = y[i];
     }
   }
-  __device__ __forceinline__ void load_k(const uint8_t* blk) {
-    load_words<KW>(k, blk + k_at);
-    ks = blk[ks_at];
+  __device__ __forceinline__ void read(const char* raw) {
+    words<VW>(v, raw + v_at);
+    words<VT / 4>(vs, raw + vs_at);
   }
-  __device__ __forceinline__ void load_v(const uint8_t* blk) {
-    load_words<VW>(v, blk + v_at);
-    load_words<VT / 4>(vs, blk + vs_at);
-  }
-  // K: D / 64 chunks of 8 channels of token row 8 w + lane / 8
-  __device__ __forceinline__ void store_k(char* dst, int w) const {
-    const int lane = threadIdx.x & 63, r = 8 * w + lane / 8, c0 = lane % 8 * (D / 64);
-    const float f = mx_scale(ks);
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      u32x4 x;
-      if constexpr (kBits == 4)
-        x = u32x4{mx_up<4, 0>(k[c], f), mx_up<4, 1>(k[c], f), mx_up<4, 2>(k[c], f), mx_up<4, 3>(k[c], f)};
-      else
-        x = u32x4{mx_up<8, 0>(k[2 * c], f), mx_up<8, 1>(k[2 * c], f), mx_up<8, 0>(k[2 * c + 1], f), mx_up<8, 1>(k[2 * c + 1], f)};
-      *reinterpret_cast<u32x4*>(dst + r * DT::RB + (((c0 + c) ^ DT::swz(r)) << 4)) = x;
-    }
-  }
-  // V: a dword (a channel pair of one token) at a time, a wave's lanes a whole row; of this wave's 8 tokens only
+  // A dword (a channel pair of one token) at a time, a wave's lanes a whole row; of this wave's 8 tokens only
   // the first `left` count, the others become zeros
-  __device__ __forceinline__ void store_v(char* dst, int w, int left) const {
-    const int lane = threadIdx.x & 63, pair = lane % (D / 2), t0 = lane / (D / 2) * VT;
+  __device__ __forceinline__ void store(char* dst, int left) const {
+    const int t0 = (threadIdx.x & 63) / (D / 2) * VT;
     auto put = [&](auto t_c) {
       constexpr int t = decltype(t_c)::value;
       if constexpr (t < VT) {
-        const int r = 8 * w + t0 + t;
         const float f = mx_scale_of<t % 4>(vs[t / 4]);
         uint32_t x;
         if constexpr (kBits == 4) x = mx_up<4, t % 4>(v[t / 4], f);
         else x = mx_up<8, t % 2>(v[t / 2], f);
         if (left < 8) x = t0 + t < left ? x : 0u;
-        *reinterpret_cast<uint32_t*>(dst + r * DT::RB + (((pair >> 2) ^ DT::swz(r)) << 4) + (pair & 3) * 4) = x;
+        // the lane's first token has row 8 w + t0, and the row t further the same slots but for swz's bits of t
+        *reinterpret_cast<uint32_t*>(dst + (v_to ^ (DT::swz(t) << 4)) + t * DT::RB) = x;
       }
     };
     put(std::integral_constant<int, 0>{});
@@ -660,6 +675,10 @@ template <int D, int kBits> struct MxStage {
     put(std::integral_constant<int, 7>{});
   }
 };
+
+// Bytes of a K stage in LDS.
+template <int D, int kBits> struct KTileBytes { static constexpr int value = MxKTile<D, kBits>::kBytes; };
+template <int D> struct KTileBytes<D, 0> { static constexpr int value = DmaTile<D>::BYTES; };
 
 // ------------------------------------------------------------------------------------------------
 // Prefill-append work item: one (sequence, kv-head g, q-tile).  The tile holds 256 q-rows =
@@ -696,13 +715,19 @@ template <int D, int kBits> struct MxStage {
 // (the copies issued since stay in flight).
 // ------------------------------------------------------------------------------------------------
 //
-// Over a cache of MX blocks (kBits 4 or 8 an element; 0: bf16 pools) only the way of a stage into its buffers
-// differs: a wave loads its 8 tokens' codes and scales of K(j+3) and V(j+2) into registers in its softmax phase of
-// pair j, after it has turned those it loaded a pair before, K(j+2) and V(j+1), into bf16 (exactly) and
-// stored them in the same buffers.  Everything from the buffers on is the same.
+// Over a cache of MX blocks (kBits 4 or 8 an element; 0: bf16 pools) the phases, the buffers' order and all from the scores
+// on are the same.  In a wave's softmax phase of pair j, K(j+2) (waves 0-3) and V(j+3) (waves 4-7) are copied as they are.
+// K stays so (MxKTile; the lane halves take the two halves of the channels, the queries likewise), its operands become
+// bf16 between the MFMAs.  V(j+1), copied two pairs before, becomes a bf16 tile (MxV) behind the softmax.
+// Both this kernel and the one on bf16 pools run at the card's power limit (clock 1.9-2.0 GHz with the MFMAs busy 46% of
+// the time, against 1.6-1.7 GHz and 63-70%): the conversions cost 10% there.  Four turns of 64-400 tokens on 4-24K
+// contexts, six of 512-2048 on 4-16K (4 bits) and eight prompts of 500-3000 at d = 64 (8 bits), us a call on one card:
+// 466, 1286, 129 so; K and V loaded into registers and both stored as bf16 tiles 482, 1321, 137; K so and V through
+// registers 477, 1308, 135; V's conversion before the softmax 473, 1298, 127.
 // at_end: called by every thread when the stages are done, before the epilogue.
 template <int D, int kBits, typename AtEnd>
-__device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int code, int g, char* kb0, char* vb0, AtEnd at_end) {
+__device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int code, int g, char* kb0, char* vb0, char* raw0,
+                                                AtEnd at_end) {
   constexpr int KB = D / 16;                        // 16-wide k blocks of the QK product
   constexpr int MB = D / 32;                        // 32-wide dim blocks of the PV product
   constexpr int SK = kKeysPerStage;                 // keys per stage
@@ -712,7 +737,7 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
   constexpr int RB = DT::RB;
   // buffer r of each tensor (r = stage % 3 is a compile-time constant wherever a buffer is used, so
   // every LDS address is a per-lane offset plus an immediate)
-  auto kbuf = [&](int r) { return kb0 + r * DT::BYTES; };
+  auto kbuf = [&](int r) { return kb0 + r * KTileBytes<D, kBits>::value; };
   auto vbuf = [&](int r) { return vb0 + r * DT::BYTES; };
 
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -738,9 +763,11 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
 
   bf16x8 qop[KB];
   {
-    const uint16_t* qrow = a.q + ((size_t)(si.q_start + (row_ok ? tok : t0)) * H_q + h) * D + 8 * half;
+    // channels of k block kb: 16 kb + 8 half .., over MX blocks D / 2 half + 8 kb ..
+    constexpr int kStep = kBits == 0 ? 16 : 8;
+    const uint16_t* qrow = a.q + ((size_t)(si.q_start + (row_ok ? tok : t0)) * H_q + h) * D + (kBits == 0 ? 8 : D / 2) * half;
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) qop[kb] = row_ok ? as_bf16x8(ld16(qrow + 16 * kb)) : zero_bf16x8();
+    for (int kb = 0; kb < KB; ++kb) qop[kb] = row_ok ? as_bf16x8(ld16(qrow + kStep * kb)) : zero_bf16x8();
   }
   f32x16 oacc[MB];
 #pragma unroll
@@ -801,17 +828,34 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
     }
   };
 
-  // MX blocks: this wave's 8 tokens of a K and a V stage as loaded, and their way into the buffers.  K: 8 lanes
-  // a token row, D / 8 channels each.  V: a channel pair a lane, for D / 16 tokens.
+  // MX blocks
   static_assert(kBits == 0 || DT::RPW == 8, "a wave's tokens of a stage are half a page");
-  MxStage<D, kBits == 0 ? 4 : kBits> raw(lane, w);
-  auto mx_block = [&](int entry) {
-    return a.cache + ((size_t)clamp_page(entry, a.num_pages) * H_kv + g) * MxStage<D, kBits == 0 ? 4 : kBits>::MX::kBytes;
+  constexpr int kB = kBits == 0 ? 4 : kBits;
+  using MK = MxKTile<D, kB>;
+  using MX = MxBlock<D, kB>;
+  const MK mk(lane);
+  MxV<D, kB> mv(lane, w);
+  auto mx_block = [&](int entry) { return a.cache + ((size_t)clamp_page(entry, a.num_pages) * H_kv + g) * MX::kBytes; };
+  auto entry_of = [&](int j, int page) { return bt_c[min((step_begin + j) * (SK / kPage) + page, last_pidx)]; };
+  auto raw_buf = [&](int r) { return raw0 + r * MxV<D, kB>::kRawBytes; };
+  // Waves 0-3 copy a page each of K(j + 2), waves 4-7 of V(j + 3), as pair j's: V is turned into a tile a pair before K is
+  // read.  mx_next: this wave's block-table entry of the next pair to send.
+  auto mx_stage_of = [&](int j) { return j + (w < 4 ? 2 : 3); };
+  auto mx_has = [&](int j) { return mx_stage_of(j) >= 0 && mx_stage_of(j) < n; };
+  auto mx_entry = [&](int j) { return entry_of(max(min(mx_stage_of(j), n - 1), 0), w & 3); };
+  int mx_next = 0;
+  auto mx_send = [&](int j, char* k_tile, char* raw) {
+    if (mx_has(j)) mk.send(mx_block(mx_next), lane, w, w < 4 ? k_tile : raw);
+    mx_next = mx_entry(j + 1);
   };
-  auto mx_store_v = [&](int j, char* dst) { raw.store_v(dst, w, kv_needed - ((step_begin + j) * SK + DT::RPW * w)); };
+  auto mx_store_v = [&](int j, char* tile) { mv.store(tile, kv_needed - ((step_begin + j) * SK + DT::RPW * w)); };
+  // the lane's places in a K tile: row l % 32 of sub-tile 0, the pieces and scales of its half of the channels
+  const int mx_slot = lane & 15, mx_page = (lane >> 4) & 1;
+  const int mx_k = mx_page * MX::kCodes + mx_slot * MX::kRow + ((half * MK::NP) ^ MK::swz(mx_slot)) * 16;
+  const int mx_ks = MK::kPages * MX::kCodes + mx_page * MK::kScales + MX::k_scale(mx_slot, half * (D / 64)) - MX::kKScales;
 
   // block-table entries of the next copies: pid_k for K rows, pid_v for V rows (pid_n: the K
-  // rows after those, read ahead by group B).  MX blocks: of the next loads, of stages j + 3 and j + 2.
+  // rows after those, read ahead by group B)
   int pid_v = 1 < n ? page_of(1) : 0, pid_k = 2 < n ? page_of(2) : 0, pid_n = 0;
 
   f32x16 s[NST];                                    // S^T of the stage between its M and V phases
@@ -865,6 +909,49 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
     const char* kb_ = kbuf(R);
     const char* vb_ = vbuf((R + 2) % 3);
     if (!prefetched) prefetch(r_c);
+    if constexpr (kBits != 0) {
+      // K's raw words of a sub-tile are read 5 MFMAs before its first one, an operand is converted behind the
+      // MFMA before its own
+      constexpr int kAhead = NPV < 5 ? NPV : 5, KW = KB * kB / 4;    // KW: dwords of a lane's D / 2 channels
+      uint32_t kw[NST][KW], ks[NST][D / 64];
+      bf16x8 kop;
+      auto k_operand = [&](int q) {
+        const int st = q / KB, kb = q - (q / KB) * KB;
+        const float f = mx_scale(ks[st][kb / 4]);
+        const uint32_t* x = &kw[st][kb * kB / 4];
+        if constexpr (kB == 4)
+          return as_bf16x8(u32x4{mx_up<4, 0>(x[0], f), mx_up<4, 1>(x[0], f), mx_up<4, 2>(x[0], f), mx_up<4, 3>(x[0], f)});
+        else
+          return as_bf16x8(u32x4{mx_up<8, 0>(x[0], f), mx_up<8, 1>(x[0], f), mx_up<8, 0>(x[1], f), mx_up<8, 1>(x[1], f)});
+      };
+#pragma unroll
+      for (int i = 0; i < NM; ++i) {
+        if (i < NPV) {
+          const bf16x8 op = ring[i % kLead];
+          if (i + kLead < NPV) ring[i % kLead] = operand(i + kLead, kb_, vb_);
+          mfma_slot(i, op);
+        } else {
+          mfma_slot(i, kop);
+        }
+#pragma unroll
+        for (int st = 0; st < NST; ++st)
+          if (i == NPV + st * KB - kAhead) {
+            const int page = 2 * st * MX::kCodes;
+#pragma unroll
+            for (int x = 0; x < MK::NP; ++x) {
+              const u32x4 y = *reinterpret_cast<const u32x4*>(kb_ + page + (mx_k ^ (16 * x)));
+#pragma unroll
+              for (int z = 0; z < 4; ++z) kw[st][4 * x + z] = y[z];
+            }
+#pragma unroll
+            for (int x = 0; x < D / 64; ++x)
+              ks[st][x] = *reinterpret_cast<const uint8_t*>(kb_ + 2 * st * MK::kScales + mx_ks + 4 * x);
+          }
+        if (i + 1 >= NPV && i + 1 < NM) kop = k_operand(i + 1 - NPV);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NM; ++i) {
       const bf16x8 op = ring[i % kLead];
@@ -953,7 +1040,12 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
   // the barrier without the release fence of __syncthreads (which would drain every copy)
   constexpr int P = DT::NDMA;                       // DMA instructions per tensor and stage
   auto end_phase = [&](int t) {
-    if constexpr (kBits != 0) {                     // the compiler waits for its loads itself, where it uses them
+    if constexpr (kBits != 0) {
+      // t = 2 j + 1: K(j + 1) and V(j + 2) are read from the next phase on; pair j's own copies stay in flight
+      if ((t & 1) != 0) {
+        if (mx_has(t >> 1)) __builtin_amdgcn_s_waitcnt(PEARL_VMCNT(MK::kCopies));
+        else __builtin_amdgcn_s_waitcnt(PEARL_VMCNT(0));
+      }
       __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       return;
     }
@@ -985,36 +1077,29 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
     __builtin_amdgcn_s_waitcnt(PEARL_VMCNT(0));     // Q loads and the first copies (also this item's)
     __asm__ volatile("s_barrier" ::: "memory");
   } else {
-    const uint8_t* b0 = mx_block(page_of(0));
-    raw.load_k(b0);
-    raw.load_v(b0);
-    raw.store_k(kbuf(0), w);
+    // K(0), K(1), V(0), V(1), V(2), of which V(0) becomes a tile here
+    mx_next = mx_entry(-3);
+    mx_send(-3, kbuf(2), raw_buf(0));               // V(0)
+    mx_send(-2, kbuf(0), raw_buf(1));               // K(0), V(1)
+    mx_send(-1, kbuf(1), raw_buf(2));               // K(1), V(2)
+    __asm__ volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // also the item before has left the buffers
+    mv.read(raw_buf(0));
     mx_store_v(0, vbuf(0));
-    if (1 < n) {
-      raw.load_k(mx_block(pid_v));
-      raw.store_k(kbuf(1), w);
-      raw.load_v(mx_block(pid_v));                  // pair 0: K(2), V(1)
-    }
-    if (2 < n) raw.load_k(mx_block(pid_k));
 #pragma unroll
     for (int i = 0; i < DT::BYTES / (kThreads * 16); ++i)
       *reinterpret_cast<u32x4*>(vbuf(2) + (i * kThreads + threadIdx.x) * 16) = u32x4{0u, 0u, 0u, 0u};
-    pid_v = pid_k;
-    if (3 < n) pid_k = page_of(3);
     __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   }
-  // MX blocks, in the softmax phase of pair j (R = j % 3): what was loaded for the pair goes into the buffers, the
-  // next pair's loads go out.
-  auto mx_pair = [&](auto r_c, int j) {
+  // MX blocks, in the softmax phase of pair j (R = j % 3): V(j + 1), in raw buffer (j + 1) % 3, becomes a tile; K(j + 2) and
+  // V(j + 3) are sent, V(j + 3) into the raw buffer whose V(j) became a tile a pair ago
+  auto mx_before = [&](auto r_c, int j) {           // before the softmax
+    constexpr int R = decltype(r_c)::value;
+    mx_send(j, kbuf((R + 2) % 3), raw_buf(R));
+    if (j + 1 < n) mv.read(raw_buf((R + 1) % 3));
+  };
+  auto mx_after = [&](auto r_c, int j) {            // behind it
     constexpr int R = decltype(r_c)::value;
     if (j + 1 < n) mx_store_v(j + 1, vbuf((R + 1) % 3));
-    if (j + 2 < n) {
-      raw.store_k(kbuf((R + 2) % 3), w);
-      raw.load_v(mx_block(pid_v));
-    }
-    if (j + 3 < n) raw.load_k(mx_block(pid_k));
-    pid_v = pid_k;
-    if (j + 4 < n) pid_k = page_of(j + 4);
   };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
@@ -1037,8 +1122,9 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
         if (j + 3 < n) pid_k = page_of(j + 3);
         phase_v(j);
       } else {
+        mx_before(r_c, j);
         phase_v(j);
-        mx_pair(r_c, j);
+        mx_after(r_c, j);
       }
       prefetch(std::integral_constant<int, (R + 1) % 3>{});
       end_phase(2 * j + 1);
@@ -1071,8 +1157,9 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
         if (j + 3 < n) pid_n = page_of(j + 3);
         phase_v(j - 1);
       } else {
+        mx_before(r_c, j);
         phase_v(j - 1);
-        mx_pair(r_c, j);
+        mx_after(r_c, j);
       }
       prefetch(r_c);
       end_phase(2 * j);
@@ -1087,7 +1174,8 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
       copy_k(I0{}, 0);
       if (3 < n) pid_n = page_of(3);
     } else {
-      mx_pair(I0{}, 0);
+      mx_before(I0{}, 0);
+      mx_after(I0{}, 0);
     }
     end_phase(0);
     phase_m(I0{}, false);
@@ -1532,7 +1620,8 @@ __global__ __launch_bounds__((KernelCfg<D, kKinds>::NT)) void attn_kernel(AttnAr
   char* stageB = (kKinds == 2) ? stageB_ : smem + NW * PageTile<D>::BYTES;
   // prefill-only kernels: three K and three V stage buffers, each set contiguous
   constexpr int kDT = (kKinds == 1) ? DmaTile<D>::BYTES : 16;
-  __shared__ __attribute__((aligned(16))) char pk[3 * kDT], pv[3 * kDT];
+  __shared__ __attribute__((aligned(16))) char pk[kKinds == 1 ? 3 * KTileBytes<D, kBits>::value : 16], pv[3 * kDT];
+  __shared__ __attribute__((aligned(16))) char raw[kBits != 0 ? 3 * MxV<D, kBits == 0 ? 4 : kBits>::kRawBytes : 16];
   __shared__ int s_item[2][2];                      // next item and claim mode
   const int n_items = a.ws_hdr[kHdrNumItems];
   const int n_pre = a.ws_hdr[kHdrNumPre];
@@ -1627,13 +1716,13 @@ __global__ __launch_bounds__((KernelCfg<D, kKinds>::NT)) void attn_kernel(AttnAr
         static_assert(NW == kWaves, "prefill tiles use 8 waves");
         const int2 en = a.entries[e];
         if constexpr (kKinds == 1) {
-          prefill_tile_pp<D, kBits>(a, en.x, en.y, g, pk, pv, send_claim);
+          prefill_tile_pp<D, kBits>(a, en.x, en.y, g, pk, pv, raw, send_claim);
         } else {
           // the mixed kernel's prefill stage buffers share its LDS region with the decode stages (a
           // workgroup runs one item at a time, and items are separated by a drained barrier)
           constexpr int B = DmaTile<D>::BYTES;
           static_assert(6 * B <= Lds<D, NW, kKinds>::bytes, "stage buffers fit the shared region");
-          prefill_tile_pp<D, 0>(a, en.x, en.y, g, smem, smem + 3 * B, send_claim);
+          prefill_tile_pp<D, 0>(a, en.x, en.y, g, smem, smem + 3 * B, raw, send_claim);
         }
       }
     } else {
