@@ -27,32 +27,41 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ u16x2 as_u16x2(uint32_t x) { return __builtin_bit_cast(u16x2, x); }
+__device__ __forceinline__ uint32_t as_u32(u16x2 x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) { return as_u32(__builtin_elementwise_max(as_u16x2(a), as_u16x2(b))); }
+
+// The maximum, in each half of a dword, with the lane that a DPP control names.
 template <int kCtrl> __device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
-  const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false);
-  return x > y ? x : y;
+  return pk_max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false));
 }
 constexpr int kQuadXor1 = 0xB1, kQuadXor2 = 0x4E, kRowRor = 0x120;
 
-// The larger magnitude of a dword's two bf16, as bits: NaN and infinity are the largest.
-__device__ __forceinline__ uint32_t mag2(uint32_t w) {
-  const uint32_t a = w & 0x7fffu, b = (w >> 16) & 0x7fffu;
-  return a > b ? a : b;
+// The magnitudes of a dword's two bf16, as bits: NaN and infinity are the largest.
+__device__ __forceinline__ uint32_t mags(uint32_t w) { return w & 0x7fff7fffu; }
+
+// The scale bytes of two blocks, in the halves of a dword, from the bits of their largest magnitudes: the exponent, one
+// more if the 7 mantissa bits are over 96 (1.75 = 1 + 96 / 128; adding 31 carries then), less emax, at least 1; 0xffff
+// (byte 255) from infinity on.
+template <int kBits> __device__ __forceinline__ uint32_t scale_bytes(uint32_t amax) {
+  const u16x2 m = as_u16x2(amax);
+  const u16x2 e = (m + (u16x2){31, 31}) >> (u16x2){7, 7};
+  constexpr unsigned short least = kBits == 4 ? 3 : 9;      // emax + 1
+  const u16x2 s = __builtin_elementwise_max(e, (u16x2){least, least}) - (u16x2){least - 1, least - 1};
+  typedef short s16x2_ __attribute__((ext_vector_type(2)));
+  const s16x2_ bad = __builtin_bit_cast(s16x2_, m + (u16x2){0x80, 0x80}) >> (s16x2_){15, 15};
+  return as_u32(s) | __builtin_bit_cast(uint32_t, bad);
 }
 
-// The scale byte of a block whose largest magnitude has these bf16 bits.
-template <int kBits> __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
-  const int e = (int)(amax >> 7), s = e - (kBits == 4 ? 2 : 8) + ((amax & 127u) > 96u);
-  return e == 255 ? 255u : (uint32_t)(s < 1 ? 1 : s);
-}
-
-// Two bf16 as codes: a byte (4 bits) or 16 bits (8 bits).
-template <int kBits> __device__ __forceinline__ uint32_t mx_down(uint32_t w, float scale) {
-  if constexpr (kBits == 4) {
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, w), scale, 0) & 0xffu;
-  } else {
-    const s16x2 r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, __builtin_bit_cast(bf16x2, w), scale, false);
-    return (uint32_t)(uint16_t)r[0];
-  }
+// Two bf16 as codes into part kSel of a dword: a byte of four (4 bits), or a half (8 bits).
+template <int kBits, int kSel> __device__ __forceinline__ uint32_t mx_down(uint32_t old, uint32_t w, float scale) {
+  if constexpr (kBits == 4)
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(bf16x2, w), scale, kSel);
+  else
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(
+        __builtin_bit_cast(s16x2, old), __builtin_bit_cast(bf16x2, w), scale, kSel != 0));
 }
 
 // The (page, kv-head) of a workgroup: its slots [s0, s1) hold the rows row0 .. of this call.
@@ -76,6 +85,98 @@ __device__ __forceinline__ PageRows page_rows(int item, const int32_t* bt, int b
                   bt[(size_t)b * bt_stride + lp], (size_t)(q_start + first - ctx)};
 }
 
+// One page of a kv-head: its slots [s0, s1), all of them if kWhole.
+template <int D, int kBits, bool kWhole>
+__device__ __forceinline__ void append_page(const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new,
+                                            uint8_t* __restrict__ blk, const PageRows& p, int h, int num_kv_heads) {
+  using MX = MxBlock<D, kBits>;
+  constexpr int kRowThreads = D / 8, kIters = kPage / 8;    // 8 rows of K at once
+  const int tid = threadIdx.x;
+  const int row_len = num_kv_heads * D;
+  // slot 0's row (of slots before s0 none is read): a uniform base, and a lane's 32-bit offsets from it
+  const long long base = ((long long)p.row0 - p.s0) * row_len + (long long)h * D;
+  auto holds = [&](int slot) { return kWhole || (slot >= p.s0 && slot < p.s1); };
+  // all loads first: K 16 bytes of rows tid / kRowThreads + {0, 8}, V 4 bytes of 8 tokens
+  const int kr = tid / kRowThreads, kc = tid % kRowThreads;
+  const int pair = tid % (D / 2), half = tid / (D / 2);
+  u32x4 k[kIters];
+  uint32_t v[8];
+#pragma unroll
+  for (int i = 0; i < kIters; ++i)
+    k[i] = holds(kr + 8 * i) ? *reinterpret_cast<const u32x4*>(k_new + (base + (long long)8 * i * row_len) + (unsigned)(kr * row_len + 8 * kc))
+                             : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int t = 0; t < 8; ++t)
+    v[t] = holds(8 * half + t)
+               ? *reinterpret_cast<const uint32_t*>(v_new + (base + (long long)t * row_len) + (unsigned)(8 * half * row_len + 2 * pair))
+               : 0u;
+#pragma unroll
+  for (int i = 0; i < kIters; ++i) {
+    const int slot = kr + 8 * i;
+    uint32_t m = pk_max(pk_max(mags(k[i][0]), mags(k[i][1])), pk_max(mags(k[i][2]), mags(k[i][3])));
+    m = pk_max(m, m >> 16 | m << 16);
+    m = dpp_max<kQuadXor2>(dpp_max<kQuadXor1>(m));
+    const uint32_t s = scale_bytes<kBits>(m) & 0xffu;
+    const float f = mx_scale(s);
+    u32x2 c;
+    if constexpr (kBits == 4)
+      c = u32x2{mx_down<4, 3>(mx_down<4, 2>(mx_down<4, 1>(mx_down<4, 0>(0u, k[i][0], f), k[i][1], f), k[i][2], f), k[i][3], f), 0u};
+    else
+      c = u32x2{mx_down<8, 1>(mx_down<8, 0>(0u, k[i][0], f), k[i][1], f), mx_down<8, 1>(mx_down<8, 0>(0u, k[i][2], f), k[i][3], f)};
+    if (s == 255u) c = u32x2{0u, 0u};
+    if (holds(slot)) {
+      if constexpr (kBits == 4) *reinterpret_cast<uint32_t*>(blk + slot * MX::kRow + 4 * kc) = c[0];
+      else *reinterpret_cast<u32x2*>(blk + slot * MX::kRow + 8 * kc) = c;
+      if ((kc & 3) == 0) blk[MX::k_scale(slot, kc >> 2)] = (uint8_t)s;
+    }
+  }
+  // V: tokens 2 x and 2 x + 1 side by side in the halves of a dword, from their maxima to their scales
+  uint32_t s2[4], c[kBits / 2];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const uint32_t a = mags(v[2 * x]), b = mags(v[2 * x + 1]);
+    uint32_t m = pk_max(__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(b, a, 0x07060302u));
+    m = dpp_max<kRowRor + 8>(m);
+    m = dpp_max<kRowRor + 4>(m);
+    m = dpp_max<kRowRor + 2>(m);
+    m = dpp_max<kRowRor + 1>(m);
+    s2[x] = scale_bytes<kBits>(m);
+    const float f0 = mx_scale(s2[x] & 0xffu), f1 = mx_scale(s2[x] >> 16 & 0xffu);
+    if constexpr (kBits == 4) {
+      if (x % 2 == 0) c[x / 2] = mx_down<4, 1>(mx_down<4, 0>(0u, v[2 * x], f0), v[2 * x + 1], f1);
+      else c[x / 2] = mx_down<4, 3>(mx_down<4, 2>(c[x / 2], v[2 * x], f0), v[2 * x + 1], f1);
+    } else {
+      c[x] = mx_down<8, 1>(mx_down<8, 0>(0u, v[2 * x], f0), v[2 * x + 1], f1);
+    }
+  }
+  if (__ballot(((s2[0] | s2[1] | s2[2] | s2[3]) & 0xff00ff00u) != 0u)) {   // some block has no scale: codes 0
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      if (s2[t / 2] >> (16 * (t % 2) + 8) & 1u) {
+        if constexpr (kBits == 4) c[t / 4] &= ~(0xffu << (8 * (t % 4)));
+        else c[t / 2] &= ~(0xffffu << (16 * (t % 2)));
+      }
+  }
+  const u32x2 s8 = {__builtin_amdgcn_perm(s2[1], s2[0], 0x06040200u), __builtin_amdgcn_perm(s2[3], s2[2], 0x06040200u)};
+  const bool scales = (pair & 15) == 0;
+  uint8_t* const vc = blk + MX::v_code(8 * half, pair);
+  uint8_t* const vs = blk + MX::v_scale(8 * half, pair >> 4);
+  const int lo = p.s0 - 8 * half, hi = p.s1 - 8 * half;       // this thread's tokens are lo <= t < hi
+  if (kWhole || (lo <= 0 && hi >= 8)) {
+    if constexpr (kBits == 4) *reinterpret_cast<u32x2*>(vc) = u32x2{c[0], c[1]};
+    else *reinterpret_cast<u32x4*>(vc) = u32x4{c[0], c[1], c[2], c[3]};
+    if (scales) *reinterpret_cast<u32x2*>(vs) = s8;
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      if (t < lo || t >= hi) continue;
+      if constexpr (kBits == 4) vc[t] = (uint8_t)(c[t / 4] >> (8 * (t % 4)));
+      else reinterpret_cast<uint16_t*>(vc)[t] = (uint16_t)(c[t / 2] >> (16 * (t % 2)));
+      if (scales) vs[t] = (uint8_t)(s8[t / 4] >> (8 * (t % 4)));
+    }
+  }
+}
+
 }  // namespace
 
 // blockIdx.x = (b * pages_per_seq + rel) * num_kv_heads + h.  Rows of a page id outside [0, num_pages) are skipped.
@@ -87,7 +188,6 @@ __global__ __launch_bounds__(D) void kv_append_mx_kernel(
     const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
     const int32_t* __restrict__ cu, int pages_per_seq, int num_kv_heads, int num_pages, int total_q, ZeroWords zero) {
   using MX = MxBlock<D, kBits>;
-  constexpr int kRowThreads = D / 8, kRowsAtOnce = D / kRowThreads, kIters = kPage / kRowsAtOnce;   // 8 rows, 2 turns
   if (blockIdx.x == 0) {
     if (zero.hdr && threadIdx.x < kHdrWords) zero.hdr[threadIdx.x] = 0;
     for (int i = threadIdx.x; i < zero.n_cnt; i += D) zero.cnt[i] = 0;
@@ -95,76 +195,11 @@ __global__ __launch_bounds__(D) void kv_append_mx_kernel(
   const int item = blockIdx.x / num_kv_heads, h = blockIdx.x - item * num_kv_heads;
   const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, pages_per_seq, total_q);
   if (p.s0 >= p.s1 || p.page < 0 || p.page >= num_pages) return;
-  const int tid = threadIdx.x;
   uint8_t* const blk = cache + ((size_t)p.page * num_kv_heads + h) * MX::kBytes;
-  auto row = [&](const uint16_t* rows, int slot) {  // slot in [s0, s1)
-    return rows + ((p.row0 + (slot - p.s0)) * num_kv_heads + h) * D;
-  };
-  // all loads first: K 16 bytes of rows tid / kRowThreads + {0, 8}, V 4 bytes of 8 tokens
-  const int kr = tid / kRowThreads, kc = tid % kRowThreads;
-  u32x4 k[kIters];
-#pragma unroll
-  for (int i = 0; i < kIters; ++i) {
-    const int slot = kr + i * kRowsAtOnce;
-    k[i] = slot >= p.s0 && slot < p.s1 ? *reinterpret_cast<const u32x4*>(row(k_new, slot) + 8 * kc) : u32x4{0u, 0u, 0u, 0u};
-  }
-  const int pair = tid % (D / 2), half = tid / (D / 2);
-  uint32_t v[8];
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    const int slot = 8 * half + t;
-    v[t] = slot >= p.s0 && slot < p.s1 ? *reinterpret_cast<const uint32_t*>(row(v_new, slot) + 2 * pair) : 0u;
-  }
-#pragma unroll
-  for (int i = 0; i < kIters; ++i) {
-    const int slot = kr + i * kRowsAtOnce;
-    uint32_t m = max(max(mag2(k[i][0]), mag2(k[i][1])), max(mag2(k[i][2]), mag2(k[i][3])));
-    m = dpp_max<kQuadXor2>(dpp_max<kQuadXor1>(m));
-    const uint32_t s = scale_byte<kBits>(m);
-    const float f = mx_scale(s);
-    uint32_t c[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = s == 255u ? 0u : mx_down<kBits>(k[i][j], f);
-    if (slot >= p.s0 && slot < p.s1) {
-      if constexpr (kBits == 4)
-        *reinterpret_cast<uint32_t*>(blk + slot * MX::kRow + 4 * kc) = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
-      else
-        *reinterpret_cast<u32x2*>(blk + slot * MX::kRow + 8 * kc) = u32x2{c[0] | c[1] << 16, c[2] | c[3] << 16};
-      if ((kc & 3) == 0) blk[MX::k_scale(slot, kc >> 2)] = (uint8_t)s;
-    }
-  }
-  uint32_t c[8], s[8];
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    uint32_t m = mag2(v[t]);
-    m = dpp_max<kRowRor + 8>(m);
-    m = dpp_max<kRowRor + 4>(m);
-    m = dpp_max<kRowRor + 2>(m);
-    m = dpp_max<kRowRor + 1>(m);
-    s[t] = scale_byte<kBits>(m);
-    c[t] = s[t] == 255u ? 0u : mx_down<kBits>(v[t], mx_scale(s[t]));
-  }
-  const int lo = p.s0 - 8 * half, hi = p.s1 - 8 * half;       // this thread's tokens are lo <= t < hi
-  if (lo >= 8 || hi <= 0) return;
-  const bool scales = (pair & 15) == 0;
-  uint8_t* const vc = blk + MX::v_code(8 * half, pair);
-  uint8_t* const vs = blk + MX::v_scale(8 * half, pair >> 4);
-  if (lo <= 0 && hi >= 8) {
-    if constexpr (kBits == 4)
-      *reinterpret_cast<u32x2*>(vc) = u32x2{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24};
-    else
-      *reinterpret_cast<u32x4*>(vc) = u32x4{c[0] | c[1] << 16, c[2] | c[3] << 16, c[4] | c[5] << 16, c[6] | c[7] << 16};
-    if (scales)
-      *reinterpret_cast<u32x2*>(vs) = u32x2{s[0] | s[1] << 8 | s[2] << 16 | s[3] << 24, s[4] | s[5] << 8 | s[6] << 16 | s[7] << 24};
-  } else {
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      if (t < lo || t >= hi) continue;
-      if constexpr (kBits == 4) vc[t] = (uint8_t)c[t];
-      else reinterpret_cast<uint16_t*>(vc)[t] = (uint16_t)c[t];
-      if (scales) vs[t] = (uint8_t)s[t];
-    }
-  }
+  if (p.s0 == 0 && p.s1 == kPage)
+    append_page<D, kBits, true>(k_new, v_new, blk, p, h, num_kv_heads);
+  else
+    append_page<D, kBits, false>(k_new, v_new, blk, p, h, num_kv_heads);
 }
 
 // The rows of the same token ranges, as bf16: zeros for a page id outside [0, num_pages).
