@@ -16,7 +16,9 @@
 // A workgroup of D threads takes one (page, kv-head).  K: a thread quantises 8 channels of a
 // token, four threads share a block (a maximum over a quad).  V: a thread takes one channel pair for 8 tokens and
 // 16 neighbouring threads are a block, so the transposed unit is complete in the thread's registers.
-// Bound by HBM: bf16 rows one way (512 bytes a token and kv-head at D = 128), MX blocks the other (136 or 264).
+// Bound by HBM: bf16 rows one way (512 bytes a token and kv-head at D = 128), MX blocks the other (136 or 264).  80K tokens
+// of 8 kv-heads in 4 bits: append 76 us (5.6 TB/s of rows and blocks), read-back 78 us (5.4); a decode step's 64 tokens 4
+// and 3 us.
 
 #include "mx_format.h"
 
@@ -85,8 +87,14 @@ __device__ __forceinline__ PageRows page_rows(int item, const int32_t* bt, int b
                   bt[(size_t)b * bt_stride + lp], (size_t)(q_start + first - ctx)};
 }
 
+template <bool kOnce, typename T> __device__ __forceinline__ T read_row(const uint16_t* p) {
+  const T* q = reinterpret_cast<const T*>(p);
+  if constexpr (kOnce) return __builtin_nontemporal_load(q);
+  else return *q;
+}
+
 // One page of a kv-head: its slots [s0, s1), all of them if kWhole.
-template <int D, int kBits, bool kWhole>
+template <int D, int kBits, bool kOnce, bool kWhole>
 __device__ __forceinline__ void append_page(const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new,
                                             uint8_t* __restrict__ blk, const PageRows& p, int h, int num_kv_heads) {
   using MX = MxBlock<D, kBits>;
@@ -103,12 +111,12 @@ __device__ __forceinline__ void append_page(const uint16_t* __restrict__ k_new, 
   uint32_t v[8];
 #pragma unroll
   for (int i = 0; i < kIters; ++i)
-    k[i] = holds(kr + 8 * i) ? *reinterpret_cast<const u32x4*>(k_new + (base + (long long)8 * i * row_len) + (unsigned)(kr * row_len + 8 * kc))
+    k[i] = holds(kr + 8 * i) ? read_row<kOnce, u32x4>(k_new + (base + (long long)8 * i * row_len) + (unsigned)(kr * row_len + 8 * kc))
                              : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
   for (int t = 0; t < 8; ++t)
     v[t] = holds(8 * half + t)
-               ? *reinterpret_cast<const uint32_t*>(v_new + (base + (long long)t * row_len) + (unsigned)(8 * half * row_len + 2 * pair))
+               ? read_row<kOnce, uint32_t>(v_new + (base + (long long)t * row_len) + (unsigned)(8 * half * row_len + 2 * pair))
                : 0u;
 #pragma unroll
   for (int i = 0; i < kIters; ++i) {
@@ -182,7 +190,8 @@ __device__ __forceinline__ void append_page(const uint16_t* __restrict__ k_new, 
 // blockIdx.x = (b * pages_per_seq + rel) * num_kv_heads + h.  Rows of a page id outside [0, num_pages) are skipped.
 // The first workgroup also clears `zero` (a decode step's append and its decode are then two launches, as decode
 // alone).
-template <int D, int kBits>
+// kOnce: the rows are read past the caches.
+template <int D, int kBits, bool kOnce>
 __global__ __launch_bounds__(D) void kv_append_mx_kernel(
     const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new, uint8_t* __restrict__ cache,
     const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
@@ -197,9 +206,9 @@ __global__ __launch_bounds__(D) void kv_append_mx_kernel(
   if (p.s0 >= p.s1 || p.page < 0 || p.page >= num_pages) return;
   uint8_t* const blk = cache + ((size_t)p.page * num_kv_heads + h) * MX::kBytes;
   if (p.s0 == 0 && p.s1 == kPage)
-    append_page<D, kBits, true>(k_new, v_new, blk, p, h, num_kv_heads);
+    append_page<D, kBits, kOnce, true>(k_new, v_new, blk, p, h, num_kv_heads);
   else
-    append_page<D, kBits, false>(k_new, v_new, blk, p, h, num_kv_heads);
+    append_page<D, kBits, kOnce, false>(k_new, v_new, blk, p, h, num_kv_heads);
 }
 
 // The rows of the same token ranges, as bf16: zeros for a page id outside [0, num_pages).
@@ -279,6 +288,13 @@ int64_t page_items(int batch, int max_q_len, int num_kv_heads, int* pages_per_se
 }
 }  // namespace
 
+namespace {
+template <bool kOnce> auto append_kernel_of(int head_dim, int bits) {
+  return head_dim == 64 ? (bits == 4 ? kv_append_mx_kernel<64, 4, kOnce> : kv_append_mx_kernel<64, 8, kOnce>)
+                        : (bits == 4 ? kv_append_mx_kernel<128, 4, kOnce> : kv_append_mx_kernel<128, 8, kOnce>);
+}
+}  // namespace
+
 hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* v_new, uint8_t* cache,
                                const int32_t* block_table, int bt_stride, const int32_t* ctx_lens,
                                const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
@@ -287,8 +303,11 @@ hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* 
   int pages = 0;
   const int64_t blocks = page_items(batch, max_q_len, num_kv_heads, &pages);
   if (blocks < 0) return hipErrorInvalidValue;
-  auto kernel = head_dim == 64 ? (bits == 4 ? kv_append_mx_kernel<64, 4> : kv_append_mx_kernel<64, 8>)
-                               : (bits == 4 ? kv_append_mx_kernel<128, 4> : kv_append_mx_kernel<128, 8>);
+  // Rows of 48 MiB on are read with non-temporal loads: they would only push each other out of the caches.  us of an append
+  // and its read-back without and with them, 8 kv-heads, d = 128: 8K tokens (34 MB of rows) in 4 bits 17.5 and 18.0, in 8
+  // bits 19.4 and 20.5; 16K 38.0 and 32.5; 33K 68.7 and 61.1, in 8 bits 81.7 and 72.4; 66K 150 and 125.
+  const bool once = 4 * (int64_t)total_q * num_kv_heads * head_dim >= (int64_t)48 << 20;
+  auto kernel = once ? append_kernel_of<true>(head_dim, bits) : append_kernel_of<false>(head_dim, bits);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(head_dim), 0, stream, k_new, v_new, cache, block_table,
                      bt_stride, ctx_lens, cu_q_lens, pages, num_kv_heads, num_pages, total_q, zero);
   return hipGetLastError();

@@ -124,6 +124,23 @@ def test_every_bf16_and_every_code(fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+def test_rows_beyond_the_caches(fmt):
+    """An append of over 48 MiB of rows (read past the caches) gives the bytes of its parts' appends."""
+    say("large append fmt=%d" % fmt)
+    rng, n, hkv, d = np.random.default_rng(5), 13000, 8, 128
+    k, v = (torch.randn((n, hkv, d), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    pages = n // 16 + 3
+    bt = dev(rng.permutation(pages).astype(np.int32)[None])
+    ctx = dev(np.array([5], np.int32))
+    whole, parts = (torch.zeros((pages, hkv, oracle.mx_block_bytes(d, fmt)), dtype=torch.uint8, device="cuda") for _ in range(2))
+    pa.kv_append_mx(k, v, whole, bt, ctx, dev(np.array([0, n], np.int32)), n, n + 5)
+    for a, b in ((0, 6001), (6001, n)):
+        pa.kv_append_mx(k[a:b].contiguous(), v[a:b].contiguous(), parts, bt, ctx + a, dev(np.array([0, b - a], np.int32)), b - a, n + 5)
+    torch.cuda.synchronize()
+    assert torch.equal(whole, parts)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_pages_out_of_range_and_null_cu(fmt):
     say("bad pages fmt=%d" % fmt)
     cache, k, v, bt, ctx, cu = case(fmt, 128, 2, [40, 3, 70], [1, 1, 1], 7)
