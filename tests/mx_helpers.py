@@ -84,3 +84,63 @@ def check(case, out, lse, rows=None):
     if lse is not None:
         off = np.abs(lse.cpu().numpy().astype(np.float64) - ref_lse)
         assert (off <= tol_lse)[rows].all(), (float(off[rows].max()), float(tol_lse[rows].min()))
+
+
+def torch_attention(q, k, v, scale):
+    """One sequence in float64 on the GPU: q [n][hq][d], k and v [L][hkv][d], new token i at position L - n + i; (out, lse)."""
+    n, hq, d = q.shape
+    L, hkv, _ = k.shape
+    G = hq // hkv
+    q = q.double().view(n, hkv, G, d).permute(1, 2, 0, 3).reshape(hkv, G * n, d)
+    s = torch.matmul(q, k.double().permute(1, 2, 0).contiguous()) * float(np.float32(scale))
+    hidden = torch.arange(L, device=q.device)[None, :] > L - n + torch.arange(n, device=q.device)[:, None]
+    s = s.view(hkv, G, n, L).masked_fill_(hidden, float("-inf"))
+    lse = torch.logsumexp(s, -1)
+    o = torch.matmul((s - lse[..., None]).exp_().view(hkv, G * n, L), v.double().transpose(0, 1).contiguous())
+    return o.view(hkv, G, n, d).permute(2, 0, 1, 3).reshape(n, hq, d), lse.permute(2, 0, 1).reshape(n, hq)
+
+
+class BigCase:
+    """Sequences too large for the numpy oracle: a cache of quantised normal rows in random pages, on the GPU."""
+
+    def __init__(self, fmt, d, hkv, G, ctx, new, seed):
+        import paper_2609_35158_amd as pa
+        rng = np.random.default_rng(seed)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(seed)
+        self.d, self.hkv, self.hq, self.scale = d, hkv, hkv * G, float(np.float32(d ** -0.5))
+        self.kv = np.asarray(ctx) + np.asarray(new)
+        pages = (self.kv + 15) // 16
+        num_pages = int(pages.sum()) + 5
+        perm = rng.permutation(num_pages).astype(np.int32)
+        bt = np.full((len(pages), int(pages.max())), -1, np.int32)
+        at = 0
+        for b, n in enumerate(pages):
+            bt[b, :n] = perm[at:at + n]
+            at += n
+        # every page once, as pages of one long sequence
+        self.cache = pa.mx_cache(num_pages, hkv, d, fmt)
+        every, step = dev(np.arange(num_pages, dtype=np.int32)[None]), 4096
+        for p in range(0, num_pages, step):
+            n = 16 * min(step, num_pages - p)
+            k, v = (torch.randn((n, hkv, d), generator=gen, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+            pa.kv_append_mx(k, v, self.cache, every, dev(np.array([16 * p], np.int32)), dev(np.array([0, n], np.int32)), n, 16 * num_pages)
+        self.bt, self.ctx = dev(bt), dev(np.asarray(ctx, np.int32))
+        self.cu = dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32))
+        self.starts, self.new = np.concatenate([[0], np.cumsum(new)]), np.asarray(new)
+        self.q = torch.randn((int(self.new.sum()), self.hq, d), generator=gen, device="cuda", dtype=torch.bfloat16)
+        self.max_q, self.max_kv = int(self.new.max()), int(self.kv.max())
+
+    def check(self, out, lse, seqs):
+        """Sampled sequences: out within a rounding to bf16 and the weights' (2^-9 of a value of about 1), lse."""
+        import paper_2609_35158_amd as pa
+        zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+        for b in seqs:
+            n, r = int(self.kv[b]), slice(int(self.starts[b]), int(self.starts[b] + self.new[b]))
+            k, v = pa.kv_pack_mx(self.cache, self.bt[b:b + 1], zero, dev(np.array([0, n], np.int32)), n, n, n)
+            ref, ref_lse = torch_attention(self.q[r], k, v, self.scale)
+            off = (out[r].double() - ref).abs()
+            assert bool((off <= 2.0 ** -8 * ref.abs() + 2.0 ** -9 * 4).all()), (b, float(off.max()))
+            rel = float(off.norm() / ref.norm())
+            assert rel < 2.6e-3, (b, rel)          # 2^-8 / sqrt(3) / 2 from either rounding, in the 2-norm
+            assert float((lse[r].double() - ref_lse).abs().max()) < 2e-5, b

@@ -159,3 +159,25 @@ def test_two_graphs_of_one_workspace_and_other_streams():
         out, lse = pa.decode_mx(q, cache, bt, ctx, c.max_kv, scale=c.scale, return_lse=True, workspace=ws)
     side.synchronize()
     assert torch.equal(out, want[0][0]) and torch.equal(lse, want[0][1])
+
+
+# Batches whose workgroups hold several kv-heads (8, 4, 2 of them; a last block that overlaps the one before), shares of
+# whole and of cut sequences
+BIG = [(4, 128, 8, 4, 64, 2048, 8192), (8, 128, 4, 8, 40, 4000, 9000), (4, 128, 2, 2, 256, 1000, 6000),
+       (4, 64, 71, 1, 40, 700, 1000), (8, 64, 12, 2, 120, 800, 3000), (4, 128, 16, 1, 100, 900, 4000)]
+
+
+@pytest.mark.parametrize("n", range(len(BIG)))
+def test_large_batches(n):
+    from mx_helpers import BigCase
+    fmt, d, hkv, G, batch, lo, hi = BIG[n]
+    say("decode_mx large fmt=%d d=%d hkv=%d G=%d batch=%d" % (fmt, d, hkv, G, batch))
+    rng = np.random.default_rng(n)
+    ctx = rng.integers(lo, hi, size=batch)
+    c = BigCase(fmt, d, hkv, G, ctx, np.ones(batch, np.int64), n)
+    lse = torch.full((batch, c.hq), float("nan"), device="cuda")
+    out, lse = pa.decode_mx(c.q, c.cache, c.bt, c.ctx, c.max_kv, scale=c.scale, lse=lse)
+    again, _ = pa.decode_mx(c.q, c.cache, c.bt, c.ctx, c.max_kv, scale=c.scale, return_lse=True)
+    torch.cuda.synchronize()
+    assert torch.isfinite(lse).all() and torch.equal(out, again)       # every row written; no result depends on timing
+    c.check(out, lse, [0, 1, batch // 2, batch - 2, batch - 1] + [int(np.argmax(ctx)), int(np.argmin(ctx))])
