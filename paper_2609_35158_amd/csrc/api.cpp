@@ -332,8 +332,8 @@ pearl_status run_decode_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pea
     d.batch = std::min(q->batch - b0, kDecPlanMaxSeqs);
     d.max_kv_len = q->max_kv_len;
     d.max_dec = (int)pl.lay.max_dec;
-    set_decode_runs(d, s->num_kv_heads, grid, /*share_runs=*/true);
-    ZeroWords zero = decode_zero_words(a, d, /*share_runs=*/true);
+    set_decode_runs(d, s->num_kv_heads, grid);
+    ZeroWords zero = decode_zero_words(a, d);
     if (b0 > 0) zero.hdr = nullptr;                 // an earlier group's error flag stays
     hipError_t e;
     if (k_new) {

@@ -2250,7 +2250,7 @@ int decode_grid(int head_dim) {
   return c.num_cu * c.occ_dec[head_dim == 128 ? 1 : 0];
 }
 
-void set_decode_runs(DecPlanArgs& d, int num_kv_heads, int grid, bool share_runs) {
+void set_decode_runs(DecPlanArgs& d, int num_kv_heads, int grid) {
   // a run leaves at most two partials per head, the second ones also at most one per sequence
   const int cap = std::max(1, std::max(d.max_dec / 2, d.max_dec - d.batch));
   // a workgroup per run if they are all resident; with more kv-heads than that, runs for several rounds
@@ -2266,9 +2266,8 @@ void set_decode_runs(DecPlanArgs& d, int num_kv_heads, int grid, bool share_runs
   if (d.heads < 4 && num_kv_heads > 64) d.heads = kWaves;
   const int blocks = (num_kv_heads + d.heads - 1) / d.heads;
   d.runs_heads = std::max(1, grid / blocks);
-  const int per_run = share_runs ? kWaves / d.heads : 1;      // runs, for their slots, of a workgroup's head
-  if (8 * (int64_t)cap >= 7 * (int64_t)d.runs_heads * per_run && cap >= per_run) {   // not enough slots for a full grid of them, nearly
-    d.runs_heads = std::min(d.runs_heads, cap / per_run);
+  if (8 * cap >= 7 * d.runs_heads) {                // not enough slots for a full grid of them, nearly
+    d.runs_heads = std::min(d.runs_heads, cap);
   } else {
     d.heads = 1;
     d.runs_heads = 0;
@@ -2278,10 +2277,9 @@ void set_decode_runs(DecPlanArgs& d, int num_kv_heads, int grid, bool share_runs
   d.grid = std::max(grid, std::max(std::max(d.runs_one, d.runs_whole) * num_kv_heads, d.runs_heads * blocks));
 }
 
-ZeroWords decode_zero_words(const AttnArgs& a, const DecPlanArgs& d, bool share_runs) {
+ZeroWords decode_zero_words(const AttnArgs& a, const DecPlanArgs& d) {
   // a counter per sequence and kv-head, or per run and kv-head if that is fewer
-  const int runs_heads = share_runs ? d.runs_heads * (kWaves / d.heads) : d.runs_heads;
-  return ZeroWords{a.ws_hdr, a.split_cnt, std::min(d.batch, std::max(d.runs_one, runs_heads)) * a.num_kv_heads};
+  return ZeroWords{a.ws_hdr, a.split_cnt, std::min(d.batch, std::max(d.runs_one, d.runs_heads)) * a.num_kv_heads};
 }
 
 hipError_t launch_zero_words(const ZeroWords& zero, hipStream_t stream) {

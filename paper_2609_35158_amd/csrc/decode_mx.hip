@@ -461,18 +461,18 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     }
   }
 
-  // Several kv-heads in the workgroup: a wave finishes by itself, each share a run of its own.  Its partials go to the
-  // workspace from the registers, it counts itself in on their pairs and merges those whose last it is; no wave waits for
-  // another one.  (Through LDS and together, as below: 64 sequences of 2K-16K tokens in 4 bits 116 us, so 111.)
-  if (sh.heads > 1) {
+  // A kv-head of its own for every wave: its share is the run, so it finishes by itself.  Its partials go to the workspace
+  // from the registers, it counts itself in on their pairs and merges those whose last it is; no wave waits for another one.
+  // (8 kv-heads and 4 bits, through LDS and together as below and so: 64 sequences of 2K-16K tokens 115.7 and 112.8 us, at
+  // d = 64 256 of 200-3000 58.9 and 57.9.  Where waves share a kv-head, below wins, as it joins them first: 4 bits, 2
+  // kv-heads, 256 sequences of 1K-8K tokens 64.9 us, with every share a run of its own 69.0; 8 bits, 4 kv-heads, 200 of
+  // 300-3000 71.0 and 76.2.)
+  if (sh.heads == kWaves) {
     if (r.n <= 0 || r.j_w < r.dup) return;
-    const int subs = sh.subs(), x = r.x * subs + r.sub, n_runs = sh.n_runs * subs;
-    const bool per_pair = B < n_runs;
-    const int stride = per_pair ? 1 : 2;
     CutPair cut[2];
     auto store = [&](int b, const f32x4* o, float m, float l) {
       const int pu = uni(P.pre[b]), second = pu > r.t0;       // the pair's first entry
-      const int own = second ? (per_pair ? n_runs + b : 2 * x + 1) : stride * x;
+      const int own = second ? (r.per_pair ? sh.n_runs + b : 2 * r.x + 1) : r.slot_stride * r.x;
       float* to = a.part_o + (((size_t)g * d.max_dec + own) * G + hh) * D + 8 * group;
 #pragma unroll
       for (int p = 0; p < TP; ++p)
@@ -483,9 +483,9 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
           if (hh < G && odd == (p >= TP / 2)) st_dev2(to + 32 * p + 2 * i, odd ? other : mine, odd ? mine : other);
         }
       if (hh < G && lane < 8) st_dev2(&a.part_ml[2 * (((size_t)g * d.max_dec + own) * G + hh)], m, l);
-      const int x0 = sh.share_of(pu), x1 = sh.share_of(uni(P.pre[b + 1]) - 1);
+      const int x0 = sh.run_of(pu), x1 = sh.run_of(uni(P.pre[b + 1]) - 1);
       const bool at_start = pu <= sh.begin(x0);
-      return CutPair{b, x0, x1 - x0 + 1, at_start ? stride * x0 : (per_pair ? n_runs + b : 2 * x0 + 1)};
+      return CutPair{b, x0, x1 - x0 + 1, at_start ? r.slot_stride * x0 : (r.per_pair ? sh.n_runs + b : 2 * x0 + 1)};
     };
     cut[0].b = cut[1].b = -1;
     if (first_b >= 0) cut[0] = store(first_b, o_first, m_first, l_first);
@@ -494,13 +494,13 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     int seen = -1;
     const int b_mine = lane == 0 ? cut[0].b : cut[1].b, x_mine = lane == 0 ? cut[0].x0 : cut[1].x0;
     if (lane < 2 && b_mine >= 0)
-      seen = __hip_atomic_fetch_add(&a.split_cnt[per_pair ? g * B + b_mine : g * n_runs + x_mine], 1, __ATOMIC_RELAXED,
+      seen = __hip_atomic_fetch_add(&a.split_cnt[r.per_pair ? g * B + b_mine : g * sh.n_runs + x_mine], 1, __ATOMIC_RELAXED,
                                     __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
       const CutPair c = which == 0 ? cut[0] : cut[1];
       if (c.b < 0 || __builtin_amdgcn_readlane(seen, which) != c.n - 1) continue;
-      for (int pass = 0; pass < (G + 3) / 4; ++pass) merge_pair<D>(a, c, g, stride, d.max_dec, pass);
+      for (int pass = 0; pass < (G + 3) / 4; ++pass) merge_pair<D>(a, c, g, r.slot_stride, d.max_dec, pass);
     }
     return;
   }

@@ -178,11 +178,11 @@ template <class Cut> struct DecShares {
   }
   __device__ __forceinline__ int subs() const { return kWaves / heads; }   // shares per run
   __device__ __forceinline__ int begin(int share) const { return share * len + min(share, more); }
-  __device__ __forceinline__ int share_of(int t) const {                   // the share that holds entry t
+  __device__ __forceinline__ int run_of(int t) const {                     // the run that holds entry t
     const int big = more * (len + 1);
-    return t < big ? (unsigned)t / (unsigned)(len + 1) : more + (unsigned)(t - big) / (unsigned)max(len, 1);
+    const int share = t < big ? (unsigned)t / (unsigned)(len + 1) : more + (unsigned)(t - big) / (unsigned)max(len, 1);
+    return (unsigned)share / (unsigned)subs();
   }
-  __device__ __forceinline__ int run_of(int t) const { return (unsigned)share_of(t) / (unsigned)subs(); }
 };
 
 // A wave's partials at the end of its share, in the space of its own page stages: [0] the first

@@ -212,11 +212,10 @@ hipError_t launch_merge(const AttnArgs& a, int head_dim, int batch, hipStream_t 
 // Decode planned in-kernel (batch <= kDecPlanMaxSeqs): the zeroing prologue, then the kernel.
 // Workgroups that are resident together.
 int decode_grid(int head_dim);
-// Sets d's run counts and grid for so many resident workgroups, from d.batch and d.max_dec.  share_runs: where
-// workgroups hold several kv-heads, every wave's share is a run of its own (decode over MX blocks).
-void set_decode_runs(DecPlanArgs& d, int num_kv_heads, int grid, bool share_runs = false);
+// Sets d's run counts and grid for so many resident workgroups, from d.batch and d.max_dec.
+void set_decode_runs(DecPlanArgs& d, int num_kv_heads, int grid);
 // What a decode launch needs cleared.
-ZeroWords decode_zero_words(const AttnArgs& a, const DecPlanArgs& d, bool share_runs = false);
+ZeroWords decode_zero_words(const AttnArgs& a, const DecPlanArgs& d);
 hipError_t launch_zero_words(const ZeroWords& zero, hipStream_t stream);
 hipError_t launch_decode_prologue(const AttnArgs& a, const DecPlanArgs& d, hipStream_t stream);
 hipError_t launch_decode(const AttnArgs& a, const DecPlanArgs& d, int head_dim, hipStream_t stream);
