@@ -235,7 +235,8 @@ pearl_status pearl_kv_unpack(const pearl_kv_shape* shape, const pearl_seq_desc* 
  *   for E2M1, 8 for E4M3), at least 1, and an element is x * 2^(127 - s) rounded to nearest, ties to
  *   the even code, zeros keeping their sign; magnitudes above 6 in E2M1 become 6.  If an x is NaN or
  *   infinite, s is 255 and the codes are 0.  A value read back is code * 2^(s - 127) in bf16, exact (values
- *   under 2^-133 are rounded); quantising what was read back gives the same values.
+ *   under 2^-133 are rounded, and x from 1.75 * 2^127 on can come back as infinity, where the nearest element is
+ *   2^128); quantising what was read back gives the same values, of finite ones.
  *   cache: uint8 [num_pages][num_kv_heads][pearl_mx_block_bytes(head_dim, format)], 16-byte aligned.  A
  *   block holds the 16 tokens of one page and kv-head, nb = head_dim / 32:
  *     K codes, 16 rows: slot's channels in order (E2M1: two to a byte, the even channel in the low bits);

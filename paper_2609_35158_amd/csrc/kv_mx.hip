@@ -66,15 +66,45 @@ template <int kBits, int kSel> __device__ __forceinline__ uint32_t mx_down(uint3
         __builtin_bit_cast(s16x2, old), __builtin_bit_cast(bf16x2, w), scale, kSel != 0));
 }
 
+// How a launch's items, (sequence, logical page) pairs, are counted: per_seq a sequence, or, if that is 0, as
+// many as `batch` sequences' token counts can give.
+struct PageItems {
+  int per_seq, batch;
+};
+
 // The (page, kv-head) of a workgroup: its slots [s0, s1) hold the rows row0 .. of this call.
 struct PageRows {
   int s0, s1, page;                                 // s0 >= s1: nothing to do
   size_t row0;
 };
 
+// Where items are not pages_per_seq a sequence (PageItems), sequence b's start at cu[b] / 16 + 2 b: n tokens
+// starting anywhere touch at most n / 16 + 2 pages.  The sequence of an item is found by counting these
+// starts with ballots: 64 evenly spaced probes, then 64 in the gap between two, until there is none.
+__device__ __forceinline__ int first_item(const int32_t* cu, int b) { return max(cu[b], 0) / kPage + 2 * b; }
+__device__ __forceinline__ int seq_of(int item, const int32_t* cu, int batch) {
+  const int lane = threadIdx.x & 63;
+  int b = 0, n = batch;                             // it is one of b .. b + n - 1
+  while (n > 1) {
+    const int gap = (n + 63) / 64, probe = lane * gap;
+    const int at = max(__popcll(__ballot(probe < n && first_item(cu, b + min(probe, n - 1)) <= item)) - 1, 0) * gap;
+    b += at;
+    n = min(gap, n - at);
+  }
+  return __builtin_amdgcn_readfirstlane(b);
+}
+
 __device__ __forceinline__ PageRows page_rows(int item, const int32_t* bt, int bt_stride, const int32_t* ctx_lens,
-                                              const int32_t* cu, int pages_per_seq, int total_q) {
-  const int b = item / pages_per_seq, rel = item - b * pages_per_seq;
+                                              const int32_t* cu, const PageItems& it, int total_q) {
+  int b, rel;
+  if (it.per_seq > 0) {
+    b = item / it.per_seq;
+    rel = item - b * it.per_seq;
+  } else {
+    b = seq_of(item, cu, it.batch);
+    rel = item - first_item(cu, b);
+    if (rel < 0) return PageRows{0, 0, -1, 0};
+  }
   const int q_start = cu ? cu[b] : b;
   const int ctx = ctx_lens[b];
   const int q_len = min(cu ? cu[b + 1] - q_start : 1, total_q - q_start);
@@ -187,7 +217,7 @@ __device__ __forceinline__ void append_page(const uint16_t* __restrict__ k_new, 
 
 }  // namespace
 
-// blockIdx.x = (b * pages_per_seq + rel) * num_kv_heads + h.  Rows of a page id outside [0, num_pages) are skipped.
+// blockIdx.x = item * num_kv_heads + h.  Rows of a page id outside [0, num_pages) are skipped.
 // The first workgroup also clears `zero` (a decode step's append and its decode are then two launches, as decode
 // alone).
 // kOnce: the rows are read past the caches.
@@ -195,14 +225,14 @@ template <int D, int kBits, bool kOnce>
 __global__ __launch_bounds__(D) void kv_append_mx_kernel(
     const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new, uint8_t* __restrict__ cache,
     const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
-    const int32_t* __restrict__ cu, int pages_per_seq, int num_kv_heads, int num_pages, int total_q, ZeroWords zero) {
+    const int32_t* __restrict__ cu, PageItems items, int num_kv_heads, int num_pages, int total_q, ZeroWords zero) {
   using MX = MxBlock<D, kBits>;
   if (blockIdx.x == 0) {
     if (zero.hdr && threadIdx.x < kHdrWords) zero.hdr[threadIdx.x] = 0;
     for (int i = threadIdx.x; i < zero.n_cnt; i += D) zero.cnt[i] = 0;
   }
   const int item = blockIdx.x / num_kv_heads, h = blockIdx.x - item * num_kv_heads;
-  const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, pages_per_seq, total_q);
+  const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, items, total_q);
   if (p.s0 >= p.s1 || p.page < 0 || p.page >= num_pages) return;
   uint8_t* const blk = cache + ((size_t)p.page * num_kv_heads + h) * MX::kBytes;
   if (p.s0 == 0 && p.s1 == kPage)
@@ -216,11 +246,11 @@ template <int D, int kBits>
 __global__ __launch_bounds__(D) void kv_pack_mx_kernel(
     const uint8_t* __restrict__ cache, uint16_t* __restrict__ k_rows, uint16_t* __restrict__ v_rows,
     const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
-    const int32_t* __restrict__ cu, int pages_per_seq, int num_kv_heads, int num_pages, int total_q) {
+    const int32_t* __restrict__ cu, PageItems items, int num_kv_heads, int num_pages, int total_q) {
   using MX = MxBlock<D, kBits>;
   constexpr int kRowThreads = D / 8, kRowsAtOnce = D / kRowThreads, kIters = kPage / kRowsAtOnce;
   const int item = blockIdx.x / num_kv_heads, h = blockIdx.x - item * num_kv_heads;
-  const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, pages_per_seq, total_q);
+  const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, items, total_q);
   if (p.s0 >= p.s1) return;
   const bool ok = p.page >= 0 && p.page < num_pages;
   const int tid = threadIdx.x;
@@ -279,12 +309,19 @@ __global__ __launch_bounds__(D) void kv_pack_mx_kernel(
 }
 
 namespace {
-// Workgroups of a launch over the token ranges, or -1 if they pass the grid's limit: a range of n tokens
-// starting anywhere touches at most ceil((n + 15) / 16) pages.
-int64_t page_items(int batch, int max_q_len, int num_kv_heads, int* pages_per_seq) {
-  *pages_per_seq = (max_q_len + 2 * kPage - 2) / kPage;
-  const int64_t blocks = (int64_t)batch * *pages_per_seq * num_kv_heads;
-  return blocks > INT32_MAX ? -1 : blocks;
+// Workgroups of a launch over the token ranges, or -1 if they pass the grid's limit of 2^32 threads.  A sequence of up
+// to max_q_len tokens touches at most ceil((max_q_len + 15) / 16) pages.  As many items for each sequence are found without
+// a search, but where few are as long as the longest most items hold nothing.  us of an append, 8 kv-heads, d = 128, 4 bits,
+// with as many for each and by the token counts, and how many times more items the first gives: 256 sequences of 20 new
+// tokens (0.92) 9.0 and 10.0; 200 of 1-64 (1.23) 9.7 and 10.4; 32 of 1-4096 (1.89) 63.7 and 60.5; 63 of 100 and one of 330
+// (2.60) 10.0 and 8.5; 255 of one and one of 8192 (126) 376 and 12.
+int64_t page_items(int batch, int max_q_len, int total_q, bool ragged, int num_kv_heads, int head_dim, PageItems* items) {
+  const int64_t per_seq = ragged ? (max_q_len + 2 * kPage - 2) / kPage : 1;
+  const int64_t even = batch * per_seq, least = (int64_t)total_q / kPage + 2 * (int64_t)batch;
+  const bool by_count = 2 * even > 3 * least;
+  *items = PageItems{by_count ? 0 : (int)per_seq, batch};
+  const int64_t blocks = (by_count ? least : even) * num_kv_heads;
+  return blocks * head_dim > UINT32_MAX ? -1 : blocks;
 }
 }  // namespace
 
@@ -300,8 +337,8 @@ hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* 
                                const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
                                int num_pages, int total_q, const ZeroWords& zero, hipStream_t stream) {
   if (max_q_len <= 0 || batch <= 0 || total_q <= 0) return hipSuccess;
-  int pages = 0;
-  const int64_t blocks = page_items(batch, max_q_len, num_kv_heads, &pages);
+  PageItems items;
+  const int64_t blocks = page_items(batch, max_q_len, total_q, cu_q_lens != nullptr, num_kv_heads, head_dim, &items);
   if (blocks < 0) return hipErrorInvalidValue;
   // Rows of 48 MiB on are read with non-temporal loads: they would only push each other out of the caches.  us of an append
   // and its read-back without and with them, 8 kv-heads, d = 128: 8K tokens (34 MB of rows) in 4 bits 17.5 and 18.0, in 8
@@ -309,7 +346,7 @@ hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* 
   const bool once = 4 * (int64_t)total_q * num_kv_heads * head_dim >= (int64_t)48 << 20;
   auto kernel = once ? append_kernel_of<true>(head_dim, bits) : append_kernel_of<false>(head_dim, bits);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(head_dim), 0, stream, k_new, v_new, cache, block_table,
-                     bt_stride, ctx_lens, cu_q_lens, pages, num_kv_heads, num_pages, total_q, zero);
+                     bt_stride, ctx_lens, cu_q_lens, items, num_kv_heads, num_pages, total_q, zero);
   return hipGetLastError();
 }
 
@@ -318,13 +355,13 @@ hipError_t launch_kv_pack_mx(int bits, const uint8_t* cache, uint16_t* k_rows, u
                              const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
                              int num_pages, int total_q, hipStream_t stream) {
   if (max_q_len <= 0 || batch <= 0 || total_q <= 0) return hipSuccess;
-  int pages = 0;
-  const int64_t blocks = page_items(batch, max_q_len, num_kv_heads, &pages);
+  PageItems items;
+  const int64_t blocks = page_items(batch, max_q_len, total_q, cu_q_lens != nullptr, num_kv_heads, head_dim, &items);
   if (blocks < 0) return hipErrorInvalidValue;
   auto kernel = head_dim == 64 ? (bits == 4 ? kv_pack_mx_kernel<64, 4> : kv_pack_mx_kernel<64, 8>)
                                : (bits == 4 ? kv_pack_mx_kernel<128, 4> : kv_pack_mx_kernel<128, 8>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(head_dim), 0, stream, cache, k_rows, v_rows, block_table,
-                     bt_stride, ctx_lens, cu_q_lens, pages, num_kv_heads, num_pages, total_q);
+                     bt_stride, ctx_lens, cu_q_lens, items, num_kv_heads, num_pages, total_q);
   return hipGetLastError();
 }
 

@@ -89,6 +89,28 @@ def test_append_and_pack(fmt, d, hkv, n):
     assert_rows(bits(again), bits(rows))
 
 
+@pytest.mark.parametrize("batch", (2, 7, 63, 64, 65, 200, 4100))
+@pytest.mark.parametrize("fmt,d,hkv", ((4, 64, 3), (8, 128, 1)))
+def test_one_long_sequence_among_short_ones(fmt, d, hkv, batch):
+    """Token counts of which few are near the longest, where the kernels look an item's sequence up: the long one
+    first, last or between, and sequences without a new token on both sides of it."""
+    rng = np.random.default_rng(batch)
+    for at in sorted({0, batch // 2, batch - 1}):
+        say("ragged fmt=%d batch=%d long at %d" % (fmt, batch, at))
+        new = rng.integers(0, 3, size=batch)
+        new[at] = 40 * batch if batch <= 65 else 1500
+        cache, k, v, bt, ctx, cu = case(fmt, d, hkv, rng.integers(0, 40, size=batch), new, batch + at)
+        want = oracle.mx_append(cache, fmt, bits(k), bits(v), bt, ctx, cu)
+        c, btd, ctxd, cud = dev(cache), dev(bt), dev(ctx), dev(cu)
+        max_q, max_kv = int(new.max()), int((ctx + new).max())
+        pa.kv_append_mx(k.cuda(), v.cuda(), c, btd, ctxd, cud, max_q, max_kv)
+        rows = pa.kv_pack_mx(c, btd, ctxd, cud, int(cu[-1]), max_q, max_kv)
+        torch.cuda.synchronize()
+        got = c.cpu().numpy()
+        assert np.array_equal(got, want), np.argwhere(got != want)[:5]
+        assert_rows(bits(rows), oracle.mx_pack(want, d, fmt, bt, ctx, cu))
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_every_bf16_and_every_code(fmt):
     """All bf16 numbers through the quantiser, alone in their block and beside a larger one, and all codes under all
