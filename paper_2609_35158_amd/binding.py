@@ -409,14 +409,14 @@ def mx_cache(num_pages: int, num_kv_heads: int, head_dim: int, fmt: int, device=
 
 
 @functools.lru_cache(maxsize=256)
-def _mx_geometry(num_q_heads: int, cache_shape: Tuple[int, int, int]):
+def _mx_geometry(num_q_heads: Optional[int], cache_shape: Tuple[int, int, int]):
     """(KvShape, format, a reference to the shape for the library) of a cache [num_pages][H_kv][block]."""
     if not _MX_BLOCKS:
         _MX_BLOCKS.update({mx_block_bytes(d, f): (d, f) for d in (64, 128) for f in (MXFP4, MXFP8)})
     if len(cache_shape) != 3 or cache_shape[2] not in _MX_BLOCKS:
         raise ValueError("cache must be [num_pages][num_kv_heads][mx_block_bytes(head_dim, fmt)]")
     d, fmt = _MX_BLOCKS[cache_shape[2]]
-    shape = KvShape(num_q_heads or cache_shape[1], cache_shape[1], d, PAGE_SIZE, cache_shape[0])
+    shape = KvShape(cache_shape[1] if num_q_heads is None else num_q_heads, cache_shape[1], d, PAGE_SIZE, cache_shape[0])
     return shape, fmt, ctypes.byref(shape)
 
 

@@ -197,3 +197,13 @@ def test_attention_refusals(fn):
         assert st == INVALID and "cu_q_lens" in msg
         assert call(shape(), desc(total=5))[0] == INVALID
     assert call(shape(), desc(batch=1, stride=(1 << 21) + 1, max_kv=(1 << 25) + 1, **({} if not prefill else dict(cu=FAKE, total=1))))[0] == UNSUPPORTED
+
+
+def test_no_query_heads_are_not_taken_for_as_many_as_kv_heads():
+    cache = (5, 2, pa.mx_block_bytes(64, pa.MXFP4))
+    assert bd._mx_geometry(None, cache)[0].num_q_heads == 2
+    none, _, ref = bd._mx_geometry(0, cache)
+    assert none.num_q_heads == 0
+    q = desc()
+    assert pa.load().pearl_attn_workspace_bytes(ref, ctypes.byref(q)) == 0
+    assert "num_q_heads (0)" in bd.last_error()
