@@ -17,8 +17,7 @@
 // token, four threads share a block (a maximum over a quad).  V: a thread takes one channel pair for 8 tokens and
 // 16 neighbouring threads are a block, so the transposed unit is complete in the thread's registers.
 // Bound by HBM: bf16 rows one way (512 bytes a token and kv-head at D = 128), MX blocks the other (136 or 264).  80K tokens
-// of 8 kv-heads in 4 bits: append 76 us (5.6 TB/s of rows and blocks), read-back 78 us (5.4); a decode step's 64 tokens 4
-// and 3 us.
+// of 8 kv-heads in 4 bits: append 76 us (5.6 TB/s of rows and blocks), read-back 78 us (5.4).
 
 #include "mx_format.h"
 
@@ -94,6 +93,21 @@ __device__ __forceinline__ int seq_of(int item, const int32_t* cu, int batch) {
   return __builtin_amdgcn_readfirstlane(b);
 }
 
+// The rel-th page that sequence b's new tokens touch.
+__device__ __forceinline__ PageRows rows_of(int b, int rel, const int32_t* bt, int bt_stride, const int32_t* ctx_lens,
+                                            const int32_t* cu, int total_q) {
+  const int q_start = cu ? cu[b] : b;
+  const int ctx = ctx_lens[b];
+  const int q_len = min(cu ? cu[b + 1] - q_start : 1, total_q - q_start);
+  if (q_len <= 0 || q_start < 0 || ctx < 0) return PageRows{0, 0, -1, 0};
+  const int lp = ctx / kPage + rel;
+  const long long first = max((long long)ctx, (long long)lp * kPage);
+  const long long end = min((long long)ctx + q_len, ((long long)lp + 1) * kPage);
+  if (first >= end || lp >= bt_stride) return PageRows{0, 0, -1, 0};
+  return PageRows{(int)(first - (long long)lp * kPage), (int)(end - (long long)lp * kPage),
+                  bt[(size_t)b * bt_stride + lp], (size_t)(q_start + first - ctx)};
+}
+
 __device__ __forceinline__ PageRows page_rows(int item, const int32_t* bt, int bt_stride, const int32_t* ctx_lens,
                                               const int32_t* cu, const PageItems& it, int total_q) {
   int b, rel;
@@ -105,16 +119,7 @@ __device__ __forceinline__ PageRows page_rows(int item, const int32_t* bt, int b
     rel = item - first_item(cu, b);
     if (rel < 0) return PageRows{0, 0, -1, 0};
   }
-  const int q_start = cu ? cu[b] : b;
-  const int ctx = ctx_lens[b];
-  const int q_len = min(cu ? cu[b + 1] - q_start : 1, total_q - q_start);
-  if (q_len <= 0 || q_start < 0 || ctx < 0) return PageRows{0, 0, -1, 0};
-  const int lp = ctx / kPage + rel;
-  const long long first = max((long long)ctx, (long long)lp * kPage);
-  const long long end = min((long long)ctx + q_len, ((long long)lp + 1) * kPage);
-  if (first >= end || lp >= bt_stride) return PageRows{0, 0, -1, 0};
-  return PageRows{(int)(first - (long long)lp * kPage), (int)(end - (long long)lp * kPage),
-                  bt[(size_t)b * bt_stride + lp], (size_t)(q_start + first - ctx)};
+  return rows_of(b, rel, bt, bt_stride, ctx_lens, cu, total_q);
 }
 
 template <bool kOnce, typename T> __device__ __forceinline__ T read_row(const uint16_t* p) {
@@ -218,19 +223,13 @@ __device__ __forceinline__ void append_page(const uint16_t* __restrict__ k_new, 
 }  // namespace
 
 // blockIdx.x = item * num_kv_heads + h.  Rows of a page id outside [0, num_pages) are skipped.
-// The first workgroup also clears `zero` (a decode step's append and its decode are then two launches, as decode
-// alone).
 // kOnce: the rows are read past the caches.
 template <int D, int kBits, bool kOnce>
 __global__ __launch_bounds__(D) void kv_append_mx_kernel(
     const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new, uint8_t* __restrict__ cache,
     const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
-    const int32_t* __restrict__ cu, PageItems items, int num_kv_heads, int num_pages, int total_q, ZeroWords zero) {
+    const int32_t* __restrict__ cu, PageItems items, int num_kv_heads, int num_pages, int total_q) {
   using MX = MxBlock<D, kBits>;
-  if (blockIdx.x == 0) {
-    if (zero.hdr && threadIdx.x < kHdrWords) zero.hdr[threadIdx.x] = 0;
-    for (int i = threadIdx.x; i < zero.n_cnt; i += D) zero.cnt[i] = 0;
-  }
   const int item = blockIdx.x / num_kv_heads, h = blockIdx.x - item * num_kv_heads;
   const PageRows p = page_rows(item, bt, bt_stride, ctx_lens, cu, items, total_q);
   if (p.s0 >= p.s1 || p.page < 0 || p.page >= num_pages) return;
@@ -308,6 +307,94 @@ __global__ __launch_bounds__(D) void kv_pack_mx_kernel(
   token(std::integral_constant<int, 7>{});
 }
 
+// Up to one token a sequence, as in a decode step: a wave takes a (sequence, kv-head), a lane a channel pair of K and of V
+// (at D = 64 the half-waves take one each).  The rows are on their way while the page is looked up, and no vector work goes
+// into the 15 other slots.  The append's first workgroup also clears `zero` (a decode step's append and its decode are then
+// two launches, as decode alone).  us of an append and of a read-back, 8 kv-heads, d = 128, 4 bits, by the kernels above
+// and so: one sequence 2.9 and 2.0, so 2.1 and 1.9; 64 3.4 and 2.4, so 2.2 and 2.1; 512 7.2 and 4.4, so 3.7 and 2.9; 4096 34 and
+// 21, so 13 and 11.
+constexpr int kTokenWaves = 4;                      // of a workgroup
+
+namespace {
+// A lane's dwords of a token: which of K (0) and V (1) they are of, where its codes and, in a block's first lane, its scale
+// are in the MX block.
+template <int D, int kBits> struct TokenLane {
+  using MX = MxBlock<D, kBits>;
+  static constexpr int kWords = D / 64, kCodeBytes = kBits / 4;
+  int lane, pair;
+  __device__ __forceinline__ TokenLane() : lane(threadIdx.x & 63), pair(lane % (D / 2)) {}
+  __device__ __forceinline__ int is_v(int i) const { return kWords == 2 ? i : lane >> 5; }
+  __device__ __forceinline__ int code(int i, int slot) const { return is_v(i) ? MX::v_code(slot, pair) : slot * MX::kRow + pair * kCodeBytes; }
+  __device__ __forceinline__ int scale(int i, int slot) const { return is_v(i) ? MX::v_scale(slot, pair >> 4) : MX::k_scale(slot, pair >> 4); }
+};
+}  // namespace
+
+template <int D, int kBits>
+__global__ __launch_bounds__(64 * kTokenWaves) void kv_append_token_mx_kernel(
+    const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new, uint8_t* __restrict__ cache,
+    const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
+    const int32_t* __restrict__ cu, int batch, int num_kv_heads, int num_pages, int total_q, ZeroWords zero) {
+  using MX = MxBlock<D, kBits>;
+  using T = TokenLane<D, kBits>;
+  if (blockIdx.x == 0) {
+    if (zero.hdr && threadIdx.x < kHdrWords) zero.hdr[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < zero.n_cnt; i += 64 * kTokenWaves) zero.cnt[i] = 0;
+  }
+  const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * kTokenWaves + (int)(threadIdx.x >> 6));
+  if (item >= batch * num_kv_heads) return;
+  const int b = item / num_kv_heads, h = item - b * num_kv_heads;
+  const T t;
+  const size_t at = ((size_t)min(max(cu ? cu[b] : b, 0), total_q - 1) * num_kv_heads + h) * D + 2 * t.pair;
+  uint32_t x[T::kWords];
+#pragma unroll
+  for (int i = 0; i < T::kWords; ++i) x[i] = *reinterpret_cast<const uint32_t*>((t.is_v(i) ? v_new : k_new) + at);
+  const PageRows p = rows_of(b, 0, bt, bt_stride, ctx_lens, cu, total_q);
+  if (p.s0 >= p.s1 || p.page < 0 || p.page >= num_pages) return;
+  uint8_t* const blk = cache + ((size_t)p.page * num_kv_heads + h) * MX::kBytes;
+  uint32_t m = mags(x[0]);                          // the larger magnitude, or K's and V's
+  if constexpr (T::kWords == 2) m = pk_max(__builtin_amdgcn_perm(mags(x[1]), m, 0x05040100u), __builtin_amdgcn_perm(mags(x[1]), m, 0x07060302u));
+  else m = pk_max(m, m >> 16 | m << 16);
+  m = dpp_max<kRowRor + 8>(m);
+  m = dpp_max<kRowRor + 4>(m);
+  m = dpp_max<kRowRor + 2>(m);
+  m = dpp_max<kRowRor + 1>(m);
+  const uint32_t s2 = scale_bytes<kBits>(m);
+#pragma unroll
+  for (int i = 0; i < T::kWords; ++i) {
+    const uint32_t s = s2 >> (16 * i) & 0xffu;
+    const uint32_t c = s == 255u ? 0u : mx_down<kBits, 0>(0u, x[i], mx_scale(s));
+    uint8_t* const to = blk + t.code(i, p.s0);
+    if constexpr (kBits == 4) *to = (uint8_t)c;
+    else *reinterpret_cast<uint16_t*>(to) = (uint16_t)c;
+    if ((t.lane & 15) == 0) blk[t.scale(i, p.s0)] = (uint8_t)s;
+  }
+}
+
+template <int D, int kBits>
+__global__ __launch_bounds__(64 * kTokenWaves) void kv_pack_token_mx_kernel(
+    const uint8_t* __restrict__ cache, uint16_t* __restrict__ k_rows, uint16_t* __restrict__ v_rows,
+    const int32_t* __restrict__ bt, int bt_stride, const int32_t* __restrict__ ctx_lens,
+    const int32_t* __restrict__ cu, int batch, int num_kv_heads, int num_pages, int total_q) {
+  using MX = MxBlock<D, kBits>;
+  using T = TokenLane<D, kBits>;
+  const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * kTokenWaves + (int)(threadIdx.x >> 6));
+  if (item >= batch * num_kv_heads) return;
+  const int b = item / num_kv_heads, h = item - b * num_kv_heads;
+  const PageRows p = rows_of(b, 0, bt, bt_stride, ctx_lens, cu, total_q);
+  if (p.s0 >= p.s1) return;
+  const bool ok = p.page >= 0 && p.page < num_pages;
+  const uint8_t* const blk = cache + ((size_t)(ok ? p.page : 0) * num_kv_heads + h) * MX::kBytes;
+  const T t;
+  const size_t at = (p.row0 * num_kv_heads + h) * D + 2 * t.pair;
+#pragma unroll
+  for (int i = 0; i < T::kWords; ++i) {
+    const uint8_t* const from = blk + t.code(i, p.s0);
+    const uint32_t c = kBits == 4 ? *from : *reinterpret_cast<const uint16_t*>(from);
+    const uint32_t x = mx_up<kBits, 0>(c, mx_scale(blk[t.scale(i, p.s0)]));
+    *reinterpret_cast<uint32_t*>((t.is_v(i) ? v_rows : k_rows) + at) = ok ? x : 0u;
+  }
+}
+
 namespace {
 // Workgroups of a launch over the token ranges, or -1 if they pass the grid's limit of 2^32 threads.  A sequence of up
 // to max_q_len tokens touches at most ceil((max_q_len + 15) / 16) pages.  As many items for each sequence are found without
@@ -315,17 +402,19 @@ namespace {
 // with as many for each and by the token counts, and how many times more items the first gives: 256 sequences of 20 new
 // tokens (0.92) 9.0 and 10.0; 200 of 1-64 (1.23) 9.7 and 10.4; 32 of 1-4096 (1.89) 63.7 and 60.5; 63 of 100 and one of 330
 // (2.60) 10.0 and 8.5; 255 of one and one of 8192 (126) 376 and 12.
-int64_t page_items(int batch, int max_q_len, int total_q, bool ragged, int num_kv_heads, int head_dim, PageItems* items) {
-  const int64_t per_seq = ragged ? (max_q_len + 2 * kPage - 2) / kPage : 1;
+int64_t page_items(int batch, int max_q_len, int total_q, int num_kv_heads, int head_dim, PageItems* items) {
+  const int64_t per_seq = (max_q_len + 2 * kPage - 2) / kPage;
   const int64_t even = batch * per_seq, least = (int64_t)total_q / kPage + 2 * (int64_t)batch;
   const bool by_count = 2 * even > 3 * least;
   *items = PageItems{by_count ? 0 : (int)per_seq, batch};
   const int64_t blocks = (by_count ? least : even) * num_kv_heads;
   return blocks * head_dim > UINT32_MAX ? -1 : blocks;
 }
-}  // namespace
+int64_t token_blocks(int batch, int num_kv_heads) {
+  const int64_t blocks = ((int64_t)batch * num_kv_heads + kTokenWaves - 1) / kTokenWaves;
+  return blocks * 64 * kTokenWaves > UINT32_MAX ? -1 : blocks;
+}
 
-namespace {
 template <bool kOnce> auto append_kernel_of(int head_dim, int bits) {
   return head_dim == 64 ? (bits == 4 ? kv_append_mx_kernel<64, 4, kOnce> : kv_append_mx_kernel<64, 8, kOnce>)
                         : (bits == 4 ? kv_append_mx_kernel<128, 4, kOnce> : kv_append_mx_kernel<128, 8, kOnce>);
@@ -337,8 +426,17 @@ hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* 
                                const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
                                int num_pages, int total_q, const ZeroWords& zero, hipStream_t stream) {
   if (max_q_len <= 0 || batch <= 0 || total_q <= 0) return hipSuccess;
+  if (max_q_len == 1 || !cu_q_lens) {
+    const int64_t blocks = token_blocks(batch, num_kv_heads);
+    if (blocks < 0) return hipErrorInvalidValue;
+    auto kernel = head_dim == 64 ? (bits == 4 ? kv_append_token_mx_kernel<64, 4> : kv_append_token_mx_kernel<64, 8>)
+                                 : (bits == 4 ? kv_append_token_mx_kernel<128, 4> : kv_append_token_mx_kernel<128, 8>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kTokenWaves), 0, stream, k_new, v_new, cache, block_table,
+                       bt_stride, ctx_lens, cu_q_lens, batch, num_kv_heads, num_pages, total_q, zero);
+    return hipGetLastError();
+  }
   PageItems items;
-  const int64_t blocks = page_items(batch, max_q_len, total_q, cu_q_lens != nullptr, num_kv_heads, head_dim, &items);
+  const int64_t blocks = page_items(batch, max_q_len, total_q, num_kv_heads, head_dim, &items);
   if (blocks < 0) return hipErrorInvalidValue;
   // Rows of 48 MiB on are read with non-temporal loads: they would only push each other out of the caches.  us of an append
   // and its read-back without and with them, 8 kv-heads, d = 128: 8K tokens (34 MB of rows) in 4 bits 17.5 and 18.0, in 8
@@ -346,7 +444,7 @@ hipError_t launch_kv_append_mx(int bits, const uint16_t* k_new, const uint16_t* 
   const bool once = 4 * (int64_t)total_q * num_kv_heads * head_dim >= (int64_t)48 << 20;
   auto kernel = once ? append_kernel_of<true>(head_dim, bits) : append_kernel_of<false>(head_dim, bits);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(head_dim), 0, stream, k_new, v_new, cache, block_table,
-                     bt_stride, ctx_lens, cu_q_lens, items, num_kv_heads, num_pages, total_q, zero);
+                     bt_stride, ctx_lens, cu_q_lens, items, num_kv_heads, num_pages, total_q);
   return hipGetLastError();
 }
 
@@ -355,8 +453,17 @@ hipError_t launch_kv_pack_mx(int bits, const uint8_t* cache, uint16_t* k_rows, u
                              const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
                              int num_pages, int total_q, hipStream_t stream) {
   if (max_q_len <= 0 || batch <= 0 || total_q <= 0) return hipSuccess;
+  if (max_q_len == 1 || !cu_q_lens) {
+    const int64_t blocks = token_blocks(batch, num_kv_heads);
+    if (blocks < 0) return hipErrorInvalidValue;
+    auto kernel = head_dim == 64 ? (bits == 4 ? kv_pack_token_mx_kernel<64, 4> : kv_pack_token_mx_kernel<64, 8>)
+                                 : (bits == 4 ? kv_pack_token_mx_kernel<128, 4> : kv_pack_token_mx_kernel<128, 8>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kTokenWaves), 0, stream, cache, k_rows, v_rows, block_table,
+                       bt_stride, ctx_lens, cu_q_lens, batch, num_kv_heads, num_pages, total_q);
+    return hipGetLastError();
+  }
   PageItems items;
-  const int64_t blocks = page_items(batch, max_q_len, total_q, cu_q_lens != nullptr, num_kv_heads, head_dim, &items);
+  const int64_t blocks = page_items(batch, max_q_len, total_q, num_kv_heads, head_dim, &items);
   if (blocks < 0) return hipErrorInvalidValue;
   auto kernel = head_dim == 64 ? (bits == 4 ? kv_pack_mx_kernel<64, 4> : kv_pack_mx_kernel<64, 8>)
                                : (bits == 4 ? kv_pack_mx_kernel<128, 4> : kv_pack_mx_kernel<128, 8>);
