@@ -34,8 +34,11 @@ namespace pearl {
 
 namespace {
 
-struct MxCut {                                      // 2176 bytes of K and V a page and kv-head at 4 bits, d = 128
-  static constexpr int kMinPages = 32, kPieceCost = 8, kWholePages = 56;
+// 2176 bytes of K and V a page and kv-head at 4 bits, d = 128.  Shares of 70 pages of 512 sequences (64-1024 tokens) took
+// 2.2 us a unit and 2.0 a sequence more, so the ones with 5 or 6 sequences ended last: with a sequence's start counted as
+// 4 pages 68.1 us, with 0 71.2, with 8 67.8.
+struct MxCut {
+  static constexpr int kMinPages = 32, kPieceCost = 8, kWholePages = 56, kSeqCost = 4;
 };
 
 // A unit: kPages pages of one (sequence, kv-head) and how they lie in a wave's buffer.
@@ -471,7 +474,7 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     if (r.n <= 0 || r.j_w < r.dup) return;
     CutPair cut[2];
     auto store = [&](int b, const f32x4* o, float m, float l) {
-      const int pu = uni(P.pre[b]), second = pu > r.t0;       // the pair's first entry
+      const int second = uni(P.pre[b]) > r.t0;
       const int own = second ? (r.per_pair ? sh.n_runs + b : 2 * r.x + 1) : r.slot_stride * r.x;
       float* to = a.part_o + (((size_t)g * d.max_dec + own) * G + hh) * D + 8 * group;
 #pragma unroll
@@ -483,9 +486,7 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
           if (hh < G && odd == (p >= TP / 2)) st_dev2(to + 32 * p + 2 * i, odd ? other : mine, odd ? mine : other);
         }
       if (hh < G && lane < 8) st_dev2(&a.part_ml[2 * (((size_t)g * d.max_dec + own) * G + hh)], m, l);
-      const int x0 = sh.run_of(pu), x1 = sh.run_of(uni(P.pre[b + 1]) - 1);
-      const bool at_start = pu <= sh.begin(x0);
-      return CutPair{b, x0, x1 - x0 + 1, at_start ? r.slot_stride * x0 : (r.per_pair ? sh.n_runs + b : 2 * x0 + 1)};
+      return sh.cut_of(P, r, b);
     };
     cut[0].b = cut[1].b = -1;
     if (first_b >= 0) cut[0] = store(first_b, o_first, m_first, l_first);

@@ -98,18 +98,23 @@ struct PageCursor {
   int b, p, np, kv;
 };
 
-// The place of entry t (< pre[B]) of the list: the sequence is found by counting prefix sums with
-// ballots (64 evenly spaced probes, then the gap between two).
-__device__ __forceinline__ PageCursor locate(const DecPlanLds& P, int t, int B) {
+// The last sequence b with pre[b] + kCost * b <= t, found by counting prefix sums with ballots (64 evenly spaced
+// probes, then the gap between two).
+template <int kCost> __device__ __forceinline__ int seq_at(const DecPlanLds& P, int t, int B) {
   const int lane = threadIdx.x & 63;
   const int gap = (B + 63) / 64;
-  const int blk = __popcll(__ballot(lane * gap < B && P.pre[min(lane * gap, B)] <= t)) - 1;
+  const int blk = __popcll(__ballot(lane * gap < B && P.pre[min(lane * gap, B)] + kCost * lane * gap <= t)) - 1;
   int b = blk * gap;
   if (gap > 1) {
     const int i1 = b + 1 + lane;
-    b += __popcll(__ballot(lane < gap - 1 && i1 < B && P.pre[min(i1, B)] <= t));
+    b += __popcll(__ballot(lane < gap - 1 && i1 < B && P.pre[min(i1, B)] + kCost * i1 <= t));
   }
-  b = uni(b);
+  return uni(b);
+}
+
+// The place of entry t (< pre[B]) of the list.
+__device__ __forceinline__ PageCursor locate(const DecPlanLds& P, int t, int B) {
+  const int b = seq_at<0>(P, t, B);
   const int first = uni(P.pre[b]);
   const int np = uni(P.pre[b + 1]) - first;
   return PageCursor{b, t - first, np, (np - 1) * kPage + uni(P.tail[b]) + 1};
@@ -137,14 +142,30 @@ __device__ __forceinline__ bool all_within(DecPlanLds& P, int B, int most, int l
 // How a kernel's list of pages is cut: runs of at least kMinPages pages; several kv-heads share a
 // workgroup if kPieceCost times the pieces of the longest sequence are at most the pages of a wave's
 // share (DecShares); runs hold whole sequences if that makes none longer than an equal run by more than
-// kWholePages (DecRun).
+// kWholePages (DecRun); where a workgroup holds 8 kv-heads, so that shares are runs and equal ones all there is, a
+// sequence's start counts as kSeqCost pages.
 struct PoolCut {                                    // bf16 pools: 8 KiB of K and V a page and kv-head (d = 128)
-  static constexpr int kMinPages = 16, kPieceCost = 8, kWholePages = 28;
+  static constexpr int kMinPages = 16, kPieceCost = 8, kWholePages = 28, kSeqCost = 0;
+};
+
+// What a workgroup of a decode launch takes: run x of the kv-heads [g0, g0 + heads), and its wave's share.
+struct DecRun {
+  int x, g0, dup;                                   // the first dup kv-heads are another workgroup's too
+  int sub, j_w;                                     // the wave's share of the run and its kv-head, of the workgroup's
+  int run0, t0, n;                                  // the run's first page, of all pages; the wave's first one and pages
+  bool per_pair;
+  int slot_stride;
+};
+
+// A pair cut by the workgroup's boundaries: its sequence (< 0: none), first run, runs, first slot.
+struct CutPair {
+  int b, x0, n, slot0;
 };
 
 // The cut of the page list.  A workgroup takes `heads` kv-heads (a power of two up to 8 that
 // divides H) and one of n_runs runs of 8 / heads consecutive shares; the first `more` shares hold
-// len + 1 entries, the others len.  Several heads per workgroup read the adjacent blocks of a page
+// len + 1 entries, the others len, of the list in which `cost` entries stand before each sequence's
+// pages.  Several heads per workgroup read the adjacent blocks of a page
 // together, which HBM serves faster (2% of a share's time at 8 heads, 9% at 64).  But then every
 // share's end cuts a pair between workgroups, and the last merges take longer the more pieces a pair
 // is cut into.  So workgroups take several heads if the longest pair's pieces, longest / len, are few
@@ -157,6 +178,7 @@ struct PoolCut {                                    // bf16 pools: 8 KiB of K an
 //     2K-30K (64, 29) 171 and 188; 8 of 4K-16K, 16 kv-heads (39, 25) 116 and 135; 32 of 500-2000, 16
 //     kv-heads (19, 6) 59 and 66; 200 of 500-2000, 4 kv-heads (30, 4) 89.5 and 90.1.
 template <class Cut> struct DecShares {
+  int cost;                                         // entries before a sequence's pages
   int heads, n_runs, len, more;
   __device__ __forceinline__ DecShares(DecPlanLds& P, int pages, int most, const DecPlanArgs& d) {
     // which form and how many runs: any wave and workgroup finds the same, exact quotients are not needed
@@ -172,16 +194,29 @@ template <class Cut> struct DecShares {
       const int least = Cut::kMinPages + (int)((float)pages * d.inv_64_seqs);
       n_runs = max(1, min(d.runs_one, (int)((float)pages * __builtin_amdgcn_rcpf((float)least))));
     }
-    const int n = n_runs * subs();
-    len = (int)((unsigned)pages / (unsigned)n);
-    more = pages - len * n;
+    cost = Cut::kSeqCost > 0 && heads == kWaves ? Cut::kSeqCost : 0;
+    const int n = n_runs * subs(), entries = pages + cost * d.batch;
+    len = (int)((unsigned)entries / (unsigned)n);
+    more = entries - len * n;
   }
   __device__ __forceinline__ int subs() const { return kWaves / heads; }   // shares per run
   __device__ __forceinline__ int begin(int share) const { return share * len + min(share, more); }
+  __device__ __forceinline__ int first_page(const DecPlanLds& P, int t, int B) const {   // of all pages, from entry t on
+    if (cost == 0) return t;
+    const int b = seq_at<Cut::kSeqCost>(P, t, B), pre = uni(P.pre[b]);
+    return uni(pre + max(t - (pre + cost * b) - cost, 0));
+  }
   __device__ __forceinline__ int run_of(int t) const {                     // the run that holds entry t
     const int big = more * (len + 1);
     const int share = t < big ? (unsigned)t / (unsigned)(len + 1) : more + (unsigned)(t - big) / (unsigned)max(len, 1);
     return (unsigned)share / (unsigned)subs();
+  }
+  // The runs of sequence b's pages, cut between workgroups, and where its partials are: a run's first slot, or for a
+  // start behind another sequence's pages the second one.
+  __device__ __forceinline__ CutPair cut_of(const DecPlanLds& P, const DecRun& r, int b) const {
+    const int at = uni(P.pre[b]) + cost * b, x0 = run_of(at + cost), x1 = run_of(uni(P.pre[b + 1]) + cost * b + cost - 1);
+    const bool at_start = at <= begin(x0 * subs());
+    return CutPair{b, x0, x1 - x0 + 1, at_start ? r.slot_stride * x0 : (r.per_pair ? n_runs + b : 2 * x0 + 1)};
   }
 };
 
@@ -195,10 +230,6 @@ template <int D> struct ShareEnd {
 // one started before the share, and whether the share holds pages at all.
 struct SharePairs {
   int first_b, last_b, before, used;
-};
-// A pair cut by the workgroup's boundaries: its sequence (< 0: none), first run, runs, first slot.
-struct CutPair {
-  int b, x0, n, slot0;
 };
 
 // Two adjacent floats as one device-scope access: stores are written through to the level where
@@ -277,15 +308,6 @@ __device__ __forceinline__ void merge_pair(const AttnArgs& a, const CutPair& c, 
   if (dim == 0 && a.lse) a.lse[row] = (M + flog2(L)) * kLn2;
 }
 
-// What a workgroup of a decode launch takes: run x of the kv-heads [g0, g0 + heads), and its wave's share.
-struct DecRun {
-  int x, g0, dup;                                   // the first dup kv-heads are another workgroup's too
-  int sub, j_w;                                     // the wave's share of the run and its kv-head, of the workgroup's
-  int run0, t0, n;                                  // the run's first entry; the wave's first one and entries
-  bool per_pair;
-  int slot_stride;
-};
-
 // Finds a workgroup's run; false if it has none.
 // Runs of whole sequences, as many sequences each (one, if the grid holds a workgroup for every
 // (sequence, kv-head) pair), instead of equal runs, where no run gets much longer by it: then no pair
@@ -327,17 +349,21 @@ __device__ __forceinline__ bool decode_run(const AttnArgs& a, const DecPlanArgs&
   r.dup = blk0 - r.g0;
   r.sub = w / sh.heads;
   r.j_w = w % sh.heads;
+  int run0, t0, end;
   if (whole_runs) {
-    r.run0 = uni(P.pre[whole_begin(r.x)]);
-    const int len = uni(P.pre[whole_begin(r.x + 1)]) - r.run0, q = len / kWaves, rest = len % kWaves;
-    r.t0 = r.run0 + w * q + min(w, rest);
-    r.n = q + (w < rest);
+    run0 = uni(P.pre[whole_begin(r.x)]);
+    const int len = uni(P.pre[whole_begin(r.x + 1)]) - run0, q = len / kWaves, rest = len % kWaves;
+    t0 = run0 + w * q + min(w, rest);
+    end = t0 + q + (w < rest);
   } else {
     const int share = r.x * sh.subs() + r.sub;
-    r.run0 = sh.begin(r.x * sh.subs());
-    r.t0 = sh.begin(share);
-    r.n = sh.begin(share + 1) - r.t0;
+    t0 = sh.first_page(P, sh.begin(share), B);
+    end = sh.first_page(P, sh.begin(share + 1), B);
+    run0 = sh.first_page(P, sh.begin(r.x * sh.subs()), B);
   }
+  r.run0 = run0;
+  r.t0 = t0;
+  r.n = end - t0;
   // partial slots and counters of a kv-head: two slots and a counter per run, or a slot per run,
   // and a slot and a counter per sequence, if that is fewer
   r.per_pair = B < sh.n_runs;
@@ -422,9 +448,7 @@ __device__ __forceinline__ void finish_shares(const AttnArgs& a, const DecPlanAr
         }
       }
       if (cut && threadIdx.x == 0) {
-        const int x0 = sh.run_of(pu), x1 = sh.run_of(uni(P.pre[b + 1]) - 1);
-        const bool at_start = pu <= sh.begin(x0 * subs);
-        F.cut[second] = CutPair{b, x0, x1 - x0 + 1, at_start ? r.slot_stride * x0 : (r.per_pair ? slot2 : 2 * x0 + 1)};
+        F.cut[second] = sh.cut_of(P, r, b);
       }
     }
   }

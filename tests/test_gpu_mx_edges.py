@@ -134,3 +134,17 @@ def test_turns_on_long_contexts(n):
     out, lse = pa.prefill_append_mx(c.q, c.cache, c.bt, c.ctx, c.cu, c.max_q, c.max_kv, scale=c.scale, lse=lse)
     torch.cuda.synchronize()
     c.check(out, lse, range(len(ctx)))
+
+
+@pytest.mark.parametrize("fmt,d,hkv,lo,hi", ((4, 128, 8, 1, 400), (8, 64, 16, 30, 200), (4, 64, 8, 100, 103)))
+def test_many_short_sequences(fmt, d, hkv, lo, hi):
+    """Shares of many sequences, cut anywhere in them and between them."""
+    say("decode_mx many short fmt=%d d=%d hkv=%d" % (fmt, d, hkv))
+    ctx = np.random.default_rng(hi).integers(lo, hi, size=900)
+    c = BigCase(fmt, d, hkv, 2, ctx, np.ones(900, np.int64), hi)
+    lse = torch.full((900, c.hq), float("nan"), device="cuda")
+    out, lse = pa.decode_mx(c.q, c.cache, c.bt, c.ctx, c.max_kv, scale=c.scale, lse=lse)
+    again = pa.decode_mx(c.q, c.cache, c.bt, c.ctx, c.max_kv, scale=c.scale)
+    torch.cuda.synchronize()
+    assert torch.isfinite(lse).all() and torch.equal(out, again)
+    c.check(out, lse, list(range(0, 900, 9)) + [897, 898, 899])
