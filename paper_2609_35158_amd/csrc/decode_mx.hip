@@ -476,15 +476,19 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     auto store = [&](int b, const f32x4* o, float m, float l) {
       const int second = uni(P.pre[b]) > r.t0;
       const int own = second ? (r.per_pair ? sh.n_runs + b : 2 * r.x + 1) : r.slot_stride * r.x;
-      float* to = a.part_o + (((size_t)g * d.max_dec + own) * G + hh) * D + 8 * group;
+      float* to = a.part_o + (((size_t)g * d.max_dec + own) * G + hh) * D + 8 * group + 4 * odd;
 #pragma unroll
-      for (int p = 0; p < TP; ++p)
+      for (int p = 0; p < TP; ++p) {                // four channels from either column half: a group's 8 are 32 bytes
+        float mine[2], other[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {               // two channels a store: half of the groups from either column half
-          const float mine = o[p][i];
-          const float other = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, mine), 0x128, 0xf, 0xf, false));   // row_ror:8
-          if (hh < G && odd == (p >= TP / 2)) st_dev2(to + 32 * p + 2 * i, odd ? other : mine, odd ? mine : other);
+        for (int i = 0; i < 2; ++i) {
+          const float give = odd ? o[p][i] : o[p][2 + i];
+          mine[i] = odd ? o[p][2 + i] : o[p][i];
+          other[i] = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, give), 0x128, 0xf, 0xf, false));   // row_ror:8
         }
+        const f32x4 x = odd ? f32x4{other[0], mine[0], other[1], mine[1]} : f32x4{mine[0], other[0], mine[1], other[1]};
+        if (hh < G) st_dev4(to + 32 * p, x);
+      }
       if (hh < G && lane < 8) st_dev2(&a.part_ml[2 * (((size_t)g * d.max_dec + own) * G + hh)], m, l);
       return sh.cut_of(P, r, b);
     };

@@ -239,6 +239,11 @@ __device__ __forceinline__ void st_dev2(float* p, float x, float y) {
                                ((unsigned long long)__builtin_bit_cast(unsigned, y) << 32);
   __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+// Four floats at a 16-byte aligned place, likewise; to be waited for by vmcnt, like any store.  (The nop: a store of over
+// 8 bytes still reads its data in the cycle after, which the compiler cannot know of an asm statement.)
+__device__ __forceinline__ void st_dev4(float* p, f32x4 x) {
+  __asm__ volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" : : "v"(p), "v"(x) : "memory");
+}
 __device__ __forceinline__ void ld_dev2(const float* p, float& x, float& y) {
   const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED,
                                                  __HIP_MEMORY_SCOPE_AGENT);
