@@ -171,6 +171,10 @@ def _need(t: torch.Tensor, name: str, dtype: torch.dtype) -> None:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+# The current device, without the check of torch.cuda.current_device() for a context, which the tensors have (0.1 us).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream() -> int:
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
@@ -188,16 +192,17 @@ def make_desc(block_table: torch.Tensor, ctx_lens: torch.Tensor, cu_q_lens: Opti
               total_q: int, max_q_len: int, max_kv_len: int, need=_need) -> SeqDesc:
     need(block_table, "block_table", torch.int32)
     need(ctx_lens, "ctx_lens", torch.int32)
-    if block_table.dim() != 2:
+    table = block_table.shape
+    if len(table) != 2:
         raise ValueError("block_table must be [batch][bt_stride]")
     batch = int(ctx_lens.shape[0])
-    if block_table.shape[0] != batch:
-        raise ValueError("block_table rows (%d) != batch (%d)" % (block_table.shape[0], batch))
+    if table[0] != batch:
+        raise ValueError("block_table rows (%d) != batch (%d)" % (table[0], batch))
     if cu_q_lens is not None:
         need(cu_q_lens, "cu_q_lens", torch.int32)
         if cu_q_lens.shape[0] != batch + 1:
             raise ValueError("cu_q_lens must have batch+1 entries")
-    return SeqDesc(block_table.data_ptr(), int(block_table.shape[1]), ctx_lens.data_ptr(),
+    return SeqDesc(block_table.data_ptr(), int(table[1]), ctx_lens.data_ptr(),
                    _ptr(cu_q_lens), batch, int(total_q), int(max_q_len), int(max_kv_len))
 
 
@@ -417,6 +422,7 @@ def _mx_geometry(num_q_heads: Optional[int], cache_shape: Tuple[int, int, int]):
         raise ValueError("cache must be [num_pages][num_kv_heads][mx_block_bytes(head_dim, fmt)]")
     d, fmt = _MX_BLOCKS[cache_shape[2]]
     shape = KvShape(cache_shape[1] if num_q_heads is None else num_q_heads, cache_shape[1], d, PAGE_SIZE, cache_shape[0])
+    shape.row = (cache_shape[1], d)                 # of the rows bf16 [tokens][num_kv_heads][head_dim]
     return shape, fmt, ctypes.byref(shape)
 
 
@@ -426,13 +432,14 @@ class _MxCall:
 
     def __init__(self, cache: torch.Tensor, num_q_heads: Optional[int] = None):
         _need(cache, "cache", torch.uint8)
-        self.shape, self.fmt, self.ref = _mx_geometry(num_q_heads, tuple(cache.shape))
+        shape, self.fmt, self.ref = _mx_geometry(num_q_heads, tuple(cache.shape))
+        self.row = shape.row
         self.dev = cache.get_device()
-        if self.dev != torch.cuda.current_device():
-            raise ValueError("cache is on cuda:%d, the current device is cuda:%d" % (self.dev, torch.cuda.current_device()))
+        if self.dev != _current_device():
+            raise ValueError("cache is on cuda:%d, the current device is cuda:%d" % (self.dev, _current_device()))
 
     def need(self, t: torch.Tensor, name: str, dtype: torch.dtype) -> None:
-        if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.get_device() == self.dev and t.is_contiguous()):
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == self.dev and t.is_contiguous()):
             _need(t, name, dtype)
             raise ValueError("%s must be on the cache's device (cuda:%d), got %s" % (name, self.dev, t.device))
 
@@ -449,9 +456,10 @@ def kv_append_mx(k_new: torch.Tensor, v_new: torch.Tensor, cache: torch.Tensor, 
     c = _MxCall(cache)
     c.need(k_new, "k_new", torch.bfloat16)
     c.need(v_new, "v_new", torch.bfloat16)
-    total = k_new.shape[0]
-    if k_new.shape != (total, c.shape.num_kv_heads, c.shape.head_dim) or v_new.shape != k_new.shape:
-        raise ValueError("k_new and v_new must be [total_q][%d][%d]" % (c.shape.num_kv_heads, c.shape.head_dim))
+    rows = k_new.shape
+    if rows[1:] != c.row or v_new.shape != rows:
+        raise ValueError("k_new and v_new must be [total_q][%d][%d]" % c.row)
+    total = rows[0]
     desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, c.need)
     st = load().pearl_kv_append_mx(c.ref, ctypes.byref(desc), c.fmt, k_new.data_ptr(), v_new.data_ptr(),
                                    cache.data_ptr(), c.stream())
@@ -464,7 +472,7 @@ def kv_pack_mx(cache: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.T
     """Read token ranges [ctx_lens[b], ctx_lens[b] + n_b) of every sequence back out of a cache of MX
     blocks, as bf16 [2][total][H_kv][d] (pearl_kv_pack_mx)."""
     c = _MxCall(cache)
-    want = (2, int(total), c.shape.num_kv_heads, c.shape.head_dim)
+    want = (2, int(total)) + c.row
     if out is None:
         out = torch.empty(want, dtype=torch.bfloat16, device=cache.device)
     else:
@@ -496,11 +504,11 @@ def _attention_mx(fname: str, q: torch.Tensor, new, cache: torch.Tensor, block_t
     total_q, H_q, d = q.shape
     c = _MxCall(cache, H_q)
     c.need(q, "q", torch.bfloat16)
-    if d != c.shape.head_dim:
-        raise ValueError("q has head_dim %d, the cache %d" % (d, c.shape.head_dim))
+    if d != c.row[1]:
+        raise ValueError("q has head_dim %d, the cache %d" % (d, c.row[1]))
     for t, n in zip(new, ("k_new", "v_new")):
         c.need(t, n, torch.bfloat16)
-        if t.shape != (total_q, c.shape.num_kv_heads, d):
+        if t.shape != (total_q,) + c.row:
             raise ValueError("k_new and v_new must be [batch][num_kv_heads][head_dim]")
     desc = make_desc(block_table, ctx_lens, cu_q_lens, total_q, max_q_len, max_kv_len, c.need)
     if out is None:
