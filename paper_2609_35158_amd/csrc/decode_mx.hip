@@ -37,8 +37,8 @@ namespace {
 // 2176 bytes of K and V a page and kv-head at 4 bits, d = 128.  Shares of 70 pages of 512 sequences (64-1024 tokens) took
 // 2.2 us a unit and 2.0 a sequence more, so the ones with 5 or 6 sequences ended last: with a sequence's start counted as
 // 4 pages 68.1 us, with 0 71.2, with 8 67.8.
-struct MxCut {
-  static constexpr int kMinPages = 32, kPieceCost = 8, kWholePages = 56, kSeqCost = 4;
+template <int kPages> struct MxCut {
+  static constexpr int kPieceCost = 8, kWholePages = 56, kSeqCost = 4, kUnit = kPages;
 };
 
 // A unit: kPages pages of one (sequence, kv-head) and how they lie in a wave's buffer.
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ws_hdr[kHdrError] = 1;
     return;
   }
-  DecShares<MxCut> sh(P, total_pages, most, d);
+  DecShares<MxCut<kPages>> sh(P, total_pages, most, d);
   DecRun r;
   if (!decode_run(a, d, P, most, total_pages, sh, r)) return;
   const int g = r.g0 + r.j_w;

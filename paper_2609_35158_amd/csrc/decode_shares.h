@@ -139,13 +139,14 @@ __device__ __forceinline__ bool all_within(DecPlanLds& P, int B, int most, int l
   return P.over == 0;
 }
 
-// How a kernel's list of pages is cut: runs of at least kMinPages pages; several kv-heads share a
+// How a kernel's list of pages is cut: runs of at least kMinPages pages, or, where a wave takes units of
+// kUnit > 1 pages, of whole units a wave; several kv-heads share a
 // workgroup if kPieceCost times the pieces of the longest sequence are at most the pages of a wave's
 // share (DecShares); runs hold whole sequences if that makes none longer than an equal run by more than
 // kWholePages (DecRun); where a workgroup holds 8 kv-heads, so that shares are runs and equal ones all there is, a
 // sequence's start counts as kSeqCost pages.
 struct PoolCut {                                    // bf16 pools: 8 KiB of K and V a page and kv-head (d = 128)
-  static constexpr int kMinPages = 16, kPieceCost = 8, kWholePages = 28, kSeqCost = 0;
+  static constexpr int kMinPages = 16, kPieceCost = 8, kWholePages = 28, kSeqCost = 0, kUnit = 1;
 };
 
 // What a workgroup of a decode launch takes: run x of the kv-heads [g0, g0 + heads), and its wave's share.
@@ -189,10 +190,24 @@ template <class Cut> struct DecShares {
       n_runs = d.runs_heads;
     } else {
       heads = 1;
-      // Long sequences in few pairs take somewhat longer runs, so that a pair is not merged from 100
-      // pieces: three of 5-20K tokens on one kv-head 22.0 us a call with kMinPages alone, 19.4 so.
-      const int least = Cut::kMinPages + (int)((float)pages * d.inv_64_seqs);
-      n_runs = max(1, min(d.runs_one, (int)((float)pages * __builtin_amdgcn_rcpf((float)least))));
+      if constexpr (Cut::kUnit > 1) {
+        // Every wave takes so many whole units: one, and more where the longest sequence's merge would cost more than the
+        // units it saves (a run more in it costs about as much as a third of a page in every wave).  us a call with runs of
+        // 32 pages and 1/64 of a sequence, as of bf16 pools, and so: one sequence at 8 kv-heads, 4 bits, 1500 tokens 14.6 and
+        // 11.3, 2731 13.7 and 11.9, 10000 17.0 and 14.7, 30000 19.7 and 19.7; 8 bits 1500 16.8 and 12.1, 12000 16.5 and 17.2;
+        // three of 5-20K at one kv-head 21.4 and 20.5.  With half a page for a third: 8 bits, 16000 17.9 for 17.3; with a
+        // fifth: 4 bits, 16000 17.5 for 16.5.  (Beyond 64 sequences, where a wave does not hold all lengths, runs of one unit
+        // a wave are only as many as fill the grid.)
+        constexpr int kRun = kWaves * Cut::kUnit, kLong = 3 * Cut::kUnit * kRun;
+        int units = 1;
+        if (d.batch <= 64) while (__any(most > units * (units + 1) * kLong)) ++units;
+        n_runs = max(1, min(d.runs_one, (int)((unsigned)(pages + units * kRun - 1) / (unsigned)(units * kRun))));
+      } else {
+        // Long sequences in few pairs take somewhat longer runs, so that a pair is not merged from 100
+        // pieces: three of 5-20K tokens on one kv-head 22.0 us a call with kMinPages alone, 19.4 so.
+        const int least = Cut::kMinPages + (int)((float)pages * d.inv_64_seqs);
+        n_runs = max(1, min(d.runs_one, (int)((float)pages * __builtin_amdgcn_rcpf((float)least))));
+      }
     }
     cost = Cut::kSeqCost > 0 && heads == kWaves ? Cut::kSeqCost : 0;
     const int n = n_runs * subs(), entries = pages + cost * d.batch;
