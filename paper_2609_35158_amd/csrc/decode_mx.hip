@@ -85,7 +85,7 @@ template <int N> __device__ __forceinline__ void copy_codes(const uint8_t* base,
                      "global_load_lds_dwordx4 %3, %2 nt\n\t"
                      "global_load_lds_dwordx4 %3, %2 offset:1024 nt\n\t"
                      "global_load_lds_dwordx4 %3, %2 offset:2048 nt\n\t"
-                     "global_load_lds_dwordx4 %3, %2 offset:3072 nt\n\t"
+                     "global_load_lds_dwordx4 %3, %2 offset:3*1024 nt\n\t"
                      "s_mov_b32 m0, %0"
                      : "=&s"(saved) : "s"(lds), "s"(base), "v"(lane16) : "memory");
 }
