@@ -180,8 +180,8 @@ hipError_t launch_kv_pack(const uint16_t* k_pool, const uint16_t* v_pool, uint16
                           const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
                           int num_pages, int total_q, hipStream_t stream);
 
-// The same for a cache of MX blocks; bits: 4 or 8 an element.  zero: words that the launch also clears (the
-// decode that follows it needs them cleared).
+// The same for a cache of MX blocks; bits: 4 or 8 an element.  zero: words that the launch of a decode step's append
+// (one token a sequence) also clears, as the decode that follows it needs; none in other launches.
 struct ZeroWords {
   int32_t* hdr;                                     // kHdrWords, or null
   int32_t* cnt;
