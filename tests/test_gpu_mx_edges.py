@@ -4,8 +4,9 @@ import numpy as np
 import pytest
 import torch
 
+import oracle
 import paper_2609_35158_amd as pa
-from gpu_helpers import say
+from gpu_helpers import bits, say
 from mx_helpers import BigCase, MxCase, dev
 
 pytestmark = pytest.mark.gpu
@@ -148,3 +149,21 @@ def test_many_short_sequences(fmt, d, hkv, lo, hi):
     torch.cuda.synchronize()
     assert torch.isfinite(lse).all() and torch.equal(out, again)
     c.check(out, lse, list(range(0, 900, 9)) + [897, 898, 899])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("new", ([0, 1, 0, 0, 1, 1, 0], [0, 40, 0, 0, 1, 3, 0], [0, 0, 0, 0, 1, 0, 0]))
+def test_sequences_without_new_tokens_and_rows_behind_the_last(fmt, d, new):
+    """Appended: the sequences' tokens and nothing else.  Read back: rows behind the last sequence stay as they were."""
+    say("append/pack fmt=%d d=%d new=%s and 5 rows behind" % (fmt, d, new))
+    c = MxCase(fmt, d, 3, 1, [5, 15, 16, 0, 31, 100, 7], new, 70 + d + fmt)
+    behind = torch.full((5, 3, d), 2.0, dtype=torch.bfloat16)
+    cache, bt, ctx, cu, _, _, _ = c.device(appended=False)
+    pa.kv_append_mx(torch.cat([c.k_new, behind]).cuda(), torch.cat([c.v_new, behind]).cuda(), cache, bt, ctx, cu, c.max_q, c.max_kv)
+    rows = torch.full((2, c.total + 5, 3, d), 3.0, dtype=torch.bfloat16, device="cuda")
+    pa.kv_pack_mx(cache, bt, ctx, cu, c.total + 5, c.max_q, c.max_kv, out=rows)
+    torch.cuda.synchronize()
+    assert np.array_equal(cache.cpu().numpy(), c.after)
+    want = oracle.mx_pack(c.after, d, fmt, c.bt, c.ctx, c.cu)
+    assert np.array_equal(bits(rows[:, :c.total]), want) and bool((rows[:, c.total:] == 3.0).all())
