@@ -36,9 +36,12 @@ namespace {
 
 // 2176 bytes of K and V a page and kv-head at 4 bits, d = 128.  Shares of 70 pages of 512 sequences (64-1024 tokens) took
 // 2.2 us a unit and 2.0 a sequence more, so the ones with 5 or 6 sequences ended last: with a sequence's start counted as
-// 4 pages 68.1 us, with 0 71.2, with 8 67.8.
-template <int kPages> struct MxCut {
-  static constexpr int kPieceCost = 8, kWholePages = 56, kSeqCost = 4, kUnit = kPages;
+// 4 pages 68.1 us, with 0 71.2, with 8 67.8.  Several kv-heads a workgroup (us a call with kPieceCost 8 and 3): at d = 64
+// and 8 bits, where a pair's partials are small and a workgroup has the compute unit to itself, 48 sequences of 500-6000 36.9
+// and 34.1, 32 of 2K-8K 37.9 and 36.7, 200 of 1K-5K at 2 kv-heads 38.2 and 37.0; at d = 64 and 4 bits 64 of 2K-6K 38.7 and
+// 41.3; at d = 128 and 4 bits (8 and 4) 48 of 2K-6K 44.8 and 47.7, 200 of 500-2000 at 4 kv-heads 38.5 and 42.3.
+template <int D, int kBits, int kPages> struct MxCut {
+  static constexpr int kPieceCost = D == 64 && kBits == 8 ? 3 : 8, kWholePages = 56, kSeqCost = 4, kUnit = kPages;
 };
 
 // A unit: kPages pages of one (sequence, kv-head) and how they lie in a wave's buffer.
@@ -296,7 +299,7 @@ __global__ __launch_bounds__(kThreads, D * kBits == 256 ? 4 : 2) void decode_mx_
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ws_hdr[kHdrError] = 1;
     return;
   }
-  DecShares<MxCut<kPages>> sh(P, total_pages, most, d);
+  DecShares<MxCut<D, kBits, kPages>> sh(P, total_pages, most, d);
   DecRun r;
   if (!decode_run(a, d, P, most, total_pages, sh, r)) return;
   const int g = r.g0 + r.j_w;
