@@ -21,6 +21,12 @@
 // Weights enter P.V in two bf16 parts, the nearest bf16 and the rest, in a product each: 16 bits of a weight.  One
 // part alone is 2-6% faster (64 sequences of 2K-16K tokens 122.4 us, with both 125.9) but off by up to 2^-9 a
 // weight, as much as rounding the outputs to bf16 is.
+// The other channel of a pair meets a weight of 0 in each column half, and 0 times an infinity or NaN is NaN.  So every
+// unit is tested for scales and codes that stand for such elements of V; where there are any, they are counted in a
+// product of their own and added to the outputs, and become zeros for the weights' product: an infinite element of an
+// attended token makes its own channel infinite, and no other one anything.  (The test: 64 sequences of 2K-16K tokens in
+// 4 bits 113.0 us for 112.9, at d = 64 256 of 200-3000 59.0 for 58.2; in 8 bits, with all codes, 64 of 2K-16K 189.7 for
+// 188.9, at d = 64 48 of 500-6000 34.9 for 33.9.)
 // The running maximum may lag the true one by 8 (log2 units), as in the prefill kernel: most units look for none.
 
 #include "decode_shares.h"
@@ -124,6 +130,21 @@ template <int kBits> __device__ __forceinline__ bf16x8 eight_up(const uint32_t* 
     return as_bf16x8(u32x4{mx_up<8, 0>(w[0], f), mx_up<8, 1>(w[0], f), mx_up<8, 0>(w[1], f), mx_up<8, 1>(w[1], f)});
 }
 
+// Of a pair of V in bf16: 1 for an infinite element, 2^8 for minus infinity, 2^16 for NaN (in bf16), so that a sum over a
+// unit's up to 64 tokens counts each kind exactly; `mask` covers these elements.
+__device__ __forceinline__ uint32_t odd_kinds(uint32_t x, uint32_t& mask) {
+  mask = (mx_low_not_finite(x) ? 0x0000ffffu : 0u) | (mx_high_not_finite(x) ? 0xffff0000u : 0u);
+  auto kind = [](uint32_t b) -> uint32_t { return (b & 0x7fu) ? 0x4780u : (b & 0x8000u) ? 0x4380u : 0x3f80u; };
+  return (kind(x & 0xffffu) | kind(x >> 16) << 16) & mask;
+}
+// x and the elements that were so counted in n.
+__device__ __forceinline__ float with_odd(float x, float n) {
+  const int k = (int)n;
+  if (k == 0) return x;
+  const bool nan = k >= 1 << 16 || ((k & 255) != 0 && k >= 1 << 8);
+  return x + (nan ? __builtin_nanf("") : k >= 1 << 8 ? -INFINITY : INFINITY);
+}
+
 // x in bf16 in both halves of a dword.
 __device__ __forceinline__ uint32_t twice_bf16(float x) {
   const bf16x2 y = {(__bf16)x, (__bf16)x};
@@ -139,6 +160,7 @@ template <int D, int kBits> struct Attend {
   static constexpr int KW = D * kBits / 128;        // dwords of it
   static constexpr int VW = TG * kBits / 16;        // dwords of a channel pair's tokens
   int k, ks, v, vs;
+  int vs_any, vs_tok;                               // this lane's word of all of the unit's V scales, and its first token
   int k_shift;                                      // of the scale word: tile t's byte becomes byte t
   __device__ __forceinline__ explicit Attend(int lane) {
     const int row = lane & 15, group = lane >> 4;
@@ -150,28 +172,65 @@ template <int D, int kBits> struct Attend {
     const int vt = group * TG;
     v = vt / kPage * U::kPageBytes + MX::v_code(vt % kPage, row);
     vs = U::kScales + vt / kPage * U::kScaleBytes + MX::kVScales - 2 * MX::kCodes + vt % kPage;
+    constexpr int kWords = kPage * MX::kBlocks / 4;  // of a page
+    const int word = lane % (U::kPages * kWords), page = word / kWords, at = word % kWords * 4;
+    vs_any = U::kScales + page * U::kScaleBytes + MX::kVScales - 2 * MX::kCodes + at;
+    vs_tok = page * kPage + at % kPage - group * TG;
+  }
+
+  // The first `left` (0 to 4) bytes of a word.
+  __device__ static __forceinline__ uint32_t bytes(int left) { return left >= 4 ? 0xffffffffu : (1u << (8 * max(left, 0))) - 1u; }
+
+  // Adds the unit's infinite and NaN elements of V to the outputs, and makes them zeros in buf (a scale of 255 becomes 0).
+  // Rare: a token at a time, in few registers.
+  __device__ __forceinline__ void take_odd(char* buf, f32x4* oacc, int lim, uint32_t half) const {
+    const uint32_t one = 0x3f803f80u & half;
+    int codes = v, scales = vs;
+    __asm__ volatile("" : "+v"(codes), "+v"(scales));   // (else the addresses below are kept in registers all along)
+#pragma unroll
+    for (int q = 0; q < U::TP; ++q) {
+      f32x4 n = {0.f, 0.f, 0.f, 0.f};               // counts of each channel
+#pragma unroll 1
+      for (int j = 0; j < TG; ++j) {
+        char* const code = buf + codes + 256 * q + (kBits == 4 ? j : j / 8 * (D / 2 * 16) + j % 8 * 2);
+        uint8_t* const scale = reinterpret_cast<uint8_t*>(buf + scales + kPage * q + j);
+        const uint32_t w = kBits == 4 ? *reinterpret_cast<const uint8_t*>(code) : *reinterpret_cast<const uint16_t*>(code);
+        uint32_t m, kinds = odd_kinds(mx_up<kBits, 0>(w, mx_scale(*scale)), m);
+        kinds = j < lim ? kinds : 0u;
+        n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4{kinds, 0u, 0u, 0u}), as_bf16x8(u32x4{one, 0u, 0u, 0u}), n, 0, 0, 0);
+        if constexpr (kBits == 4) *reinterpret_cast<uint8_t*>(code) = (uint8_t)(w & ~((m & 0x0fu) | (m >> 16 & 0xf0u)));
+        else *reinterpret_cast<uint16_t*>(code) = (uint16_t)(w & ~((m & 0xffu) | (m >> 16 & 0xff00u)));
+        if (*scale == 255) *scale = 0;              // (of all 16 lanes alike)
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) oacc[q][i] = with_odd(oacc[q][i], n[i]);
+    }
   }
 
   // Attends the heads to the unit in buf.  lim: how many of this lane group's tokens count (TG unless kTail).
   template <bool kTail>
-  __device__ __forceinline__ void unit(const char* buf, const bf16x8* qop, f32x4* oacc, float& m_run, float& l_run, float c,
+  __device__ __forceinline__ void unit(char* buf, const bf16x8* qop, f32x4* oacc, float& m_run, float& l_run, float c,
                                        int lim, uint32_t half) const {
     // All of the unit's operands are read before the first is used, so that one LDS latency passes and not one a
     // tile (the barrier keeps the compiler from moving each read to its use).
-    uint32_t scale[kPieces], kw[NT][KW], vw[U::TP][VW], vsc[U::TP][TG / 4];
+    uint32_t scale[kPieces], kw[NT][KW], vw[U::TP][VW], vsc[U::TP][TG / 4], large;
+    lds_words<1>(&large, buf + vs_any);
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) lds_words<1>(&scale[p], buf + ks + 8 * p);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) lds_words<KW / kPieces>(&kw[t][p * (KW / kPieces)], buf + k + 4 * t * MX::kRow + 64 * p);
+    auto read_v = [&]() {
 #pragma unroll
-    for (int q = 0; q < U::TP; ++q) {
-      lds_words<TG / 4>(vsc[q], buf + vs + kPage * q);
+      for (int q = 0; q < U::TP; ++q) {
+        lds_words<TG / 4>(vsc[q], buf + vs + kPage * q);
 #pragma unroll
-      for (int x = 0; x < VW; x += 4)               // (8 words: tokens 0-7 and 8-15, a unit each)
-        lds_words<VW < 4 ? VW : 4>(&vw[q][x], buf + v + 256 * q + x / 4 * (D / 2 * 16));
-    }
+        for (int x = 0; x < VW; x += 4)             // (8 words: tokens 0-7 and 8-15, a unit each)
+          lds_words<VW < 4 ? VW : 4>(&vw[q][x], buf + v + 256 * q + x / 4 * (D / 2 * 16));
+      }
+    };
+    read_v();
     __builtin_amdgcn_sched_barrier(0);
     f32x4 s[NT];
 #pragma unroll
@@ -233,11 +292,11 @@ template <int D, int kBits> struct Attend {
       pop[j] = both & half;
       rest[j] = twice_bf16(p[j] - __builtin_bit_cast(float, both & 0xffff0000u)) & half;
     }
-    if constexpr (kTail) {                          // codes and scales past the end become zeros (0 times NaN is NaN)
+    auto end_v = [&]() {                            // codes and scales past the end become zeros (0 times NaN is NaN)
 #pragma unroll
       for (int x = 0; x < TG / 4; ++x) {
         const int left = min(max(lim - 4 * x, 0), 4);
-        const uint32_t mask = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
+        const uint32_t mask = bytes(left);
 #pragma unroll
         for (int q = 0; q < U::TP; ++q) {
           vsc[q][x] &= mask;
@@ -249,6 +308,24 @@ template <int D, int kBits> struct Attend {
           }
         }
       }
+    };
+    if constexpr (kTail) {
+      end_v();
+      large &= bytes(lim - vs_tok);
+    }
+    uint32_t odd = mx_large_scale<kBits>(large);
+    if constexpr (kBits == 8) {
+      uint32_t nan = 0u;
+#pragma unroll
+      for (int q = 0; q < U::TP; ++q)
+#pragma unroll
+        for (int x = 0; x < VW; ++x) nan |= mx_nan_code(vw[q][x]);
+      odd |= nan & kMxNanBits;
+    }
+    if (__builtin_expect(__ballot(odd != 0u) != 0, 0)) {
+      take_odd(buf, oacc, lim, half);
+      read_v();
+      if constexpr (kTail) end_v();
     }
 #pragma unroll
     for (int u = 0; u < TG / 4; ++u) {

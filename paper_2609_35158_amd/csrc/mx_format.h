@@ -56,6 +56,21 @@ template <int k> __device__ __forceinline__ float mx_scale_of(uint32_t w) {
   return __builtin_bit_cast(float, k < 3 ? w << (23 - 8 * k) : w >> 1);
 }
 
+// Whether an element under one of a word's four scales can be infinite or NaN because of the scale (a bit per byte):
+// finite ones are the largest under 252 at 4 bits (6 * 2^125) and 246 at 8 (448 * 2^119).  From 240 on at 8 bits, which
+// takes fewer instructions: what asks only does more work then.
+template <int kBits> __device__ __forceinline__ uint32_t mx_large_scale(uint32_t w) {
+  if constexpr (kBits == 4) return ((w >> 2 & 0x3f3f3f3fu) + 0x01010101u) & 0x40404040u;   // 252 and more
+  else return ((w >> 4 & 0x0f0f0f0fu) + 0x01010101u) & 0x10101010u;                        // 240 and more
+}
+// Whether one of a word's four 8-bit elements is E4M3's NaN, 0x7f or 0xff: its byte's bit in kMxNanBits.
+constexpr uint32_t kMxNanBits = 0x80808080u;
+__device__ __forceinline__ uint32_t mx_nan_code(uint32_t w) { return (w & 0x7f7f7f7fu) + 0x01010101u; }
+
+// Whether the low or the high one of two bf16 in a dword is infinite or NaN.
+__device__ __forceinline__ bool mx_low_not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
+__device__ __forceinline__ bool mx_high_not_finite(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+
 // Two elements (byte kSel of w, or 16-bit half kSel at 8 bits) as bf16 in a dword: exact, except values
 // under 2^-133, the least bf16, which are rounded to it.
 template <int kBits, int kSel> __device__ __forceinline__ uint32_t mx_up(uint32_t w, float scale) {

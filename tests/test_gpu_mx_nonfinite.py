@@ -1,0 +1,169 @@
+"""GPU attention over a cache of MX blocks whose attended elements of V are infinite or NaN: in the outputs of their own
+channel, of the rows that attend them, and nowhere else.
+
+Such elements come from E4M3's NaN codes, from scales above the ones that keep every element finite, from appended numbers of
+1.75 * 2^127 and more, which are read back as infinity, and from appended infinities and NaN, which make all 32
+channels of their block NaN."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_35158_amd as pa
+from gpu_helpers import bits, say
+from mx_helpers import MxCase, dev
+from oracle.mx_cache import _places
+
+pytestmark = pytest.mark.gpu
+
+FORMATS = (pa.MXFP4, pa.MXFP8)
+LARGEST = float(torch.finfo(torch.bfloat16).max)
+
+
+def _codes(c, b, h, pos, channel):
+    """(page, byte, shift, mask) of the code of V's element."""
+    byte = int(_places(pos % 16, c.d, c.fmt)[1][channel // 2 if c.fmt == 4 else channel])
+    shift = 4 * (channel % 2) if c.fmt == 4 else 0
+    return int(c.bt[b, pos // 16]), byte, shift, 15 if c.fmt == 4 else 255
+
+
+def put(c, cache, b, h, pos, channel, code, scale=None):
+    """Writes one element's code, and its block's scale with zeros in the other 31 elements."""
+    if scale is not None:
+        for i in range(channel // 32 * 32, channel // 32 * 32 + 32):
+            put(c, cache, b, h, pos, i, 0)
+        cache[int(c.bt[b, pos // 16]), h, int(_places(pos % 16, c.d, c.fmt)[3][channel // 32])] = scale
+    page, byte, shift, mask = _codes(c, b, h, pos, channel)
+    cache[page, h, byte] = (int(cache[page, h, byte]) & ~(mask << shift)) | code << shift
+
+
+def without(c, cache):
+    """The cache with zeros in place of V's infinite and NaN elements, wherever they are."""
+    out = cache.copy()
+    _, v = oracle.mx_pools(cache, c.d, c.fmt)
+    odd = (v & 0x7f80) == 0x7f80                                   # [pages, heads, 16, d]
+    for slot in range(16):
+        _, vc, _, vs = _places(slot, c.d, c.fmt)
+        for ch in range(c.d):
+            byte, shift = (vc[ch // 2], 4 * (ch % 2)) if c.fmt == 4 else (vc[ch], 0)
+            mask = (15 if c.fmt == 4 else 255) << shift
+            out[:, :, byte] = np.where(odd[:, :, slot, ch], out[:, :, byte] & (255 ^ mask), out[:, :, byte])
+        for blk in range(c.d // 32):                               # (0 times NaN)
+            out[:, :, vs[blk]] = np.where(out[:, :, vs[blk]] == 255, 1, out[:, :, vs[blk]])
+    return out
+
+
+def expected(c, cache):
+    """What the outputs are that infinities and NaN reach, 0 elsewhere: of a row's attended elements of its channel."""
+    _, v = oracle.mx_pools(cache, c.d, c.fmt)
+    v = oracle.bf16_bits_to_f64(v)
+    v = np.where(np.isfinite(v), 0.0, v)
+    out = np.zeros((c.total, c.hq, c.d))
+    for b in range(len(c.ctx)):
+        pos = np.arange(c.kv[b])
+        rows = v[c.bt[b, pos // 16], :, pos % 16]                  # [kv, heads, d]
+        with np.errstate(invalid="ignore"):
+            upto = np.cumsum(rows, axis=0)
+        for t in range(int(c.new[b])):
+            out[c.cu[b] + t] = np.repeat(upto[c.ctx[b] + t], c.G, 0)
+    return out
+
+
+def check(c, cache, out, lse):
+    odd = expected(c, cache)
+    got = oracle.bf16_bits_to_f64(bits(out))
+    where = ~np.isfinite(odd) | ~np.isfinite(got)
+    assert np.array_equal(got[where], odd[where], equal_nan=True), [
+        (tuple(i), got[tuple(i)], odd[tuple(i)]) for i in np.argwhere(where)
+        if not np.array_equal(got[tuple(i)], odd[tuple(i)], equal_nan=True)][:6]
+    kept, c.after = c.after, without(c, cache)
+    ref, ref_lse, tol, tol_lse = c.oracle()
+    c.after = kept
+    bad = ~where & ~(np.abs(got - ref) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:4], np.abs(got - ref)[~where].max())
+    assert (np.abs(lse.cpu().numpy().astype(np.float64) - ref_lse) <= tol_lse).all()
+
+
+def decode(c, cache, **kw):
+    _, bt, ctx, _, q, _, _ = c.device()
+    out, lse = pa.decode_mx(q, dev(cache), bt, ctx, c.max_kv, scale=c.scale, return_lse=True, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+# the code of a large element and the scales under which it is infinite: the least one, and the largest
+LARGE = {4: (6, 253, 254), 8: (0x7e, 247, 254)}
+
+
+def plant(c, rng, per_sequence):
+    """A cache with so many infinite and NaN elements of V at random places that every sequence attends to."""
+    cache = c.after.copy()
+    code, *scales = LARGE[c.fmt]
+    for b in range(len(c.ctx)):
+        for _ in range(per_sequence):
+            pos = int(rng.integers(c.kv[b]))
+            h, ch, sign = int(rng.integers(c.hkv)), int(rng.integers(c.d)), int(rng.integers(2))
+            if c.fmt == 8 and rng.random() < 0.4:
+                put(c, cache, b, h, pos, ch, 0x7f | sign << 7)
+            else:
+                put(c, cache, b, h, pos, ch, code | sign << (c.fmt - 1), int(scales[rng.integers(2)]))
+    return cache
+
+
+DECODE = ([0], [40], [300, 5, 1000], [63], [5000], [200] * 70, [17, 900, 33, 31])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("n", range(len(DECODE)))
+def test_decode(fmt, d, n):
+    say("decode_mx with infinite and NaN values fmt=%d d=%d ctx=%s" % (fmt, d, DECODE[n][:5]))
+    G, hkv = (1, 2, 4, 8)[n % 4], (2, 1, 3)[n % 3]
+    rng = np.random.default_rng(100 + n + d + fmt)
+    c = MxCase(fmt, d, hkv, G, DECODE[n], [1] * len(DECODE[n]), 200 + n + d + fmt)
+    cache = plant(c, rng, 3)
+    check(c, cache, *decode(c, cache))
+    # every kind in neighbouring channels of the new token, the largest of its own sequence by a wide margin
+    cache = c.after.copy()
+    code, s, _ = LARGE[fmt]
+    for b in range(len(c.ctx)):
+        put(c, cache, b, 0, int(c.ctx[b]), 6, code, s)
+        put(c, cache, b, 0, int(c.ctx[b]), 9, code | 1 << (fmt - 1))
+        put(c, cache, b, 0, int(c.ctx[b]), 12, code)
+        put(c, cache, b, 0, int(c.ctx[b]), 13, code | 1 << (fmt - 1))
+        if c.ctx[b]:
+            put(c, cache, b, 0, int(c.ctx[b]) - 1, 12, code | 1 << (fmt - 1), s)    # both signs: NaN
+    check(c, cache, *decode(c, cache))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("channel", (6, 7, 95))
+def test_appended_numbers_that_are_read_back_as_infinity(fmt, channel):
+    """The largest bf16, finite, in an even and in an odd channel: its own channel is infinite, as prefill's."""
+    say("decode_append_mx of the largest bf16 fmt=%d channel=%d" % (fmt, channel))
+    c = MxCase(fmt, 128, 2, 4, [300, 5, 1000, 0], [1] * 4, 300 + fmt)
+    c.v_new[:, 1, channel] = torch.tensor([LARGEST, -LARGEST, LARGEST, -LARGEST], dtype=torch.bfloat16)
+    cache, bt, ctx, cu, q, _, _ = c.device(appended=False)
+    out, lse = pa.decode_append_mx(q, c.k_new.cuda(), c.v_new.cuda(), cache, bt, ctx, c.max_kv, scale=c.scale, return_lse=True)
+    torch.cuda.synchronize()
+    after = oracle.mx_append(c.cache, fmt, bits(c.k_new), bits(c.v_new), c.bt, c.ctx, c.cu)
+    assert np.array_equal(cache.cpu().numpy(), after)
+    assert np.isinf(expected(c, after)[:, 4:, channel]).all()
+    check(c, after, out, lse)
+    turn, _ = pa.prefill_append_mx(q, cache, bt, ctx, cu, 1, c.max_kv, scale=c.scale, return_lse=True)
+    torch.cuda.synchronize()
+    same = np.isfinite(oracle.bf16_bits_to_f64(bits(turn)))
+    got = oracle.bf16_bits_to_f64(bits(out))
+    assert np.array_equal(np.isfinite(got), same)
+    assert np.array_equal(got[~same], oracle.bf16_bits_to_f64(bits(turn))[~same])
+
+
+def test_decode_of_several_kv_heads_a_workgroup():
+    """Workgroups of 8 kv-heads, whose waves finish by themselves, and of 4, joined in LDS."""
+    for fmt, d, hkv in ((4, 128, 8), (8, 64, 8), (4, 64, 4)):
+        say("decode_mx with infinite and NaN values fmt=%d d=%d hkv=%d" % (fmt, d, hkv))
+        rng = np.random.default_rng(hkv + d)
+        ctx = rng.integers(200, 420, size=40)
+        c = MxCase(fmt, d, hkv, 1, ctx, [1] * len(ctx), 400 + d + hkv)
+        cache = plant(c, rng, 2)
+        check(c, cache, *decode(c, cache))
