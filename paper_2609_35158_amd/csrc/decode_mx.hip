@@ -194,12 +194,12 @@ template <int D, int kBits> struct Attend {
       for (int j = 0; j < TG; ++j) {
         char* const code = buf + codes + 256 * q + (kBits == 4 ? j : j / 8 * (D / 2 * 16) + j % 8 * 2);
         uint8_t* const scale = reinterpret_cast<uint8_t*>(buf + scales + kPage * q + j);
-        const uint32_t w = kBits == 4 ? *reinterpret_cast<const uint8_t*>(code) : *reinterpret_cast<const uint16_t*>(code);
+        const uint32_t w = kBits == 4 ? *reinterpret_cast<const uint8_t*>(code) : *reinterpret_cast<const u16_any*>(code);
         uint32_t m, kinds = odd_kinds(mx_up<kBits, 0>(w, mx_scale(*scale)), m);
         kinds = j < lim ? kinds : 0u;
         n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4{kinds, 0u, 0u, 0u}), as_bf16x8(u32x4{one, 0u, 0u, 0u}), n, 0, 0, 0);
         if constexpr (kBits == 4) *reinterpret_cast<uint8_t*>(code) = (uint8_t)(w & ~((m & 0x0fu) | (m >> 16 & 0xf0u)));
-        else *reinterpret_cast<uint16_t*>(code) = (uint16_t)(w & ~((m & 0xffu) | (m >> 16 & 0xff00u)));
+        else *reinterpret_cast<u16_any*>(code) = (uint16_t)(w & ~((m & 0xffu) | (m >> 16 & 0xff00u)));
         if (*scale == 255) *scale = 0;              // (of all 16 lanes alike)
       }
 #pragma unroll

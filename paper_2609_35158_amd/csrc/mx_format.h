@@ -71,6 +71,9 @@ __device__ __forceinline__ uint32_t mx_nan_code(uint32_t w) { return (w & 0x7f7f
 __device__ __forceinline__ bool mx_low_not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }
 __device__ __forceinline__ bool mx_high_not_finite(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
 
+// 16 bits of a buffer that is read in other types too.
+typedef uint16_t u16_any __attribute__((may_alias));
+
 // Two elements (byte kSel of w, or 16-bit half kSel at 8 bits) as bf16 in a dword: exact, except values
 // under 2^-133, the least bf16, which are rounded to it.
 template <int kBits, int kSel> __device__ __forceinline__ uint32_t mx_up(uint32_t w, float scale) {
