@@ -245,6 +245,9 @@ pearl_status pearl_kv_unpack(const pearl_kv_shape* shape, const pearl_seq_desc* 
  *       (tokens 0-7 before 8-15 in E4M3, i);
  *     K scales [slot % 4][nb][slot / 4], V scales [nb][slot].
  *   Any bytes are valid contents of slots that no attended position owns.
+ *   An infinite or NaN element of V makes its own channel infinite or NaN in the outputs of the rows that attend its
+ *   token, and reaches nothing else (no row before it in a prefill, no other channel).  Weights times values are summed in
+ *   32 bits: values above 2^95 can overflow there.
  */
 typedef enum { PEARL_MXFP4 = 4, PEARL_MXFP8 = 8 } pearl_mx_format;
 

@@ -614,6 +614,24 @@ template <int D, int kBits> struct MxKTile {
   }
 };
 
+// The infinite and NaN elements of an item's V.  A key that a row of the tile does not attend has weight 0 there, and 0
+// times such an element is NaN: a later token's would reach the rows before it.  So an item with an output that is not
+// finite is computed again (prefill_rows_again) with zeros in their place, and they are added to the rows from their
+// position on.  (Looking for them in each stage's scales and codes instead took 0.6-3% more time.)
+template <int D> struct OddV {
+  int first[D][2];                                  // a channel's least position that is infinity or NaN; minus infinity or NaN
+  int again;
+  __device__ __forceinline__ void clear() {
+    static_assert(2 * D < kThreads, "a thread each");
+    if (threadIdx.x < 2 * D) first[threadIdx.x / 2][threadIdx.x % 2] = INT32_MAX;
+    if (threadIdx.x == 2 * D) again = 0;
+  }
+  __device__ __forceinline__ float add(float x, int channel, int last) const {   // to the row that attends up to `last`
+    const bool up = first[channel][0] <= last, down = first[channel][1] <= last;
+    return up || down ? x + (up ? (down ? __builtin_nanf("") : INFINITY) : -INFINITY) : x;
+  }
+};
+
 // This wave's 8 tokens of a V stage: a channel pair a lane, for D / 16 tokens.
 template <int D, int kBits> struct MxV {
   using MX = MxBlock<D, kBits>;
@@ -680,6 +698,133 @@ template <int D, int kBits> struct MxV {
 template <int D, int kBits> struct KTileBytes { static constexpr int value = MxKTile<D, kBits>::kBytes; };
 template <int D> struct KTileBytes<D, 0> { static constexpr int value = DmaTile<D>::BYTES; };
 
+// A wave's 32 rows of a prefill item over MX blocks, computed again with zeros for the infinite and NaN elements of V, which
+// are added at the end (OddV).  The products and layouts are prefill_tile_pp's (rows: this lane's query row q_row, which
+// attends keys k0 .. min(row_limit, k_end - 1)), their operands come straight from the cache, 32 keys at a time.  Rare, so
+// in little code and few registers: four turns of 64-400 tokens on 4K-24K contexts whose last tiles hold such elements
+// take 1.9 ms for 0.46.  All waves of the workgroup together.
+template <int D, int kBits>
+__device__ __forceinline__ void prefill_rows_again(const AttnArgs& a, ConstI32Ptr bt, int g, size_t q_row, int k0, int k_end,
+                                                   int row_limit, f32x16* oacc, float& m_run, float& l_tot, OddV<D>& odd) {
+  using MX = MxBlock<D, kBits>;
+  constexpr int KB = D / 16, MB = D / 32;
+  int lane = threadIdx.x & 63;
+  __asm__ volatile("" : "+v"(lane));                // (what follows from it is not kept in registers before)
+  const int row = lane & 31, half = lane >> 5;
+  auto block = [&](int key) {
+    const int page = clamp_page(bt[min(key, k_end - 1) / kPage], a.num_pages);
+    return a.cache + ((size_t)page * a.num_kv_heads + g) * MX::kBytes;
+  };
+  bf16x8 qop[KB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) qop[kb] = as_bf16x8(ld16(a.q + q_row * D + D / 2 * half + 8 * kb));
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[mb][r] = 0.f;
+  m_run = -INFINITY;
+  float l_run = 0.f;
+#pragma unroll 1
+  for (int k = k0; k < k_end; k += 32) {
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    {
+      const uint8_t* const blk = block(k + row);
+      const uint8_t* const codes = blk + row % kPage * MX::kRow + half * (MX::kRow / 2);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const float f = mx_scale(blk[MX::k_scale(row % kPage, half * (D / 64) + kb / 4)]);
+        u32x4 x;
+        if constexpr (kBits == 4) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + 4 * kb);
+          x = u32x4{mx_up<4, 0>(w, f), mx_up<4, 1>(w, f), mx_up<4, 2>(w, f), mx_up<4, 3>(w, f)};
+        } else {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(codes + 8 * kb);
+          x = u32x4{mx_up<8, 0>(w[0], f), mx_up<8, 1>(w[0], f), mx_up<8, 0>(w[1], f), mx_up<8, 1>(w[1], f)};
+        }
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), qop[kb], s, 0, 0, 0);
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = k + (r & 3) + 8 * (r >> 2) + 4 * half;
+      s[r] = key > row_limit || key >= k_end ? -INFINITY : s[r];
+      mx = fmaxf(mx, s[r]);
+    }
+    mx = xor32_max(mx) * a.scale_log2;
+    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = fexp2(m_run - m_use);
+    m_run = m_new;
+    l_run *= alpha;
+    bf16x8 pop[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float p = fexp2(__builtin_fmaf(s[r], a.scale_log2, -m_use));
+      l_run += p;
+      pop[r >> 3][r & 7] = (__bf16)p;
+    }
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) oacc[mb] *= alpha;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {                // a page: V of slots 4 half .. and 8 + 4 half .. for this lane's channels
+      const int first = k + kPage * kk + 4 * half;
+      const uint8_t* const blk = block(k + kPage * kk);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        const int dim = 32 * mb + row, pair = dim >> 1;
+        uint32_t x[8], not_finite = 0u, nan = 0u, neg = 0u;
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const int slot = 8 * z + 4 * half;
+          const uint32_t f = *reinterpret_cast<const uint32_t*>(blk + MX::v_scale(slot, pair >> 4));
+          if constexpr (kBits == 4) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + MX::v_code(slot, pair));
+            x[4 * z] = mx_up<4, 0>(w, mx_scale_of<0>(f));
+            x[4 * z + 1] = mx_up<4, 1>(w, mx_scale_of<1>(f));
+            x[4 * z + 2] = mx_up<4, 2>(w, mx_scale_of<2>(f));
+            x[4 * z + 3] = mx_up<4, 3>(w, mx_scale_of<3>(f));
+          } else {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(blk + MX::v_code(slot, pair));
+            x[4 * z] = mx_up<8, 0>(w[0], mx_scale_of<0>(f));
+            x[4 * z + 1] = mx_up<8, 1>(w[0], mx_scale_of<1>(f));
+            x[4 * z + 2] = mx_up<8, 0>(w[1], mx_scale_of<2>(f));
+            x[4 * z + 3] = mx_up<8, 1>(w[1], mx_scale_of<3>(f));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] = dim & 1 ? x[i] >> 16 : x[i] & 0xffffu;
+          if (first + 8 * (i >> 2) + (i & 3) >= k_end) x[i] = 0u;
+          if (mx_low_not_finite(x[i])) {
+            not_finite |= 1u << i;
+            if (x[i] & 0x7fu) nan |= 1u << i;
+            if (x[i] & 0x8000u) neg |= 1u << i;
+            x[i] = 0u;
+          }
+        }
+#pragma unroll 1
+        while (not_finite) {
+          const int i = __builtin_ctz(not_finite), key = first + 8 * (i >> 2) + (i & 3);
+          const bool is_nan = nan >> i & 1u, is_neg = neg >> i & 1u;
+          not_finite &= not_finite - 1u;
+          if (is_nan || !is_neg) atomicMin(&odd.first[dim][0], key);
+          if (is_nan || is_neg) atomicMin(&odd.first[dim][1], key);
+        }
+        const u32x4 op = {x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16};
+        oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(op), pop[kk], oacc[mb], 0, 0, 0);
+      }
+    }
+  }
+  l_tot = xor32_add(l_run);
+  __syncthreads();
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[mb][r] = odd.add(oacc[mb][r], 32 * mb + 8 * (r >> 2) + 4 * half + (r & 3), row_limit);
+}
+
 // ------------------------------------------------------------------------------------------------
 // Prefill-append work item: one (sequence, kv-head g, q-tile).  The tile holds 256 q-rows =
 // tokens_per_tile tokens x G heads of the group (row rho -> token rho / G, head rho % G), so every
@@ -727,7 +872,7 @@ template <int D> struct KTileBytes<D, 0> { static constexpr int value = DmaTile<
 // at_end: called by every thread when the stages are done, before the epilogue.
 template <int D, int kBits, typename AtEnd>
 __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int code, int g, char* kb0, char* vb0, char* raw0,
-                                                AtEnd at_end) {
+                                                OddV<D>* odd, AtEnd at_end) {
   constexpr int KB = D / 16;                        // 16-wide k blocks of the QK product
   constexpr int MB = D / 32;                        // 32-wide dim blocks of the PV product
   constexpr int SK = kKeysPerStage;                 // keys per stage
@@ -1078,6 +1223,7 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
     __asm__ volatile("s_barrier" ::: "memory");
   } else {
     // K(0), K(1), V(0), V(1), V(2), of which V(0) becomes a tile here
+    odd->clear();                                   // (every thread is past the barrier behind the item before)
     mx_next = mx_entry(-3);
     mx_send(-3, kbuf(2), raw_buf(0));               // V(0)
     mx_send(-2, kbuf(0), raw_buf(1));               // K(0), V(1)
@@ -1195,10 +1341,29 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
   }
 
 
+  if constexpr (kBits != 0) {
+    uint32_t most = 0u;                             // bits of the largest magnitude: NaN above infinity above the others
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float o = oacc[mb][r];                // (a bit cast of the element itself takes element 0)
+        most = max(most, __builtin_bit_cast(uint32_t, o) & 0x7fffffffu);
+      }
+    if (__ballot(most >= 0x7f800000u)) odd->again = 1;
+    __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
   at_end();
   // epilogue: combine the two half-row sums; a split item stores its fp32 partial state, a whole
   // item normalises and stores bf16 O and the fp32 LSE
-  const float l_tot = xor32_add(l_run);
+  float l_tot = xor32_add(l_run);
+  if constexpr (kBits != 0) {
+    if (__builtin_expect(uni(odd->again), 0)) {
+      const int k0 = step_begin * SK, k_end = min(step_end * SK, kv_needed);
+      prefill_rows_again<D, kBits>(a, bt_c, g, (size_t)(si.q_start + (row_ok ? tok : t0)) * H_q + h, k0, k_end,
+                                   row_ok ? row_limit : ctx + t0, oacc, m_run, l_tot, *odd);
+    }
+  }
   if (row_ok && n_split > 1) {
     const int slot = a.split_base[b] + split * ((si.q_len + a.tokens_per_tile - 1) / a.tokens_per_tile) + tile;
     const size_t prow = (size_t)(slot * H_kv + g) * kRowsPerTile + rho;
@@ -1622,6 +1787,7 @@ __global__ __launch_bounds__((KernelCfg<D, kKinds>::NT)) void attn_kernel(AttnAr
   constexpr int kDT = (kKinds == 1) ? DmaTile<D>::BYTES : 16;
   __shared__ __attribute__((aligned(16))) char pk[kKinds == 1 ? 3 * KTileBytes<D, kBits>::value : 16], pv[3 * kDT];
   __shared__ __attribute__((aligned(16))) char raw[kBits != 0 ? 3 * MxV<D, kBits == 0 ? 4 : kBits>::kRawBytes : 16];
+  __shared__ OddV<kBits != 0 ? D : 1> odd;
   __shared__ int s_item[2][2];                      // next item and claim mode
   const int n_items = a.ws_hdr[kHdrNumItems];
   const int n_pre = a.ws_hdr[kHdrNumPre];
@@ -1716,13 +1882,13 @@ __global__ __launch_bounds__((KernelCfg<D, kKinds>::NT)) void attn_kernel(AttnAr
         static_assert(NW == kWaves, "prefill tiles use 8 waves");
         const int2 en = a.entries[e];
         if constexpr (kKinds == 1) {
-          prefill_tile_pp<D, kBits>(a, en.x, en.y, g, pk, pv, raw, send_claim);
+          prefill_tile_pp<D, kBits>(a, en.x, en.y, g, pk, pv, raw, reinterpret_cast<OddV<D>*>(&odd), send_claim);
         } else {
           // the mixed kernel's prefill stage buffers share its LDS region with the decode stages (a
           // workgroup runs one item at a time, and items are separated by a drained barrier)
           constexpr int B = DmaTile<D>::BYTES;
           static_assert(6 * B <= Lds<D, NW, kKinds>::bytes, "stage buffers fit the shared region");
-          prefill_tile_pp<D, 0>(a, en.x, en.y, g, smem, smem + 3 * B, raw, send_claim);
+          prefill_tile_pp<D, 0>(a, en.x, en.y, g, smem, smem + 3 * B, raw, nullptr, send_claim);
         }
       }
     } else {

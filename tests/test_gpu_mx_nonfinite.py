@@ -167,3 +167,66 @@ def test_decode_of_several_kv_heads_a_workgroup():
         c = MxCase(fmt, d, hkv, 1, ctx, [1] * len(ctx), 400 + d + hkv)
         cache = plant(c, rng, 2)
         check(c, cache, *decode(c, cache))
+
+
+def prefill(c, cache, **kw):
+    _, bt, ctx, cu, q, _, _ = c.device()
+    out, lse = pa.prefill_append_mx(q, dev(cache), bt, ctx, cu, c.max_q, c.max_kv, scale=c.scale, return_lse=True, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+# single rows, page, stage (64 keys) and tile edges, several tiles, long contexts whose keys are split over workgroups
+TURNS = [([0], [17]), ([63, 64, 65, 0], [1, 2, 0, 64]), ([5, 0, 130], [255, 256, 31]), ([1500, 3], [300, 70]), ([0], [520]),
+         ([9000], [40]), ([6000, 20], [3, 90])]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("n", range(len(TURNS)))
+def test_prefill(fmt, d, n):
+    """In the rows from an element's position on, whether its key is masked for rows of the same tile or not."""
+    ctx, new = TURNS[n]
+    say("prefill_mx with infinite and NaN values fmt=%d d=%d ctx=%s new=%s" % (fmt, d, ctx, new))
+    G, hkv = (1, 2, 4, 8)[n % 4], (2, 1, 3)[n % 3]
+    rng = np.random.default_rng(500 + n + d + fmt)
+    c = MxCase(fmt, d, hkv, G, ctx, new, 600 + n + d + fmt)
+    cache = plant(c, rng, 2)
+    for b in range(len(ctx)):                                      # and among the new tokens
+        code, s, _ = LARGE[fmt]
+        for _ in range(3 if new[b] else 0):
+            pos, ch = int(ctx[b] + rng.integers(new[b])), int(rng.integers(d))
+            put(c, cache, b, int(rng.integers(hkv)), pos, ch, code | int(rng.integers(2)) << (fmt - 1), s)
+    check(c, cache, *prefill(c, cache))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("value", (float("nan"), float("inf"), -LARGEST))
+def test_a_turns_values_do_not_reach_the_tokens_before_them(fmt, value):
+    say("prefill_mx with a new value of %s fmt=%d" % (value, fmt))
+    c = MxCase(fmt, 128, 2, 4, [40, 1000, 0], [100, 30, 7], 700 + fmt)
+    v_new, at = c.v_new.clone(), {0: 53, 1: 4, 2: 6}               # the token of each sequence
+    for b, t in at.items():
+        v_new[int(c.cu[b]) + t, 1, 77] = value
+    cache, bt, ctx, cu, q, k, _ = c.device(appended=False)
+    pa.kv_append_mx(k, v_new.cuda(), cache, bt, ctx, cu, c.max_q, c.max_kv)
+    out, lse = pa.prefill_append_mx(q, cache, bt, ctx, cu, c.max_q, c.max_kv, scale=c.scale, return_lse=True)
+    torch.cuda.synchronize()
+    check(c, cache.cpu().numpy(), out, lse)
+    reached = torch.zeros_like(out, dtype=torch.bool)
+    for b, t in at.items():
+        reached[int(c.cu[b]) + t:int(c.cu[b + 1]), 4:, slice(64, 96) if not np.isfinite(value) else 77] = True
+    assert torch.equal(~torch.isfinite(out), reached)
+
+
+def test_prefill_items_one_after_another():
+    """More items than workgroups, some with such elements: none are left over for the next item."""
+    say("prefill_mx with infinite and NaN values in some of many items")
+    rng = np.random.default_rng(9)
+    ctx, new = [0] * 160, [3 + (5 * i) % 20 for i in range(160)]
+    c = MxCase(4, 64, 4, 1, ctx, new, 800)
+    cache = c.after.copy()
+    code, s, _ = LARGE[4]
+    for b in range(0, 160, 7):
+        put(c, cache, b, int(rng.integers(4)), int(rng.integers(new[b])), int(rng.integers(64)), code, s)
+    check(c, cache, *prefill(c, cache))
