@@ -2254,14 +2254,14 @@ __global__ __launch_bounds__(256) void merge_prefill_kernel(AttnArgs a) {
       float M_new = M;
 #pragma unroll
       for (int u = 0; u < U; ++u) M_new = fmaxf(M_new, m[u]);
-      const float alpha = s0 == 0 ? 0.f : fexp2(M - M_new);
+      const float base = M_new == -INFINITY ? 0.f : M_new, alpha = fexp2(M - base);   // (as in merge_pair)
       L *= alpha;
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] *= alpha;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (s0 + u >= ns) break;
-        const float f = fexp2(m[u] - M_new);
+        const float f = fexp2(m[u] - base);
         L += f * l[u];
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] += f * v[u][i];

@@ -278,7 +278,7 @@ template <int D, int kBits> struct Attend {
       const bool grow = mx * c > m_run;
       const float m_new = grow ? mx * c : m_run;
       const float alpha = grow ? fexp2(m_run - m_new) : 1.0f;
-      sum = weights(m_new);
+      sum = weights(m_new == -INFINITY ? 0.f : m_new);   // (every score so far is minus infinity: weights of 0)
       l_run *= alpha;
 #pragma unroll
       for (int q = 0; q < U::TP; ++q) oacc[q] *= alpha;

@@ -267,7 +267,8 @@ __device__ __forceinline__ void ld_dev2(const float* p, float& x, float& y) {
 }
 
 // Merge of a cut pair (kv-head g) from its partials, in the workgroup that counted itself in last:
-//   o = sum_s 2^(m_s - m*) o~_s / sum_s 2^(m_s - m*) l_s,   lse = (m* + log2 l*) ln 2.
+//   o = sum_s 2^(m_s - m*) o~_s / sum_s 2^(m_s - m*) l_s,   lse = (m* + log2 l*) ln 2
+// (of partials whose scores are all minus infinity m_s is too: weight 0).
 // A lane takes D/16 dims of a q-head and the (m, l) of that head (4 heads a pass), up to kMergeBlock
 // partials in flight at a time and no load beyond the pair's own (one sequence of 2732 keys, 10
 // partials a pair: 13.8 us a call with blocks of 8, 13.15 with 12, 13.2 with 16; with the last
@@ -301,14 +302,14 @@ __device__ __forceinline__ void merge_pair(const AttnArgs& a, const CutPair& c, 
     float M_new = M;
 #pragma unroll
     for (int u = 0; u < U; ++u) M_new = fmaxf(M_new, m[u]);
-    const float alpha = s0 == 0 ? 0.f : fexp2(M - M_new);
+    const float base = M_new == -INFINITY ? 0.f : M_new, alpha = fexp2(M - base);
     L *= alpha;
 #pragma unroll
     for (int i = 0; i < PER; ++i) acc[i] *= alpha;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (s0 + u < ns) {                            // uniform
-        const float f = fexp2(m[u] - M_new);
+        const float f = fexp2(m[u] - base);
         L += f * l[u];
 #pragma unroll
         for (int i = 0; i < PER; ++i) acc[i] += f * v[u][i];
@@ -447,7 +448,7 @@ __device__ __forceinline__ void finish_shares(const AttnArgs& a, const DecPlanAr
           const ShareEnd<D>& E = *reinterpret_cast<const ShareEnd<D>*>(stage + (q * sh.heads + j) * stage_bytes);
           const float m = E.ml[which][head][0], l = E.ml[which][head][1];
           const float M_new = fmaxf(M, m);
-          const float fa = M == -INFINITY ? 0.f : fexp2(M - M_new), fb = fexp2(m - M_new);
+          const float base = M_new == -INFINITY ? 0.f : M_new, fa = fexp2(M - base), fb = fexp2(m - base);
           L = fa * L + fb * l;
           o0 = fa * o0 + fb * E.o[which][head][dim];
           o1 = fa * o1 + fb * E.o[which][head][dim + 1];

@@ -230,3 +230,83 @@ def test_prefill_items_one_after_another():
     for b in range(0, 160, 7):
         put(c, cache, b, int(rng.integers(4)), int(rng.integers(new[b])), int(rng.integers(64)), code, s)
     check(c, cache, *prefill(c, cache))
+
+
+def put_k(c, cache, b, positions, channel):
+    """K of these positions: an element of 2^128 or more, which is read back as infinity, and 31 zeros in its block."""
+    code, _, scale = LARGE[c.fmt]
+    for pos in positions:
+        page = int(c.bt[b, pos // 16])
+        codes, _, scales, _ = _places(pos % 16, c.d, c.fmt)
+        at = codes.reshape(c.d // 32, -1)[channel // 32]
+        cache[page][:, at] = 0
+        cache[page][:, scales[channel // 32]] = scale
+        byte = int(codes[channel // 2 if c.fmt == 4 else channel])
+        cache[page][:, byte] = code << (4 * (channel % 2) if c.fmt == 4 else 0)
+
+
+def check_k(c, cache, out, lse):
+    """Against the oracle, where scores of minus infinity are weights of 0; bounds as MxCase.oracle's, with the largest
+    attended |v| for the weighted sums of them, whose weights these keys change."""
+    k, v = oracle.mx_pools(cache, c.d, c.fmt)
+    with np.errstate(invalid="ignore"):
+        ref, ref_lse = oracle.attention(bits(c.q), k, v, c.bt, c.ctx, c.cu, c.scale)
+    got = oracle.bf16_bits_to_f64(bits(out))
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    kn = vm = 0.0
+    for b in range(len(c.ctx)):
+        pos = np.arange(c.kv[b])
+        for x, is_v in ((k, False), (v, True)):
+            rows = oracle.bf16_bits_to_f64(x[c.bt[b, pos // 16], :, pos % 16])
+            rows = np.where(np.isfinite(rows), rows, 0.0)
+            if is_v:
+                vm = max(vm, float(np.abs(rows).max()))
+            else:
+                kn = max(kn, float(np.linalg.norm(rows, axis=-1).max()))
+    score = c.scale * np.linalg.norm(oracle.bf16_bits_to_f64(bits(c.q)), axis=-1) * kn
+    off = c.d * 2.0 ** -24 * score + 2.0 ** -21 * score
+    sums = (c.max_kv / 4 + 64) * 2.0 ** -24
+    weight = 2.0 ** -16 if c.max_q == 1 else 2.0 ** -8
+    tol = 2.0 ** -8 * np.abs(ref) + (2 * off + 2 * sums + weight)[..., None] * vm
+    seen = ~np.isnan(ref)
+    assert (np.abs(got - ref) <= tol)[seen].all(), float(np.abs(got - ref)[seen].max())
+    seen = ~np.isnan(ref_lse)
+    tol_lse = off + sums + 2.0 ** -21 * np.abs(ref_lse) + 1e-6
+    assert (np.abs(lse.cpu().numpy().astype(np.float64) - ref_lse) <= tol_lse)[seen].all()
+
+
+def against(c, channel):
+    """Heads 0, 2, .. whose scores with such keys are minus infinity, and the others, where they are infinity: NaN."""
+    sign = torch.tensor([-1.0, 1.0] * c.hq)[:c.hq]
+    c.q[:, :, channel] = (c.q[:, :, channel].float().abs() + 0.25).to(torch.bfloat16) * sign.to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d,hkv", ((64, 2), (128, 2), (128, 8)))
+def test_keys_whose_scores_are_minus_infinity(fmt, d, hkv):
+    """They have weight 0, also where a unit, a share or a split of the keys holds no others."""
+    say("mx attention with infinite keys fmt=%d d=%d hkv=%d" % (fmt, d, hkv))
+    ctx = [64, 16, 200, 1000, 33, 5000]
+    c = MxCase(fmt, d, hkv, 2, ctx, [1] * len(ctx), 900 + d + fmt + hkv)
+    against(c, 3)
+    cache = c.after.copy()
+    for b, n in enumerate(ctx):                                    # the new token, alone in its page or not
+        put_k(c, cache, b, [n], 3)
+    put_k(c, cache, 2, range(64), 3)                               # the first units
+    put_k(c, cache, 3, range(900), 3)
+    put_k(c, cache, 5, range(200, 4700), 3)                        # whole shares
+    check_k(c, cache, *decode(c, cache))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", (64, 128))
+def test_a_turns_keys_whose_scores_are_minus_infinity(fmt, d):
+    say("prefill_mx with infinite keys fmt=%d d=%d" % (fmt, d))
+    c = MxCase(fmt, d, 2, 2, [100, 0, 6000, 300], [30, 90, 3, 64], 950 + d + fmt)
+    against(c, 3)
+    cache = c.after.copy()
+    put_k(c, cache, 0, [107], 3)                                   # a new token
+    put_k(c, cache, 1, range(10, 80), 3)
+    put_k(c, cache, 2, range(5900), 3)                             # splits without other keys
+    put_k(c, cache, 3, range(64), 3)                               # the first stage
+    check_k(c, cache, *prefill(c, cache))
