@@ -306,7 +306,8 @@ pearl_status pearl_attn_prefill_append_mx(const pearl_kv_shape* shape, const pea
  * every library call made on the calling thread records `before` on its stream immediately
  * before launching its main kernel (the attention kernel for the three attention calls, the
  * page-copy kernel for pearl_kv_append, pearl_kv_pack, pearl_kv_unpack and their _mx forms) and `after`
- * immediately after it.  The handles are
+ * immediately after it.  (A decode over MX blocks of more than 1024 sequences has a main kernel for each group of
+ * them: `before` the first, `after` the last.)  The handles are
  * hipEvent_t values created and owned by the caller; pass NULL, NULL to clear.  The pair stays
  * set until changed, so a caller timing several calls sets a fresh pair before each one.
  */

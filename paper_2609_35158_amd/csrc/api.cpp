@@ -345,11 +345,11 @@ pearl_status run_decode_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pea
       e = launch_zero_words(zero, hs);
     }
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "decode prologue launch: %s", hipGetErrorString(e));
-    e = record_before(hs);
+    if (b0 == 0) e = record_before(hs);             // the events enclose all groups
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
     e = launch_decode_mx(a, d, s->head_dim, bits, hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "decode launch: %s", hipGetErrorString(e));
-    e = record_after(hs);
+    if (b0 + d.batch == q->batch) e = record_after(hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
   }
   return debug_check(static_cast<const char*>(ws), pl, hs);
