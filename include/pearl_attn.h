@@ -280,7 +280,8 @@ pearl_status pearl_kv_pack_mx(const pearl_kv_shape* shape, const pearl_seq_desc*
  * pearl_attn_decode_mx, with the same results bit for bit, in as many launches as the decode alone.
  *   workspace: as for the other attention calls, of pearl_attn_workspace_bytes(shape, seqs).
  * Sequences are taken in groups of 1024 in order; where a length violates the host bounds, the attention
- * of its group writes nothing (an append still takes place).
+ * of its group writes nothing (an append still takes place).  A group of sequences of max_kv_len tokens may hold up to 2^31
+ * - 1 pages, 4 more counted for each sequence.
  */
 pearl_status pearl_attn_decode_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, pearl_mx_format format,
                                   const void* q, const void* cache, float softmax_scale, void* out, float* lse,

@@ -311,6 +311,10 @@ pearl_status run_decode_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pea
   if (st != PEARL_OK) return st;
   if (k_new && (!aligned16(k_new) || !aligned16(v_new)))
     return fail(PEARL_ERR_INVALID_ARG, "k_new and v_new must be 16-byte aligned");
+  // the kernel counts a group's pages, and its sequences' starts as pages, in int32
+  const int64_t group = std::min(q->batch, kDecPlanMaxSeqs);
+  if (group * (cdiv(q->max_kv_len, kPage) + kMxSeqCost) > INT32_MAX)
+    return fail(PEARL_ERR_UNSUPPORTED, "%lld sequences of max_kv_len (%d) tokens exceed int32 pages", (long long)group, q->max_kv_len);
   const Plan pl = make_plan(s, q, kModeDecode);
   if (pl.lay.max_dec * (int64_t)s->num_kv_heads > INT32_MAX)
     return fail(PEARL_ERR_UNSUPPORTED, "partial slots (%lld x %d kv-heads) exceed int32", (long long)pl.lay.max_dec, s->num_kv_heads);

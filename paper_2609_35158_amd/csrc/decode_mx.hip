@@ -47,7 +47,7 @@ namespace {
 // and 34.1, 32 of 2K-8K 37.9 and 36.7, 200 of 1K-5K at 2 kv-heads 38.2 and 37.0; at d = 64 and 4 bits 64 of 2K-6K 38.7 and
 // 41.3; at d = 128 and 4 bits (8 and 4) 48 of 2K-6K 44.8 and 47.7, 200 of 500-2000 at 4 kv-heads 38.5 and 42.3.
 template <int D, int kBits, int kPages> struct MxCut {
-  static constexpr int kPieceCost = D == 64 && kBits == 8 ? 3 : 8, kWholePages = 56, kSeqCost = 4, kUnit = kPages;
+  static constexpr int kPieceCost = D == 64 && kBits == 8 ? 3 : 8, kWholePages = 56, kSeqCost = kMxSeqCost, kUnit = kPages;
 };
 
 // A unit: kPages pages of one (sequence, kv-head) and how they lie in a wave's buffer.

@@ -46,6 +46,8 @@ constexpr int kNumXcd = 8;
 // Decode batches of up to this many sequences are planned inside the attention kernel (in LDS);
 // larger ones go through plan_kernel.
 constexpr int kDecPlanMaxSeqs = 1024;
+// Decode over MX blocks: pages that a sequence's start counts as where shares are made equal (MxCut).
+constexpr int kMxSeqCost = 4;
 // With more kv-heads than resident workgroups, runs for about this many rounds of them.
 constexpr int kDecRounds = 4;
 
