@@ -40,12 +40,19 @@ namespace pearl {
 
 namespace {
 
-// 2176 bytes of K and V a page and kv-head at 4 bits, d = 128.  Shares of 70 pages of 512 sequences (64-1024 tokens) took
-// 2.2 us a unit and 2.0 a sequence more, so the ones with 5 or 6 sequences ended last: with a sequence's start counted as
-// 4 pages 68.1 us, with 0 71.2, with 8 67.8.  Several kv-heads a workgroup (us a call with kPieceCost 8 and 3): at d = 64
-// and 8 bits, where a pair's partials are small and a workgroup has the compute unit to itself, 48 sequences of 500-6000 36.9
-// and 34.1, 32 of 2K-8K 37.9 and 36.7, 200 of 1K-5K at 2 kv-heads 38.2 and 37.0; at d = 64 and 4 bits 64 of 2K-6K 38.7 and
-// 41.3; at d = 128 and 4 bits (8 and 4) 48 of 2K-6K 44.8 and 47.7, 200 of 500-2000 at 4 kv-heads 38.5 and 42.3.
+// 2176 bytes of K and V a page and kv-head at 4 bits, d = 128.  Each line is drawn by type, where the times of batches on
+// both sides of it say so (us a call, 8 kv-heads unless said).
+// kPieceCost, several kv-heads a workgroup, 8 and 3: d = 64 in 8 bits 48 sequences of 500-6000 tokens 35.9 and 34.0, 32 of
+//   2K-8K 37.4 and 36.0, 200 of 1K-5K at 2 kv-heads 38.0 and 36.9; but in 4 bits 64 of 2K-6K 38.7 and 41.3; d = 128 in 8 bits
+//   48 of 2K-6K 67.8 and 70.8, 32 of 2K-8K 58.8 and 64.4, 200 of 500-2000 at 4 kv-heads 53.6 and 57.6; in 4 bits, 8 and
+//   4, 48 of 2K-6K 44.8 and 47.7, 200 of 500-2000 at 4 kv-heads 38.5 and 42.3.  (Why d = 64 in 8 bits differs is not known.)
+// kWholePages, no runs of whole sequences, and with 28, 56 and 112: 4 bits, 24 of 500-1000 16.1 / 13.6 / 13.4 / 13.6, 24 of
+//   500-1200 16.1 / 16.1 / 15.7 / 15.7, 300 of 100-500 at 2 kv-heads 21.0 / 21.0 / 20.0 / 20.2, at d = 64 100 of 200-1500 at 2
+//   16.8 / 16.9 / 16.8 / 15.1; 8 bits, 24 of 500-1200 17.4 / 17.3 / 16.8 / 16.9, at d = 64 40 of 200-1200 17.3 / 17.3 / 17.1 / 19.0.
+// kSeqCost, 0, 4 and 8: shares of 70 pages of 512 sequences (64-1024 tokens) took 2.2 us a unit and 2.0 a sequence more, so
+//   those with 5 or 6 sequences ended last: 65.8 / 62.9 / 63.5; 900 of 1-400 57.9 / 53.2 / 53.2, 64 of 2K-16K 109.5 / 108.0 /
+//   106.9; at d = 64 700 of 64-1024 59.2 / 58.0 / 59.6, in 8 bits 900 of 64-512 61.0 / 56.1 / 57.3; d = 128 in 8 bits 512 of
+//   64-1024 105.0 / 106.3 / 108.5.
 template <int D, int kBits, int kPages> struct MxCut {
   static constexpr int kPieceCost = D == 64 && kBits == 8 ? 3 : 8, kWholePages = 56, kSeqCost = kMxSeqCost, kUnit = kPages;
 };

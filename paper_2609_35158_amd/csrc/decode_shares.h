@@ -140,7 +140,7 @@ __device__ __forceinline__ bool all_within(DecPlanLds& P, int B, int most, int l
 }
 
 // How a kernel's list of pages is cut: runs of at least kMinPages pages, or, where a wave takes units of
-// kUnit > 1 pages, of whole units a wave; several kv-heads share a
+// kUnit > 1 pages, of as many pages as some number of units for each of its waves; several kv-heads share a
 // workgroup if kPieceCost times the pieces of the longest sequence are at most the pages of a wave's
 // share (DecShares); runs hold whole sequences if that makes none longer than an equal run by more than
 // kWholePages (DecRun); where a workgroup holds 8 kv-heads, so that shares are runs and equal ones all there is, a
@@ -191,9 +191,10 @@ template <class Cut> struct DecShares {
     } else {
       heads = 1;
       if constexpr (Cut::kUnit > 1) {
-        // Every wave takes so many whole units: one, and more where the longest sequence's merge would cost more than the
-        // units it saves (a run more in it costs about as much as a third of a page in every wave).  us a call with runs of
-        // 32 pages and 1/64 of a sequence, as of bf16 pools, and so: one sequence at 8 kv-heads, 4 bits, 1500 tokens 14.6 and
+        // Every wave takes at most so many units: one, and more where the longest sequence's merge would cost more than the
+        // units it saves (a run more in it costs about as much as a third of a page in every wave).  The shares are cut
+        // evenly, so they need not be whole units: 2731 tokens in 4 bits are 48 shares of 3 or 4 pages.  us a call with runs
+        // of 32 pages and 1/64 of a sequence, as of bf16 pools, and so: one sequence at 8 kv-heads, 4 bits, 1500 tokens 14.6 and
         // 11.3, 2731 13.7 and 11.9, 10000 17.0 and 14.7, 30000 19.7 and 19.7; 8 bits 1500 16.8 and 12.1, 12000 16.5 and 17.2;
         // three of 5-20K at one kv-head 21.4 and 20.5.  With half a page for a third: 8 bits, 16000 17.9 for 17.3; with a
         // fifth: 4 bits, 16000 17.5 for 16.5.  (Beyond 64 sequences, where a wave does not hold all lengths, runs of one unit
