@@ -295,7 +295,10 @@ pearl_status pearl_attn_decode_append_mx(const pearl_kv_shape* shape, const pear
  * pearl_attn_prefill_append over a cache of MX blocks, which must already hold the new tokens (call
  * pearl_kv_append_mx first, on the same stream): every new token attends to its context and causally
  * to the new ones, all as the values that the cache stands for.  Weights enter the products in bf16.  A
- * colocated batch can take this call too: a sequence with one new token is a tile of one row.
+ * colocated batch can take this call too, where a sequence with one new token is a tile of one row.  With more than
+ * a few of those this call and pearl_attn_decode_mx one after the other take less time (4 bits, 32 query heads and 8
+ * kv-heads, contexts of 2K-8K: 8 chunks of 512 beside 192 single tokens 1189 us in one call, 578 in two; beside 4 single
+ * tokens 410 and 418).
  */
 pearl_status pearl_attn_prefill_append_mx(const pearl_kv_shape* shape, const pearl_seq_desc* seqs,
                                           pearl_mx_format format, const void* q, const void* cache,

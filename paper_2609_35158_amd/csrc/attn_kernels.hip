@@ -1123,7 +1123,7 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
   // scores jumping more than kMaxLag above m) the stage is redone with the row maximum, and m
   // moves to it only when it exceeds m by more than kMaxLag, so the O rescale is rare too.  A NaN
   // sum (a masked key against m = -inf) also takes the redo.
-  // The weights enter P.V rounded once to bf16 (their sum l is of the unrounded ones, in 32 bits): 2^-9 of each at most, so
+  // The weights enter P.V rounded once to bf16 (their sum l is of the unrounded ones, in 32 bits): 2^-8 of each at most, so
   // the outputs' error is 0.0023 of them in the 2-norm where their own rounding to bf16 alone is 0.0017.  The rest in a
   // second product, as in decode, costs 27-37%: over MX blocks a turn of 64-400 tokens on 4K-24K contexts takes 459 us
   // so and 618 with it, 512-2048 tokens on 4K-16K 1250 and 1710, prompts of 500-3000 at d = 64 in 8 bits 131 and 166.

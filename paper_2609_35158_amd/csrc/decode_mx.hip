@@ -19,7 +19,7 @@
 //     the odd channels.  (Sorted by channel first, with a byte permute per two tokens, the conversion of V
 //     took 192 instructions a unit instead of 128.)
 // Weights enter P.V in two bf16 parts, the nearest bf16 and the rest, in a product each: 16 bits of a weight.  One
-// part alone is 2-6% faster (64 sequences of 2K-16K tokens 122.4 us, with both 125.9) but off by up to 2^-9 a
+// part alone is 2-6% faster (64 sequences of 2K-16K tokens 122.4 us, with both 125.9) but off by up to 2^-8 a
 // weight, as much as rounding the outputs to bf16 is.
 // The other channel of a pair meets a weight of 0 in each column half, and 0 times an infinity or NaN is NaN.  So every
 // unit is tested for scales and codes that stand for such elements of V; where there are any, they are counted in a

@@ -90,7 +90,7 @@ def test_kv_heads_per_workgroup(n):
         assert partials not in {_partials(ctx, min(max(1, _grid(fmt, d) // -(-hkv // h)), _slot_runs(ctx, hkv, bound)), 8 // h,
                                           4 if h == 8 else 0) for h in (2, 4, 8)}
     # The weights' 16 bits (2^-16 of each) and the sums in 32 bits disappear beside the rounding of the outputs to bf16,
-    # whose errors are spread over +-2^-9 of a value: together in squares less than 1.01 of it.
+    # whose errors are spread over +-2^-8 of a value: together in squares less than 1.01 of it.
     zero = torch.zeros(1, dtype=torch.int32, device="cuda")
     err = least = 0.0
     for b in sorted({0, 1, batch // 2, batch - 2, batch - 1} | {int(x) for x in rng.integers(0, batch, size=4)}):
