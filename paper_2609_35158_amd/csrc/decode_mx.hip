@@ -34,7 +34,6 @@
 
 #include <algorithm>
 #include <atomic>
-#include <mutex>
 
 namespace pearl {
 
