@@ -1354,7 +1354,8 @@ __device__ __forceinline__ void prefill_tile_pp(const AttnArgs& a, int b, int co
         const float o = oacc[mb][r];                // (a bit cast of the element itself takes element 0)
         most = max(most, __builtin_bit_cast(uint32_t, o) & 0x7fffffffu);
       }
-    if (__ballot(most >= 0x7f800000u)) odd->again = 1;
+    // (rows past the tile's last token attend slots that no token owns, whose bytes may be anything)
+    if (__ballot(row_ok && most >= 0x7f800000u)) odd->again = 1;
     __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   }
   at_end();

@@ -56,9 +56,8 @@ template <int k> __device__ __forceinline__ float mx_scale_of(uint32_t w) {
   return __builtin_bit_cast(float, k < 3 ? w << (23 - 8 * k) : w >> 1);
 }
 
-// Whether an element under one of a word's four scales can be infinite or NaN because of the scale (a bit per byte):
-// finite ones are the largest under 252 at 4 bits (6 * 2^125) and 246 at 8 (448 * 2^119).  From 240 on at 8 bits, which
-// takes fewer instructions: what asks only does more work then.
+// Whether one of a word's four scales may make elements infinite or NaN (a bit per byte).  All are finite up to scales of
+// 252 at 4 bits (6 * 2^125) and 246 at 8 (448 * 2^119); some scales below are taken along, for fewer instructions.
 template <int kBits> __device__ __forceinline__ uint32_t mx_large_scale(uint32_t w) {
   if constexpr (kBits == 4) return ((w >> 2 & 0x3f3f3f3fu) + 0x01010101u) & 0x40404040u;   // 252 and more
   else return ((w >> 4 & 0x0f0f0f0fu) + 0x01010101u) & 0x10101010u;                        // 240 and more
