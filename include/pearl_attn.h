@@ -246,8 +246,9 @@ pearl_status pearl_kv_unpack(const pearl_kv_shape* shape, const pearl_seq_desc* 
  *     K scales [slot % 4][nb][slot / 4], V scales [nb][slot].
  *   Any bytes are valid contents of slots that no attended position owns.
  *   An infinite or NaN element of V makes its own channel infinite or NaN in the outputs of the rows that attend its
- *   token, and reaches nothing else (no row before it in a prefill, no other channel).  Weights times values are summed in
- *   32 bits: values above 2^95 can overflow there.
+ *   token, and reaches nothing else (no row before it in a prefill, no other channel); one of K makes the scores with its
+ *   token infinite or NaN, and of those minus infinity is a weight of 0.  Weights times values are summed in 32 bits:
+ *   values above 2^95 can overflow there.
  */
 typedef enum { PEARL_MXFP4 = 4, PEARL_MXFP8 = 8 } pearl_mx_format;
 
