@@ -307,10 +307,56 @@ pearl_status pearl_attn_prefill_append_mx(const pearl_kv_shape* shape, const pea
                                           size_t workspace_bytes, void* stream);
 
 /*
+ * Rotary position embedding of new query and key rows (a token's position is its place in its sequence's
+ * context; paper, Background: the context grows by each turn's tokens), with the RMS norm of each head
+ * that comes before it in models that have one.  The attention calls take rows that are rotated already.
+ *   Channel pair n = 0 .. rotary_dim / 2 - 1 of a head x of a token at position p = ctx_lens[b] + i:
+ *     a = p * inv_freq[n];  y_i = factor * (x_i cos a - x_j sin a);  y_j = factor * (x_j cos a + x_i sin a),
+ *   (i, j) = (n, n + rotary_dim / 2), or (2n, 2n + 1) if `interleaved`; channels from rotary_dim on stay.  With a
+ *   weight w the rotation's input is x_c * w_c / sqrt(mean over the head of x^2 + eps) instead of x.  Computed in 32 bits, the angle in
+ *   64, and rounded once; channels that are neither rotated nor normalised are copied.
+ */
+typedef struct {
+  const float* inv_freq; /* DEVICE fp32 [rotary_dim / 2]: radians a position */
+  int32_t rotary_dim;    /* channels rotated, the first ones: a multiple of 16, 16 .. head_dim */
+  int32_t interleaved;   /* 0 or 1 */
+  float factor;          /* of cosines and sines (1: a plain rotation); finite */
+  float eps;             /* of the norms; finite, >= 0 */
+  const void* q_weight;  /* DEVICE bf16 [head_dim], 16-byte aligned: queries are normalised; NULL: not */
+  const void* k_weight;  /* the same for keys */
+} pearl_rope;
+
+/*
+ * Rotates a batch's q and k rows into row buffers, for the calls that append keys themselves or take them
+ * in MX blocks (pearl_attn_decode_append, _decode_append_mx, pearl_kv_append_mx).
+ *   q: bf16 [total_q][num_q_heads][head_dim], k_new: bf16 [total_q][num_kv_heads][head_dim] (read): a token's rows
+ *      contiguous, q_stride / k_stride elements from a token to the next one (multiples of 8, at least a token's
+ *      rows), so that they can be parts of a fused projection's output;
+ *   q_out, k_out: the same, contiguous (written); they may be q and k_new where those are contiguous, and must
+ *      not overlap any input otherwise.
+ * Rows of no sequence (behind cu_q_lens[batch]) and of sequences with a negative ctx_lens[b] are left as they were.
+ * seqs->block_table, bt_stride and max_kv_len are not used.
+ */
+pearl_status pearl_rope_rows(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, const pearl_rope* rope, const void* q,
+                             int64_t q_stride, const void* k_new, int64_t k_stride, void* q_out, void* k_out, void* stream);
+
+/*
+ * pearl_kv_append with the rotation on the way: q into q_out as above, the rotated k_new and v_new into their slots of
+ * the pools, in one launch.  The results are those of pearl_rope_rows followed by pearl_kv_append, bit for
+ * bit.  No other byte of the pools changes; K/V rows whose page id is outside [0, num_pages) or whose logical page is beyond
+ * bt_stride are skipped (their q row is written all the same).
+ *   v_new, v_stride: as k_new and k_stride.
+ */
+pearl_status pearl_kv_append_rope(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, const pearl_rope* rope,
+                                  const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new,
+                                  int64_t v_stride, void* q_out, void* k_pool, void* v_pool, void* stream);
+
+/*
  * Timing hook for benchmarks and profilers (not part of the computation).  While a pair is set,
  * every library call made on the calling thread records `before` on its stream immediately
  * before launching its main kernel (the attention kernel for the three attention calls, the
- * page-copy kernel for pearl_kv_append, pearl_kv_pack, pearl_kv_unpack and their _mx forms) and `after`
+ * page-copy kernel for pearl_kv_append, pearl_kv_pack, pearl_kv_unpack and their _mx forms, the one kernel of
+ * pearl_rope_rows, pearl_kv_append_rope and pearl_latent_append) and `after`
  * immediately after it.  (A decode over MX blocks of more than 1024 sequences has a main kernel for each group of
  * them: `before` the first, `after` the last.)  The handles are
  * hipEvent_t values created and owned by the caller; pass NULL, NULL to clear.  The pair stays

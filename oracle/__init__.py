@@ -7,3 +7,4 @@ from .paged_attention import (  # noqa: F401
 from .mx_cache import (  # noqa: F401
     mx_append, mx_block_bytes, mx_element_values, mx_pack, mx_pools, mx_quantise, mx_values,
 )
+from .rotary import norm_rows, positions, rope_rows, rotate  # noqa: F401

@@ -41,13 +41,24 @@ class SeqDesc(ctypes.Structure):
                 ("max_q_len", ctypes.c_int32), ("max_kv_len", ctypes.c_int32)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("factor", ctypes.c_float), ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p)]
+
+
+class LatentShape(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("latent_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
 EXPORTED = ("pearl_abi_version", "pearl_status_str", "pearl_last_error", "pearl_kv_append",
             "pearl_attn_workspace_bytes", "pearl_attn_prefill_append", "pearl_attn_decode",
             "pearl_attn_mixed", "pearl_kv_pack", "pearl_kv_unpack", "pearl_set_kernel_events",
             "pearl_hbm_copy", "pearl_hbm_read", "pearl_hbm_read_nt", "pearl_hbm_fill", "pearl_attn_decode_static",
             "pearl_attn_decode_static_max_bytes", "pearl_attn_decode_append", "pearl_mx_block_bytes",
             "pearl_kv_append_mx", "pearl_kv_pack_mx", "pearl_attn_decode_mx", "pearl_attn_decode_append_mx",
-            "pearl_attn_prefill_append_mx")
+            "pearl_attn_prefill_append_mx", "pearl_rope_rows", "pearl_kv_append_rope", "pearl_latent_append")
 
 
 def load(path: str = LIB_PATH):
@@ -111,6 +122,13 @@ def load(path: str = LIB_PATH):
                                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_float,
                                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
                                                 ctypes.c_void_p]
+    R, I64, V = P(RopeDesc), ctypes.c_int64, ctypes.c_void_p
+    lib.pearl_rope_rows.restype = ctypes.c_int
+    lib.pearl_rope_rows.argtypes = [P(KvShape), P(SeqDesc), R, V, I64, V, I64, V, V, V]
+    lib.pearl_kv_append_rope.restype = ctypes.c_int
+    lib.pearl_kv_append_rope.argtypes = [P(KvShape), P(SeqDesc), R, V, I64, V, I64, V, I64, V, V, V, V]
+    lib.pearl_latent_append.restype = ctypes.c_int
+    lib.pearl_latent_append.argtypes = [P(LatentShape), P(SeqDesc), R, V, I64, V, I64, V, V, V]
     lib.pearl_set_kernel_events.restype = None
     lib.pearl_set_kernel_events.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
     # measurement tooling (include/pearl_bench.h)
@@ -558,6 +576,191 @@ def prefill_append_mx(q, cache, block_table, ctx_lens, cu_q_lens, max_q_len, max
     (pearl_attn_prefill_append_mx)."""
     return _attention_mx("pearl_attn_prefill_append_mx", q, (), cache, block_table, ctx_lens, cu_q_lens, max_q_len,
                          max_kv_len, scale, return_lse, out, lse, workspace)
+
+
+# ------------------------------------------------------------------------------------------------
+# Rotary position embedding
+# ------------------------------------------------------------------------------------------------
+
+class Rope:
+    """The rotation of a layer's queries and keys (pearl_rope): inv_freq fp32 [rotary_dim / 2] radians a position; pairs of
+    channels (n, n + rotary_dim / 2), or (2n, 2n + 1) if interleaved; cosines and sines times `factor`; q_weight and k_weight
+    bf16 [head_dim], or None, of the RMS norm that comes before (latent_append: k_weight [latent_dim], q_weight None).  Keeps its tensors; build it once a layer."""
+
+    def __init__(self, inv_freq: torch.Tensor, interleaved: bool = False, factor: float = 1.0,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        _need(inv_freq, "inv_freq", torch.float32)
+        if inv_freq.dim() != 1:
+            raise ValueError("inv_freq must be [rotary_dim / 2]")
+        for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None:
+                _need(t, n, torch.bfloat16)
+                if t.dim() != 1 or t.get_device() != inv_freq.get_device():
+                    raise ValueError("%s must be one row on inv_freq's device" % n)
+        self.inv_freq, self.q_weight, self.k_weight = inv_freq, q_weight, k_weight
+        self.dev = inv_freq.get_device()
+        self.desc = RopeDesc(inv_freq.data_ptr(), 2 * inv_freq.shape[0], int(bool(interleaved)), float(factor), float(eps),
+                             _ptr(q_weight), _ptr(k_weight))
+        self.ref = ctypes.byref(self.desc)
+
+    def weights(self, q: Optional[int], k: int) -> None:
+        """That the norms' weights are of so many channels (q None: queries have none)."""
+        if self.q_weight is not None and self.q_weight.shape[0] != q:
+            raise ValueError("q_weight has %d channels, %s" % (self.q_weight.shape[0], "the call takes none" if q is None else "a head %d" % q))
+        if self.k_weight is not None and self.k_weight.shape[0] != k:
+            raise ValueError("k_weight has %d channels, not %d" % (self.k_weight.shape[0], k))
+
+
+def _on(dev: int):
+    """What checks a call's tensors: type, contiguity, and that they are on the current device, where the library launches."""
+    if dev != _current_device():
+        raise ValueError("tensors are on cuda:%d, the current device is cuda:%d" % (dev, _current_device()))
+
+    def need(t: torch.Tensor, name: str, dtype: torch.dtype) -> None:
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()):
+            _need(t, name, dtype)
+            raise ValueError("%s must be on cuda:%d, got %s" % (name, dev, t.device))
+    return need
+
+
+def _rows(t: torch.Tensor, name: str, dev: int, shape: Tuple[Optional[int], ...]) -> int:
+    """The elements from a token to the next one of bf16 rows [tokens][heads][channels], of which a token's are contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.get_device() != dev:
+        _need(t, name, torch.bfloat16)
+        raise ValueError("%s must be on cuda:%d, got %s" % (name, dev, t.device))
+    size = t.shape
+    if len(size) != 3 or any(w is not None and w != n for w, n in zip(shape, size)):
+        raise ValueError("%s must be [%s]" % (name, "][".join("any" if w is None else str(w) for w in shape)))
+    stride = t.stride()
+    if (size[2] > 1 and stride[2] != 1) or (size[1] > 1 and stride[1] != size[2]):
+        raise ValueError("a token's rows of %s must be contiguous" % name)
+    return stride[0] if size[0] > 1 else size[1] * size[2]
+
+
+def rope_rows(q: torch.Tensor, k_new: torch.Tensor, rope: Rope, ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor],
+              max_q_len: int, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Queries [total_q][H_q][d] and keys [total_q][H_kv][d] normalised and rotated at positions ctx_lens[b] + i
+    (pearl_rope_rows); both may be parts of wider rows.  q_out / k_out: contiguous, allocated if not given, q and k_new
+    themselves where those are contiguous.  Returns (q_out, k_out)."""
+    need = _on(rope.dev)
+    q_stride = _rows(q, "q", rope.dev, (None, None, None))
+    total, H_q, d = q.shape
+    k_stride = _rows(k_new, "k_new", rope.dev, (total, None, d))
+    H_kv = k_new.shape[1]
+    rope.weights(d, d)
+    outs = []
+    for t, x, n in ((q_out, q, "q_out"), (k_out, k_new, "k_out")):
+        if t is None:
+            t = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+        need(t, n, torch.bfloat16)
+        if t.shape != x.shape:
+            raise ValueError("%s must have shape %s" % (n, tuple(x.shape)))
+        outs.append(t)
+    desc = _lens_desc(ctx_lens, cu_q_lens, total, max_q_len, need)
+    shape = KvShape(H_q, H_kv, d, PAGE_SIZE, 1)
+    st = load().pearl_rope_rows(ctypes.byref(shape), ctypes.byref(desc), rope.ref, q.data_ptr(), q_stride, k_new.data_ptr(),
+                                k_stride, outs[0].data_ptr(), outs[1].data_ptr(), _stream())
+    _check(st, "pearl_rope_rows")
+    return outs[0], outs[1]
+
+
+def _lens_desc(ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor], total_q: int, max_q_len: int, need) -> SeqDesc:
+    """A batch of which no page is read or written."""
+    need(ctx_lens, "ctx_lens", torch.int32)
+    batch = int(ctx_lens.shape[0])
+    if cu_q_lens is not None:
+        need(cu_q_lens, "cu_q_lens", torch.int32)
+        if cu_q_lens.shape[0] != batch + 1:
+            raise ValueError("cu_q_lens must have batch+1 entries")
+    return SeqDesc(None, 0, ctx_lens.data_ptr(), _ptr(cu_q_lens), batch, int(total_q), int(max_q_len), 0)
+
+
+def kv_append_rope(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, rope: Rope, k_pool: torch.Tensor,
+                   v_pool: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                   cu_q_lens: Optional[torch.Tensor], max_q_len: int, max_kv_len: int,
+                   q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """rope_rows with k_new (rotated) and v_new going into the pools (pearl_kv_append_rope); returns q_out."""
+    need = _on(rope.dev)
+    for t, n in ((k_pool, "k_pool"), (v_pool, "v_pool")):
+        need(t, n, torch.bfloat16)
+    shape = make_shape(q.shape[1] if q.dim() == 3 else 0, k_pool)
+    if v_pool.shape != k_pool.shape:
+        raise ValueError("k_pool and v_pool must have one shape")
+    H_kv, d = k_pool.shape[1], k_pool.shape[3]
+    q_stride = _rows(q, "q", rope.dev, (None, None, d))
+    total = q.shape[0]
+    k_stride = _rows(k_new, "k_new", rope.dev, (total, H_kv, d))
+    v_stride = _rows(v_new, "v_new", rope.dev, (total, H_kv, d))
+    rope.weights(d, d)
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    need(q_out, "q_out", torch.bfloat16)
+    if q_out.shape != q.shape:
+        raise ValueError("q_out must have shape %s" % (tuple(q.shape),))
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, need)
+    st = load().pearl_kv_append_rope(ctypes.byref(shape), ctypes.byref(desc), rope.ref, q.data_ptr(), q_stride,
+                                     k_new.data_ptr(), k_stride, v_new.data_ptr(), v_stride, q_out.data_ptr(),
+                                     k_pool.data_ptr(), v_pool.data_ptr(), _stream())
+    _check(st, "pearl_kv_append_rope")
+    return q_out
+
+
+# ------------------------------------------------------------------------------------------------
+# Attention over a paged cache of latent vectors
+# ------------------------------------------------------------------------------------------------
+
+_LATENT_DIMS = {576: (512, 64), 288: (256, 32)}     # row width -> (latent_dim, rope_dim)
+
+
+def latent_cache(num_pages: int, latent_dim: int, rope_dim: int, device="cuda") -> torch.Tensor:
+    """A cache of latent rows, zeroed: bf16 [num_pages][16][latent_dim + rope_dim], (512, 64) or (256, 32).  Both dims follow from
+    the row's width, so the calls below take the cache alone."""
+    if _LATENT_DIMS.get(latent_dim + rope_dim) != (latent_dim, rope_dim):
+        raise ValueError("(latent_dim, rope_dim) must be (512, 64) or (256, 32)")
+    return torch.zeros((num_pages, PAGE_SIZE, latent_dim + rope_dim), dtype=torch.bfloat16, device=device)
+
+
+def _latent_shape(num_q_heads: int, cache: torch.Tensor) -> LatentShape:
+    if cache.dim() != 3 or cache.shape[1] != PAGE_SIZE or cache.shape[2] not in _LATENT_DIMS:
+        raise ValueError("cache must be [num_pages][16][latent_dim + rope_dim], (512, 64) or (256, 32)")
+    dc, dr = _LATENT_DIMS[cache.shape[2]]
+    return LatentShape(num_q_heads, dc, dr, PAGE_SIZE, cache.shape[0])
+
+
+def latent_append(q_rope: torch.Tensor, rows_new: torch.Tensor, rope: Rope, q: torch.Tensor, cache: torch.Tensor,
+                  block_table: torch.Tensor, ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor], max_q_len: int,
+                  max_kv_len: int) -> None:
+    """New latent rows [total_q][latent_dim + rope_dim] into the cache, the latent part normalised (rope.k_weight), the
+    rest rotated; q_rope [total_q][H][rope_dim], rotated, into the last channels of the absorbed queries q
+    [total_q][H][latent_dim + rope_dim] (pearl_latent_append).  rows_new may be a part of wider rows, q_rope of wider heads."""
+    need = _on(rope.dev)
+    need(cache, "cache", torch.bfloat16)
+    need(q, "q", torch.bfloat16)
+    if q.dim() != 3:
+        raise ValueError("q must be [total_q][num_q_heads][latent_dim + rope_dim]")
+    total, H, width = q.shape
+    shape = _latent_shape(H, cache)
+    if width != cache.shape[2]:
+        raise ValueError("q has %d channels, the cache %d" % (width, cache.shape[2]))
+    if rows_new.dim() != 2:
+        raise ValueError("rows_new must be [total_q][latent_dim + rope_dim]")
+    rows_stride = _rows(rows_new[:, None], "rows_new", rope.dev, (total, 1, width))
+    if q_rope.dim() != 3 or tuple(q_rope.shape) != (total, H, shape.rope_dim):
+        raise ValueError("q_rope must be [%d][%d][%d]" % (total, H, shape.rope_dim))
+    by_token, by_head, _ = q_rope.stride()
+    if H == 1:
+        by_head = by_token
+    elif total > 1 and by_token != H * by_head:
+        raise ValueError("q_rope's heads must be evenly spaced, a token's last to the next one's first alike")
+    if total * H <= 1:
+        by_head = shape.rope_dim
+    _rows(q_rope.as_strided((total * H, 1, shape.rope_dim), (by_head, shape.rope_dim, q_rope.stride(2))), "q_rope", rope.dev,
+          (total * H, 1, shape.rope_dim))
+    rope.weights(None, shape.latent_dim)
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, need)
+    st = load().pearl_latent_append(ctypes.byref(shape), ctypes.byref(desc), rope.ref, q_rope.data_ptr(), by_head,
+                                    rows_new.data_ptr(), rows_stride, q.data_ptr(), cache.data_ptr(), _stream())
+    _check(st, "pearl_latent_append")
 
 
 # ------------------------------------------------------------------------------------------------

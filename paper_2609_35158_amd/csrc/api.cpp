@@ -3,6 +3,7 @@
 // include/pearl_attn.h.
 
 #include "../../include/pearl_attn.h"
+#include "../../include/pearl_latent.h"
 #include "pearl_internal.h"
 
 #include <hip/hip_runtime.h>
@@ -67,12 +68,13 @@ pearl_status check_shape(const pearl_kv_shape* s) {
   return PEARL_OK;
 }
 
-pearl_status check_seqs(const pearl_seq_desc* q, bool need_q_lens) {
+// need_table: the call reads or writes pages.
+pearl_status check_seqs(const pearl_seq_desc* q, bool need_q_lens, bool need_table = true) {
   if (!q) return fail(PEARL_ERR_INVALID_ARG, "seqs is NULL");
   if (q->batch <= 0) return fail(PEARL_ERR_INVALID_ARG, "batch (%d) must be > 0", q->batch);
-  if (!q->block_table) return fail(PEARL_ERR_INVALID_ARG, "block_table is NULL");
+  if (need_table && !q->block_table) return fail(PEARL_ERR_INVALID_ARG, "block_table is NULL");
   if (!q->ctx_lens) return fail(PEARL_ERR_INVALID_ARG, "ctx_lens is NULL");
-  if (q->bt_stride <= 0) return fail(PEARL_ERR_INVALID_ARG, "bt_stride (%d) must be > 0", q->bt_stride);
+  if (need_table && q->bt_stride <= 0) return fail(PEARL_ERR_INVALID_ARG, "bt_stride (%d) must be > 0", q->bt_stride);
   if (q->total_q < 0 || q->max_q_len < 0 || q->max_kv_len < 0)
     return fail(PEARL_ERR_INVALID_ARG, "total_q, max_q_len and max_kv_len must be >= 0");
   if (need_q_lens && !q->cu_q_lens) return fail(PEARL_ERR_INVALID_ARG, "cu_q_lens is NULL");
@@ -82,6 +84,7 @@ pearl_status check_seqs(const pearl_seq_desc* q, bool need_q_lens) {
     if (q->max_q_len < 1) return fail(PEARL_ERR_INVALID_ARG, "max_q_len (%d) < 1 with one token per sequence", q->max_q_len);
   }
   if (q->max_q_len > q->total_q) return fail(PEARL_ERR_INVALID_ARG, "max_q_len (%d) > total_q (%d)", q->max_q_len, q->total_q);
+  if (!need_table) return PEARL_OK;
   if (q->max_q_len > q->max_kv_len && q->total_q > 0)
     return fail(PEARL_ERR_INVALID_ARG, "max_q_len (%d) > max_kv_len (%d)", q->max_q_len, q->max_kv_len);
   if ((int64_t)q->bt_stride * kPage < q->max_kv_len)
@@ -96,6 +99,85 @@ pearl_status check_seqs(const pearl_seq_desc* q, bool need_q_lens) {
 pearl_status check_format(pearl_mx_format f) {
   if (f != PEARL_MXFP4 && f != PEARL_MXFP8)
     return fail(PEARL_ERR_UNSUPPORTED, "cache format %d is neither PEARL_MXFP4 nor PEARL_MXFP8", (int)f);
+  return PEARL_OK;
+}
+
+// max_dim: channels of a head (or, for latent rows, of the rotated part).
+pearl_status check_rope(const pearl_rope* r, int max_dim) {
+  if (!r) return fail(PEARL_ERR_INVALID_ARG, "rope is NULL");
+  if (!r->inv_freq) return fail(PEARL_ERR_INVALID_ARG, "inv_freq is NULL");
+  if ((reinterpret_cast<uintptr_t>(r->inv_freq) & 3) != 0) return fail(PEARL_ERR_INVALID_ARG, "inv_freq must be 4-byte aligned");
+  if (r->rotary_dim < 16 || r->rotary_dim > max_dim || r->rotary_dim % 16 != 0)
+    return fail(PEARL_ERR_UNSUPPORTED, "rotary_dim %d is not a multiple of 16 in 16 .. %d", r->rotary_dim, max_dim);
+  if (r->interleaved != 0 && r->interleaved != 1) return fail(PEARL_ERR_INVALID_ARG, "interleaved (%d) must be 0 or 1", r->interleaved);
+  if (!std::isfinite(r->factor)) return fail(PEARL_ERR_INVALID_ARG, "factor must be finite");
+  if (!std::isfinite(r->eps) || r->eps < 0.f) return fail(PEARL_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (!aligned16(r->q_weight) || !aligned16(r->k_weight))
+    return fail(PEARL_ERR_INVALID_ARG, "q_weight and k_weight must be 16-byte aligned");
+  return PEARL_OK;
+}
+
+// Elements from a row to the next one, of rows of `least` elements.
+pearl_status check_stride(const char* name, int64_t stride, int64_t least, int64_t rows) {
+  if (stride < least || stride % 8 != 0)
+    return fail(PEARL_ERR_INVALID_ARG, "%s (%lld) must be a multiple of 8 and >= %lld", name, (long long)stride, (long long)least);
+  if (rows > 0 && stride > INT64_MAX / 4 / rows) return fail(PEARL_ERR_INVALID_ARG, "%s (%lld) too large", name, (long long)stride);
+  return PEARL_OK;
+}
+
+RopeArgs rope_args(const pearl_rope* r) {
+  return RopeArgs{r->inv_freq, static_cast<const uint16_t*>(r->q_weight), static_cast<const uint16_t*>(r->k_weight), r->rotary_dim,
+                  r->interleaved, r->factor, r->eps};
+}
+
+RopeSeqs rope_seqs(const pearl_seq_desc* q, int num_pages) {
+  return RopeSeqs{q->block_table, q->ctx_lens, q->cu_q_lens, q->bt_stride, num_pages, q->batch, q->total_q};
+}
+
+// Rotation into row buffers, or (v_new given) into the pools.
+pearl_status run_rope(const pearl_kv_shape* s, const pearl_seq_desc* q, const pearl_rope* rope, const void* qp, int64_t q_stride,
+                      const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out, void* k_out,
+                      void* v_out, bool to_pool, void* stream) {
+  pearl_status st = check_shape(s);
+  if (st != PEARL_OK) return st;
+  st = check_seqs(q, false, to_pool);
+  if (st != PEARL_OK) return st;
+  st = check_rope(rope, s->head_dim);
+  if (st != PEARL_OK) return st;
+  const int64_t q_row = (int64_t)s->num_q_heads * s->head_dim, k_row = (int64_t)s->num_kv_heads * s->head_dim;
+  st = check_stride("q_stride", q_stride, q_row, q->total_q);
+  if (st == PEARL_OK) st = check_stride("k_stride", k_stride, k_row, q->total_q);
+  if (st == PEARL_OK && to_pool) st = check_stride("v_stride", v_stride, k_row, q->total_q);
+  if (st != PEARL_OK) return st;
+  if (q->total_q == 0) return PEARL_OK;
+  if (!qp || !k_new || !q_out || !k_out || (to_pool && (!v_new || !v_out)))
+    return fail(PEARL_ERR_INVALID_ARG, to_pool ? "q, k_new, v_new, q_out, k_pool and v_pool must be non-NULL"
+                                               : "q, k_new, q_out and k_out must be non-NULL");
+  if (!aligned16(qp) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(v_out))
+    return fail(PEARL_ERR_INVALID_ARG, "rows and pools must be 16-byte aligned");
+  if ((q_out == qp && q_stride != q_row) || (!to_pool && k_out == k_new && k_stride != k_row))
+    return fail(PEARL_ERR_INVALID_ARG, "rows are rotated in place only where they are contiguous");
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const RopeRows rows = {static_cast<const uint16_t*>(qp), static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new),
+                         static_cast<uint16_t*>(q_out), static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out),
+                         q_stride, k_stride, v_stride, s->num_q_heads, s->num_kv_heads};
+  hipError_t e = record_before(hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+  e = launch_rope(rope_args(rope), rope_seqs(q, s->num_pages), rows, s->head_dim, to_pool, hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "rope launch: %s", hipGetErrorString(e));
+  e = record_after(hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+  return PEARL_OK;
+}
+
+pearl_status check_latent_shape(const pearl_latent_shape* s) {
+  if (!s) return fail(PEARL_ERR_INVALID_ARG, "shape is NULL");
+  if (s->num_q_heads <= 0) return fail(PEARL_ERR_INVALID_ARG, "num_q_heads (%d) must be > 0", s->num_q_heads);
+  if (s->num_q_heads > kLatentMaxHeads) return fail(PEARL_ERR_UNSUPPORTED, "num_q_heads %d > %d", s->num_q_heads, kLatentMaxHeads);
+  if (!(s->latent_dim == 512 && s->rope_dim == 64) && !(s->latent_dim == 256 && s->rope_dim == 32))
+    return fail(PEARL_ERR_UNSUPPORTED, "latent_dim %d with rope_dim %d: neither 512 with 64 nor 256 with 32", s->latent_dim, s->rope_dim);
+  if (s->page_size != kPage) return fail(PEARL_ERR_UNSUPPORTED, "page_size %d != 16", s->page_size);
+  if (s->num_pages <= 0) return fail(PEARL_ERR_INVALID_ARG, "num_pages (%d) must be > 0", s->num_pages);
   return PEARL_OK;
 }
 
@@ -655,6 +737,64 @@ pearl_status pearl_attn_decode_append_mx(const pearl_kv_shape* shape, const pear
                          workspace_bytes, stream);
   } catch (...) {
     return fail(PEARL_ERR_HIP, "unexpected exception in pearl_attn_decode_append_mx");
+  }
+}
+
+pearl_status pearl_rope_rows(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, const pearl_rope* rope, const void* q,
+                             int64_t q_stride, const void* k_new, int64_t k_stride, void* q_out, void* k_out, void* stream) {
+  try {
+    g_err[0] = 0;
+    return run_rope(shape, seqs, rope, q, q_stride, k_new, k_stride, nullptr, 0, q_out, k_out, nullptr, false, stream);
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_rope_rows");
+  }
+}
+
+pearl_status pearl_kv_append_rope(const pearl_kv_shape* shape, const pearl_seq_desc* seqs, const pearl_rope* rope, const void* q,
+                                  int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                                  void* q_out, void* k_pool, void* v_pool, void* stream) {
+  try {
+    g_err[0] = 0;
+    return run_rope(shape, seqs, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, k_pool, v_pool, true, stream);
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_kv_append_rope");
+  }
+}
+
+pearl_status pearl_latent_append(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const pearl_rope* rope,
+                                 const void* q_rope, int64_t q_rope_stride, const void* rows_new, int64_t rows_stride, void* q,
+                                 void* cache, void* stream) {
+  try {
+    g_err[0] = 0;
+    pearl_status st = check_latent_shape(shape);
+    if (st != PEARL_OK) return st;
+    st = check_seqs(seqs, false);
+    if (st != PEARL_OK) return st;
+    st = check_rope(rope, shape->rope_dim);
+    if (st != PEARL_OK) return st;
+    if (rope->rotary_dim != shape->rope_dim)
+      return fail(PEARL_ERR_INVALID_ARG, "rotary_dim (%d) != rope_dim (%d)", rope->rotary_dim, shape->rope_dim);
+    if (rope->q_weight) return fail(PEARL_ERR_INVALID_ARG, "q_weight must be NULL");
+    st = check_stride("q_rope_stride", q_rope_stride, shape->rope_dim, (int64_t)seqs->total_q * shape->num_q_heads);
+    if (st == PEARL_OK) st = check_stride("rows_stride", rows_stride, shape->latent_dim + shape->rope_dim, seqs->total_q);
+    if (st != PEARL_OK) return st;
+    if (seqs->total_q == 0) return PEARL_OK;
+    if (!q_rope || !rows_new || !q || !cache)
+      return fail(PEARL_ERR_INVALID_ARG, "q_rope, rows_new, q and cache must be non-NULL");
+    if (!aligned16(q_rope) || !aligned16(rows_new) || !aligned16(q) || !aligned16(cache))
+      return fail(PEARL_ERR_INVALID_ARG, "q_rope, rows_new, q and cache must be 16-byte aligned");
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    const LatentRows rows = {static_cast<const uint16_t*>(q_rope), static_cast<const uint16_t*>(rows_new), static_cast<uint16_t*>(q),
+                             static_cast<uint16_t*>(cache), q_rope_stride, rows_stride, shape->num_q_heads};
+    hipError_t e = record_before(hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+    e = launch_latent_append(rope_args(rope), rope_seqs(seqs, shape->num_pages), rows, shape->latent_dim, shape->rope_dim, hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "latent_append launch: %s", hipGetErrorString(e));
+    e = record_after(hs);
+    if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+    return PEARL_OK;
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_latent_append");
   }
 }
 

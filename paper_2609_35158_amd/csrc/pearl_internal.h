@@ -1,5 +1,5 @@
 // Internal interface between the C-ABI host layer (api.cpp) and the gfx950 kernels
-// (attn_kernels.hip, decode_mx.hip, kv_pages.hip, kv_mx.hip).  Not installed; callers use include/pearl_attn.h.
+// (attn_kernels.hip, decode_mx.hip, kv_pages.hip, kv_mx.hip, rope.hip).  Not installed; callers use include/pearl_attn.h.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -50,6 +50,9 @@ constexpr int kDecPlanMaxSeqs = 1024;
 constexpr int kMxSeqCost = 4;
 // With more kv-heads than resident workgroups, runs for about this many rounds of them.
 constexpr int kDecRounds = 4;
+
+// Query heads of an attention call over a cache of latent vectors, at most.
+constexpr int kLatentMaxHeads = 128;
 
 enum Mode : int { kModePrefill = 0, kModeDecode = 1, kModeMixed = 2 };
 
@@ -198,6 +201,39 @@ hipError_t launch_kv_pack_mx(int bits, const uint8_t* cache, uint16_t* k_rows, u
                              const int32_t* block_table, int bt_stride, const int32_t* ctx_lens,
                              const int32_t* cu_q_lens, int batch, int max_q_len, int num_kv_heads, int head_dim,
                              int num_pages, int total_q, hipStream_t stream);
+
+// Rotary position embedding (rope.hip).
+struct RopeArgs {
+  const float* inv_freq;
+  const uint16_t* q_weight;  // RMS norm weights, or null: none
+  const uint16_t* k_weight;
+  int rotary_dim;
+  int next;                  // pairs (2n, 2n + 1); 0: (n, n + rotary_dim / 2)
+  float factor, eps;
+};
+struct RopeSeqs {
+  const int32_t* block_table;
+  const int32_t* ctx_lens;
+  const int32_t* cu;         // may be null: one token a sequence
+  int bt_stride, num_pages, batch, total_q;
+};
+// Strides are elements from one token's rows to the next one's.
+struct RopeRows {
+  const uint16_t *q, *k, *v;
+  uint16_t *q_out, *k_out, *v_out;  // k_out and v_out: the pools, or k_out the row buffer
+  int64_t q_stride, k_stride, v_stride;
+  int num_q_heads, num_kv_heads;
+};
+struct LatentRows {
+  const uint16_t *q_rope, *rows;
+  uint16_t *q, *cache;
+  int64_t q_rope_stride;     // from one head's row to the next one's
+  int64_t rows_stride;
+  int num_q_heads;
+};
+hipError_t launch_rope(const RopeArgs& r, const RopeSeqs& seqs, const RopeRows& rows, int head_dim, bool to_pool, hipStream_t stream);
+hipError_t launch_latent_append(const RopeArgs& r, const RopeSeqs& seqs, const LatentRows& rows, int latent_dim, int rope_dim,
+                                hipStream_t stream);
 
 hipError_t launch_plan(const PlanParams& p, const int32_t* ctx_lens, const int32_t* cu_q_lens,
                        void* workspace, const WsLayout& lay, hipStream_t stream);
