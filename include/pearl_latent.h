@@ -52,6 +52,32 @@ pearl_status pearl_latent_append(const pearl_latent_shape* shape, const pearl_se
                                  const void* q_rope, int64_t q_rope_stride, const void* rows_new, int64_t rows_stride,
                                  void* q, void* cache, void* stream);
 
+/*
+ * Bytes of device workspace that an attention call below needs for (shape, seqs): the list of tiles that are cut along the
+ * keys, and their partial results (fp32), 512 of at most 64 rows: up to 67 MB.  A function of the shape and the host
+ * bounds only; needs no initialisation.  0 if the arguments are invalid (pearl_last_error() says why).
+ */
+size_t pearl_latent_workspace_bytes(const pearl_latent_shape* shape, const pearl_seq_desc* seqs);
+
+/*
+ * Batched single-token decode: seqs->cu_q_lens must be NULL; row b of q and out is sequence b's new token at position
+ * ctx_lens[b], whose row the cache already holds (pearl_latent_append first, on the same stream).
+ * Contexts are cut into shares that run in parallel and are joined by log-sum-exp.  Weights enter the second product in bf16.
+ */
+pearl_status pearl_attn_latent_decode(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const void* q,
+                                      const void* cache, float softmax_scale, void* out, float* lse, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/*
+ * Prefill-append: every new token of every sequence attends to its context and causally to the new ones, whose rows the
+ * cache already holds.  Sequences without new tokens are skipped; rows behind the last sequence are left as they
+ * were.  A batch of single tokens, or of a few each (drafted tokens that are verified), can take this call too.
+ * A row of the cache with an infinite or NaN channel makes outputs infinite or NaN in the tokens that attend to it only.
+ */
+pearl_status pearl_attn_latent_prefill_append(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const void* q,
+                                              const void* cache, float softmax_scale, void* out, float* lse, void* workspace,
+                                              size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,3 +8,4 @@ from .mx_cache import (  # noqa: F401
     mx_append, mx_block_bytes, mx_element_values, mx_pack, mx_pools, mx_quantise, mx_values,
 )
 from .rotary import norm_rows, positions, rope_rows, rotate  # noqa: F401
+from .latent import latent_attention, latent_rows  # noqa: F401

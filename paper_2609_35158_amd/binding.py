@@ -58,7 +58,8 @@ EXPORTED = ("pearl_abi_version", "pearl_status_str", "pearl_last_error", "pearl_
             "pearl_hbm_copy", "pearl_hbm_read", "pearl_hbm_read_nt", "pearl_hbm_fill", "pearl_attn_decode_static",
             "pearl_attn_decode_static_max_bytes", "pearl_attn_decode_append", "pearl_mx_block_bytes",
             "pearl_kv_append_mx", "pearl_kv_pack_mx", "pearl_attn_decode_mx", "pearl_attn_decode_append_mx",
-            "pearl_attn_prefill_append_mx", "pearl_rope_rows", "pearl_kv_append_rope", "pearl_latent_append")
+            "pearl_attn_prefill_append_mx", "pearl_rope_rows", "pearl_kv_append_rope", "pearl_latent_append",
+            "pearl_latent_workspace_bytes", "pearl_attn_latent_decode", "pearl_attn_latent_prefill_append")
 
 
 def load(path: str = LIB_PATH):
@@ -129,6 +130,12 @@ def load(path: str = LIB_PATH):
     lib.pearl_kv_append_rope.argtypes = [P(KvShape), P(SeqDesc), R, V, I64, V, I64, V, I64, V, V, V, V]
     lib.pearl_latent_append.restype = ctypes.c_int
     lib.pearl_latent_append.argtypes = [P(LatentShape), P(SeqDesc), R, V, I64, V, I64, V, V, V]
+    lib.pearl_latent_workspace_bytes.restype = ctypes.c_size_t
+    lib.pearl_latent_workspace_bytes.argtypes = [P(LatentShape), P(SeqDesc)]
+    for name in ("pearl_attn_latent_decode", "pearl_attn_latent_prefill_append"):
+        f = getattr(lib, name)
+        f.restype = ctypes.c_int
+        f.argtypes = [P(LatentShape), P(SeqDesc), V, V, ctypes.c_float, V, V, V, ctypes.c_size_t, V]
     lib.pearl_set_kernel_events.restype = None
     lib.pearl_set_kernel_events.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
     # measurement tooling (include/pearl_bench.h)
@@ -761,6 +768,66 @@ def latent_append(q_rope: torch.Tensor, rows_new: torch.Tensor, rope: Rope, q: t
     st = load().pearl_latent_append(ctypes.byref(shape), ctypes.byref(desc), rope.ref, q_rope.data_ptr(), by_head,
                                     rows_new.data_ptr(), rows_stride, q.data_ptr(), cache.data_ptr(), _stream())
     _check(st, "pearl_latent_append")
+
+
+def workspace_bytes_latent(num_q_heads: int, cache: torch.Tensor, desc: SeqDesc) -> int:
+    """Bytes of workspace that the attention calls over this cache need (pearl_latent_workspace_bytes)."""
+    shape = _latent_shape(int(num_q_heads), cache)
+    n = load().pearl_latent_workspace_bytes(ctypes.byref(shape), ctypes.byref(desc))
+    if n == 0:
+        raise PearlError(1, "pearl_latent_workspace_bytes", last_error())
+    return int(n)
+
+
+def _attention_latent(fname: str, q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                      cu_q_lens: Optional[torch.Tensor], max_q_len: int, max_kv_len: int, scale: float, return_lse: bool,
+                      out: Optional[torch.Tensor], lse: Optional[torch.Tensor], workspace: Optional[torch.Tensor]):
+    _need(cache, "cache", torch.bfloat16)
+    need = _on(cache.get_device())
+    need(q, "q", torch.bfloat16)
+    if q.dim() != 3:
+        raise ValueError("q must be [total_q][num_q_heads][latent_dim + rope_dim]")
+    total, H, width = q.shape
+    shape = _latent_shape(H, cache)
+    if width != cache.shape[2]:
+        raise ValueError("q has %d channels, the cache %d" % (width, cache.shape[2]))
+    desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, need)
+    want = (total, H, shape.latent_dim)
+    if out is None:
+        out = torch.empty(want, dtype=torch.bfloat16, device=q.device)
+    else:
+        need(out, "out", torch.bfloat16)
+        if out.shape != want:
+            raise ValueError("out must have shape %s" % (want,))
+    if lse is not None:
+        need(lse, "lse", torch.float32)
+        if lse.shape != (total, H):
+            raise ValueError("lse must be [total_q][num_q_heads]")
+    elif return_lse:
+        lse = torch.empty((total, H), dtype=torch.float32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(workspace_bytes_latent(H, cache, desc), dtype=torch.uint8, device=q.device)
+    else:
+        need(workspace, "workspace", torch.uint8)    # the library checks its size
+    st = getattr(load(), fname)(ctypes.byref(shape), ctypes.byref(desc), q.data_ptr(), cache.data_ptr(), float(scale),
+                                out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, fname)
+    return (out, lse) if lse is not None else out
+
+
+def latent_decode(q, cache, block_table, ctx_lens, max_kv_len, scale, return_lse=False, out=None, lse=None, workspace=None):
+    """Single-token decode over a cache of latent rows (pearl_attn_latent_decode): q [batch][H][latent_dim + rope_dim] absorbed
+    queries, out [batch][H][latent_dim].  `scale` has no default: it goes by the head's width before absorption."""
+    return _attention_latent("pearl_attn_latent_decode", q, cache, block_table, ctx_lens, None, 1, max_kv_len, scale, return_lse,
+                             out, lse, workspace)
+
+
+def latent_prefill_append(q, cache, block_table, ctx_lens, cu_q_lens, max_q_len, max_kv_len, scale, return_lse=False, out=None,
+                          lse=None, workspace=None):
+    """Causal prefill-append attention over a cache of latent rows that holds the new tokens
+    (pearl_attn_latent_prefill_append)."""
+    return _attention_latent("pearl_attn_latent_prefill_append", q, cache, block_table, ctx_lens, cu_q_lens, max_q_len,
+                             max_kv_len, scale, return_lse, out, lse, workspace)
 
 
 # ------------------------------------------------------------------------------------------------

@@ -181,6 +181,95 @@ pearl_status check_latent_shape(const pearl_latent_shape* s) {
   return PEARL_OK;
 }
 
+// With PEARL_DEBUG=1: waits for the call and reports what its kernels refused.
+pearl_status debug_check(const char* hdr, hipStream_t hs) {
+  if (!debug_mode()) return PEARL_OK;
+  hipError_t e = hipStreamSynchronize(hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "PEARL_DEBUG sync: %s", hipGetErrorString(e));
+  int32_t flag = 0;
+  e = hipMemcpy(&flag, hdr + 4 * kHdrError, sizeof(flag), hipMemcpyDeviceToHost);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "PEARL_DEBUG readback: %s", hipGetErrorString(e));
+  if (flag == 1) return fail(PEARL_ERR_INVALID_ARG, "device lengths violate the host bounds (total_q/max_q_len/max_kv_len/bt_stride) or decode q_len != 1; nothing was computed");
+  if (flag != 0) return fail(PEARL_ERR_INVALID_ARG, "work list exceeded its capacity; nothing was computed");
+  return PEARL_OK;
+}
+
+// How an attention call over latent vectors is cut, and its workspace.
+struct LatentPlan {
+  int tile, group;
+  size_t jobs, part_o, part_ml, total;
+};
+
+LatentPlan latent_plan(const pearl_latent_shape* s, const pearl_seq_desc* q) {
+  LatentPlan p;
+  // rows (token, head) of a workgroup: no more than a sequence has, 64 at most
+  const int64_t rows = (int64_t)q->max_q_len * s->num_q_heads;
+  p.tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  // workgroups that read the same keys together: as many as a sequence has tiles, on average, 4 at most
+  const int64_t tiles = cdiv((int64_t)q->total_q * s->num_q_heads, (int64_t)q->batch * p.tile);
+  p.group = tiles >= 8 ? 4 : tiles >= 2 ? 2 : 1;
+  size_t off = align256(sizeof(int32_t) * kHdrWords);
+  p.jobs = off; off = align256(off + sizeof(int4) * kLatentGrid);
+  p.part_o = off; off = align256(off + sizeof(float) * 2 * kLatentGrid * (size_t)p.tile * s->latent_dim);
+  p.part_ml = off; off = align256(off + sizeof(float) * 4 * kLatentGrid * (size_t)p.tile);
+  p.total = off;
+  return p;
+}
+
+pearl_status run_latent(bool decode, const pearl_latent_shape* s, const pearl_seq_desc* q, const void* qp, const void* cache,
+                        float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  pearl_status st = check_latent_shape(s);
+  if (st != PEARL_OK) return st;
+  st = check_seqs(q, false);
+  if (st != PEARL_OK) return st;
+  if (decode && q->cu_q_lens) return fail(PEARL_ERR_INVALID_ARG, "decode requires cu_q_lens == NULL (one token per sequence)");
+  if (!qp || !cache || !out) return fail(PEARL_ERR_INVALID_ARG, "q, cache and out must be non-NULL");
+  if (!ws) return fail(PEARL_ERR_WORKSPACE, "workspace is NULL");
+  if (!aligned16(qp) || !aligned16(cache) || !aligned16(out))
+    return fail(PEARL_ERR_INVALID_ARG, "q, cache and out must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) return fail(PEARL_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (lse && (reinterpret_cast<uintptr_t>(lse) & 3) != 0) return fail(PEARL_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(PEARL_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+  if ((int64_t)q->total_q * s->num_q_heads > INT32_MAX)
+    return fail(PEARL_ERR_UNSUPPORTED, "total_q (%d) x num_q_heads (%d) exceeds int32", q->total_q, s->num_q_heads);
+  const LatentPlan p = latent_plan(s, q);
+  if (ws_bytes < p.total) return fail(PEARL_ERR_WORKSPACE, "workspace_bytes %zu < required %zu", ws_bytes, p.total);
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  char* const w = static_cast<char*>(ws);
+  LatentArgs a = {};
+  a.q = static_cast<const uint16_t*>(qp);
+  a.cache = static_cast<const uint16_t*>(cache);
+  a.block_table = q->block_table;
+  a.ctx_lens = q->ctx_lens;
+  a.cu = q->cu_q_lens;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.ws_hdr = reinterpret_cast<int32_t*>(w);
+  a.jobs = reinterpret_cast<int4*>(w + p.jobs);
+  a.part_o = reinterpret_cast<float*>(w + p.part_o);
+  a.part_ml = reinterpret_cast<float*>(w + p.part_ml);
+  a.bt_stride = q->bt_stride;
+  a.num_pages = s->num_pages;
+  a.batch = q->batch;
+  a.total_q = q->total_q;
+  a.max_q_len = q->max_q_len;
+  a.max_kv_len = q->max_kv_len;
+  a.heads = s->num_q_heads;
+  a.group = p.group;
+  a.slope = 128 * p.group * p.tile / s->num_q_heads;
+  a.min_share = p.tile == 16 ? 128 : p.tile == 32 ? 192 : 256;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  hipError_t e = record_before(hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+  e = launch_latent(a, s->latent_dim, p.tile, false, hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "attention launch: %s", hipGetErrorString(e));
+  e = record_after(hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
+  e = launch_latent(a, s->latent_dim, p.tile, true, hs);
+  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "merge launch: %s", hipGetErrorString(e));
+  return debug_check(w, hs);
+}
+
 // The pointers and sizes of an attention call over a cache of MX blocks.
 pearl_status check_mx_pointers(const pearl_kv_shape* s, const pearl_seq_desc* q, const void* qp, const void* cache,
                                const void* out, const float* lse, float scale, const void* ws) {
@@ -259,19 +348,6 @@ AttnArgs attn_args(const pearl_kv_shape* s, const pearl_seq_desc* q, const Plan&
   a.tokens_per_tile = pl.p.tokens_per_tile;
   a.scale_log2 = scale * 1.4426950408889634f;
   return a;
-}
-
-// With PEARL_DEBUG=1: waits for the call and reports what its kernels refused.
-pearl_status debug_check(const char* w, const Plan& pl, hipStream_t hs) {
-  if (!debug_mode()) return PEARL_OK;
-  hipError_t e = hipStreamSynchronize(hs);
-  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "PEARL_DEBUG sync: %s", hipGetErrorString(e));
-  int32_t flag = 0;
-  e = hipMemcpy(&flag, w + pl.lay.hdr + 4 * kHdrError, sizeof(flag), hipMemcpyDeviceToHost);
-  if (e != hipSuccess) return fail(PEARL_ERR_HIP, "PEARL_DEBUG readback: %s", hipGetErrorString(e));
-  if (flag == 1) return fail(PEARL_ERR_INVALID_ARG, "device lengths violate the host bounds (total_q/max_q_len/max_kv_len/bt_stride) or decode q_len != 1; nothing was computed");
-  if (flag != 0) return fail(PEARL_ERR_INVALID_ARG, "work list exceeded its capacity; nothing was computed");
-  return PEARL_OK;
 }
 
 // static_ws: use the library's static per-device workspace (pearl_attn_decode_static) instead of
@@ -374,7 +450,7 @@ pearl_status run_attention(int mode, const pearl_kv_shape* s, const pearl_seq_de
     e = launch_merge_prefill(a, s->head_dim, pl.p.pre_jobs_cap, hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "prefill merge launch: %s", hipGetErrorString(e));
   }
-  return debug_check(w, pl, hs);
+  return debug_check(w + pl.lay.hdr, hs);
 }
 
 // Decode (k_new / v_new: with its append) over a cache of MX blocks, in groups of up to kDecPlanMaxSeqs
@@ -438,7 +514,7 @@ pearl_status run_decode_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pea
     if (b0 + d.batch == q->batch) e = record_after(hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
   }
-  return debug_check(static_cast<const char*>(ws), pl, hs);
+  return debug_check(static_cast<const char*>(ws) + pl.lay.hdr, hs);
 }
 
 pearl_status run_prefill_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pearl_mx_format format, const void* qp,
@@ -474,7 +550,7 @@ pearl_status run_prefill_mx(const pearl_kv_shape* s, const pearl_seq_desc* q, pe
     e = launch_merge_prefill(a, s->head_dim, pl.p.pre_jobs_cap, hs);
     if (e != hipSuccess) return fail(PEARL_ERR_HIP, "prefill merge launch: %s", hipGetErrorString(e));
   }
-  return debug_check(static_cast<const char*>(ws), pl, hs);
+  return debug_check(static_cast<const char*>(ws) + pl.lay.hdr, hs);
 }
 
 }  // namespace
@@ -795,6 +871,40 @@ pearl_status pearl_latent_append(const pearl_latent_shape* shape, const pearl_se
     return PEARL_OK;
   } catch (...) {
     return fail(PEARL_ERR_HIP, "unexpected exception in pearl_latent_append");
+  }
+}
+
+size_t pearl_latent_workspace_bytes(const pearl_latent_shape* shape, const pearl_seq_desc* seqs) {
+  try {
+    g_err[0] = 0;
+    if (check_latent_shape(shape) != PEARL_OK) return 0;
+    if (check_seqs(seqs, false) != PEARL_OK) return 0;
+    return latent_plan(shape, seqs).total;
+  } catch (...) {
+    set_err("unexpected exception in pearl_latent_workspace_bytes");
+    return 0;
+  }
+}
+
+pearl_status pearl_attn_latent_decode(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const void* q,
+                                      const void* cache, float softmax_scale, void* out, float* lse, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+  try {
+    g_err[0] = 0;
+    return run_latent(true, shape, seqs, q, cache, softmax_scale, out, lse, workspace, workspace_bytes, stream);
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_attn_latent_decode");
+  }
+}
+
+pearl_status pearl_attn_latent_prefill_append(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const void* q,
+                                              const void* cache, float softmax_scale, void* out, float* lse, void* workspace,
+                                              size_t workspace_bytes, void* stream) {
+  try {
+    g_err[0] = 0;
+    return run_latent(false, shape, seqs, q, cache, softmax_scale, out, lse, workspace, workspace_bytes, stream);
+  } catch (...) {
+    return fail(PEARL_ERR_HIP, "unexpected exception in pearl_attn_latent_prefill_append");
   }
 }
 

@@ -1,5 +1,5 @@
 // Internal interface between the C-ABI host layer (api.cpp) and the gfx950 kernels
-// (attn_kernels.hip, decode_mx.hip, kv_pages.hip, kv_mx.hip, rope.hip).  Not installed; callers use include/pearl_attn.h.
+// (attn_kernels.hip, decode_mx.hip, kv_pages.hip, kv_mx.hip, rope.hip, latent.hip).  Not installed; callers use include/pearl_attn.h.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -53,6 +53,8 @@ constexpr int kDecRounds = 4;
 
 // Query heads of an attention call over a cache of latent vectors, at most.
 constexpr int kLatentMaxHeads = 128;
+// Workgroups of such a call: one a compute unit (a fixed number, which sizes the workspace).
+constexpr int kLatentGrid = kPlanComputeUnits;
 
 enum Mode : int { kModePrefill = 0, kModeDecode = 1, kModeMixed = 2 };
 
@@ -234,6 +236,29 @@ struct LatentRows {
 hipError_t launch_rope(const RopeArgs& r, const RopeSeqs& seqs, const RopeRows& rows, int head_dim, bool to_pool, hipStream_t stream);
 hipError_t launch_latent_append(const RopeArgs& r, const RopeSeqs& seqs, const LatentRows& rows, int latent_dim, int rope_dim,
                                 hipStream_t stream);
+
+// Attention over a cache of latent vectors (latent.hip).
+struct LatentArgs {
+  const uint16_t* q;
+  const uint16_t* cache;
+  const int32_t* block_table;
+  const int32_t* ctx_lens;
+  const int32_t* cu;         // may be null: one token a sequence
+  uint16_t* out;
+  float* lse;                // may be null
+  int32_t* ws_hdr;
+  int4* jobs;                // [kLatentGrid]: cut tiles to be joined
+  float* part_o;             // [2 kLatentGrid][tile][latent_dim] unnormalised partial outputs
+  float* part_ml;            // [2 kLatentGrid][tile][2] running max (log2 units) and sum
+  int bt_stride, num_pages, batch, total_q, max_q_len, max_kv_len;
+  int heads;
+  int group;                 // workgroups that take neighbouring tiles of one share
+  int slope;                 // 128 group * tile / heads
+  int min_share;             // keys of a share, at least
+  float scale_log2;
+};
+// merge: the join of cut tiles, launched after the attention itself.
+hipError_t launch_latent(const LatentArgs& a, int latent_dim, int tile, bool merge, hipStream_t stream);
 
 hipError_t launch_plan(const PlanParams& p, const int32_t* ctx_lens, const int32_t* cu_q_lens,
                        void* workspace, const WsLayout& lay, hipStream_t stream);
