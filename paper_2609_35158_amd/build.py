@@ -7,6 +7,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -16,7 +18,7 @@ SOURCES = ["attn_kernels.hip", "decode_mx.hip", "kv_pages.hip", "kv_mx.hip", "ro
            "api.cpp", "pd_engine.cpp"]
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # never form packed-fp32 VALU instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # single-lane atomics stay plain: the atomic optimizer's wave reduction waits for the returned
@@ -33,10 +35,12 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
-def build(verbose: bool = False) -> str:
-    tmp = LIB + ".tmp"
-    cmd = [hipcc()] + HIPCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-o", tmp] + \
-          [os.path.join(CSRC, s) for s in SOURCES]
+# Of one source: the outputs of its matrix instructions stay in vector registers, where its rare stages scale them, and
+# the accumulation registers hold operands (latent.hip).
+SOURCE_FLAGS = {"latent.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+
+
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -45,6 +49,18 @@ def build(verbose: bool = False) -> str:
         raise RuntimeError("hipcc failed (%d):\n%s" % (res.returncode, out))
     if verbose and out.strip():
         print(out)
+
+
+def build(verbose: bool = False) -> str:
+    tmp = LIB + ".tmp"
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(max_workers=4) as pool:
+        names = [os.path.join(objects, s + ".o") for s in SOURCES]
+        jobs = [pool.submit(_run, [hipcc()] + HIPCC_FLAGS + SOURCE_FLAGS.get(s, []) +
+                            ["-I", os.path.join(ROOT, "include"), "-c", "-o", o, os.path.join(CSRC, s)], verbose)
+                for s, o in zip(SOURCES, names)]
+        for j in jobs:
+            j.result()
+        _run([hipcc()] + HIPCC_FLAGS + ["-shared", "-o", tmp] + names, verbose)
     os.replace(tmp, LIB)
     return LIB
 

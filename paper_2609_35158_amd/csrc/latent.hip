@@ -33,6 +33,8 @@ constexpr int kLatWaves = kLatThreads / 64;
 constexpr int kLatKeys = kLatWaves * kPage;         // of a stage
 constexpr float kLag = 8.f;
 
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
 __device__ __forceinline__ void barrier_lds() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void wait_copies() { __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -45,6 +47,17 @@ __device__ __forceinline__ float xor16_add(float x) {
   const unsigned u = __builtin_bit_cast(unsigned, x);
   const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
   return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+
+// Keep a value in vector or in accumulation registers at this place.  The outputs stay in vector registers, which the rare stages that
+// scale them need, and the queries in accumulation registers, from which the products read them; left to itself the compiler moves
+// the outputs between the two in every stage.
+__device__ __forceinline__ void in_vector(f32x4& x) { __asm__ volatile("" : "+v"(x)); }
+__device__ __forceinline__ void in_acc(bf16x8& x) { __asm__ volatile("" : "+a"(x)); }
+
+__device__ __forceinline__ long long uni64(long long x) {
+  const unsigned lo = uni((int)x), hi = uni((int)(x >> 32));
+  return (long long)((unsigned long long)hi << 32 | lo);
 }
 
 // A staged page: 16 rows of DC channels, then 16 rows of DR.  Chunk (16 bytes) c of latent row r is in slot c ^ f(r) of
@@ -66,9 +79,10 @@ template <int DC, int DR> struct LatCopies {
   using Page = LatPage<DC, DR>;
   static constexpr int kRows = 1024 / Page::kRowBytes;       // of an instruction
   static constexpr int kLatent = kPage / kRows, kRot = kPage * Page::kRotBytes / 1024;
-  int lane16;                                       // 16 times the slot, swizzled by the lane's part of the row
-  int row;                                          // byte offset of the lane's row of an instruction's
-  int rot[kRot];
+  static_assert(Page::kWidth % 32 == 0 && (DR == 32 || Page::kWidth % 128 == 0), "the swizzle takes bits above the rows' alignment");
+  // 16 times the lane's slot, swizzled by its part of the row, and the offset of its row among an instruction's; the same of the
+  // rotated parts' first instruction.
+  int lane16, row, rot;
 
   __device__ __forceinline__ LatCopies() {
     const int l = threadIdx.x & 63;
@@ -79,25 +93,25 @@ template <int DC, int DR> struct LatCopies {
       row = (l >> 5) * Page::kWidth;
     }
     constexpr int kChunks = Page::kRotBytes / 16;
-#pragma unroll
-    for (int i = 0; i < kRot; ++i) {
-      const int r = (64 * i + l) / kChunks, slot = l % kChunks;
-      rot[i] = r * Page::kWidth + Page::kRowBytes + 16 * (slot ^ Page::rot_f(r));
-    }
+    const int r = l / kChunks, slot = l % kChunks;
+    rot = r * Page::kWidth + Page::kRowBytes + 16 * (slot ^ Page::rot_f(r));
   }
 
   // The page at src to LDS.  An instruction's immediate offset advances both addresses, 1 KiB each.
   __device__ __forceinline__ void copy(const char* src, const char* lds) const {
+    int lane_off = lane16, rot_off = rot;
+    __asm__ volatile("" : "+v"(lane_off), "+v"(rot_off));   // formed here each time: kept over the stages, the offsets would be spilled
 #pragma unroll
     for (int i = 0; i < kLatent; i += 4) {
       int off[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        off[k] = (lane16 ^ (Page::f(kRows * (i + k)) << 4)) + row + k * (kRows * Page::kWidth - 1024);
+        off[k] = (lane_off ^ (Page::f(kRows * (i + k)) << 4)) + row + k * (kRows * Page::kWidth - 1024);
       copy4(src + i * kRows * Page::kWidth, off, lds + 1024 * i);
     }
+    // 8 rows further (DR = 64) the swizzle differs in chunk bit 2
 #pragma unroll
-    for (int i = 0; i < kRot; ++i) copy1(src, rot[i], lds + Page::kRot + 1024 * i);
+    for (int i = 0; i < kRot; ++i) copy1(src + i * 8 * Page::kWidth, rot_off ^ (64 * i), lds + Page::kRot + 1024 * i);
   }
 
   __device__ static __forceinline__ unsigned lds_address(const char* p) {
@@ -171,6 +185,21 @@ struct LatPlan {
   }
 };
 
+// `total` cut into `shares`, which differ by 1 at most.
+struct LatShares {
+  long long each;
+  int more, shares;                                 // the first `more` are one longer
+  __device__ __forceinline__ LatShares(long long total, int n) : each(total / n), more((int)(total - each * n)), shares(n) {}
+  __device__ __forceinline__ long long start(int s) const { return each * s + min(s, more); }
+  // the share that position `at` is in
+  __device__ __forceinline__ int of(long long at) const {
+    int s = min((int)((float)at / (float)each), shares - 1);   // off by 1 at most
+    while (s > 0 && start(s) > at) --s;
+    while (s + 1 < shares && start(s + 1) <= at) ++s;
+    return s;
+  }
+};
+
 __device__ __forceinline__ LatSeq lat_seq(const LatentArgs& a, int b) {
   if (!a.cu) return LatSeq{b, 1, a.ctx_lens[b]};
   const int start = a.cu[b];
@@ -198,11 +227,15 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
   constexpr int kSteps = DC / 32, kRotSteps = DR / 32;
   constexpr int kBlocks = DC / kLatWaves / 16;      // blocks of 16 channels of a wave
   constexpr int kStage = kLatWaves * Page::kBytes;
+  constexpr int kAhead = 3;                         // LDS reads of the products' operands, ahead of them
+  constexpr int kKeepQ = M == 64 ? (DC == 512 ? 16 : kSteps + kRotSteps) : M == 32 ? kSteps + kRotSteps : 0;   // steps whose queries are in accumulation registers
   __shared__ __attribute__((aligned(256))) char s_stage[2 * kStage];
   __shared__ __attribute__((aligned(256))) char s_p[M * kLatKeys * 2];
   __shared__ float s_max[kLatWaves][M];
+  __shared__ int s_limit[M];
   __shared__ int s_flag[2];                         // some score is far above its row's maximum; one a stage in turn
-  __shared__ int s_odd[2];                          // some value of a stage that rows see in part is not finite; likewise
+  __shared__ int s_odd[DC];                         // of each channel: the first key with a value that is not finite and ..
+  __shared__ int s_any_odd;                         // .. whether there is one, among those that only some of the tile's rows see
   __shared__ long long s_sum[kLatWaves];
   __shared__ int s_found, s_bad;
   __shared__ long long s_before;
@@ -216,7 +249,8 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
   int share = index / group;
   const int member = index - share * group;
   const LatPlan plan{a.group * M, a.slope, a.heads};
-  if (tid == 0) { s_bad = 0; s_flag[0] = s_flag[1] = s_odd[0] = s_odd[1] = 0; }
+  if (tid == 0) { s_bad = 0; s_flag[0] = s_flag[1] = s_any_odd = 0; }
+  for (int i = tid; i < DC; i += kLatThreads) s_odd[i] = INT32_MAX;
   __syncthreads();
   const int per = (a.batch + kLatThreads - 1) / kLatThreads;
   long long mine = 0;
@@ -245,22 +279,23 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
 #pragma unroll
   for (int v = 0; v < kLatWaves; ++v) {
     if (v == w) upto += total;
-    total += s_sum[v];
+    total += uni64(s_sum[v]);
   }
   int shares = (int)gridDim.x / group;
   if (total < (long long)shares * a.min_share) shares = (int)max(1ll, total / a.min_share);
-  if (s_bad || total == 0 || share >= shares) {
+  if (uni(s_bad) || total == 0 || share >= shares) {
     if (tid == 0) *job = int4{0, 0, 0, 0};
     return;
   }
-  const long long lo = total * share / shares, hi = total * (share + 1) / shares;
+  const LatShares cut(total, shares);
+  const long long lo = cut.start(share), hi = cut.start(share + 1);
   if (upto - mine <= lo && lo < upto) {
     s_found = tid;
     s_before = upto - mine;
   }
   __syncthreads();
   int b = uni(s_found) * per;
-  long long at = s_before;                          // cost before sequence b
+  long long at = uni64(s_before);                   // cost before sequence b
   LatSeq seq = lat_seq(a, b);
   for (;;) {
     const long long c = plan.before(seq, plan.tiles(seq));
@@ -273,11 +308,9 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
 
   // ---- lanes' addresses
   const LatCopies<DC, DR> copies;
-  int k_off[4], rot_off[DR / 32 > 0 ? DR / 32 : 1];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) k_off[i] = l16 * Page::kRowBytes + 16 * ((4 * i) ^ g16 ^ Page::f(l16));
-#pragma unroll
-  for (int i = 0; i < kRotSteps; ++i) rot_off[i] = Page::kRot + l16 * Page::kRotBytes + 16 * ((4 * i + g16) ^ Page::rot_f(l16));
+  // of a key's chunk g16; those of the steps after it differ in address bits 6 and 7, and by whole 256 bytes
+  const int k_off = l16 * Page::kRowBytes + 16 * (g16 ^ Page::f(l16));
+  const int rot_off = Page::kRot + l16 * Page::kRotBytes + 16 * (g16 ^ Page::rot_f(l16));
   int v_off[2];                                     // of block 0: the wave's channels start at chunk (DC / 32) w
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -301,13 +334,7 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
       const int j1 = ends ? stages : min(LatPlan::stage_at(hi - t0, all_stages), stages);
       const int slot = 2 * index + (starts ? 1 : 0);
       const size_t row0 = (size_t)seq.q_start * a.heads + r0;
-      if (starts && !ends) {
-        const int last = (int)(((t1 - 1) * shares + shares - 1) / total);   // at most one off
-        int end = last;
-        while (end > share && total * end / shares >= t1) --end;
-        while (end + 1 < shares && total * (end + 1) / shares < t1) ++end;
-        my_job = int4{(int)row0, n_rows, index, end - share + 1};
-      }
+      if (starts && !ends) my_job = int4{(int)row0, n_rows, index, cut.of(t1 - 1) - share + 1};
       if (j0 >= j1) {
         if (!(starts && ends) && tid < M) reinterpret_cast<float2*>(a.part_ml)[(size_t)slot * M + tid] = float2{-FLT_MAX, 0.f};
       } else {
@@ -324,14 +351,15 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
         int id = page_id(j0 + 1);
         // queries: 16 bytes of row l16 of each group, channels 32 step + 8 g16
         bf16x8 q[RG][kSteps + kRotSteps];
-        int limit[RG];                              // the last key of the lane's rows
+        // the last key that a row sees
+        barrier_lds();
+        if (tid < M) s_limit[tid] = seq.ctx + (r0 + min(tid, n_rows - 1)) / a.heads;
 #pragma unroll
         for (int rg = 0; rg < RG; ++rg) {
           const int r = 16 * rg + l16;
           const uint16_t* const src = a.q + (row0 + min(r, n_rows - 1)) * (size_t)(DC + DR) + 8 * g16;
 #pragma unroll
           for (int k = 0; k < kSteps + kRotSteps; ++k) q[rg][k] = as_bf16x8(ld16(src + 32 * k));
-          limit[rg] = seq.ctx + (r0 + min(r, n_rows - 1)) / a.heads;
         }
         const int first_limit = seq.ctx + r0 / a.heads;    // keys behind it are not all rows'
         const bool in_part = (r0 + n_rows - 1) / a.heads != r0 / a.heads;
@@ -344,150 +372,198 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
 #pragma unroll
           for (int d = 0; d < kBlocks; ++d) o[d][rg] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-#pragma unroll 1
-        for (int j = j0; j < j1; ++j) {
-          char* const stage = s_stage + (j & 1) * kStage;
-          char* const page = stage + w * Page::kBytes;
-          const int key0 = j * kLatKeys;
-          wait_copies();
-          const int valid = kv - key0 - kPage * w;  // rows of this wave's page
-          if (valid < kPage) {                      // the others become zeros
-            const int from = max(valid, 0);
-            for (int i = from * Page::kRowBytes + 16 * lane; i < Page::kRot; i += 1024) *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
-            for (int i = Page::kRot + from * Page::kRotBytes + 16 * lane; i < Page::kBytes; i += 1024)
-              *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
-          }
-          const bool masked = key0 + kLatKeys - 1 > first_limit;
-          const bool look = masked && in_part;
-          if (look) {
-            // a key that only some of the rows see has weight 0 in the others, and 0 times a value that is not finite is NaN
-            uint32_t bad = 0;
-            for (int i = 16 * lane; i < Page::kRot; i += 1024) {
-              const u32x4 x = *reinterpret_cast<const u32x4*>(page + i);
+        f32x4 s[RG];                                // scores of the wave's 16 keys
+        float sum[RG];
+        // Weights with the rows' maxima so far, to P; the largest exponent.
+        auto weigh = [&]() {
+          float top = -FLT_MAX;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) bad |= (uint32_t)((x[e] & 0x7f80u) == 0x7f80u) | (uint32_t)((x[e] & 0x7f800000u) == 0x7f800000u);
+          for (int rg = 0; rg < RG; ++rg) {
+            float x[4], p[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              x[r] = fmaf(s[rg][r], a.scale_log2, -m[rg]);
+              p[r] = fexp2(x[r]);
             }
-            if (__ballot(bad != 0) && lane == 0) s_odd[j & 1] = 1;
+            top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+            sum[rg] = (p[0] + p[1]) + (p[2] + p[3]);
+            *reinterpret_cast<bf16x4*>(s_p + 2048 * rg + p_write) = bf16x4{(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3]};
           }
-          barrier_lds();                            // the stage is there; the other buffer and P are free
-          if (j + 1 < j1) {
-            issue(j + 1, id);
-            if (j + 2 < j1) id = page_id(j + 2);
-          }
-          if (tid == 0) s_flag[(j + 1) & 1] = s_odd[(j + 1) & 1] = 0;
-          // scores of this wave's 16 keys
-          f32x4 s[RG];
-#pragma unroll
-          for (int rg = 0; rg < RG; ++rg) s[rg] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k < kSteps + kRotSteps; ++k) {
-            const int off = k < kSteps ? k_off[k & 3] + 256 * (k >> 2) : rot_off[k - kSteps];
-            const bf16x8 key = as_bf16x8(*reinterpret_cast<const u32x4*>(page + off));
-#pragma unroll
-            for (int rg = 0; rg < RG; ++rg) s[rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[rg][k], s[rg], 0, 0, 0);
-          }
-          if (masked) {
-            const int key = key0 + kPage * w + 4 * g16;
-#pragma unroll
-            for (int rg = 0; rg < RG; ++rg)
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (key + r > limit[rg]) s[rg][r] = -__builtin_inff();
-          }
-          // weights with the rows' maxima so far
-          float sum[RG], top = -FLT_MAX;
-          auto weigh = [&]() {
-            top = -FLT_MAX;
-#pragma unroll
-            for (int rg = 0; rg < RG; ++rg) {
-              float x[4], p[4];
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                x[r] = fmaf(s[rg][r], a.scale_log2, -m[rg]);
-                p[r] = fexp2(x[r]);
-              }
-              top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-              sum[rg] = (p[0] + p[1]) + (p[2] + p[3]);
-              typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-              *reinterpret_cast<bf16x4*>(s_p + 2048 * rg + p_write) = bf16x4{(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3]};
-            }
-          };
-          weigh();
-          if (__ballot(top > kLag) && lane == 0) s_flag[j & 1] = 1;
-          barrier_lds();
-          if (uni(s_flag[j & 1])) {
-#pragma unroll
-            for (int rg = 0; rg < RG; ++rg) {
-              float x = fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])) * a.scale_log2;
-              x = xor32_max(xor16_max(x));
-              if (g16 == 0) s_max[w][16 * rg + l16] = x;
-            }
-            barrier_lds();
-#pragma unroll
-            for (int rg = 0; rg < RG; ++rg) {
-              float x = m[rg];
-#pragma unroll
-              for (int v = 0; v < kLatWaves; ++v) x = fmaxf(x, s_max[v][16 * rg + l16]);
-              const float alpha = fexp2(m[rg] - x);
-              m[rg] = x;
-              l[rg] *= alpha;
-#pragma unroll
-              for (int d = 0; d < kBlocks; ++d) o[d][rg] *= alpha;
-            }
-            weigh();
-            barrier_lds();
-          }
+          return top;
+        };
+        auto add_values = [&](const char* stage) {
 #pragma unroll
           for (int rg = 0; rg < RG; ++rg) l[rg] += sum[rg];
-          if (look && uni(s_odd[j & 1])) {
-            // this stage's values by vector arithmetic, each to the rows that see its key
+          // value operands are read kAhead blocks ahead of their products
+          int off0 = v_off[0], off1 = v_off[1];
+          __asm__ volatile("" : "+v"(off0), "+v"(off1));
+          auto value_of = [&](int i) {
+            const char* const at = stage + i / kBlocks * 2 * Page::kBytes;
+            return concat_tr(lds_read_tr(at, off0 ^ (32 * (i % kBlocks))), lds_read_tr(at, off1 ^ (32 * (i % kBlocks))));
+          };
+          bf16x8 p[RG], value[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) value[i] = value_of(i);
+#pragma unroll
+          for (int i = 0; i < kLatKeys / 32 * kBlocks; ++i) {
+            if (i % kBlocks == 0) {
+#pragma unroll
+              for (int rg = 0; rg < RG; ++rg)
+                p[rg] = as_bf16x8(*reinterpret_cast<const u32x4*>(s_p + 2048 * rg + (p_read ^ (64 * (i / kBlocks)))));
+            }
+            const bf16x8 x = value[i % kAhead];
+#pragma unroll
+            for (int rg = 0; rg < RG; ++rg)
+              o[i % kBlocks][rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[rg], o[i % kBlocks][rg], 0, 0, 0);
+            if (i + kAhead < kLatKeys / 32 * kBlocks) value[i % kAhead] = value_of(i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        };
+        int j = j0;
+        // Stages whose scores are near the maxima so far run in the inner loop; the others, the first one among them, behind it (inside it,
+        // their scaling would have the compiler copy all outputs in every stage).
+        for (;;) {
+          bool above = false;
 #pragma unroll 1
-            for (int k = 0; k < kLatKeys; ++k) {
-              const int r = k & 15, base = (k >> 4) * Page::kBytes + r * Page::kRowBytes;
-              float p[RG];
+          for (; j < j1; ++j) {
+            if constexpr (kKeepQ > 0) {
+#pragma unroll
+              for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+                for (int k = 0; k < kKeepQ; ++k) in_acc(q[rg][k]);
+            }
+            char* const page = s_stage + (j & 1) * kStage + w * Page::kBytes;
+            const int key0 = j * kLatKeys;
+            wait_copies();
+            const int valid = kv - key0 - kPage * w;  // rows of this wave's page
+            if (valid < kPage) {                    // the others become zeros
+              const int from = max(valid, 0);
+              for (int i = from * Page::kRowBytes + 16 * lane; i < Page::kRot; i += 1024) *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+              for (int i = Page::kRot + from * Page::kRotBytes + 16 * lane; i < Page::kBytes; i += 1024)
+                *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+            }
+            barrier_lds();                          // the other buffer and P are free
+            if (j + 1 < j1) {
+              issue(j + 1, id);
+              if (j + 2 < j1) id = page_id(j + 2);
+            }
+            if (tid == 0) s_flag[(j + 1) & 1] = 0;
+#pragma unroll
+            for (int rg = 0; rg < RG; ++rg) s[rg] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // key operands are read kAhead steps ahead of their products
+            int at = k_off, at_rot = rot_off;
+            __asm__ volatile("" : "+v"(at), "+v"(at_rot));
+            auto key_of = [&](int k) {
+              const int off = k < kSteps ? (at ^ (64 * (k & 3))) + 256 * (k >> 2) : at_rot ^ (64 * (k - kSteps));
+              return as_bf16x8(*reinterpret_cast<const u32x4*>(page + off));
+            };
+            bf16x8 key[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
+#pragma unroll
+            for (int k = 0; k < kSteps + kRotSteps; ++k) {
+              const bf16x8 x = key[k % kAhead];
+#pragma unroll
+              for (int rg = 0; rg < RG; ++rg) s[rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[rg][k], s[rg], 0, 0, 0);
+              if (k + kAhead < kSteps + kRotSteps) key[k % kAhead] = key_of(k + kAhead);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            if (key0 + kLatKeys - 1 > first_limit) {
+              const int key = key0 + kPage * w + 4 * g16;
 #pragma unroll
               for (int rg = 0; rg < RG; ++rg) {
-                const uint16_t bits = *reinterpret_cast<const uint16_t*>(s_p + 2048 * rg + l16 * 128 + 16 * ((k >> 3) ^ h16) + 2 * (k & 7));
-                p[rg] = __builtin_bit_cast(float, (uint32_t)bits << 16);
+                const int limit = s_limit[16 * rg + l16];
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  if (key + r > limit) s[rg][r] = -__builtin_inff();
               }
+              // Keys that only some of the rows see have weight 0 in the others, and 0 times a value that is not finite is NaN: it becomes 0 and
+              // its channel is noted.  (The value is part of its key too: in rows that see it its score is NaN or infinite, so its
+              // channel's output is NaN there, if not the whole row, which is what the end of the tile makes of the note.)
+              if (in_part) {
+                for (int i = lane; i < kPage * DC / 8; i += 64) {
+                  const int r = i / (DC / 8), c = i % (DC / 8);
+                  u32x4 x = *reinterpret_cast<const u32x4*>(page + 16 * i);
+                  bool bad = false;
 #pragma unroll
-              for (int d = 0; d < kBlocks; ++d) {
-                const int c = DC / 32 * w + 2 * d + (g16 >> 1);
-                const u32x2 x = *reinterpret_cast<const u32x2*>(stage + base + 16 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + 8 * (g16 & 1));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float v = __builtin_bit_cast(float, e & 1 ? x[e >> 1] & 0xffff0000u : x[e >> 1] << 16);
-#pragma unroll
-                  for (int rg = 0; rg < RG; ++rg)
-                    if (key0 + k <= limit[rg]) o[d][rg][e] = fmaf(p[rg], v, o[d][rg][e]);
+                  for (int e = 0; e < 8; ++e) {
+                    const uint32_t half = e & 1 ? 0x7f800000u : 0x7f80u;
+                    if ((x[e >> 1] & half) == half) {
+                      x[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
+                      atomicMin(&s_odd[8 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + e], key0 + kPage * w + r);
+                      bad = true;
+                    }
+                  }
+                  if (bad) {
+                    *reinterpret_cast<u32x4*>(page + 16 * i) = x;
+                    s_any_odd = 1;
+                  }
                 }
               }
             }
-          } else {
-#pragma unroll
-            for (int t = 0; t < kLatKeys / 32; ++t) {
-              bf16x8 p[RG];
-#pragma unroll
-              for (int rg = 0; rg < RG; ++rg) p[rg] = as_bf16x8(*reinterpret_cast<const u32x4*>(s_p + 2048 * rg + (p_read ^ (64 * t))));
-#pragma unroll
-              for (int d = 0; d < kBlocks; ++d) {
-                const bf16x8 v = concat_tr(lds_read_tr(stage + 2 * t * Page::kBytes, v_off[0] ^ (32 * d)),
-                                           lds_read_tr(stage + 2 * t * Page::kBytes, v_off[1] ^ (32 * d)));
-#pragma unroll
-                for (int rg = 0; rg < RG; ++rg) o[d][rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[rg], o[d][rg], 0, 0, 0);
-              }
+            const float top = weigh();
+            if (__ballot(top > kLag) && lane == 0) s_flag[j & 1] = 1;
+            barrier_lds();
+            if (uni(s_flag[j & 1])) {
+              above = true;
+              break;
             }
+#pragma unroll
+            for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+              for (int d = 0; d < kBlocks; ++d) in_vector(o[d][rg]);
+            add_values(s_stage + (j & 1) * kStage);
           }
+          if (!above) break;
+          // the waves agree on new maxima and weigh the stage again
+#pragma unroll
+          for (int rg = 0; rg < RG; ++rg) {
+            float x = fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])) * a.scale_log2;
+            x = xor32_max(xor16_max(x));
+            if (g16 == 0) s_max[w][16 * rg + l16] = x;
+          }
+          barrier_lds();
+#pragma unroll
+          for (int rg = 0; rg < RG; ++rg) {
+            float x = m[rg];
+#pragma unroll
+            for (int v = 0; v < kLatWaves; ++v) x = fmaxf(x, s_max[v][16 * rg + l16]);
+            const float alpha = fexp2(m[rg] - x);
+            m[rg] = x;
+            l[rg] *= alpha;
+#pragma unroll
+            for (int d = 0; d < kBlocks; ++d) o[d][rg] *= alpha;
+          }
+          weigh();
+          barrier_lds();
+          add_values(s_stage + (j & 1) * kStage);
+          ++j;
         }
         // ---- the rows' sums over lanes and waves, then the output or the partial
         barrier_lds();
-        if (tid == 0) s_flag[0] = s_flag[1] = s_odd[0] = s_odd[1] = 0;
+        const bool odd = uni(s_any_odd) != 0;
+        if (odd) {
+#pragma unroll
+          for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int first = s_odd[DC / kLatWaves * w + 16 * d + 4 * g16 + e];
+#pragma unroll
+              for (int rg = 0; rg < RG; ++rg)
+                if (first <= s_limit[16 * rg + l16]) o[d][rg][e] = __builtin_nanf("");
+            }
+        }
+        if (tid == 0) s_flag[0] = s_flag[1] = 0;
 #pragma unroll
         for (int rg = 0; rg < RG; ++rg) {
           const float x = xor32_add(xor16_add(l[rg]));
           if (g16 == 0) s_max[w][16 * rg + l16] = x;
         }
         barrier_lds();
+        if (odd) {                                  // all have read it; the next tile's stages are behind another barrier
+          for (int i = tid; i < DC; i += kLatThreads) s_odd[i] = INT32_MAX;
+          if (tid == 0) s_any_odd = 0;
+        }
 #pragma unroll
         for (int rg = 0; rg < RG; ++rg) {
           const int r = 16 * rg + l16;
@@ -501,7 +577,6 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
               uint16_t* const dst = a.out + (row0 + r) * DC + channel;
 #pragma unroll
               for (int d = 0; d < kBlocks; ++d) {
-                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
                 const f32x4 y = o[d][rg] * inv;
                 *reinterpret_cast<bf16x4*>(dst + 16 * d) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
               }
@@ -553,7 +628,6 @@ __global__ __launch_bounds__(DC / 4) void latent_merge_kernel(LatentArgs a) {
   }
   const size_t row = (size_t)job.x + r;
   const f32x4 y = o * (1.f / l);
-  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
   *reinterpret_cast<bf16x4*>(a.out + row * DC + c) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
   if (a.lse && threadIdx.x == 0) a.lse[row] = (top + flog2(l)) * kLn2;
 }
