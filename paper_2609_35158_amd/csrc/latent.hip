@@ -7,14 +7,17 @@
 // rho % H.  The softmax is online, in base 2, with state in 32 bits; weights enter the second product in bf16.
 //
 // A workgroup of 4 waves takes M rows and stages of 64 keys (4 pages):
-//   S^T (keys x rows) = K . Q^T: wave w takes the keys of page w of the stage for all rows; Q stays in registers, so K is
-//                       read from LDS once;
+//   S^T (keys x rows) = K . Q^T: Q stays in registers.  M = 16 or 32: wave w takes the keys of page w for all rows; M = 64: 32 keys
+//                       for 32 rows, so that K is read from LDS twice, with half the registers for Q;
 //   O^T (channels x rows) += V^T . P^T: wave w takes a quarter of the channels, V^T by transposing reads of the same LDS
 //                       rows, once; P goes through LDS, 2 bytes a weight.
-// (16x16x32 MFMA: A row l%16, k 8(l/16)+e; B column l%16, k 8(l/16)+e; D column l%16, row 4(l/16)+r.)  With rows
-// dealt to waves instead, every wave would read every key: at 64 rows 4 times the LDS reads, which then bound both products.
-// A row's maximum is common to the waves.  It may lag the true one by kLag (log2 units), so most stages go on with the old one after
-// one barrier; where some score is further above, the waves exchange their maxima and weigh the stage again.
+// MFMA layouts (lane l): 16x16x32 (M = 16, 32): A row l%16, k 8(l/16)+e; B column l%16, k 8(l/16)+e; D column l%16, row
+// 4(l/16)+r.  32x32x16 (M = 64): A row l%32, k 8(l/32)+e; B column l%32, k 8(l/32)+e; D column l%32, row r%4 + 8(r/4) + 4(l/32).
+// At M = 64 a wave has its SIMD to itself, in order, and what bounds it is the number of its instructions: hence the larger
+// products, two copies a group, and operand addresses that differ in constants.
+// A row's maximum is common to the waves.  It may lag the true one by kLag (log2 units), so most stages go on with the old one; where
+// some score is further above, a wave weighs with a maximum of its own, and the waves join theirs behind the barrier that they meet at for
+// the weights anyway.
 //
 // Work is cut into equal shares of keys, in the order (sequence, tile, key), on the device from the lengths: each
 // workgroup finds its share by itself.  A tile cut by shares leaves (o~, m, l) in the workspace, joined by
@@ -25,11 +28,13 @@
 
 #include <float.h>
 
+#include <type_traits>
+
 namespace pearl {
 namespace {
 
-constexpr int kLatThreads = 256;
-constexpr int kLatWaves = kLatThreads / 64;
+constexpr int kLatWaves = 4;
+constexpr int kLatThreads = 64 * kLatWaves;
 constexpr int kLatKeys = kLatWaves * kPage;         // of a stage
 constexpr float kLag = 8.f;
 
@@ -52,8 +57,18 @@ __device__ __forceinline__ float xor16_add(float x) {
 // Keep a value in vector or in accumulation registers at this place.  The outputs stay in vector registers, which the rare stages that
 // scale them need, and the queries in accumulation registers, from which the products read them; left to itself the compiler moves
 // the outputs between the two in every stage.
-__device__ __forceinline__ void in_vector(f32x4& x) { __asm__ volatile("" : "+v"(x)); }
+template <typename T> __device__ __forceinline__ void in_vector(T& x) { __asm__ volatile("" : "+v"(x)); }
 __device__ __forceinline__ void in_acc(bf16x8& x) { __asm__ volatile("" : "+a"(x)); }
+
+// The kernel's arguments, read anew where they are used outside the stages: kept over them, they would be spilled.
+typedef const __attribute__((address_space(4))) LatentArgs* LatArgsPtr;
+__device__ __forceinline__ LatArgsPtr args_anew() {
+  LatArgsPtr p = (LatArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  __asm__ volatile("" : "+s"(p));
+  return p;
+}
+
+__device__ __forceinline__ unsigned lds_address(const char* p) { return (unsigned)(uintptr_t)((LDS_AS const char*)p); }
 
 __device__ __forceinline__ long long uni64(long long x) {
   const unsigned lo = uni((int)x), hi = uni((int)(x >> 32));
@@ -61,88 +76,452 @@ __device__ __forceinline__ long long uni64(long long x) {
 }
 
 // A staged page: 16 rows of DC channels, then 16 rows of DR.  Chunk (16 bytes) c of latent row r is in slot c ^ f(r) of
-// its 16 (the row reads of 16 lanes fall into 16 slots, and the transposing reads of 32 lanes, rows {0-3, 8-11} or {4-7,
-// 12-15} and two chunks each, into 16); of the rotated part in slot c ^ (r / 2) (DR = 64; 32: r / 4), where 2 (4)
-// rows share the banks.
-template <int DC, int DR> struct LatPage {
+// its 16, f a permutation of the rows, so that the row reads of 16 lanes fall into 16 slots.  The transposing reads of 32 lanes take two
+// chunks of each of the rows {0-3, 8-11} or {4-7, 12-15} at M = 16 and 32 (kWide false), four chunks of 4 consecutive rows at M = 64:
+// f keeps these apart likewise.  Chunks of the rotated part are in slot c ^ (r / 2) (DR = 64; 32: r / 4), where 2 (4) rows share the banks.
+template <int DC, int DR, bool kWide> struct LatPage {
   static constexpr int kWidth = (DC + DR) * 2;      // bytes of a cached row
   static constexpr int kRowBytes = DC * 2, kRotBytes = DR * 2;
   static constexpr int kRot = kPage * kRowBytes;    // offset of the rotated parts
   static constexpr int kBytes = kPage * kWidth;
   static_assert(kBytes % 256 == 0 && kRowBytes % 256 == 0, "the swizzle takes address bits 4 .. 7");
-  __device__ static __forceinline__ int f(int r) { return (r & 8) | ((r & 3) << 1) | ((r >> 2) & 1); }
-  __device__ static __forceinline__ int rot_f(int r) { return DR == 64 ? (r >> 1) & 7 : (r >> 2) & 3; }
+  __device__ static __forceinline__ constexpr int f(int r) {
+    return kWide ? ((r & 3) << 2) | ((r >> 2) & 3) : (r & 8) | ((r & 3) << 1) | ((r >> 2) & 1);
+  }
+  __device__ static __forceinline__ constexpr int rot_f(int r) { return DR == 64 ? (r >> 1) & 7 : (r >> 2) & 3; }
 };
 
-// The lanes' parts of a page's copies, 1 KiB an instruction.
-template <int DC, int DR> struct LatCopies {
-  using Page = LatPage<DC, DR>;
-  static constexpr int kRows = 1024 / Page::kRowBytes;       // of an instruction
-  static constexpr int kLatent = kPage / kRows, kRot = kPage * Page::kRotBytes / 1024;
-  static_assert(Page::kWidth % 32 == 0 && (DR == 32 || Page::kWidth % 128 == 0), "the swizzle takes bits above the rows' alignment");
-  // 16 times the lane's slot, swizzled by its part of the row, and the offset of its row among an instruction's; the same of the
-  // rotated parts' first instruction.
-  int lane16, row, rot;
+// The copies of a page by a wave, 1 KiB an instruction, kRows rows' latent parts each, and then the rotated parts.
+template <int DC, int DR, bool kWide> struct LatCopies {
+  using Page = LatPage<DC, DR, kWide>;
+  static constexpr int kRows = 1024 / Page::kRowBytes;
+  static constexpr int kLatent = kPage / kRows, kCopies = kLatent + kPage * Page::kRotBytes / 1024;
+  static_assert(kLatent % 2 == 0 && Page::kWidth % 32 == 0 && (DR == 32 || Page::kWidth % 128 == 0), "copies in pairs; the swizzle's bits");
 
-  __device__ __forceinline__ LatCopies() {
+  // The lane's source offset in the page, of copy i.
+  __device__ static __forceinline__ int offset(int i) {
     const int l = threadIdx.x & 63;
-    lane16 = 16 * l;
-    row = 0;
-    if constexpr (kRows == 2) {
-      lane16 = 16 * ((l & 31) ^ Page::f(l >> 5));
-      row = (l >> 5) * Page::kWidth;
+    if (i < kLatent) {
+      const int r = kRows * i + (kRows == 2 ? l >> 5 : 0), slot = kRows == 2 ? l & 31 : l;
+      return r * Page::kWidth + 16 * (slot ^ Page::f(r));
     }
     constexpr int kChunks = Page::kRotBytes / 16;
-    const int r = l / kChunks, slot = l % kChunks;
-    rot = r * Page::kWidth + Page::kRowBytes + 16 * (slot ^ Page::rot_f(r));
+    const int r = (64 * (i - kLatent) + l) / kChunks;
+    return r * Page::kWidth + Page::kRowBytes + 16 * ((l % kChunks) ^ Page::rot_f(r));
   }
 
-  // The page at src to LDS.  An instruction's immediate offset advances both addresses, 1 KiB each.
-  __device__ __forceinline__ void copy(const char* src, const char* lds) const {
-    int lane_off = lane16, rot_off = rot;
-    __asm__ volatile("" : "+v"(lane_off), "+v"(rot_off));   // formed here each time: kept over the stages, the offsets would be spilled
+  // Copies i and (if there is one) i + 1 of the page at src to the page at the LDS address lds, if `go`.  The branch is the
+  // instructions' own: one that the compiler sees splits the products' code in two, with moves of all outputs between them.  An
+  // instruction's immediate offset advances both addresses.  (i is a constant where this is inlined.)
+  __device__ static __forceinline__ void copy2(int i, const char* src, unsigned lds, int go) {
+    const unsigned to = uni((int)lds + 1024 * i);
+    if (i + 1 < kCopies)
+      __asm__ volatile(
+          "s_cmp_eq_u32 %4, 0\n\t"
+          "s_cbranch_scc1 .Lno_copy%=\n\t"
+          "s_mov_b32 m0, %3\n\t"
+          "s_nop 0\n\t"
+          "global_load_lds_dwordx4 %0, %2\n\t"
+          "global_load_lds_dwordx4 %1, %2 offset:1024\n"
+          ".Lno_copy%=:"
+          :
+          : "v"(offset(i)), "v"(offset(i + 1) - 1024), "s"(src), "s"(to), "s"(uni(go))
+          : "memory", "scc", "m0");
+    else
+      __asm__ volatile(
+          "s_cmp_eq_u32 %3, 0\n\t"
+          "s_cbranch_scc1 .Lno_copy%=\n\t"
+          "s_mov_b32 m0, %2\n\t"
+          "s_nop 0\n\t"
+          "global_load_lds_dwordx4 %0, %1\n"
+          ".Lno_copy%=:"
+          :
+          : "v"(offset(i)), "s"(src), "s"(to), "s"(uni(go))
+          : "memory", "scc", "m0");
+  }
+
+  // Zeros in place of the rows from `valid` on.
+  __device__ static __forceinline__ void clear(char* page, int valid) {
+    const int l = threadIdx.x & 63;
+    for (int i = valid * Page::kRowBytes + 16 * l; i < Page::kRot; i += 1024) *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+    for (int i = Page::kRot + valid * Page::kRotBytes + 16 * l; i < Page::kBytes; i += 1024)
+      *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+  }
+};
+
+template <int DC, int DR, int M> struct LatLds {
+  static constexpr bool kWide = M == 64;
+  static constexpr int kStage = kLatWaves * LatPage<DC, DR, kWide>::kBytes;
+  static constexpr int kKeyParts = kWide ? 2 : 4;   // waves that share a row's scores
+  char stage[2][kStage];
+  char p[M * kLatKeys * 2];                         // weights: rows of 128 bytes, chunk c of row r in slot c ^ (r / 2)
+  float max[kLatWaves][M];                          // a row's maximum in each part of the keys; at the end its sums
+  int odd[DC];                                      // of each channel: the first key with a value that is not finite and ..
+  int any_odd;                                      // .. whether there is one, among those that only some of the tile's rows see
+  int limit[M];                                     // the last key that a row sees
+  int flag[2];                                      // some score is far above its row's maximum; one a stage in turn
+  long long sum[kLatWaves], before;
+  int found, bad;
+};
+
+// What a wave holds of a tile of M rows, and its parts of a stage.  `stage` is the stage's place in LDS.
+template <int DC, int DR, int M> struct LatRows {   // M = 16 or 32
+  using Page = LatPage<DC, DR, false>;
+  using Copies = LatCopies<DC, DR, false>;
+  using Lds = LatLds<DC, DR, M>;
+  static constexpr int RG = M / 16;                 // row groups
+  static constexpr int kSteps = DC / 32, kAll = kSteps + DR / 32;
+  static constexpr int kBlocks = DC / kLatWaves / 16;   // of 16 channels
+  static constexpr int kAhead = 3;                  // LDS reads of the products' operands, ahead of them
+  bf16x8 q[RG][kAll];
+  f32x4 o[kBlocks][RG], s[RG];
+  float m[RG], l[RG], sum[RG], ref[RG], factor[kLatKeys / 32][RG];
+  int w, g16, l16;
+
+  __device__ __forceinline__ void start(int wave, const uint16_t* rows, int n_rows) {
+    w = wave;
+    g16 = (threadIdx.x & 63) >> 4;
+    l16 = threadIdx.x & 15;
 #pragma unroll
-    for (int i = 0; i < kLatent; i += 4) {
-      int off[4];
+    for (int rg = 0; rg < RG; ++rg) {
+      const uint16_t* const src = rows + min(16 * rg + l16, n_rows - 1) * (size_t)(DC + DR) + 8 * g16;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        off[k] = (lane_off ^ (Page::f(kRows * (i + k)) << 4)) + row + k * (kRows * Page::kWidth - 1024);
-      copy4(src + i * kRows * Page::kWidth, off, lds + 1024 * i);
+      for (int k = 0; k < kAll; ++k) q[rg][k] = as_bf16x8(ld16(src + 32 * k));
+      m[rg] = -FLT_MAX;
+      l[rg] = 0.f;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) o[d][rg] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // 8 rows further (DR = 64) the swizzle differs in chunk bit 2
+  }
+  __device__ __forceinline__ void pin_queries() {
+    if constexpr (RG > 1) {
 #pragma unroll
-    for (int i = 0; i < kRot; ++i) copy1(src + i * 8 * Page::kWidth, rot_off ^ (64 * i), lds + Page::kRot + 1024 * i);
+      for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+        for (int k = 0; k < kAll; ++k) in_acc(q[rg][k]);
+    }
   }
+  __device__ __forceinline__ void pin_outputs() {
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg)
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) in_vector(o[d][rg]);
+  }
+  template <typename Next> __device__ __forceinline__ void scores(const char* stage, Next&& next_copies) {
+    const char* const page = stage + w * Page::kBytes;
+    // of the lane's first chunk; those of the steps after it differ in address bits 6 and 7, and by whole 256 bytes
+    const int at = l16 * Page::kRowBytes + 16 * (g16 ^ Page::f(l16)), rot = Page::kRot + l16 * Page::kRotBytes + 16 * (g16 ^ Page::rot_f(l16));
+    auto key_of = [&](int k) {
+      return as_bf16x8(*reinterpret_cast<const u32x4*>(page + (k < kSteps ? (at ^ (64 * (k & 3))) + 256 * (k >> 2) : rot ^ (64 * (k - kSteps)))));
+    };
+    bf16x8 key[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) s[rg] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kAll; ++k) {
+      const bf16x8 x = key[k % kAhead];
+#pragma unroll
+      for (int rg = 0; rg < RG; ++rg) s[rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[rg][k], s[rg], 0, 0, 0);
+      if (k + kAhead < kAll) key[k % kAhead] = key_of(k + kAhead);
+      if (k % 2 == 0) next_copies(k);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __device__ __forceinline__ void mask(const Lds& lds, int key0) {
+    const int key = key0 + kPage * w + 4 * g16;
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const int limit = lds.limit[16 * rg + l16];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (key + r > limit) s[rg][r] = -__builtin_inff();
+    }
+  }
+  // Weights, to P.  They are taken with the rows' maxima so far, unless some are over 2^kLag then: with the wave's own maxima, rounded up
+  // to whole numbers, so that their join scales by powers of two.
+  __device__ __forceinline__ void weigh(Lds& lds, int stage, float scale) {
+    float top = -FLT_MAX;
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      ref[rg] = m[rg];
+      top = fmaxf(top, fmaf(fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])), scale, -m[rg]));
+    }
+    if (__ballot(top > kLag)) {
+#pragma unroll
+      for (int rg = 0; rg < RG; ++rg) {
+        const float x = fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])) * scale;
+        ref[rg] = fmaxf(m[rg], ceilf(xor32_max(xor16_max(x))));
+      }
+      lds.flag[stage & 1] = 1;
+    }
+    char* const to = lds.p + l16 * 128 + 16 * ((2 * w + (g16 >> 1)) ^ (l16 >> 1)) + 8 * (g16 & 1);
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      float p[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[r] = fexp2(fmaf(s[rg][r], scale, -ref[rg]));
+      sum[rg] = (p[0] + p[1]) + (p[2] + p[3]);
+      *reinterpret_cast<bf16x4*>(to + 2048 * rg) = bf16x4{(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3]};
+      if (g16 == 0) lds.max[w][16 * rg + l16] = ref[rg];
+    }
+  }
+  // The waves' maxima become one; what is there is scaled to it.
+  __device__ __forceinline__ void join(const Lds& lds) {
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const float* const at = &lds.max[0][16 * rg + l16];
+      const float x = fmaxf(fmaxf(at[0], at[M]), fmaxf(at[2 * M], at[3 * M])), alpha = fexp2(m[rg] - x);
+      m[rg] = x;
+      l[rg] *= alpha;
+      sum[rg] *= fexp2(ref[rg] - x);
+#pragma unroll
+      for (int t = 0; t < kLatKeys / 32; ++t) factor[t][rg] = fexp2(at[(2 * t + (g16 >> 1)) * M] - x);   // of the weights that the lane reads
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) o[d][rg] *= alpha;
+    }
+  }
+  template <bool kScaled> __device__ __forceinline__ void add_values(const Lds& lds, const char* stage) {
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) l[rg] += sum[rg];
+    // The lane's row of 8 (g16 & 1) + 0 .. 3 of the values, channels of block 0; four rows further the swizzle differs in chunk bit 0.
+    const int r = 8 * (g16 & 1) + (l16 >> 2), c = DC / 32 * w + ((l16 >> 1) & 1);
+    const int at = (g16 >> 1) * Page::kBytes + r * Page::kRowBytes + 16 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + 8 * (l16 & 1);
+    const int at4 = (at ^ 16) + 4 * Page::kRowBytes, from = l16 * 128 + 16 * (g16 ^ (l16 >> 1));
+    auto value_of = [&](int i) {
+      const char* const pages = stage + i / kBlocks * 2 * Page::kBytes;
+      return concat_tr(lds_read_tr(pages, at ^ (32 * (i % kBlocks))), lds_read_tr(pages, at4 ^ (32 * (i % kBlocks))));
+    };
+    bf16x8 p[RG], value[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) value[i] = value_of(i);
+#pragma unroll
+    for (int i = 0; i < kLatKeys / 32 * kBlocks; ++i) {
+      const int t = i / kBlocks, d = i % kBlocks;
+      if (d == 0) {
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg) {
+          p[rg] = as_bf16x8(*reinterpret_cast<const u32x4*>(lds.p + 2048 * rg + (from ^ (64 * t))));
+          if constexpr (kScaled)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[rg][e] = (__bf16)((float)p[rg][e] * factor[t][rg]);
+        }
+      }
+      const bf16x8 x = value[i % kAhead];
+#pragma unroll
+      for (int rg = 0; rg < RG; ++rg) o[d][rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[rg], o[d][rg], 0, 0, 0);
+      if (i + kAhead < kLatKeys / 32 * kBlocks) value[i % kAhead] = value_of(i + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // Channels whose values were not finite, in the rows that see them.
+  __device__ __forceinline__ void set_odd(const Lds& lds) {
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int first = lds.odd[DC / kLatWaves * w + 16 * d + 4 * g16 + e];
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg)
+          if (first <= lds.limit[16 * rg + l16]) o[d][rg][e] = __builtin_nanf("");
+      }
+  }
+  // The rows' sums, in parts; a barrier later `each` takes (row, maximum, sum, the lane's first channel, its outputs: 4 channels every 16).
+  __device__ __forceinline__ void sums(Lds& lds) {
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const float x = xor32_add(xor16_add(l[rg]));
+      if (g16 == 0) lds.max[w][16 * rg + l16] = x;
+    }
+  }
+  template <typename F> __device__ __forceinline__ void each(const Lds& lds, F&& f) {
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const int r = 16 * rg + l16;
+      const float* const at = &lds.max[0][r];
+      const float x = (at[0] + at[M]) + (at[2 * M] + at[3 * M]);
+      f(r, m[rg], x, w == 0 && g16 == 0, [&](auto&& put) {
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d) put(DC / kLatWaves * w + 16 * d + 4 * g16, o[d][rg]);
+      });
+    }
+  }
+};
 
-  __device__ static __forceinline__ unsigned lds_address(const char* p) {
-    return __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)((LDS_AS const char*)p));
+template <int DC, int DR> struct LatRows<DC, DR, 64> {
+  static constexpr int M = 64;
+  using Page = LatPage<DC, DR, true>;
+  using Copies = LatCopies<DC, DR, true>;
+  using Lds = LatLds<DC, DR, M>;
+  static constexpr int kSteps = DC / 16, kAll = kSteps + DR / 16;
+  static constexpr int kTiles = DC / kLatWaves / 32;    // of 32 channels
+  static constexpr int kAhead = 4;
+  bf16x8 q[kAll];                                   // of the wave's 32 rows
+  f32x16 o[kTiles][2], s;                           // outputs of all rows
+  float m[2], l, sum, ref, factor[2][2];            // m: of the lane's row in both halves
+  int w, half, l32;                                 // wave w has the scores of keys 32 (w / 2) .. and rows 32 (w % 2) ..
+
+  __device__ __forceinline__ int own() const { return 32 * (w & 1) + l32; }
+  __device__ __forceinline__ float own_max() const { return w & 1 ? m[1] : m[0]; }
+  __device__ __forceinline__ void start(int wave, const uint16_t* rows, int n_rows) {
+    w = wave;
+    half = (threadIdx.x & 63) >> 5;
+    l32 = threadIdx.x & 31;
+    const uint16_t* const src = rows + min(own(), n_rows - 1) * (size_t)(DC + DR) + 8 * half;
+#pragma unroll
+    for (int k = 0; k < kAll; ++k) q[k] = as_bf16x8(ld16(src + 16 * k));
+    m[0] = m[1] = -FLT_MAX;
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][t][r] = 0.f;
   }
-  __device__ static __forceinline__ void copy4(const char* base, const int* off, const char* lds) {
-    unsigned saved;
-    __asm__ volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %6\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %5\n\t"
-        "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:3072\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds_address(lds))
-        : "memory");
+  __device__ __forceinline__ void pin_queries() {
+#pragma unroll
+    for (int k = 0; k < kAll; ++k) in_acc(q[k]);
   }
-  __device__ static __forceinline__ void copy1(const char* base, int off, const char* lds) {
-    unsigned saved;
-    __asm__ volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %3\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %2\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(off), "s"(base), "s"(lds_address(lds))
-        : "memory");
+  __device__ __forceinline__ void pin_outputs() {
+#pragma unroll
+    for (int d = 0; d < kTiles; ++d) {
+      in_vector(o[d][0]);
+      in_vector(o[d][1]);
+    }
+  }
+  template <typename Next> __device__ __forceinline__ void scores(const char* stage, Next&& next_copies) {
+    const char* const pages = stage + 2 * (w >> 1) * Page::kBytes;
+    // of the lane's first chunk; those of the steps after it differ in address bits 5 .. 7, and by whole 256 bytes
+    const int r = l32 & 15, page = (l32 >> 4) * Page::kBytes;
+    const int at = page + r * Page::kRowBytes + 16 * (half ^ Page::f(r)), rot = page + Page::kRot + r * Page::kRotBytes + 16 * (half ^ Page::rot_f(r));
+    auto key_of = [&](int k) {
+      return as_bf16x8(*reinterpret_cast<const u32x4*>(pages + (k < kSteps ? (at ^ (32 * (k & 7))) + 256 * (k >> 3) : rot ^ (32 * (k - kSteps)))));
+    };
+    bf16x8 key[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kAll; ++k) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key[k % kAhead], q[k], s, 0, 0, 0);
+      if (k + kAhead < kAll) key[k % kAhead] = key_of(k + kAhead);
+      if (k % 4 == 1) next_copies(k / 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __device__ __forceinline__ void mask(const Lds& lds, int key0) {
+    const int key = key0 + 32 * (w >> 1) + 4 * half, limit = lds.limit[own()];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (key + (i & 3) + 8 * (i >> 2) > limit) s[i] = -__builtin_inff();
+  }
+  __device__ __forceinline__ float largest() const {
+    float x = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) x = fmaxf(x, fmaxf(s[i], s[i + 1]));
+    return x;
+  }
+  __device__ __forceinline__ void weigh(Lds& lds, int stage, float scale) {
+    ref = own_max();
+    const float top = largest();
+    if (__ballot(fmaf(top, scale, -ref) > kLag)) {
+      ref = fmaxf(ref, ceilf(xor32_max(top * scale)));
+      lds.flag[stage & 1] = 1;
+    }
+    char* const to = lds.p + own() * 128 + 8 * half;
+    sum = 0.f;
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      float p[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[r] = fexp2(fmaf(s[4 * a + r], scale, -ref));
+      sum += (p[0] + p[1]) + (p[2] + p[3]);
+      *reinterpret_cast<bf16x4*>(to + 16 * ((4 * (w >> 1) + a) ^ ((l32 >> 1) & 7))) = bf16x4{(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3]};
+    }
+    if (half == 0) lds.max[w >> 1][own()] = ref;
+  }
+  __device__ __forceinline__ void join(const Lds& lds) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float a = lds.max[0][32 * t + l32], b = lds.max[1][32 * t + l32], x = fmaxf(a, b), alpha = fexp2(m[t] - x);
+      m[t] = x;
+      if (t == (w & 1)) {
+        l *= alpha;
+        sum *= fexp2(ref - x);
+      }
+      factor[0][t] = fexp2(a - x);
+      factor[1][t] = fexp2(b - x);
+#pragma unroll
+      for (int d = 0; d < kTiles; ++d) o[d][t] *= alpha;
+    }
+  }
+  template <bool kScaled> __device__ __forceinline__ void add_values(const Lds& lds, const char* stage) {
+    l += sum;
+    // The lane's row of 8 (l / 32) + 0 .. 3 of the values, channels of tile 0; four rows further the swizzle differs in chunk bit 0.
+    const int j = l32 & 15, r = 8 * half + (j >> 2), c = DC / 32 * w + 2 * (l32 >> 4) + ((j >> 1) & 1);
+    const int at = r * Page::kRowBytes + 16 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + 8 * (j & 1), at4 = (at ^ 16) + 4 * Page::kRowBytes;
+    const int from = l32 * 128 + 16 * (half ^ ((l32 >> 1) & 7));
+    constexpr int kParts = kLatWaves * kTiles;      // (page, tile), tiles of a page in turn
+    auto value_of = [&](int i) {
+      const char* const page = stage + i / kTiles * Page::kBytes;
+      return concat_tr(lds_read_tr(page, at ^ (64 * (i % kTiles))), lds_read_tr(page, at4 ^ (64 * (i % kTiles))));
+    };
+    auto weights_of = [&](int page, int t) {
+      bf16x8 p = as_bf16x8(*reinterpret_cast<const u32x4*>(lds.p + 4096 * t + (from ^ (32 * page))));
+      if constexpr (kScaled)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (__bf16)((float)p[e] * factor[page >> 1][t]);
+      return p;
+    };
+    bf16x8 p[2][2], value[kAhead];                  // p: of this page and the next one
+    p[0][0] = weights_of(0, 0);
+    p[0][1] = weights_of(0, 1);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) value[i] = value_of(i);
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      const int page = i / kTiles, d = i % kTiles;
+      if (d == 0 && page + 1 < kLatWaves) {
+        p[(page + 1) & 1][0] = weights_of(page + 1, 0);
+        p[(page + 1) & 1][1] = weights_of(page + 1, 1);
+      }
+      const bf16x8 x = value[i % kAhead];
+      o[d][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[page & 1][0], o[d][0], 0, 0, 0);
+      o[d][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[page & 1][1], o[d][1], 0, 0, 0);
+      if (i + kAhead < kParts) value[i % kAhead] = value_of(i + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __device__ __forceinline__ void set_odd(const Lds& lds) {
+#pragma unroll
+    for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int first = lds.odd[DC / kLatWaves * w + 32 * d + (i & 3) + 8 * (i >> 2) + 4 * half];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (first <= lds.limit[32 * t + l32]) o[d][t][i] = __builtin_nanf("");
+      }
+  }
+  __device__ __forceinline__ void sums(Lds& lds) {
+    const float x = xor32_add(l);
+    if (half == 0) lds.max[w >> 1][own()] = x;
+  }
+  template <typename F> __device__ __forceinline__ void each(const Lds& lds, F&& f) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int r = 32 * t + l32;
+      f(r, m[t], lds.max[0][r] + lds.max[1][r], w == 0 && half == 0, [&](auto&& put) {
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+            put(DC / kLatWaves * w + 32 * d + 8 * a + 4 * half, f32x4{o[d][t][4 * a], o[d][t][4 * a + 1], o[d][t][4 * a + 2], o[d][t][4 * a + 3]});
+      });
+    }
   }
 };
 
@@ -206,6 +585,12 @@ __device__ __forceinline__ LatSeq lat_seq(const LatentArgs& a, int b) {
   return LatSeq{start, a.cu[b + 1] - start, a.ctx_lens[b]};
 }
 
+// The same of one sequence for the whole wave, in scalar registers.
+__device__ __forceinline__ LatSeq lat_seq_uni(const LatentArgs& a, int b) {
+  const LatSeq s = lat_seq(a, b);
+  return LatSeq{uni(s.q_start), uni(s.q_len), uni(s.ctx)};
+}
+
 __device__ __forceinline__ bool lat_bad(const LatentArgs& a, const LatSeq& s) {
   const long long kv = (long long)s.ctx + s.q_len;
   return s.q_len < 0 || s.ctx < 0 || s.q_start < 0 || s.q_len > a.max_q_len || (long long)s.q_start + s.q_len > a.total_q ||
@@ -219,38 +604,24 @@ __device__ __forceinline__ long long shfl_up64(long long x, int d) {
 
 }  // namespace
 
-// Work with `group` g = index % group; shares of an XCD's workgroups follow one another.
 template <int DC, int DR, int M>
 __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
-  using Page = LatPage<DC, DR>;
-  constexpr int RG = M / 16;                        // row groups
-  constexpr int kSteps = DC / 32, kRotSteps = DR / 32;
-  constexpr int kBlocks = DC / kLatWaves / 16;      // blocks of 16 channels of a wave
-  constexpr int kStage = kLatWaves * Page::kBytes;
-  constexpr int kAhead = 3;                         // LDS reads of the products' operands, ahead of them
-  constexpr int kKeepQ = M == 64 ? (DC == 512 ? 16 : kSteps + kRotSteps) : M == 32 ? kSteps + kRotSteps : 0;   // steps whose queries are in accumulation registers
-  __shared__ __attribute__((aligned(256))) char s_stage[2 * kStage];
-  __shared__ __attribute__((aligned(256))) char s_p[M * kLatKeys * 2];
-  __shared__ float s_max[kLatWaves][M];
-  __shared__ int s_limit[M];
-  __shared__ int s_flag[2];                         // some score is far above its row's maximum; one a stage in turn
-  __shared__ int s_odd[DC];                         // of each channel: the first key with a value that is not finite and ..
-  __shared__ int s_any_odd;                         // .. whether there is one, among those that only some of the tile's rows see
-  __shared__ long long s_sum[kLatWaves];
-  __shared__ int s_found, s_bad;
-  __shared__ long long s_before;
+  using Rows = LatRows<DC, DR, M>;
+  using Page = typename Rows::Page;
+  using Copies = typename Rows::Copies;
+  using Lds = LatLds<DC, DR, M>;
+  __shared__ __attribute__((aligned(256))) Lds lds;
   const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6);
-  const int g16 = lane >> 4, l16 = lane & 15;
 
-  // ---- this workgroup's share
+  // ---- this workgroup's share: workgroups with one number modulo `group` take the same member of the tiles, and shares of an XCD's follow
+  // one another
   const int group = a.group;
   const int per_xcd = (int)gridDim.x / kNumXcd;
   const int index = (int)(blockIdx.x % kNumXcd) * per_xcd + (int)(blockIdx.x / kNumXcd);
-  int share = index / group;
-  const int member = index - share * group;
-  const LatPlan plan{a.group * M, a.slope, a.heads};
-  if (tid == 0) { s_bad = 0; s_flag[0] = s_flag[1] = s_any_odd = 0; }
-  for (int i = tid; i < DC; i += kLatThreads) s_odd[i] = INT32_MAX;
+  const int share = index / group, member = index - share * group;
+  const LatPlan plan{group * M, a.slope, a.heads};
+  if (tid == 0) lds.bad = lds.flag[0] = lds.flag[1] = lds.any_odd = 0;
+  for (int i = tid; i < DC; i += kLatThreads) lds.odd[i] = INT32_MAX;
   __syncthreads();
   const int per = (a.batch + kLatThreads - 1) / kLatThreads;
   long long mine = 0;
@@ -263,7 +634,7 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
       if (lat_bad(a, s)) bad = true;
       else mine += plan.before(s, plan.tiles(s));
     }
-    if (bad) s_bad = 1;
+    if (bad) lds.bad = 1;
   }
   long long upto = mine;                            // of this wave's threads up to this one
 #pragma unroll
@@ -271,57 +642,42 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
     const long long y = shfl_up64(upto, d);
     if (lane >= d) upto += y;
   }
-  if (lane == 63) s_sum[w] = upto;
+  if (lane == 63) lds.sum[w] = upto;
   __syncthreads();
-  int4* const job = a.jobs + index;
-  if (blockIdx.x == 0 && tid == 0) a.ws_hdr[kHdrError] = s_bad;
+  if (blockIdx.x == 0 && tid == 0) a.ws_hdr[kHdrError] = lds.bad;
   long long total = 0;
 #pragma unroll
   for (int v = 0; v < kLatWaves; ++v) {
     if (v == w) upto += total;
-    total += uni64(s_sum[v]);
+    total += uni64(lds.sum[v]);
   }
   int shares = (int)gridDim.x / group;
   if (total < (long long)shares * a.min_share) shares = (int)max(1ll, total / a.min_share);
-  if (uni(s_bad) || total == 0 || share >= shares) {
-    if (tid == 0) *job = int4{0, 0, 0, 0};
+  if (uni(lds.bad) || total == 0 || share >= shares) {
+    if (tid == 0) a.jobs[index] = int4{0, 0, 0, 0};
     return;
   }
   const LatShares cut(total, shares);
   const long long lo = cut.start(share), hi = cut.start(share + 1);
   if (upto - mine <= lo && lo < upto) {
-    s_found = tid;
-    s_before = upto - mine;
+    lds.found = tid;
+    lds.before = upto - mine;
   }
   __syncthreads();
-  int b = uni(s_found) * per;
-  long long at = uni64(s_before);                   // cost before sequence b
-  LatSeq seq = lat_seq(a, b);
+  int b = uni(lds.found) * per;
+  long long at = uni64(lds.before);                 // cost before sequence b
+  LatSeq seq = lat_seq_uni(a, b);
   for (;;) {
     const long long c = plan.before(seq, plan.tiles(seq));
     if (lo < at + c) break;
     at += c;
-    seq = lat_seq(a, ++b);
+    seq = lat_seq_uni(a, ++b);
   }
   int u = plan.tile_at(seq, lo - at);
   int4 my_job = {0, 0, 0, 0};
 
-  // ---- lanes' addresses
-  const LatCopies<DC, DR> copies;
-  // of a key's chunk g16; those of the steps after it differ in address bits 6 and 7, and by whole 256 bytes
-  const int k_off = l16 * Page::kRowBytes + 16 * (g16 ^ Page::f(l16));
-  const int rot_off = Page::kRot + l16 * Page::kRotBytes + 16 * (g16 ^ Page::rot_f(l16));
-  int v_off[2];                                     // of block 0: the wave's channels start at chunk (DC / 32) w
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = 8 * (g16 & 1) + 4 * i + (l16 >> 2), c = DC / 32 * w + ((l16 >> 1) & 1);
-    v_off[i] = (g16 >> 1) * Page::kBytes + r * Page::kRowBytes + 16 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + 8 * (l16 & 1);
-  }
-  const int h16 = (l16 >> 1) & 7;                   // swizzle of P's 128-byte rows
-  const int p_write = l16 * 128 + 16 * ((2 * w + (g16 >> 1)) ^ h16) + 8 * (g16 & 1);
-  const int p_read = l16 * 128 + 16 * (g16 ^ h16);  // of keys 0 .. 31; ^ 64 of the others
-
   // ---- tiles
+  const unsigned my_page = lds_address(lds.stage[0]) + w * Page::kBytes;   // page w of a stage is this wave's to bring
   for (;;) {
     const long long t0 = at + plan.before(seq, u), t1 = at + plan.before(seq, u + 1);
     const int rows = seq.q_len * a.heads;           // below 2^28 (2^21 tokens, 128 heads)
@@ -336,270 +692,130 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent_kernel(LatentArgs a) {
       const size_t row0 = (size_t)seq.q_start * a.heads + r0;
       if (starts && !ends) my_job = int4{(int)row0, n_rows, index, cut.of(t1 - 1) - share + 1};
       if (j0 >= j1) {
-        if (!(starts && ends) && tid < M) reinterpret_cast<float2*>(a.part_ml)[(size_t)slot * M + tid] = float2{-FLT_MAX, 0.f};
+        if (!(starts && ends) && tid < M) reinterpret_cast<float2*>(args_anew()->part_ml)[(size_t)slot * M + tid] = float2{-FLT_MAX, 0.f};
       } else {
         const int kv = seq.ctx + seq.q_len, pages = (kv + kPage - 1) / kPage;
-        const ConstI32Ptr bt = (ConstI32Ptr)(a.block_table + (size_t)b * a.bt_stride);
+        const int32_t* const bt = a.block_table + (size_t)b * a.bt_stride;
         const char* const cache = reinterpret_cast<const char*>(a.cache);
-        // page w of stage j, to its buffer: the page id is read a stage ahead
-        auto page_id = [&](int j) { return clamp_page(bt[min(j * kLatWaves + w, pages - 1)], a.num_pages); };
-        auto issue = [&](int j, int id) {
-          if (j * kLatWaves + w < pages)
-            copies.copy(cache + (size_t)id * Page::kBytes, s_stage + (j & 1) * kStage + w * Page::kBytes);
-        };
-        issue(j0, page_id(j0));
-        int id = page_id(j0 + 1);
-        // queries: 16 bytes of row l16 of each group, channels 32 step + 8 g16
-        bf16x8 q[RG][kSteps + kRotSteps];
-        // the last key that a row sees
-        barrier_lds();
-        if (tid < M) s_limit[tid] = seq.ctx + (r0 + min(tid, n_rows - 1)) / a.heads;
+        // Page w of stage j (the last one where there is none; zeros take its place) goes to buffer j & 1.  Its id is read a stage
+        // ahead, as a vector: a scalar load in flight would hold up the LDS reads, whose counter it shares.
+        auto page_id = [&](int j) { return bt[min(j * kLatWaves + w, pages - 1)]; };
+        auto page_at = [&](int id) { return cache + (size_t)clamp_page(uni(id), a.num_pages) * Page::kBytes; };
+        {
+          const char* const src = page_at(page_id(j0));
 #pragma unroll
-        for (int rg = 0; rg < RG; ++rg) {
-          const int r = 16 * rg + l16;
-          const uint16_t* const src = a.q + (row0 + min(r, n_rows - 1)) * (size_t)(DC + DR) + 8 * g16;
-#pragma unroll
-          for (int k = 0; k < kSteps + kRotSteps; ++k) q[rg][k] = as_bf16x8(ld16(src + 32 * k));
+          for (int i = 0; i < Copies::kCopies; i += 2) Copies::copy2(i, src, my_page + (j0 & 1) * Lds::kStage, 1);
         }
+        int id = page_id(j0 + 1);
+        Rows x;
+        x.start(w, args_anew()->q + row0 * (DC + DR), n_rows);
+        if (tid < M) lds.limit[tid] = seq.ctx + (r0 + min(tid, n_rows - 1)) / a.heads;
         const int first_limit = seq.ctx + r0 / a.heads;    // keys behind it are not all rows'
         const bool in_part = (r0 + n_rows - 1) / a.heads != r0 / a.heads;
-        f32x4 o[kBlocks][RG];
-        float m[RG], l[RG];
-#pragma unroll
-        for (int rg = 0; rg < RG; ++rg) {
-          m[rg] = -FLT_MAX;
-          l[rg] = 0.f;
-#pragma unroll
-          for (int d = 0; d < kBlocks; ++d) o[d][rg] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        f32x4 s[RG];                                // scores of the wave's 16 keys
-        float sum[RG];
-        // Weights with the rows' maxima so far, to P; the largest exponent.
-        auto weigh = [&]() {
-          float top = -FLT_MAX;
-#pragma unroll
-          for (int rg = 0; rg < RG; ++rg) {
-            float x[4], p[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              x[r] = fmaf(s[rg][r], a.scale_log2, -m[rg]);
-              p[r] = fexp2(x[r]);
-            }
-            top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-            sum[rg] = (p[0] + p[1]) + (p[2] + p[3]);
-            *reinterpret_cast<bf16x4*>(s_p + 2048 * rg + p_write) = bf16x4{(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3]};
-          }
-          return top;
-        };
-        auto add_values = [&](const char* stage) {
-#pragma unroll
-          for (int rg = 0; rg < RG; ++rg) l[rg] += sum[rg];
-          // value operands are read kAhead blocks ahead of their products
-          int off0 = v_off[0], off1 = v_off[1];
-          __asm__ volatile("" : "+v"(off0), "+v"(off1));
-          auto value_of = [&](int i) {
-            const char* const at = stage + i / kBlocks * 2 * Page::kBytes;
-            return concat_tr(lds_read_tr(at, off0 ^ (32 * (i % kBlocks))), lds_read_tr(at, off1 ^ (32 * (i % kBlocks))));
-          };
-          bf16x8 p[RG], value[kAhead];
-#pragma unroll
-          for (int i = 0; i < kAhead; ++i) value[i] = value_of(i);
-#pragma unroll
-          for (int i = 0; i < kLatKeys / 32 * kBlocks; ++i) {
-            if (i % kBlocks == 0) {
-#pragma unroll
-              for (int rg = 0; rg < RG; ++rg)
-                p[rg] = as_bf16x8(*reinterpret_cast<const u32x4*>(s_p + 2048 * rg + (p_read ^ (64 * (i / kBlocks)))));
-            }
-            const bf16x8 x = value[i % kAhead];
-#pragma unroll
-            for (int rg = 0; rg < RG; ++rg)
-              o[i % kBlocks][rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[rg], o[i % kBlocks][rg], 0, 0, 0);
-            if (i + kAhead < kLatKeys / 32 * kBlocks) value[i % kAhead] = value_of(i + kAhead);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        };
         int j = j0;
-        // Stages whose scores are near the maxima so far run in the inner loop; the others, the first one among them, behind it (inside it,
-        // their scaling would have the compiler copy all outputs in every stage).
+        // Stages whose scores are near the maxima so far run in the inner loop; the others, the first one among them, end behind it (inside
+        // it, their scaling would have the compiler move all outputs in every stage).
         for (;;) {
           bool above = false;
 #pragma unroll 1
           for (; j < j1; ++j) {
-            if constexpr (kKeepQ > 0) {
-#pragma unroll
-              for (int rg = 0; rg < RG; ++rg)
-#pragma unroll
-                for (int k = 0; k < kKeepQ; ++k) in_acc(q[rg][k]);
-            }
-            char* const page = s_stage + (j & 1) * kStage + w * Page::kBytes;
-            const int key0 = j * kLatKeys;
+            x.pin_queries();
+            char* const stage = lds.stage[j & 1];
+            char* const page = stage + w * Page::kBytes;
+            const int key0 = j * kLatKeys, valid = kv - key0 - kPage * w;
             wait_copies();
-            const int valid = kv - key0 - kPage * w;  // rows of this wave's page
-            if (valid < kPage) {                    // the others become zeros
-              const int from = max(valid, 0);
-              for (int i = from * Page::kRowBytes + 16 * lane; i < Page::kRot; i += 1024) *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
-              for (int i = Page::kRot + from * Page::kRotBytes + 16 * lane; i < Page::kBytes; i += 1024)
-                *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
-            }
-            barrier_lds();                          // the other buffer and P are free
-            if (j + 1 < j1) {
-              issue(j + 1, id);
-              if (j + 2 < j1) id = page_id(j + 2);
-            }
-            if (tid == 0) s_flag[(j + 1) & 1] = 0;
-#pragma unroll
-            for (int rg = 0; rg < RG; ++rg) s[rg] = f32x4{0.f, 0.f, 0.f, 0.f};
-            // key operands are read kAhead steps ahead of their products
-            int at = k_off, at_rot = rot_off;
-            __asm__ volatile("" : "+v"(at), "+v"(at_rot));
-            auto key_of = [&](int k) {
-              const int off = k < kSteps ? (at ^ (64 * (k & 3))) + 256 * (k >> 2) : at_rot ^ (64 * (k - kSteps));
-              return as_bf16x8(*reinterpret_cast<const u32x4*>(page + off));
-            };
-            bf16x8 key[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
-#pragma unroll
-            for (int k = 0; k < kSteps + kRotSteps; ++k) {
-              const bf16x8 x = key[k % kAhead];
-#pragma unroll
-              for (int rg = 0; rg < RG; ++rg) s[rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[rg][k], s[rg], 0, 0, 0);
-              if (k + kAhead < kSteps + kRotSteps) key[k % kAhead] = key_of(k + kAhead);
-              __builtin_amdgcn_sched_barrier(0);
-            }
+            if (valid < kPage) Copies::clear(page, max(valid, 0));   // rows behind the sequence's end
+            barrier_lds();                          // the stage is there; the other buffer and P are free
+            const char* const src = page_at(id);
+            const unsigned dst = my_page + (~j & 1) * Lds::kStage;
+            const int more = j + 1 < j1;
+            id = page_id(j + 2);
+            if (w == 0) lds.flag[(j + 1) & 1] = 0;
+            // the next stage's copies go out among the products: issued together, they would hold the wave
+            x.scores(stage, [&](int i) {
+              if (i < Copies::kCopies) Copies::copy2(i, src, dst, more);
+            });
             if (key0 + kLatKeys - 1 > first_limit) {
-              const int key = key0 + kPage * w + 4 * g16;
-#pragma unroll
-              for (int rg = 0; rg < RG; ++rg) {
-                const int limit = s_limit[16 * rg + l16];
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                  if (key + r > limit) s[rg][r] = -__builtin_inff();
-              }
+              x.mask(lds, key0);
               // Keys that only some of the rows see have weight 0 in the others, and 0 times a value that is not finite is NaN: it becomes 0 and
               // its channel is noted.  (The value is part of its key too: in rows that see it its score is NaN or infinite, so its
               // channel's output is NaN there, if not the whole row, which is what the end of the tile makes of the note.)
               if (in_part) {
+                if (Lds::kWide) barrier_lds();      // another wave has the page's scores for the other rows
                 for (int i = lane; i < kPage * DC / 8; i += 64) {
                   const int r = i / (DC / 8), c = i % (DC / 8);
-                  u32x4 x = *reinterpret_cast<const u32x4*>(page + 16 * i);
+                  u32x4 v = *reinterpret_cast<const u32x4*>(page + 16 * i);
                   bool bad = false;
 #pragma unroll
                   for (int e = 0; e < 8; ++e) {
                     const uint32_t half = e & 1 ? 0x7f800000u : 0x7f80u;
-                    if ((x[e >> 1] & half) == half) {
-                      x[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
-                      atomicMin(&s_odd[8 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + e], key0 + kPage * w + r);
+                    if ((v[e >> 1] & half) == half) {
+                      v[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
+                      atomicMin(&lds.odd[8 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + e], key0 + kPage * w + r);
                       bad = true;
                     }
                   }
                   if (bad) {
-                    *reinterpret_cast<u32x4*>(page + 16 * i) = x;
-                    s_any_odd = 1;
+                    *reinterpret_cast<u32x4*>(page + 16 * i) = v;
+                    lds.any_odd = 1;
                   }
                 }
               }
             }
-            const float top = weigh();
-            if (__ballot(top > kLag) && lane == 0) s_flag[j & 1] = 1;
+            x.weigh(lds, j, a.scale_log2);
             barrier_lds();
-            if (uni(s_flag[j & 1])) {
+            if (uni(lds.flag[j & 1])) {
               above = true;
               break;
             }
-#pragma unroll
-            for (int rg = 0; rg < RG; ++rg)
-#pragma unroll
-              for (int d = 0; d < kBlocks; ++d) in_vector(o[d][rg]);
-            add_values(s_stage + (j & 1) * kStage);
+            x.pin_outputs();
+            x.template add_values<false>(lds, stage);
           }
           if (!above) break;
-          // the waves agree on new maxima and weigh the stage again
-#pragma unroll
-          for (int rg = 0; rg < RG; ++rg) {
-            float x = fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])) * a.scale_log2;
-            x = xor32_max(xor16_max(x));
-            if (g16 == 0) s_max[w][16 * rg + l16] = x;
-          }
-          barrier_lds();
-#pragma unroll
-          for (int rg = 0; rg < RG; ++rg) {
-            float x = m[rg];
-#pragma unroll
-            for (int v = 0; v < kLatWaves; ++v) x = fmaxf(x, s_max[v][16 * rg + l16]);
-            const float alpha = fexp2(m[rg] - x);
-            m[rg] = x;
-            l[rg] *= alpha;
-#pragma unroll
-            for (int d = 0; d < kBlocks; ++d) o[d][rg] *= alpha;
-          }
-          weigh();
-          barrier_lds();
-          add_values(s_stage + (j & 1) * kStage);
+          x.join(lds);
+          x.template add_values<true>(lds, lds.stage[j & 1]);
           ++j;
         }
         // ---- the rows' sums over lanes and waves, then the output or the partial
+        const LatArgsPtr args = args_anew();
         barrier_lds();
-        const bool odd = uni(s_any_odd) != 0;
-        if (odd) {
-#pragma unroll
-          for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int first = s_odd[DC / kLatWaves * w + 16 * d + 4 * g16 + e];
-#pragma unroll
-              for (int rg = 0; rg < RG; ++rg)
-                if (first <= s_limit[16 * rg + l16]) o[d][rg][e] = __builtin_nanf("");
-            }
-        }
-        if (tid == 0) s_flag[0] = s_flag[1] = 0;
-#pragma unroll
-        for (int rg = 0; rg < RG; ++rg) {
-          const float x = xor32_add(xor16_add(l[rg]));
-          if (g16 == 0) s_max[w][16 * rg + l16] = x;
-        }
+        const bool odd = uni(lds.any_odd) != 0;
+        if (odd) x.set_odd(lds);
+        if (tid == 0) lds.flag[0] = lds.flag[1] = 0;
+        x.sums(lds);
         barrier_lds();
         if (odd) {                                  // all have read it; the next tile's stages are behind another barrier
-          for (int i = tid; i < DC; i += kLatThreads) s_odd[i] = INT32_MAX;
-          if (tid == 0) s_any_odd = 0;
+          for (int i = tid; i < DC; i += kLatThreads) lds.odd[i] = INT32_MAX;
+          if (tid == 0) lds.any_odd = 0;
         }
-#pragma unroll
-        for (int rg = 0; rg < RG; ++rg) {
-          const int r = 16 * rg + l16;
-          float x = 0.f;
-#pragma unroll
-          for (int v = 0; v < kLatWaves; ++v) x += s_max[v][r];
-          const int channel = DC / kLatWaves * w + 4 * g16;
+        x.each(lds, [&](int r, float m, float l, bool first, auto&& channels) {
           if (starts && ends) {
-            const float inv = 1.f / x;
-            if (r < n_rows) {
-              uint16_t* const dst = a.out + (row0 + r) * DC + channel;
-#pragma unroll
-              for (int d = 0; d < kBlocks; ++d) {
-                const f32x4 y = o[d][rg] * inv;
-                *reinterpret_cast<bf16x4*>(dst + 16 * d) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
-              }
-              if (a.lse && w == 0 && g16 == 0) a.lse[row0 + r] = (m[rg] + flog2(x)) * kLn2;
-            }
+            const float inv = 1.f / l;
+            if (r >= n_rows) return;
+            uint16_t* const dst = args->out + (row0 + r) * DC;
+            channels([&](int c, const f32x4& o) {
+              const f32x4 y = o * inv;
+              *reinterpret_cast<bf16x4*>(dst + c) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+            });
+            if (args->lse && first) args->lse[row0 + r] = (m + flog2(l)) * kLn2;
           } else {
-            float* const dst = a.part_o + ((size_t)slot * M + r) * DC + channel;
-#pragma unroll
-            for (int d = 0; d < kBlocks; ++d) *reinterpret_cast<f32x4*>(dst + 16 * d) = o[d][rg];
-            if (w == 0 && g16 == 0) reinterpret_cast<float2*>(a.part_ml)[(size_t)slot * M + r] = float2{m[rg], x};
+            float* const dst = args->part_o + ((size_t)slot * M + r) * DC;
+            channels([&](int c, const f32x4& o) { *reinterpret_cast<f32x4*>(dst + c) = o; });
+            if (first) reinterpret_cast<float2*>(args->part_ml)[(size_t)slot * M + r] = float2{m, l};
           }
-        }
+        });
+        barrier_lds();                              // the next tile writes the limits
       }
     }
     if (t1 >= hi) break;
     if (++u == plan.tiles(seq)) {
       at = t1;
       u = 0;
-      do seq = lat_seq(a, ++b);
+      do seq = lat_seq_uni(a, ++b);
       while (seq.q_len == 0);
     }
   }
-  if (tid == 0) *job = my_job;
+  if (tid == 0) args_anew()->jobs[index] = my_job;
 }
 
 // Joins the partials of a cut tile: job (first row, rows, index of the first piece's workgroup, shares).  Its first piece is in slot
