@@ -202,9 +202,8 @@ struct LatentPlan {
 
 LatentPlan latent_plan(const pearl_latent_shape* s, const pearl_seq_desc* q) {
   LatentPlan p;
-  // rows (token, head) of a workgroup: no more than a sequence has, 64 at most
-  const int64_t rows = (int64_t)q->max_q_len * s->num_q_heads;
-  p.tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  // rows (token, head) of a workgroup: 16 where no sequence has more
+  p.tile = (int64_t)q->max_q_len * s->num_q_heads <= 16 ? 16 : 64;
   // workgroups that read the same keys together: as many as a sequence has tiles, on average, 4 at most
   const int64_t tiles = cdiv((int64_t)q->total_q * s->num_q_heads, (int64_t)q->batch * p.tile);
   p.group = tiles >= 8 ? 4 : tiles >= 2 ? 2 : 1;
@@ -257,7 +256,7 @@ pearl_status run_latent(bool decode, const pearl_latent_shape* s, const pearl_se
   a.heads = s->num_q_heads;
   a.group = p.group;
   a.slope = 128 * p.group * p.tile / s->num_q_heads;
-  a.min_share = p.tile == 16 ? 128 : p.tile == 32 ? 192 : 256;
+  a.min_share = p.tile == 16 ? 128 : 256;
   a.scale_log2 = scale * 1.4426950408889634f;
   hipError_t e = record_before(hs);
   if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));
