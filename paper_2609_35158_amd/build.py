@@ -14,8 +14,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpearl_attn.so")
-SOURCES = ["attn_kernels.hip", "decode_mx.hip", "kv_pages.hip", "kv_mx.hip", "rope.hip", "latent.hip", "hbm_probe.hip",
-           "api.cpp", "pd_engine.cpp"]
+SOURCES = ["attn_kernels.hip", "decode_mx.hip", "kv_pages.hip", "kv_mx.hip", "rope.hip", "latent16.hip", "latent64.hip",
+           "hbm_probe.hip", "api.cpp", "pd_engine.cpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -35,9 +35,8 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
-# Of one source: the outputs of its matrix instructions stay in vector registers, where its rare stages scale them, and
-# the accumulation registers hold operands (latent.hip).
-SOURCE_FLAGS = {"latent.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# Of some sources: the outputs of their matrix instructions stay in vector registers, where they are scaled.
+SOURCE_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for s in ("latent16.hip", "latent64.hip")}
 
 
 def _run(cmd, verbose: bool) -> None:

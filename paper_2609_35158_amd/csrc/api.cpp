@@ -256,7 +256,7 @@ pearl_status run_latent(bool decode, const pearl_latent_shape* s, const pearl_se
   a.heads = s->num_q_heads;
   a.group = p.group;
   a.slope = 128 * p.group * p.tile / s->num_q_heads;
-  a.min_share = p.tile == 16 ? 128 : 256;
+  a.min_share_shift = p.tile == 16 ? 7 : 8;
   a.scale_log2 = scale * 1.4426950408889634f;
   hipError_t e = record_before(hs);
   if (e != hipSuccess) return fail(PEARL_ERR_HIP, "timing event: %s", hipGetErrorString(e));

@@ -1,0 +1,343 @@
+// gfx950 kernels of attention over a paged cache of latent vectors (absorbed form; paper, section 4.3, Eq. 1: decode
+// is bound by its cache reads, which one short row a token for all heads makes few), for up to 16 rows a sequence, and the join of what is
+// cut.
+//
+// A cached row is (c, r), DC + DR channels; a query row (token, head) is (q_c, q_r).  s_j = scale q . (c_j, r_j), over
+// keys j up to the token's position, o = sum softmax(s)_j c_j: the row is the key of every head and its latent part the
+// value.  So the rows of a tile are any (token, head) pairs of a sequence, in the order of q: row rho is token rho / H, head
+// rho % H.  The softmax is online, in base 2, with state in 32 bits; weights enter the second product in bf16.
+//   S^T (keys x rows) = K . Q^T    16x16x32 MFMA: A row l%16, k 8(l/16)+e; B column l%16, k 8(l/16)+e; D column l%16, row 4(l/16)+r
+//   O^T (channels x rows) += V^T . P^T   16x16x16 MFMA: A row l%16, k 4(l/16)+e; B column l%16, k 4(l/16)+e: P^T is where S^T was
+//
+// Work is cut into equal shares of keys, in the order (sequence, tile, key), on the device from the lengths: each
+// workgroup finds its share by itself.  A tile cut by shares leaves (o~, m, l) in the workspace, joined by
+// latent_merge_kernel.  `group` workgroups next to one another on an XCD take neighbouring tiles of the same share, so that
+// they read the same keys at the same time, from L2.
+
+#include "latent_device.h"
+
+namespace pearl {
+namespace {
+
+template <int DC, int DR> struct LatLds16 {
+  char page[kLatWaves][2][LatPage<DC, DR, false>::kBytes];   // at the end of a tile: the waves' outputs
+  LatNotes<DC, 16> notes;
+  float max[kLatWaves][16], sum[kLatWaves][16];
+  LatFind find;
+};
+
+// M = 16: what a wave holds of a tile, of which it has all rows and every fourth page.
+template <int DC, int DR> struct LatRows16 {
+  static constexpr int M = 16;
+  using Page = LatPage<DC, DR, false>;
+  using Copies = LatCopies<DC, DR, false>;
+  static constexpr int kSteps = DC / 32, kAll = kSteps + DR / 32;
+  static constexpr int kBlocks = DC / 16;           // of 16 channels
+  static constexpr int kAhead = 4;                  // LDS reads of the products' operands, ahead of them
+  bf16x8 q[kAll];
+  f32x4 o[kBlocks], s;
+  float m, l;
+  int g16, l16;
+
+  __device__ __forceinline__ void start(const uint16_t* rows, int n_rows) {
+    g16 = (threadIdx.x & 63) >> 4;
+    l16 = threadIdx.x & 15;
+    const uint16_t* const src = rows + min(l16, n_rows - 1) * (size_t)(DC + DR);
+#pragma unroll
+    for (int k = 0; k < kAll; ++k) q[k] = as_bf16x8(ld16(src + lat_channel<DC>(k, g16)));
+    m = -FLT_MAX;
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void pin_queries() {
+#pragma unroll
+    for (int k = 0; k < kAll; ++k) in_acc(q[k]);
+  }
+  __device__ __forceinline__ void scores(const char* page) {
+    const int at = l16 * Page::kRowBytes + 16 * ((4 * g16) ^ Page::f(l16)), rot = Page::kRot + l16 * Page::kRotBytes + 16 * (g16 ^ Page::rot_f(l16));
+    auto key_of = [&](int k) {
+      return as_bf16x8(*reinterpret_cast<const u32x4*>(page + (k < kSteps ? (at ^ (16 * (k & 3))) + 256 * (k >> 2) : rot ^ (64 * (k - kSteps)))));
+    };
+    bf16x8 key[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
+    s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kAll; ++k) {
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[k % kAhead], q[k], s, 0, 0, 0);
+      if (k + kAhead < kAll) key[k % kAhead] = key_of(k + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __device__ __forceinline__ void mask(const int* limits, int key0) {
+    const int limit = limits[l16];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (key0 + 4 * g16 + r > limit) s[r] = -__builtin_inff();
+  }
+  __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])); }
+  // Whether some score is far above its row's maximum so far; the new maximum.
+  __device__ __forceinline__ bool above(float scale) const { return __ballot(fmaf(largest(), scale, -m) > kLag) != 0; }
+  __device__ __forceinline__ void raise(float scale) {
+    const float x = fmaxf(m, xor32_max(xor16_max(largest() * scale)));
+    scale_to(x);
+  }
+  __device__ __forceinline__ void scale_to(float x) {
+    const float alpha = fexp2(m - x);
+    m = x;
+    l *= alpha;
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) o[d] *= alpha;
+  }
+  __device__ __forceinline__ void add_values(const char* page, float scale) {
+    // The weights of the lane's row and keys 4 g16 .. + 3 are where the product (16x16x16: A row l%16, k 4(l/16)+e; B column l%16, k
+    // 4(l/16)+e) takes them.  Of the values the lane addresses row 4 g16 + l16 / 4, four channels of block 0.
+    const int r = 4 * g16 + (l16 >> 2), at = r * Page::kRowBytes + 16 * (((l16 >> 1) & 1) ^ Page::f(r)) + 8 * (l16 & 1);
+    auto value_of = [&](int d) { return lds_read_tr(page, (at ^ (32 * (d & 7))) + 256 * (d >> 3)); };
+    i16x4 value[kAhead];
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d) value[d] = value_of(d);
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fexp2(fmaf(s[i], scale, -m));
+    l += (x[0] + x[1]) + (x[2] + x[3]);
+    const i16x4 p = __builtin_bit_cast(i16x4, bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]});
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) {
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(value[d % kAhead], p, o[d], 0, 0, 0);
+      if (d + kAhead < kBlocks) value[d % kAhead] = value_of(d + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+}  // namespace
+
+// Up to 16 rows a sequence: every wave takes pages of its own, two in LDS, and no barrier until the tile ends, where the four waves'
+// outputs are joined in LDS.  The products are far from their limit here, what counts is that copies never pause.
+template <int DC, int DR>
+__global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) {
+  using Rows = LatRows16<DC, DR>;
+  using Page = typename Rows::Page;
+  using Copies = typename Rows::Copies;
+  constexpr int M = 16;
+  __shared__ __attribute__((aligned(256))) LatLds16<DC, DR> lds;
+  const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6);
+  clear_notes(lds.notes);
+  LatWork work;
+  if (!lat_find<M, kLatWaves>(a, lds.find, work)) return;
+  char* const buffers = lds.page[w][0];
+  do {
+    work.tile<M>();
+    if (work.j0 >= work.j1) continue;
+    const LatSeq seq = work.seq;
+    const int r0 = work.r0, n_rows = work.n_rows, last = seq.ctx + (r0 + n_rows - 1) / a.heads;   // the last key
+    const int kv = seq.ctx + seq.q_len, p1 = min(work.j1 * kLatWaves, last / kPage + 1);
+    const int first_limit = seq.ctx + r0 / a.heads;        // keys behind it are not all rows'
+    const bool in_part = last != first_limit;
+    const int32_t* const bt = a.block_table + (size_t)work.b * a.bt_stride;
+    // Ids of 64 of the wave's pages at once, lane i's page p + 4 i.  They are waited for here, and the queries before the loop: the compiler,
+    // which does not know of the copies, would wait in every page, for these too.
+    auto ids_from = [&](int p) {
+      int ids = bt[min(p + kLatWaves * lane, p1 - 1)];
+      __asm__ volatile("" : "+v"(ids));
+      return ids;
+    };
+    auto page_at = [&](int ids, int i) {
+      const int id = __builtin_amdgcn_readlane(ids, i);
+      return reinterpret_cast<const char*>(a.cache) + (size_t)clamp_page(id, a.num_pages) * Page::kBytes;
+    };
+    int p = work.j0 * kLatWaves + w, ids = ids_from(p), i = 0;   // i: the page's number among the ids
+    if (p < p1) Copies::page(page_at(ids, 0), lds_address(buffers));
+    Rows x;
+    x.start(args_anew()->q + work.row0 * (DC + DR), n_rows);
+    if (tid < M) lds.notes.limit[tid] = seq.ctx + (r0 + min(tid, n_rows - 1)) / a.heads;
+    x.pin_queries();
+    barrier_lds();
+    int parity = 0;
+    for (;;) {                                      // pages whose scores are near the maxima so far; others end behind the inner loop
+      bool above = false;
+      char* page = nullptr;
+#pragma unroll 1
+      for (; p < p1; p += kLatWaves, parity ^= 1) {
+        x.pin_queries();
+        page = buffers + parity * Page::kBytes;
+        if (p + kLatWaves < p1) {
+          if (++i == 64) {
+            ids = ids_from(p + kLatWaves);
+            i = 0;
+          }
+          Copies::page(page_at(ids, i), lds_address(buffers) + (parity ^ 1) * Page::kBytes);
+          __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");
+        } else {
+          wait_copies();
+        }
+        const int key0 = p * kPage;
+        if (kv - key0 < kPage) Copies::clear(page, kv - key0);   // rows behind the sequence's end
+        x.scores(page);
+        if (key0 + kPage - 1 > first_limit) {
+          x.mask(lds.notes.limit, key0);
+          if (in_part) note_odd<Page>(page, key0, lds.notes);
+        }
+        if (x.above(a.scale_log2)) {
+          above = true;
+          break;
+        }
+        x.add_values(page, a.scale_log2);
+      }
+      if (!above) break;
+      x.raise(a.scale_log2);
+      x.add_values(page, a.scale_log2);
+      p += kLatWaves;
+      parity ^= 1;
+    }
+    // ---- the waves' maxima and sums, then their outputs scaled alike
+    x.l = xor32_add(xor16_add(x.l));
+    if (x.g16 == 0) {
+      lds.max[w][x.l16] = x.m;
+      lds.sum[w][x.l16] = x.l;
+    }
+    barrier_lds();
+    const bool odd = uni(lds.notes.any_odd) != 0;
+    const float top = fmaxf(fmaxf(lds.max[0][x.l16], lds.max[1][x.l16]), fmaxf(lds.max[2][x.l16], lds.max[3][x.l16]));
+    x.scale_to(top);
+    // outputs of a wave: rows of DC channels in 32 bits, chunk c of row r in slot c ^ r of its 16
+    constexpr int kWaveBytes = M * DC * 4;
+    static_assert(kWaveBytes <= 2 * Page::kBytes, "in the wave's own buffers");
+#pragma unroll
+    for (int d = 0; d < Rows::kBlocks; ++d)
+      *reinterpret_cast<f32x4*>(buffers + x.l16 * DC * 4 + 16 * ((4 * d + x.g16) ^ x.l16)) = x.o[d];
+    barrier_lds();
+    const LatArgsPtr args = args_anew();
+    for (int r = w; r < n_rows || (r < M && !(work.starts && work.ends)); r += kLatWaves) {
+      const float t = fmaxf(fmaxf(lds.max[0][r], lds.max[1][r]), fmaxf(lds.max[2][r], lds.max[3][r]));
+      float l = 0.f;
+#pragma unroll
+      for (int v = 0; v < kLatWaves; ++v) l = fmaf(lds.sum[v][r], fexp2(lds.max[v][r] - t), l);
+      const float inv = 1.f / l;
+#pragma unroll
+      for (int c = 0; c < DC; c += 256) {
+        const int channel = c + 4 * lane;
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < kLatWaves; ++v)
+          y += *reinterpret_cast<const f32x4*>(lds.page[v][0] + r * DC * 4 + 16 * ((channel / 4) ^ r));
+        if (odd)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (lds.notes.odd[channel + e] <= lds.notes.limit[r]) y[e] = __builtin_nanf("");
+        if (work.starts && work.ends) {
+          y *= inv;
+          *reinterpret_cast<bf16x4*>(args->out + (work.row0 + r) * DC + channel) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+        } else {
+          *reinterpret_cast<f32x4*>(args->part_o + ((size_t)work.slot * M + r) * DC + channel) = y;
+        }
+      }
+      if (lane == 0) {
+        if (!(work.starts && work.ends)) reinterpret_cast<float2*>(args->part_ml)[(size_t)work.slot * M + r] = float2{t, l};
+        else if (args->lse) args->lse[work.row0 + r] = (t + flog2(l)) * kLn2;
+      }
+    }
+    barrier_lds();                                  // the next tile writes all of it
+    if (odd) {
+      clear_notes(lds.notes);
+      barrier_lds();
+    }
+  } while (work.next(a));
+  if (tid == 0) args_anew()->jobs[work.index] = work.job;
+}
+
+// Joins the partials of a cut tile: job (first row, rows, index of the first piece's workgroup, shares).  Its first piece is in slot
+// 1 of that workgroup, the others in slot 0 of the shares that follow, in order (kLatentGrid pieces at most).  A lane takes DC / 64 channels of a
+// row.  Few pieces: a wave a row.  Many: the waves take a fourth of them each, row by row.  Workgroups run on the XCD that wrote the first piece.
+template <int DC, int M>
+__global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a) {
+  static_assert(kLatentGrid <= 64 * kLatWaves, "a lane a piece");
+  constexpr int kRows = M / 16, kC = DC / 64;       // rows of a workgroup
+  const int4 job = a.jobs[blockIdx.x % kNumXcd * (kLatentGrid / kNumXcd) + blockIdx.x / kNumXcd];
+  const int r0 = blockIdx.y * kRows;
+  if (r0 >= job.y) return;
+  __shared__ float s_top[kLatWaves], s_sum[kLatWaves];
+  __shared__ __attribute__((aligned(16))) float s_o[kLatWaves][DC];
+  const int lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6), n = job.w, end = min(r0 + kRows, job.y);
+  const bool few = n <= 16;
+  const int first = few ? 0 : w, step = few ? 1 : kLatWaves, mine = n > first ? (n - first + step - 1) / step : 0;   // this wave's pieces
+  auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * job.z + 1 : 2 * (job.z + i * a.group)) * M; };
+  for (int r = few ? r0 + w : r0; r < end; r += few ? kLatWaves : 1) {
+    // lane k holds the maximum and sum of the wave's piece k; a piece that saw nothing counts nothing, its outputs may be unwritten
+    const float2 ml = lane < mine ? reinterpret_cast<const float2*>(a.part_ml)[slot(step * lane + first) + r] : float2{-FLT_MAX, 0.f};
+    const bool seen = ml.y != 0.f;
+    float top = seen ? ml.x : -FLT_MAX;
+    top = xor32_max(xor16_max(top));
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (!few) {
+      if (lane == 0) s_top[w] = top;
+      __syncthreads();
+      top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    }
+    const float weight = seen ? fexp2(ml.x - top) : 0.f;
+    float l = seen ? weight * ml.y : 0.f;
+    l = xor32_add(xor16_add(l));
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) l += __shfl_xor(l, d);
+    const unsigned long long all_seen = __ballot(seen);
+    float o[kC];
+#pragma unroll
+    for (int c = 0; c < kC; ++c) o[c] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < mine; ++k) {
+      const bool use = all_seen >> k & 1;
+      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), k));
+      const float* const src = a.part_o + (slot(step * k + first) + r) * DC + 4 * lane;
+#pragma unroll
+      for (int c = 0; c < kC; c += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(src + 64 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[c + e] = use ? fmaf(f, x[e], o[c + e]) : o[c + e];
+      }
+    }
+    if (!few) {
+      if (lane == 0) s_sum[w] = l;
+#pragma unroll
+      for (int c = 0; c < kC; c += 4) *reinterpret_cast<f32x4*>(&s_o[w][64 * c + 4 * lane]) = f32x4{o[c], o[c + 1], o[c + 2], o[c + 3]};
+      __syncthreads();
+      if (w == 0) {
+        l = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+          const int at = 64 * (c & ~3) + 4 * lane + (c & 3);
+          o[c] = (s_o[0][at] + s_o[1][at]) + (s_o[2][at] + s_o[3][at]);
+        }
+      }
+    }
+    if (few || w == 0) {
+      const size_t row = (size_t)job.x + r;
+      const float inv = 1.f / l;
+#pragma unroll
+      for (int c = 0; c < kC; c += 4)
+        *reinterpret_cast<bf16x4*>(a.out + row * DC + 64 * c + 4 * lane) =
+            bf16x4{(__bf16)(o[c] * inv), (__bf16)(o[c + 1] * inv), (__bf16)(o[c + 2] * inv), (__bf16)(o[c + 3] * inv)};
+      if (a.lse && lane == 0) a.lse[row] = (top + flog2(l)) * kLn2;
+    }
+    if (!few) __syncthreads();                      // the next row's sums
+  }
+}
+
+namespace {
+template <int DC, int DR> hipError_t launch_dims(const LatentArgs& a, int tile, bool merge, hipStream_t stream) {
+  const dim3 grid(kLatentGrid), threads(kLatThreads), merge_grid(kLatentGrid, 16);
+  if (merge && tile == 16) hipLaunchKernelGGL((latent_merge_kernel<DC, 16>), merge_grid, threads, 0, stream, a);
+  else if (merge) hipLaunchKernelGGL((latent_merge_kernel<DC, 64>), merge_grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((latent16_kernel<DC, DR>), grid, threads, 0, stream, a);
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_latent(const LatentArgs& a, int latent_dim, int tile, bool merge, hipStream_t stream) {
+  if (!merge && tile == 64) return launch_latent64(a, latent_dim, stream);
+  return latent_dim == 512 ? launch_dims<512, 64>(a, tile, merge, stream) : launch_dims<256, 32>(a, tile, merge, stream);
+}
+
+}  // namespace pearl

@@ -1,0 +1,462 @@
+// gfx950 kernel of attention over a paged cache of latent vectors (what it computes: latent16.hip) for sequences of more than 16 rows:
+// tiles of 64 rows.
+//
+// A workgroup has 8 waves, two on each SIMD: four take the scores and their weights, four the values, a stage (32 keys, 2 pages) behind, so that
+// the one's products run while the other weighs, waits or copies.
+//   S^T (keys x rows) = K . Q^T: score wave w has the keys of page w % 2 and rows 32 (w / 2) .., Q in registers (16x16x32 MFMA: A row l%16,
+//                       k 8(l/16)+e; B column l%16, k 8(l/16)+e; D column l%16, row 4(l/16)+r);
+//   O^T (channels x rows) += V^T . P^T: value wave w has a quarter of the channels and all rows, V^T by transposing reads of the same LDS
+//                       rows (32x32x16 MFMA: A row l%32, k 8(l/32)+e; B column l%32, k 8(l/32)+e; D column l%32, row r%4 + 8(r/4) + 4(l/32)).
+// Step t between two barriers: scores of stage t, values of stage t - 1, and the copies of stage t + 2 go out (four stages in LDS: t - 1 and t in
+// use, t + 1 on its way or there).
+// A row's maximum is common to all.  It may lag the true one by kLag (log2 units), so most stages go on with the old one.  Where some score
+// is further above, a score wave weighs with a maximum of its own, rounded up to a whole number, and behind the next barrier all waves take up the
+// largest; what was weighed with another is scaled by a power of two.
+
+#include "latent_device.h"
+
+namespace pearl {
+namespace {
+
+constexpr int kWaves64 = 8, kStageKeys = 32, kStageShift = 5, kStages = 4;
+
+template <int DC, int DR> struct LatLds64 {
+  using Page = LatPage<DC, DR, true>;
+  char page[kStages][2][Page::kBytes];
+  char p[2][64 * kStageKeys * 2];                   // weights of a stage: rows of 64 bytes, chunk c of row r in slot c ^ (r / 4)
+  LatNotes<DC, 64> notes;
+  int limit2[64];                                   // notes.limit of every other tile
+  float max[2][2][64];                              // of a stage, of each page: the rows' maxima that its weights were taken with
+  float sum[2][64];                                 // at the end of a tile: the rows' sums, in parts
+  int flag[2];                                      // the last step with some score far above its row's maximum, of even and odd ones
+  LatFind find;
+};
+
+// The copies of half a page (8 rows) by a wave, 1 KiB an instruction.
+template <int DC, int DR> struct LatHalfCopies {
+  using Page = LatPage<DC, DR, true>;
+  static constexpr int kRows = 1024 / Page::kRowBytes, kLatent = 8 / kRows, kCopies = kLatent + 1;
+  static constexpr bool kRotAtOnce = 8 * Page::kRotBytes < 1024;   // one instruction takes the page's rotated parts: both waves bring all of them
+  int off[kCopies];                                 // the lane's source offsets in the page
+  __device__ __forceinline__ void start(int half) {
+    const int l = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < kLatent; ++i) {
+      const int r = 8 * half + kRows * i + (kRows == 2 ? l >> 5 : 0), slot = kRows == 2 ? l & 31 : l;
+      off[i] = r * Page::kWidth + 16 * (slot ^ Page::f(r)) - 1024 * (i & 1);   // the second of a pair has 1 KiB as its immediate
+    }
+    constexpr int kChunks = Page::kRotBytes / 16;
+    const int r = l / kChunks + (kRotAtOnce ? 0 : 8 * half);
+    off[kLatent] = r * Page::kWidth + Page::kRowBytes + 16 * ((l % kChunks) ^ Page::rot_f(r));
+  }
+  // Copies i and i + 1 (the last one, of the rotated parts, by itself) to the page at the LDS address lds, if `go`.
+  __device__ __forceinline__ void copy2(int i, int half, const char* src, unsigned lds, int go) const {
+    if (i < kLatent) {
+      const unsigned to = uni((int)lds + half * 8 * Page::kRowBytes + 1024 * i);
+      __asm__ volatile(
+          "s_cmp_eq_u32 %4, 0\n\t"
+          "s_cbranch_scc1 .Lno_copy%=\n\t"
+          "s_mov_b32 m0, %3\n\t"
+          "s_nop 0\n\t"
+          "global_load_lds_dwordx4 %0, %2\n\t"
+          "global_load_lds_dwordx4 %1, %2 offset:1024\n"
+          ".Lno_copy%=:"
+          :
+          : "v"(off[i]), "v"(off[i + 1]), "s"(src), "s"(to), "s"(uni(go))
+          : "memory", "scc", "m0");
+    } else {
+      const unsigned to = uni((int)lds + Page::kRot + (kRotAtOnce ? 0 : 1024 * half));
+      __asm__ volatile(
+          "s_cmp_eq_u32 %3, 0\n\t"
+          "s_cbranch_scc1 .Lno_copy%=\n\t"
+          "s_mov_b32 m0, %2\n\t"
+          "s_nop 0\n\t"
+          "global_load_lds_dwordx4 %0, %1\n"
+          ".Lno_copy%=:"
+          :
+          : "v"(off[kLatent]), "s"(src), "s"(to), "s"(uni(go))
+          : "memory", "scc", "m0");
+    }
+  }
+  // Zeros in place of the half's latent parts from row `valid` of the page on (of rotated parts scores alone are made, which are masked).
+  __device__ static __forceinline__ void clear(char* page, int half, int valid) {
+    for (int i = max(valid, 8 * half) * Page::kRowBytes + 16 * (threadIdx.x & 63); i < 8 * (half + 1) * Page::kRowBytes; i += 1024)
+      *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+  }
+};
+
+// A score wave: page `page` of a stage, rows 32 half ...
+template <int DC, int DR> struct LatScores {
+  using Page = LatPage<DC, DR, true>;
+  using Lds = LatLds64<DC, DR>;
+  static constexpr int kSteps = DC / 32, kAll = kSteps + DR / 32;
+  static constexpr int kAhead = 4;                  // LDS reads of the product's operands, ahead of it
+  bf16x8 q[2][kAll];
+  f32x4 s[2];
+  float m[2], l[2], sum[2], ref[2];
+  int page, row0, g16, l16, place;                  // place: of the lane's weights among a stage's
+
+  __device__ __forceinline__ void start(Lds& lds, int wave, const uint16_t* rows, int n_rows) {
+    page = wave & 1;
+    row0 = 32 * (wave >> 1);
+    g16 = (threadIdx.x & 63) >> 4;
+    l16 = threadIdx.x & 15;
+    place = (row0 + l16) * 64 + 16 * ((2 * page + (g16 >> 1)) ^ (l16 >> 2)) + 8 * (g16 & 1);
+#pragma unroll
+    for (int rg = 0; rg < 2; ++rg) {
+      const uint16_t* const src = rows + min(row0 + 16 * rg + l16, n_rows - 1) * (size_t)(DC + DR);
+#pragma unroll
+      for (int k = 0; k < kAll; ++k) q[rg][k] = as_bf16x8(ld16(src + lat_channel<DC>(k, g16)));
+      m[rg] = -FLT_MAX;
+      l[rg] = sum[rg] = 0.f;
+      ref[rg] = -FLT_MAX;
+      if (g16 < 2) lds.max[g16][page][row0 + 16 * rg + l16] = -FLT_MAX;
+    }
+  }
+  // The products; flag: of the step before, asked for among the operands' reads.
+  __device__ __forceinline__ int scores(const Lds& lds, const char* stage, int step) {
+    const int flag = lds.flag[(step - 1) & 1];
+    const char* const at_page = stage + page * Page::kBytes;
+    const int at = l16 * Page::kRowBytes + 16 * ((4 * g16) ^ Page::f(l16)), rot = Page::kRot + l16 * Page::kRotBytes + 16 * (g16 ^ Page::rot_f(l16));
+    auto key_of = [&](int k) {
+      return as_bf16x8(*reinterpret_cast<const u32x4*>(at_page + (k < kSteps ? (at ^ (16 * (k & 3))) + 256 * (k >> 2) : rot ^ (64 * (k - kSteps)))));
+    };
+    bf16x8 key[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
+    s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kAll; ++k) {
+      const bf16x8 x = key[k % kAhead];
+      s[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[0][k], s[0], 0, 0, 0);
+      s[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[1][k], s[1], 0, 0, 0);
+      if (k + kAhead < kAll) key[k % kAhead] = key_of(k + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return uni(flag);
+  }
+  __device__ __forceinline__ void mask(const int* limits, int key0) {
+    const int key = key0 + kPage * page + 4 * g16;
+#pragma unroll
+    for (int rg = 0; rg < 2; ++rg) {
+      const int limit = limits[row0 + 16 * rg + l16];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (key + r > limit) s[rg][r] = -__builtin_inff();
+    }
+  }
+  __device__ __forceinline__ void weigh(Lds& lds, int step, float scale) {
+    float p[2][4], top = -FLT_MAX;
+    auto weights = [&](int rg) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[rg][r] = fexp2(fmaf(s[rg][r], scale, -ref[rg]));
+    };
+#pragma unroll
+    for (int rg = 0; rg < 2; ++rg) {
+      ref[rg] = m[rg];
+      weights(rg);
+      top = fmaxf(top, fmaf(fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])), scale, -m[rg]));
+    }
+    if (__ballot(top > kLag)) {
+#pragma unroll
+      for (int rg = 0; rg < 2; ++rg) {
+        const float x = fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])) * scale;
+        ref[rg] = fmaxf(m[rg], ceilf(xor32_max(xor16_max(x))));
+        weights(rg);
+        if (g16 == 0) lds.max[step & 1][page][row0 + 16 * rg + l16] = ref[rg];
+      }
+      lds.flag[step & 1] = step;
+    }
+    char* const to = lds.p[step & 1] + place;
+#pragma unroll
+    for (int rg = 0; rg < 2; ++rg) {
+      sum[rg] = (p[rg][0] + p[rg][1]) + (p[rg][2] + p[rg][3]);
+      *reinterpret_cast<bf16x4*>(to + 1024 * rg) = bf16x4{(__bf16)p[rg][0], (__bf16)p[rg][1], (__bf16)p[rg][2], (__bf16)p[rg][3]};
+    }
+  }
+  // Behind the barrier after weigh(step): the stage's sums, and new maxima if there are any (flag == step), with the weights in LDS scaled to
+  // them.  A page's maxima in LDS are older ones, no larger, where its own scores are near them.
+  __device__ __forceinline__ void take_up(Lds& lds, int step, int flag) {
+    if (flag == step) {
+#pragma unroll
+      for (int rg = 0; rg < 2; ++rg) {
+        const int r = row0 + 16 * rg + l16;
+        const float x = fmaxf(m[rg], fmaxf(lds.max[step & 1][0][r], lds.max[step & 1][1][r])), f = fexp2(ref[rg] - x);
+        l[rg] *= fexp2(m[rg] - x);
+        sum[rg] *= f;
+        m[rg] = x;
+        bf16x4& p = *reinterpret_cast<bf16x4*>(lds.p[step & 1] + place + 1024 * rg);
+        p = bf16x4{(__bf16)((float)p[0] * f), (__bf16)((float)p[1] * f), (__bf16)((float)p[2] * f), (__bf16)((float)p[3] * f)};
+      }
+      barrier_lds();
+    }
+    l[0] += sum[0];
+    l[1] += sum[1];
+  }
+  __device__ __forceinline__ void sums(Lds& lds) {
+#pragma unroll
+    for (int rg = 0; rg < 2; ++rg) {
+      const float x = xor32_add(xor16_add(l[rg]));
+      if (g16 == 0) lds.sum[page][row0 + 16 * rg + l16] = x;
+    }
+  }
+};
+
+// A value wave: a quarter of the channels of all rows.
+template <int DC, int DR> struct LatValues {
+  using Page = LatPage<DC, DR, true>;
+  using Lds = LatLds64<DC, DR>;
+  static constexpr int kTiles = DC / 4 / 32;        // of 32 channels
+  static constexpr int kAhead = 4;
+  f32x16 o[kTiles][2];
+  float m[2];                                       // of rows l32 and 32 + l32
+  bf16x8 p[2][2], value[kAhead];
+  int channel0, half, l32, at;
+
+  __device__ __forceinline__ void start(int wave) {
+    channel0 = DC / 4 * wave;
+    half = (threadIdx.x & 63) >> 5;
+    l32 = threadIdx.x & 31;
+    const int j = l32 & 15, r = 8 * half + (j >> 2), c = channel0 / 8 + 2 * (l32 >> 4) + ((j >> 1) & 1);
+    at = r * Page::kRowBytes + 16 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + 8 * (j & 1);
+    m[0] = m[1] = -FLT_MAX;
+#pragma unroll
+    for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][t][r] = 0.f;
+  }
+  // New maxima.  In asm, in place: the compiler would copy all outputs to and from other registers, in every step.  It does not know there
+  // that products still write them, so they are waited for (16 passes, 19 wait states at most).
+  __device__ __forceinline__ void take_up(const Lds& lds, int step) {
+    float alpha[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float x = fmaxf(m[t], fmaxf(lds.max[step & 1][0][32 * t + l32], lds.max[step & 1][1][32 * t + l32]));
+      alpha[t] = fexp2(m[t] - x);
+      m[t] = x;
+    }
+#pragma unroll
+    for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f32x16& y = o[d][t];
+        __asm__ volatile(
+            "s_nop 15\n\t"
+            "s_nop 7\n\t"
+            "v_mul_f32 %0, %0, %16\n\t"
+            "v_mul_f32 %1, %1, %16\n\t"
+            "v_mul_f32 %2, %2, %16\n\t"
+            "v_mul_f32 %3, %3, %16\n\t"
+            "v_mul_f32 %4, %4, %16\n\t"
+            "v_mul_f32 %5, %5, %16\n\t"
+            "v_mul_f32 %6, %6, %16\n\t"
+            "v_mul_f32 %7, %7, %16\n\t"
+            "v_mul_f32 %8, %8, %16\n\t"
+            "v_mul_f32 %9, %9, %16\n\t"
+            "v_mul_f32 %10, %10, %16\n\t"
+            "v_mul_f32 %11, %11, %16\n\t"
+            "v_mul_f32 %12, %12, %16\n\t"
+            "v_mul_f32 %13, %13, %16\n\t"
+            "v_mul_f32 %14, %14, %16\n\t"
+            "v_mul_f32 %15, %15, %16\n\t"
+            "s_nop 3"
+            : "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]), "+v"(y[4]), "+v"(y[5]), "+v"(y[6]), "+v"(y[7]), "+v"(y[8]), "+v"(y[9]),
+              "+v"(y[10]), "+v"(y[11]), "+v"(y[12]), "+v"(y[13]), "+v"(y[14]), "+v"(y[15])
+            : "v"(alpha[t]));
+      }
+  }
+  // Operand i of a stage's products: page i / kTiles, channels 32 (i % kTiles) .. of the wave's.
+  __device__ __forceinline__ bf16x8 value_of(const char* stage, int i) const {
+    // at: the lane's row of 8 (l / 32) + 0 .. 3 of the values, channels of tile 0; four rows further the swizzle differs in chunk bit 0
+    const int at4 = (at ^ 16) + 4 * Page::kRowBytes;
+    const char* const page = stage + i / kTiles * Page::kBytes;
+    return concat_tr(lds_read_tr(page, at ^ (64 * (i % kTiles))), lds_read_tr(page, at4 ^ (64 * (i % kTiles))));
+  }
+  __device__ __forceinline__ void first(const char* stage) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) value[i] = value_of(stage, i);
+  }
+  __device__ __forceinline__ void weights(const Lds& lds, int step) {
+    const char* const from = lds.p[step & 1] + l32 * 64;
+#pragma unroll
+    for (int page = 0; page < 2; ++page)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        p[page][t] = as_bf16x8(*reinterpret_cast<const u32x4*>(from + 2048 * t + 16 * ((2 * page + half) ^ ((l32 >> 2) & 3))));
+  }
+  // The stage's products, behind first() and weights().
+  __device__ __forceinline__ void add(const char* stage) {
+#pragma unroll
+    for (int i = 0; i < 2 * kTiles; ++i) {
+      const int page = i / kTiles, d = i % kTiles;
+      const bf16x8 x = value[i % kAhead];
+      o[d][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[page][0], o[d][0], 0, 0, 0);
+      o[d][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[page][1], o[d][1], 0, 0, 0);
+      if (i + kAhead < 2 * kTiles) value[i % kAhead] = value_of(stage, i + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+}  // namespace
+
+template <int DC, int DR>
+__global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a) {
+  using Page = LatPage<DC, DR, true>;
+  using Copies = LatHalfCopies<DC, DR>;
+  using Lds = LatLds64<DC, DR>;
+  constexpr int M = 64;
+  __shared__ __attribute__((aligned(256))) Lds lds;
+  const int tid = threadIdx.x, w = uni(tid >> 6);
+  clear_notes(lds.notes);
+  if (tid == 0) lds.flag[0] = lds.flag[1] = -1;
+  LatWork work;
+  if (!lat_find<M, kWaves64>(a, lds.find, work)) return;
+  int step = 0;                                     // of the workgroup, over all tiles
+  int* limits = lds.notes.limit;                    // in turn with limit2: the value waves may still read the tile's before
+  do {
+    work.tile<M>();
+    if (work.j0 >= work.j1) continue;
+    const LatSeq seq = work.seq;
+    const int r0 = work.r0, n_rows = work.n_rows, last = seq.ctx + (r0 + n_rows - 1) / a.heads;   // the last key
+    const int first_limit = seq.ctx + r0 / a.heads;        // keys behind it are not all rows'
+    const int i0 = 2 * work.j0, n = min(2 * work.j1, (last >> kStageShift) + 1) - i0;   // stages
+    const bool in_part = last != first_limit;
+    auto look = [&](int i) { return in_part && ((i0 + i) << kStageShift) + kStageKeys - 1 > first_limit; };   // keys that rows see in part
+    if (tid < M) limits[tid] = seq.ctx + (r0 + min(tid, n_rows - 1)) / a.heads;
+    if (w < 4) {
+      LatScores<DC, DR> x;
+      __builtin_amdgcn_s_setprio(3);
+      x.start(lds, w, args_anew()->q + work.row0 * (DC + DR), n_rows);
+#pragma unroll 1
+      for (int i = 0; i <= n; ++i, ++step) {
+        barrier_lds();
+        const int key0 = (i0 + i) << kStageShift;
+        const int flag = i < n ? x.scores(lds, lds.page[i % kStages][0], step) : uni(lds.flag[(step - 1) & 1]);
+        if (i > 0) {
+          x.take_up(lds, step - 1, flag);
+          if (look(i - 1)) barrier_lds();           // while the value waves see to values that are not finite
+        }
+        if (i == n) continue;
+        if (key0 + kStageKeys - 1 > first_limit) x.mask(limits, key0);
+        x.weigh(lds, step, a.scale_log2);
+      }
+      x.sums(lds);
+      barrier_lds();
+    } else {
+      const int part = w & 1, page = (w >> 1) & 1;  // half `part` of page `page` of a stage is this wave's to bring
+      const int kv = seq.ctx + seq.q_len, pages = (kv + kPage - 1) / kPage;
+      const int32_t* const bt = a.block_table + (size_t)work.b * a.bt_stride;
+      // Ids of 64 stages' pages at once (the sequence's last one where there is none; zeros take its place).  They are waited for here: the
+      // compiler, which does not know of the copies, would wait in every step, for these too.
+      auto ids_from = [&](int i) {
+        int ids = bt[min(2 * (i0 + i + (tid & 63)) + page, pages - 1)];
+        __asm__ volatile("" : "+v"(ids));
+        return ids;
+      };
+      int ids = ids_from(0);
+      auto source = [&](int i) {                    // of stage i
+        const int id = __builtin_amdgcn_readlane(ids, i & 63);
+        return reinterpret_cast<const char*>(a.cache) + (size_t)clamp_page(id, a.num_pages) * Page::kBytes;
+      };
+      const unsigned pages_at = lds_address(lds.page[0][page]);
+      constexpr int kStageBytes = 2 * Page::kBytes;
+      Copies copies;
+      copies.start(part);
+      LatValues<DC, DR> x;
+      auto bring = [&](int i) {
+        const char* const src = source(i);
+#pragma unroll
+        for (int c = 0; c < Copies::kCopies; c += 2) copies.copy2(c, part, src, pages_at + i % kStages * kStageBytes, 1);
+      };
+      bring(0);
+      if (n > 1) bring(1);
+      x.start(w - 4);
+      // Behind it a stage of this wave's is there for all, and the one after it on its way.
+      auto arrive = [&](int i) {
+        if (i + 1 < n) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");
+        else wait_copies();
+        const int valid = kv - ((i0 + i) << kStageShift) - kPage * page;
+        if (i < n && valid < kPage) Copies::clear(lds.page[i % kStages][page], part, max(valid, 0));
+        barrier_lds();
+      };
+      arrive(0);
+      if (n > 2) bring(2);
+      ++step;
+#pragma unroll 1
+      for (int i = 1; i <= n; ++i, ++step) {
+        const char* const stage = lds.page[(i - 1) % kStages][0];
+        x.first(stage);                             // before the weights are there
+        if (((i + 2) & 63) == 0) ids = ids_from(i + 2);
+        const char* const src = source(i + 2);
+        arrive(i);
+        if (look(i - 1)) {
+          note_odd<Page>(lds.page[(i - 1) % kStages][page], ((i0 + i - 1) << kStageShift) + kPage * page, lds.notes, 8 * part, 8 * part + 8);
+          barrier_lds();
+          x.first(stage);
+        }
+        const int flag = lds.flag[(step - 1) & 1];
+        x.weights(lds, step - 1);
+        if (uni(flag) == step - 1) {
+          x.take_up(lds, step - 1);
+          barrier_lds();
+          x.weights(lds, step - 1);
+        }
+        // All copies at once, while the score waves have the matrix units; these waves' products are made while the others weigh.
+        const int more = i + 2 < n;
+#pragma unroll
+        for (int c = 0; c < Copies::kCopies; c += 2) copies.copy2(c, part, src, pages_at + (i + 2) % kStages * kStageBytes, more);
+        x.add(stage);
+      }
+      // ---- the output or the partial
+      barrier_lds();
+      const LatArgsPtr args = args_anew();
+      const bool odd = uni(lds.notes.any_odd) != 0, whole = work.starts && work.ends;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int r = 32 * t + x.l32, limit = limits[r];
+        const float l = lds.sum[0][r] + lds.sum[1][r], f = whole ? 1.f / l : 1.f;
+#pragma unroll
+        for (int d = 0; d < LatValues<DC, DR>::kTiles; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int channel = x.channel0 + 32 * d + 8 * e + 4 * x.half;
+            f32x4 y = f32x4{x.o[d][t][4 * e], x.o[d][t][4 * e + 1], x.o[d][t][4 * e + 2], x.o[d][t][4 * e + 3]} * f;
+            if (odd)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (lds.notes.odd[channel + k] <= limit) y[k] = __builtin_nanf("");
+            if (!whole)
+              *reinterpret_cast<f32x4*>(args->part_o + ((size_t)work.slot * M + r) * DC + channel) = y;
+            else if (r < n_rows)
+              *reinterpret_cast<bf16x4*>(args->out + (work.row0 + r) * DC + channel) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+          }
+        if (x.channel0 == 0 && x.half == 0) {
+          if (!whole) reinterpret_cast<float2*>(args->part_ml)[(size_t)work.slot * M + r] = float2{x.m[t], l};
+          else if (args->lse && r < n_rows) args->lse[work.row0 + r] = (x.m[t] + flog2(l)) * kLn2;
+        }
+      }
+    }
+    // The notes are cleared by all, behind a barrier; else the score waves go on to the next tile's queries.
+    if (in_part) {
+      barrier_lds();
+      if (uni(lds.notes.any_odd) != 0) {
+        barrier_lds();
+        clear_notes(lds.notes);
+      }
+    }
+    limits = limits == lds.limit2 ? lds.notes.limit : lds.limit2;
+  } while (work.next(a));
+  if (tid == 0) args_anew()->jobs[work.index] = work.job;
+}
+
+hipError_t launch_latent64(const LatentArgs& a, int latent_dim, hipStream_t stream) {
+  const dim3 grid(kLatentGrid), threads(64 * kWaves64);
+  if (latent_dim == 512) hipLaunchKernelGGL((latent64_kernel<512, 64>), grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((latent64_kernel<256, 32>), grid, threads, 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace pearl

@@ -1,0 +1,382 @@
+// What the gfx950 kernels of attention over latent rows (latent16.hip, latent64.hip) share: a page's place in LDS, the cut of the
+// work, and values that are not finite.
+#pragma once
+
+#include "attn_device.h"
+
+#include <float.h>
+
+namespace pearl {
+namespace {
+
+constexpr int kLatWaves = 4;
+constexpr int kLatThreads = 64 * kLatWaves;
+constexpr int kLatKeysShift = 6, kLatKeys = 1 << kLatKeysShift;   // of a stage: where work is cut
+constexpr float kLag = 8.f;
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void barrier_lds() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void wait_copies() { __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ float xor16_max(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+__device__ __forceinline__ float xor16_add(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+
+// Keep a value in vector or in accumulation registers at this place.  The outputs stay in vector registers, which the rare stages that
+// scale them need, and the queries in accumulation registers, from which the products read them; left to itself the compiler moves
+// the outputs between the two in every stage.
+template <typename T> __device__ __forceinline__ void in_vector(T& x) { __asm__ volatile("" : "+v"(x)); }
+__device__ __forceinline__ void in_acc(bf16x8& x) { __asm__ volatile("" : "+a"(x)); }
+
+// The kernel's arguments, read anew where they are used outside the stages: kept over them, they would be spilled.
+typedef const __attribute__((address_space(4))) LatentArgs* LatArgsPtr;
+__device__ __forceinline__ LatArgsPtr args_anew() {
+  LatArgsPtr p = (LatArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  __asm__ volatile("" : "+s"(p));
+  return p;
+}
+
+__device__ __forceinline__ unsigned lds_address(const char* p) { return (unsigned)(uintptr_t)((LDS_AS const char*)p); }
+
+__device__ __forceinline__ long long uni64(long long x) {
+  const unsigned lo = uni((int)x), hi = uni((int)(x >> 32));
+  return (long long)((unsigned long long)hi << 32 | lo);
+}
+
+// The first channel of the 8 that lane group g (of 16 lanes) takes in step k of the scores' product, of 32 channels: the same for keys and
+// queries.  The latent part goes in 128 channels at a time, each group through 32 of them, so that the groups' chunks of 16 bytes
+// differ in bits 2 and 3.
+template <int DC> __device__ __forceinline__ constexpr int lat_channel(int k, int g) {
+  return k < DC / 32 ? 128 * (k >> 2) + 32 * g + 8 * (k & 3) : 32 * k + 8 * g;
+}
+
+// A page in LDS: 16 rows of DC channels, then 16 rows of DR.  Chunk (16 bytes) c of latent row r is in slot c ^ f(r) of
+// its 16, f a permutation of the rows.  A 16 byte read of a row a lane is served 16 lanes at a time, rows 0-3 and 12-15 of one lane group with
+// rows 4-11 of its neighbour: f and lat_channel put these into 16 slots (with neighbouring chunks in the groups such reads take twice
+// as long: a third of all LDS cycles at 64 rows).  The transposing reads of 32 lanes take two
+// chunks of each of 8 consecutive rows at M = 16 (kWide false), four chunks of 4 consecutive rows at M = 64: f keeps these apart likewise.
+// Chunk c of the rotated part is in slot c ^ (r / 2) (DR = 64; at 32, where 4 rows share the banks, c ^ (0, 2, 3, 1)[r / 4]).
+template <int DC, int DR, bool kWide> struct LatPage {
+  static constexpr int kWidth = (DC + DR) * 2;      // bytes of a cached row
+  static constexpr int kRowBytes = DC * 2, kRotBytes = DR * 2;
+  static constexpr int kRot = kPage * kRowBytes;    // offset of the rotated parts
+  static constexpr int kBytes = kPage * kWidth;
+  static_assert(kBytes % 256 == 0 && kRowBytes % 256 == 0, "the swizzle takes address bits 4 .. 7");
+  __device__ static __forceinline__ constexpr int f(int r) {
+    return kWide ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 7) << 1) | (r >> 3);
+  }
+  __device__ static __forceinline__ constexpr int rot_f(int r) { return DR == 64 ? (r >> 1) & 7 : 0x78 >> (2 * (r >> 2)) & 3; }
+};
+
+// The copies of a page by a wave, 1 KiB an instruction, kRows rows' latent parts each, and then the rotated parts.
+// kWide: as LatPage's; without it, where a key is read by one workgroup, the copies go past the caches (nt).
+template <int DC, int DR, bool kWide> struct LatCopies {
+  using Page = LatPage<DC, DR, kWide>;
+  static constexpr int kRows = 1024 / Page::kRowBytes;
+  static constexpr int kLatent = kPage / kRows, kCopies = kLatent + kPage * Page::kRotBytes / 1024;
+  static_assert(kLatent % 2 == 0 && Page::kWidth % 32 == 0 && (DR == 32 || Page::kWidth % 128 == 0), "copies in pairs; the swizzle's bits");
+
+  // The lane's source offset in the page, of copy i.
+  __device__ static __forceinline__ int offset(int i) {
+    const int l = threadIdx.x & 63;
+    if (i < kLatent) {
+      const int r = kRows * i + (kRows == 2 ? l >> 5 : 0), slot = kRows == 2 ? l & 31 : l;
+      return r * Page::kWidth + 16 * (slot ^ Page::f(r));
+    }
+    constexpr int kChunks = Page::kRotBytes / 16;
+    const int r = (64 * (i - kLatent) + l) / kChunks;
+    return r * Page::kWidth + Page::kRowBytes + 16 * ((l % kChunks) ^ Page::rot_f(r));
+  }
+
+  // Copies i and (if there is one) i + 1 of the page at src to the page at the LDS address lds, if `go`.  The branch is the
+  // instructions' own: one that the compiler sees splits the products' code in two, with moves of all outputs between them.  An
+  // instruction's immediate offset advances both addresses.  (i is a constant where this is inlined.)
+  __device__ static __forceinline__ void copy2(int i, const char* src, unsigned lds, int go) {
+    const unsigned to = uni((int)lds + 1024 * i);
+#define PEARL_LATENT_COPY(SECOND, NT)                                                                                          \
+  __asm__ volatile("s_cmp_eq_u32 %4, 0\n\t"                                                                                    \
+                   "s_cbranch_scc1 .Lno_copy%=\n\t"                                                                            \
+                   "s_mov_b32 m0, %3\n\t"                                                                                      \
+                   "s_nop 0\n\t"                                                                                               \
+                   "global_load_lds_dwordx4 %0, %2" NT "\n\t" SECOND ".Lno_copy%=:"                                           \
+                   :                                                                                                           \
+                   : "v"(offset(i)), "v"(offset(i + 1) - 1024), "s"(src), "s"(to), "s"(uni(go))                                \
+                   : "memory", "scc", "m0")
+    if (kWide) {
+      if (i + 1 < kCopies) PEARL_LATENT_COPY("global_load_lds_dwordx4 %1, %2 offset:1024\n", "");
+      else PEARL_LATENT_COPY("", "");
+    } else {
+      if (i + 1 < kCopies) PEARL_LATENT_COPY("global_load_lds_dwordx4 %1, %2 offset:1024 nt\n", " nt");
+      else PEARL_LATENT_COPY("", " nt");
+    }
+#undef PEARL_LATENT_COPY
+  }
+
+  __device__ static __forceinline__ void page(const char* src, unsigned lds) {
+#pragma unroll
+    for (int i = 0; i < kCopies; i += 2) copy2(i, src, lds, 1);
+  }
+
+  // Zeros in place of the rows from `valid` on.
+  __device__ static __forceinline__ void clear(char* page, int valid) {
+    const int l = threadIdx.x & 63;
+    for (int i = valid * Page::kRowBytes + 16 * l; i < Page::kRot; i += 1024) *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+    for (int i = Page::kRot + valid * Page::kRotBytes + 16 * l; i < Page::kBytes; i += 1024)
+      *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+  }
+};
+
+// What finding a workgroup's share takes.
+struct LatFind {
+  long long sum[8], before;                         // a wave each
+  int found, bad;
+};
+
+// Both kernels' notes on a tile.
+template <int DC, int M> struct LatNotes {
+  int odd[DC];                                      // of each channel: the first key with a value that is not finite and ..
+  int any_odd;                                      // .. whether there is one, among those that only some of the tile's rows see
+  int limit[M];                                     // the last key that a row sees
+};
+
+// ---- the plan --------------------------------------------------------------------------------------------------------
+// A sequence's rows are cut into tiles of `tile_rows` (group * M).  Work is measured in keys: tile u costs its keys, kTileCost and
+// what its rows add, such that the cost of tiles 0 .. u - 1 is u (ctx + kTileCost) + (u (u + 1) slope >> 8), slope
+// being 256 times half the tokens of a tile.
+constexpr int kTileCost = 64;
+
+struct LatSeq {
+  int q_start, q_len, ctx;
+};
+
+struct LatPlan {
+  int tile_rows, tile_shift, slope, heads;          // tile_rows = 1 << tile_shift
+  __device__ __forceinline__ long long before(const LatSeq& s, long long u) const {
+    return u * (s.ctx + kTileCost) + ((u * (u + 1) * slope) >> 8);
+  }
+  __device__ __forceinline__ int tiles(const LatSeq& s) const {
+    return (s.q_len * heads + tile_rows - 1) >> tile_shift;   // at most 2^21 tokens of 128 heads
+  }
+  // stages of the keys that rows up to `row` see
+  __device__ __forceinline__ int stages(const LatSeq& s, int row) const {
+    return (s.ctx + row / heads + 1 + kLatKeys - 1) / kLatKeys;
+  }
+  // the stage at which cost `at` of a tile that starts at 0 is cut
+  __device__ __forceinline__ static int stage_at(long long at, int stages) {
+    const long long j = (at - kTileCost) >> kLatKeysShift;
+    return j < 0 ? 0 : j > stages ? stages : (int)j;
+  }
+  // the tile that cost `at` of a sequence falls into
+  __device__ __forceinline__ int tile_at(const LatSeq& s, long long at) const {
+    int lo = 0, hi = tiles(s);                      // before(lo) <= at < before(hi)
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (before(s, mid) <= at) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
+
+// `total` cut into `shares`, which differ by 1 at most.
+struct LatShares {
+  long long each;
+  int more, shares;                                 // the first `more` are one longer
+  LatShares() = default;
+  __device__ __forceinline__ LatShares(long long total, int n) : shares(n) {
+    each = uni64((long long)((double)total / (double)n));       // exact, below 2^53, or off by 1
+    while (each * n > total) --each;
+    while (total - each * n >= n) ++each;
+    more = (int)(total - each * n);
+  }
+  __device__ __forceinline__ long long start(int s) const { return each * s + min(s, more); }
+  // the share that position `at` is in
+  __device__ __forceinline__ int of(long long at) const {
+    int s = min((int)((float)at / (float)each), shares - 1);   // off by 1 at most
+    while (s > 0 && start(s) > at) --s;
+    while (s + 1 < shares && start(s + 1) <= at) ++s;
+    return s;
+  }
+};
+
+__device__ __forceinline__ LatSeq lat_seq(const LatentArgs& a, int b) {
+  if (!a.cu) return LatSeq{b, 1, a.ctx_lens[b]};
+  const int start = a.cu[b];
+  return LatSeq{start, a.cu[b + 1] - start, a.ctx_lens[b]};
+}
+
+// The same of one sequence for the whole wave, in scalar registers.
+__device__ __forceinline__ LatSeq lat_seq_uni(const LatentArgs& a, int b) {
+  const LatSeq s = lat_seq(a, b);
+  return LatSeq{uni(s.q_start), uni(s.q_len), uni(s.ctx)};
+}
+
+__device__ __forceinline__ bool lat_bad(const LatentArgs& a, const LatSeq& s) {
+  const long long kv = (long long)s.ctx + s.q_len;
+  return s.q_len < 0 || s.ctx < 0 || s.q_start < 0 || s.q_len > a.max_q_len || (long long)s.q_start + s.q_len > a.total_q ||
+         kv > a.max_kv_len || (kv + kPage - 1) / kPage > a.bt_stride;
+}
+
+__device__ __forceinline__ long long shfl_up64(long long x, int d) {
+  const int lo = __shfl_up((int)x, d), hi = __shfl_up((int)(x >> 32), d);
+  return (long long)(((unsigned long long)(unsigned)hi << 32) | (unsigned)lo);
+}
+
+// A workgroup's work: the tiles of its share, of each the workgroup's member and the stages.
+struct LatWork {
+  LatPlan plan;
+  LatShares cut;
+  LatSeq seq;
+  long long at, lo, hi;                             // cost before the sequence; of the share
+  int index, share, member, b, u;
+  int4 job;
+  // the tile at hand
+  long long t1;
+  int r0, n_rows, j0, j1, slot;
+  size_t row0;
+  bool starts, ends;                                // the share has the tile's first key, its last one
+
+  template <int M> __device__ __forceinline__ void tile() {
+    const long long t0 = at + plan.before(seq, u);
+    t1 = at + plan.before(seq, u + 1);
+    const int rows = seq.q_len * plan.heads;        // below 2^28 (2^21 tokens, 128 heads)
+    const int all_stages = plan.stages(seq, min((u + 1) * plan.tile_rows, rows) - 1);
+    r0 = u * plan.tile_rows + member * M;
+    n_rows = min(M, rows - r0);
+    starts = t0 >= lo;
+    ends = t1 <= hi;
+    slot = 2 * index + (starts ? 1 : 0);
+    row0 = (size_t)seq.q_start * plan.heads + r0;
+    j0 = j1 = 0;
+    if (n_rows <= 0) return;
+    const int stages = plan.stages(seq, r0 + n_rows - 1);
+    j0 = starts ? 0 : min(LatPlan::stage_at(lo - t0, all_stages), stages);
+    j1 = ends ? stages : min(LatPlan::stage_at(hi - t0, all_stages), stages);
+    if (starts && !ends) job = int4{(int)row0, n_rows, index, cut.of(t1 - 1) - share + 1};
+    // a piece of a cut tile without keys
+    if (j0 >= j1 && !(starts && ends) && threadIdx.x < M)
+      reinterpret_cast<float2*>(args_anew()->part_ml)[(size_t)slot * M + threadIdx.x] = float2{-FLT_MAX, 0.f};
+  }
+  // Whether there is a tile after this one.
+  __device__ __forceinline__ bool next(const LatentArgs& a) {
+    if (t1 >= hi) return false;
+    if (++u == plan.tiles(seq)) {
+      at = t1;
+      u = 0;
+      do seq = lat_seq_uni(a, ++b);
+      while (seq.q_len == 0);
+    }
+    return true;
+  }
+};
+
+// Finds the workgroup's share; false: it has none.  Workgroups with one number modulo `group` take the same member of the tiles, and shares
+// of an XCD's workgroups follow one another.
+template <int M, int kWaves> __device__ __forceinline__ bool lat_find(const LatentArgs& a, LatFind& lds, LatWork& work) {
+  constexpr int kThreads = 64 * kWaves;
+  const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6);
+  const int group = a.group;
+  const int per_xcd = (int)gridDim.x / kNumXcd;
+  work.index = (int)(blockIdx.x % kNumXcd) * per_xcd + (int)(blockIdx.x / kNumXcd);
+  work.share = work.index / group;
+  work.member = work.index - work.share * group;
+  work.plan = LatPlan{group * M, __builtin_ctz(group * M), a.slope, a.heads};
+  work.job = int4{0, 0, 0, 0};
+  if (tid == 0) lds.bad = 0;
+  __syncthreads();
+  const int per = (a.batch + kThreads - 1) / kThreads;
+  long long mine = 0;
+  {
+    bool bad = false;
+    for (int i = 0; i < per; ++i) {
+      const int b = tid * per + i;
+      if (b >= a.batch) break;
+      const LatSeq s = lat_seq(a, b);
+      if (lat_bad(a, s)) bad = true;
+      else mine += work.plan.before(s, work.plan.tiles(s));
+    }
+    if (bad) lds.bad = 1;
+  }
+  long long upto = mine;                            // of this wave's threads up to this one
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long y = shfl_up64(upto, d);
+    if (lane >= d) upto += y;
+  }
+  if (lane == 63) lds.sum[w] = upto;
+  __syncthreads();
+  if (blockIdx.x == 0 && tid == 0) a.ws_hdr[kHdrError] = lds.bad;
+  long long total = 0;
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) {
+    if (v == w) upto += total;
+    total += uni64(lds.sum[v]);
+  }
+  int shares = (int)gridDim.x / group;
+  if (total < (long long)shares << a.min_share_shift) shares = (int)max(1ll, total >> a.min_share_shift);
+  if (uni(lds.bad) || total == 0 || work.share >= shares) {
+    if (tid == 0) a.jobs[work.index] = work.job;
+    return false;
+  }
+  work.cut = LatShares(total, shares);
+  const long long lo = work.cut.start(work.share);
+  work.lo = lo;
+  work.hi = work.cut.start(work.share + 1);
+  if (upto - mine <= lo && lo < upto) {
+    lds.found = tid;
+    lds.before = upto - mine;
+  }
+  __syncthreads();
+  work.b = uni(lds.found) * per;
+  work.at = uni64(lds.before);
+  work.seq = lat_seq_uni(a, work.b);
+  for (;;) {
+    const long long c = work.plan.before(work.seq, work.plan.tiles(work.seq));
+    if (lo < work.at + c) break;
+    work.at += c;
+    work.seq = lat_seq_uni(a, ++work.b);
+  }
+  work.u = work.plan.tile_at(work.seq, lo - work.at);
+  return true;
+}
+
+// Keys that only some of the rows see have weight 0 in the others, and 0 times a value that is not finite is NaN.  So such a value becomes 0, in the
+// page at hand (key0: its first key), and its channel is noted.  (The value is part of its key too: in rows that see it its score is NaN or infinite, so its
+// channel's output is NaN there, if not the whole row, which is what the end of the tile makes of the note.)
+// Rows r0 .. r1 - 1 of the page.
+template <typename Page, int DC, int M> __device__ __forceinline__ void note_odd(char* page, int key0, LatNotes<DC, M>& notes, int r0 = 0, int r1 = kPage) {
+  for (int i = r0 * (DC / 8) + (threadIdx.x & 63); i < r1 * (DC / 8); i += 64) {
+    const int r = i / (DC / 8), c = i % (DC / 8);
+    u32x4 v = *reinterpret_cast<const u32x4*>(page + 16 * i);
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t half = e & 1 ? 0x7f800000u : 0x7f80u;
+      if ((v[e >> 1] & half) == half) {
+        v[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
+        atomicMin(&notes.odd[8 * ((c & ~15) | ((c & 15) ^ Page::f(r))) + e], key0 + r);
+        bad = true;
+      }
+    }
+    if (bad) {
+      *reinterpret_cast<u32x4*>(page + 16 * i) = v;
+      notes.any_odd = 1;
+    }
+  }
+}
+
+template <int DC, int M> __device__ __forceinline__ void clear_notes(LatNotes<DC, M>& notes) {
+  for (int i = threadIdx.x; i < DC; i += blockDim.x) notes.odd[i] = INT32_MAX;
+  if (threadIdx.x == 0) notes.any_odd = 0;
+}
+
+}  // namespace
+}  // namespace pearl

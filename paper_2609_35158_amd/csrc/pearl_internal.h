@@ -1,5 +1,5 @@
 // Internal interface between the C-ABI host layer (api.cpp) and the gfx950 kernels
-// (attn_kernels.hip, decode_mx.hip, kv_pages.hip, kv_mx.hip, rope.hip, latent.hip).  Not installed; callers use include/pearl_attn.h.
+// (attn_kernels.hip, decode_mx.hip, kv_pages.hip, kv_mx.hip, rope.hip, latent16.hip, latent64.hip).  Not installed; callers use include/pearl_attn.h.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -237,7 +237,7 @@ hipError_t launch_rope(const RopeArgs& r, const RopeSeqs& seqs, const RopeRows& 
 hipError_t launch_latent_append(const RopeArgs& r, const RopeSeqs& seqs, const LatentRows& rows, int latent_dim, int rope_dim,
                                 hipStream_t stream);
 
-// Attention over a cache of latent vectors (latent.hip).
+// Attention over a cache of latent vectors (latent16.hip, latent64.hip).
 struct LatentArgs {
   const uint16_t* q;
   const uint16_t* cache;
@@ -254,11 +254,12 @@ struct LatentArgs {
   int heads;
   int group;                 // workgroups that take neighbouring tiles of one share
   int slope;                 // 128 group * tile / heads
-  int min_share;             // keys of a share, at least
+  int min_share_shift;       // a share has 2^this keys, at least
   float scale_log2;
 };
 // merge: the join of cut tiles, launched after the attention itself.
 hipError_t launch_latent(const LatentArgs& a, int latent_dim, int tile, bool merge, hipStream_t stream);
+hipError_t launch_latent64(const LatentArgs& a, int latent_dim, hipStream_t stream);
 
 hipError_t launch_plan(const PlanParams& p, const int32_t* ctx_lens, const int32_t* cu_q_lens,
                        void* workspace, const WsLayout& lay, hipStream_t stream);
