@@ -254,6 +254,7 @@ pearl_status run_latent(bool decode, const pearl_latent_shape* s, const pearl_se
   a.max_q_len = q->max_q_len;
   a.max_kv_len = q->max_kv_len;
   a.heads = s->num_q_heads;
+  a.per_head = ((1ull << 35) + s->num_q_heads - 1) / s->num_q_heads;
   a.group = p.group;
   a.slope = 128 * p.group * p.tile / s->num_q_heads;
   a.min_share_shift = p.tile == 16 ? 7 : 8;

@@ -38,13 +38,14 @@ template <int DC, int DR> struct LatRows16 {
   f32x4 o[kBlocks], s;
   float m, l;
   int g16, l16;
+  LatOperand<Page> operand;
 
-  __device__ __forceinline__ void start(const uint16_t* rows, int n_rows) {
+  __device__ __forceinline__ void start(const char* queries) {
     g16 = (threadIdx.x & 63) >> 4;
     l16 = threadIdx.x & 15;
-    const uint16_t* const src = rows + min(l16, n_rows - 1) * (size_t)(DC + DR);
+    operand.start(l16, g16);
 #pragma unroll
-    for (int k = 0; k < kAll; ++k) q[k] = as_bf16x8(ld16(src + lat_channel<DC>(k, g16)));
+    for (int k = 0; k < kAll; ++k) q[k] = operand.get(queries, k);
     m = -FLT_MAX;
     l = 0.f;
 #pragma unroll
@@ -55,10 +56,7 @@ template <int DC, int DR> struct LatRows16 {
     for (int k = 0; k < kAll; ++k) in_acc(q[k]);
   }
   __device__ __forceinline__ void scores(const char* page) {
-    const int at = l16 * Page::kRowBytes + 16 * ((4 * g16) ^ Page::f(l16)), rot = Page::kRot + l16 * Page::kRotBytes + 16 * (g16 ^ Page::rot_f(l16));
-    auto key_of = [&](int k) {
-      return as_bf16x8(*reinterpret_cast<const u32x4*>(page + (k < kSteps ? (at ^ (16 * (k & 3))) + 256 * (k >> 2) : rot ^ (64 * (k - kSteps)))));
-    };
+    auto key_of = [&](int k) { return operand.get(page, k); };
     bf16x8 key[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
@@ -132,13 +130,14 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
     work.tile<M>();
     if (work.j0 >= work.j1) continue;
     const LatSeq seq = work.seq;
-    const int r0 = work.r0, n_rows = work.n_rows, last = seq.ctx + (r0 + n_rows - 1) / a.heads;   // the last key
+    const int r0 = work.r0, n_rows = work.n_rows, last = seq.ctx + work.plan.token(r0 + n_rows - 1);   // the last key
     const int kv = seq.ctx + seq.q_len, p1 = min(work.j1 * kLatWaves, last / kPage + 1);
-    const int first_limit = seq.ctx + r0 / a.heads;        // keys behind it are not all rows'
+    const int first_limit = seq.ctx + work.plan.token(r0);   // keys behind it are not all rows'
     const bool in_part = last != first_limit;
     const int32_t* const bt = a.block_table + (size_t)work.b * a.bt_stride;
-    // Ids of 64 of the wave's pages at once, lane i's page p + 4 i.  They are waited for here, and the queries before the loop: the compiler,
-    // which does not know of the copies, would wait in every page, for these too.
+    lat_queries<Page>(args_anew()->q + work.row0 * (DC + DR), n_rows, buffers + Page::kBytes);
+    // Ids of 64 of the wave's pages at once, lane i's page p + 4 i.  They are waited for here: the compiler, which does not know of the copies,
+    // would wait in every page, for these too.
     auto ids_from = [&](int p) {
       int ids = bt[min(p + kLatWaves * lane, p1 - 1)];
       __asm__ volatile("" : "+v"(ids));
@@ -151,8 +150,10 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
     int p = work.j0 * kLatWaves + w, ids = ids_from(p), i = 0;   // i: the page's number among the ids
     if (p < p1) Copies::page(page_at(ids, 0), lds_address(buffers));
     Rows x;
-    x.start(args_anew()->q + work.row0 * (DC + DR), n_rows);
-    if (tid < M) lds.notes.limit[tid] = seq.ctx + (r0 + min(tid, n_rows - 1)) / a.heads;
+    if (p < p1) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");   // the queries
+    else wait_copies();
+    x.start(buffers + Page::kBytes);
+    if (tid < M) lds.notes.limit[tid] = seq.ctx + work.plan.token(r0 + min(tid, n_rows - 1));
     x.pin_queries();
     barrier_lds();
     int parity = 0;
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
 
 // Joins the partials of a cut tile: job (first row, rows, index of the first piece's workgroup, shares).  Its first piece is in slot
 // 1 of that workgroup, the others in slot 0 of the shares that follow, in order (kLatentGrid pieces at most).  A lane takes DC / 64 channels of a
-// row.  Few pieces: a wave a row.  Many: the waves take a fourth of them each, row by row.  Workgroups run on the XCD that wrote the first piece.
+// row.  Few pieces: a wave a row.  Many: the waves take a fourth of them each, row by row.  Where all workgroups had a share, these run on the XCD that wrote the first piece.
 template <int DC, int M>
 __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a) {
   static_assert(kLatentGrid <= 64 * kLatWaves, "a lane a piece");
@@ -261,7 +262,7 @@ __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a)
   __shared__ float s_top[kLatWaves], s_sum[kLatWaves];
   __shared__ __attribute__((aligned(16))) float s_o[kLatWaves][DC];
   const int lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6), n = job.w, end = min(r0 + kRows, job.y);
-  const bool few = n <= 16;
+  const bool few = n <= (M == 16 ? 16 : 64);
   const int first = few ? 0 : w, step = few ? 1 : kLatWaves, mine = n > first ? (n - first + step - 1) / step : 0;   // this wave's pieces
   auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * job.z + 1 : 2 * (job.z + i * a.group)) * M; };
   for (int r = few ? r0 + w : r0; r < end; r += few ? kLatWaves : 1) {

@@ -94,19 +94,26 @@ template <int DC, int DR> struct LatScores {
   bf16x8 q[2][kAll];
   f32x4 s[2];
   float m[2], l[2], sum[2], ref[2];
+  LatOperand<Page> operand;
   int page, row0, g16, l16, place;                  // place: of the lane's weights among a stage's
 
+  // The queries come as pages through the last two stages; wave 2 h + p brings rows 32 h + 16 p ..
   __device__ __forceinline__ void start(Lds& lds, int wave, const uint16_t* rows, int n_rows) {
     page = wave & 1;
-    row0 = 32 * (wave >> 1);
+    const int h = wave >> 1;
+    row0 = 32 * h;
+    const int first = min(row0 + 16 * page, n_rows - 1);
+    lat_queries<Page>(rows + first * (DC + DR), min(n_rows - first, kPage), lds.page[2 + h][page]);
     g16 = (threadIdx.x & 63) >> 4;
     l16 = threadIdx.x & 15;
+    operand.start(l16, g16);
     place = (row0 + l16) * 64 + 16 * ((2 * page + (g16 >> 1)) ^ (l16 >> 2)) + 8 * (g16 & 1);
+    wait_copies();
+    barrier_lds();
 #pragma unroll
     for (int rg = 0; rg < 2; ++rg) {
-      const uint16_t* const src = rows + min(row0 + 16 * rg + l16, n_rows - 1) * (size_t)(DC + DR);
 #pragma unroll
-      for (int k = 0; k < kAll; ++k) q[rg][k] = as_bf16x8(ld16(src + lat_channel<DC>(k, g16)));
+      for (int k = 0; k < kAll; ++k) q[rg][k] = operand.get(lds.page[2 + h][rg], k);
       m[rg] = -FLT_MAX;
       l[rg] = sum[rg] = 0.f;
       ref[rg] = -FLT_MAX;
@@ -117,10 +124,7 @@ template <int DC, int DR> struct LatScores {
   __device__ __forceinline__ int scores(const Lds& lds, const char* stage, int step) {
     const int flag = lds.flag[(step - 1) & 1];
     const char* const at_page = stage + page * Page::kBytes;
-    const int at = l16 * Page::kRowBytes + 16 * ((4 * g16) ^ Page::f(l16)), rot = Page::kRot + l16 * Page::kRotBytes + 16 * (g16 ^ Page::rot_f(l16));
-    auto key_of = [&](int k) {
-      return as_bf16x8(*reinterpret_cast<const u32x4*>(at_page + (k < kSteps ? (at ^ (16 * (k & 3))) + 256 * (k >> 2) : rot ^ (64 * (k - kSteps)))));
-    };
+    auto key_of = [&](int k) { return operand.get(at_page, k); };
     bf16x8 key[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
@@ -320,12 +324,12 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
     work.tile<M>();
     if (work.j0 >= work.j1) continue;
     const LatSeq seq = work.seq;
-    const int r0 = work.r0, n_rows = work.n_rows, last = seq.ctx + (r0 + n_rows - 1) / a.heads;   // the last key
-    const int first_limit = seq.ctx + r0 / a.heads;        // keys behind it are not all rows'
+    const int r0 = work.r0, n_rows = work.n_rows, last = seq.ctx + work.plan.token(r0 + n_rows - 1);   // the last key
+    const int first_limit = seq.ctx + work.plan.token(r0);   // keys behind it are not all rows'
     const int i0 = 2 * work.j0, n = min(2 * work.j1, (last >> kStageShift) + 1) - i0;   // stages
     const bool in_part = last != first_limit;
     auto look = [&](int i) { return in_part && ((i0 + i) << kStageShift) + kStageKeys - 1 > first_limit; };   // keys that rows see in part
-    if (tid < M) limits[tid] = seq.ctx + (r0 + min(tid, n_rows - 1)) / a.heads;
+    if (tid < M) limits[tid] = seq.ctx + work.plan.token(r0 + min(tid, n_rows - 1));
     if (w < 4) {
       LatScores<DC, DR> x;
       __builtin_amdgcn_s_setprio(3);
@@ -374,6 +378,7 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
       bring(0);
       if (n > 1) bring(1);
       x.start(w - 4);
+      barrier_lds();                                // the queries are there
       // Behind it a stage of this wave's is there for all, and the one after it on its way.
       auto arrive = [&](int i) {
         if (i + 1 < n) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");
@@ -414,28 +419,49 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
       barrier_lds();
       const LatArgsPtr args = args_anew();
       const bool odd = uni(lds.notes.any_odd) != 0, whole = work.starts && work.ends;
+      // Through LDS, so that rows are stored in whole lines (half a row's share by the lane that has it: 10 times as long): 32 rows at once, in the
+      // places of the half pages that this wave brings, chunk c of row r in slot c ^ r.
+      constexpr int kShare = DC / 4, kChunks = kShare / 4;    // of a row: the wave's channels, in chunks of 4
+      static_assert(kPage * kShare * 4 == 8 * Page::kRowBytes, "16 rows are a half page's");
+      auto place = [&](int r, int c) {
+        return lds.page[r >> 4][page] + part * 8 * Page::kRowBytes + (r & 15) * kShare * 4 + 16 * (c ^ (r & 15));
+      };
+      int lane = tid & 63;
+      __asm__ volatile("" : "+v"(lane));            // else the addresses are made before the first tile, and kept in scratch memory
+      const int l32 = lane & 31, half = lane >> 5;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const int r = 32 * t + x.l32, limit = limits[r];
+        const int r = 32 * t + l32;
         const float l = lds.sum[0][r] + lds.sum[1][r], f = whole ? 1.f / l : 1.f;
+        if (x.channel0 == 0 && half == 0) {
+          if (!whole) reinterpret_cast<float2*>(args->part_ml)[(size_t)work.slot * M + r] = float2{x.m[t], l};
+          else if (args->lse && r < n_rows) args->lse[work.row0 + r] = (x.m[t] + flog2(l)) * kLn2;
+        }
 #pragma unroll
         for (int d = 0; d < LatValues<DC, DR>::kTiles; ++d)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int channel = x.channel0 + 32 * d + 8 * e + 4 * x.half;
-            f32x4 y = f32x4{x.o[d][t][4 * e], x.o[d][t][4 * e + 1], x.o[d][t][4 * e + 2], x.o[d][t][4 * e + 3]} * f;
-            if (odd)
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (lds.notes.odd[channel + k] <= limit) y[k] = __builtin_nanf("");
-            if (!whole)
-              *reinterpret_cast<f32x4*>(args->part_o + ((size_t)work.slot * M + r) * DC + channel) = y;
-            else if (r < n_rows)
-              *reinterpret_cast<bf16x4*>(args->out + (work.row0 + r) * DC + channel) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<f32x4*>(place(l32, 8 * d + 2 * e + half)) =
+                f32x4{x.o[d][t][4 * e], x.o[d][t][4 * e + 1], x.o[d][t][4 * e + 2], x.o[d][t][4 * e + 3]} * f;
+        const int c = lane % kChunks, r0 = lane / kChunks, channel = x.channel0 + 4 * c;
+        constexpr int kAtOnce = 64 / kChunks;       // rows of an instruction
+        if (odd)
+#pragma unroll 1
+          for (int r = r0; r < 32; r += kAtOnce)
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k)
+              if (lds.notes.odd[channel + k] <= limits[32 * t + r]) *reinterpret_cast<float*>(place(r, c) + 4 * k) = __builtin_nanf("");
+        if (!whole) {
+          float* const to = args->part_o + ((size_t)work.slot * M + 32 * t + r0) * DC + channel;
+#pragma unroll 4
+          for (int r = 0; r < 32; r += kAtOnce) *reinterpret_cast<f32x4*>(to + r * DC) = *reinterpret_cast<const f32x4*>(place(r + r0, c));
+        } else {
+          uint16_t* const to = args->out + (work.row0 + 32 * t + r0) * DC + channel;
+#pragma unroll 4
+          for (int r = 0; r < 32; r += kAtOnce) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(place(r + r0, c));
+            if (32 * t + r + r0 < n_rows) *reinterpret_cast<bf16x4*>(to + r * DC) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
           }
-        if (x.channel0 == 0 && x.half == 0) {
-          if (!whole) reinterpret_cast<float2*>(args->part_ml)[(size_t)work.slot * M + r] = float2{x.m[t], l};
-          else if (args->lse && r < n_rows) args->lse[work.row0 + r] = (x.m[t] + flog2(l)) * kLn2;
         }
       }
     }

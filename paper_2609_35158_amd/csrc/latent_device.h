@@ -51,17 +51,11 @@ __device__ __forceinline__ long long uni64(long long x) {
   return (long long)((unsigned long long)hi << 32 | lo);
 }
 
-// The first channel of the 8 that lane group g (of 16 lanes) takes in step k of the scores' product, of 32 channels: the same for keys and
-// queries.  The latent part goes in 128 channels at a time, each group through 32 of them, so that the groups' chunks of 16 bytes
-// differ in bits 2 and 3.
-template <int DC> __device__ __forceinline__ constexpr int lat_channel(int k, int g) {
-  return k < DC / 32 ? 128 * (k >> 2) + 32 * g + 8 * (k & 3) : 32 * k + 8 * g;
-}
-
 // A page in LDS: 16 rows of DC channels, then 16 rows of DR.  Chunk (16 bytes) c of latent row r is in slot c ^ f(r) of
 // its 16, f a permutation of the rows.  A 16 byte read of a row a lane is served 16 lanes at a time, rows 0-3 and 12-15 of one lane group with
-// rows 4-11 of its neighbour: f and lat_channel put these into 16 slots (with neighbouring chunks in the groups such reads take twice
-// as long: a third of all LDS cycles at 64 rows).  The transposing reads of 32 lanes take two
+// rows 4-11 of its neighbour: f puts these into 16 slots, given that the
+// groups' chunks differ in bits 2 and 3: in step k of the scores' product, of 32 channels, group g takes channels 128 (k / 4) + 32 g + 8 (k % 4) .., of
+// keys and queries alike (with neighbouring chunks in the groups such reads take twice as long: a third of all LDS cycles at 64 rows).  The transposing reads of 32 lanes take two
 // chunks of each of 8 consecutive rows at M = 16 (kWide false), four chunks of 4 consecutive rows at M = 64: f keeps these apart likewise.
 // Chunk c of the rotated part is in slot c ^ (r / 2) (DR = 64; at 32, where 4 rows share the banks, c ^ (0, 2, 3, 1)[r / 4]).
 template <int DC, int DR, bool kWide> struct LatPage {
@@ -74,6 +68,43 @@ template <int DC, int DR, bool kWide> struct LatPage {
     return kWide ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 7) << 1) | (r >> 3);
   }
   __device__ static __forceinline__ constexpr int rot_f(int r) { return DR == 64 ? (r >> 1) & 7 : 0x78 >> (2 * (r >> 2)) & 3; }
+};
+
+// Queries: 16 rows of a cached row's width to a page in LDS, by a wave.  The last of `valid` rows stands for those behind it.
+template <typename Page> __device__ __forceinline__ void lat_queries(const uint16_t* rows, int valid, const char* page) {
+  const int l = threadIdx.x & 63;
+  auto copy = [&](int off, int at) {
+    __asm__ volatile("s_mov_b32 m0, %2\n\t"
+                     "s_nop 0\n\t"
+                     "global_load_lds_dwordx4 %0, %1"
+                     :
+                     : "v"(off), "s"(rows), "s"(uni((int)lds_address(page) + at))
+                     : "memory", "m0");
+  };
+  constexpr int kSlots = Page::kRowBytes / 16, kChunks = Page::kRotBytes / 16;
+#pragma unroll
+  for (int i = 0; i < kPage * kSlots; i += 64) {
+    const int r = (i + l) / kSlots;
+    copy(min(r, valid - 1) * Page::kWidth + 16 * ((l % kSlots) ^ Page::f(r)), 16 * i);
+  }
+#pragma unroll
+  for (int i = 0; i < kPage * kChunks; i += 64) {
+    const int r = (i + l) / kChunks;
+    copy(min(r, valid - 1) * Page::kWidth + Page::kRowBytes + 16 * ((l % kChunks) ^ Page::rot_f(r)), Page::kRot + 16 * i);
+  }
+}
+
+// Where the scores' product finds a lane's operand of step k, in row l16 of a page.
+template <typename Page> struct LatOperand {
+  static constexpr int kSteps = Page::kRowBytes / 64;
+  int at, rot;
+  __device__ __forceinline__ void start(int l16, int g16) {
+    at = l16 * Page::kRowBytes + 16 * ((4 * g16) ^ Page::f(l16));
+    rot = Page::kRot + l16 * Page::kRotBytes + 16 * (g16 ^ Page::rot_f(l16));
+  }
+  __device__ __forceinline__ bf16x8 get(const char* page, int k) const {
+    return as_bf16x8(*reinterpret_cast<const u32x4*>(page + (k < kSteps ? (at ^ (16 * (k & 3))) + 256 * (k >> 2) : rot ^ (64 * (k - kSteps)))));
+  }
 };
 
 // The copies of a page by a wave, 1 KiB an instruction, kRows rows' latent parts each, and then the rotated parts.
@@ -159,6 +190,9 @@ struct LatSeq {
 
 struct LatPlan {
   int tile_rows, tile_shift, slope, heads;          // tile_rows = 1 << tile_shift
+  unsigned long long per_head;                      // 2^35 / heads, rounded up
+  // row / heads: exact, as rows are below 2^28 and heads 128 at most
+  __device__ __forceinline__ int token(int row) const { return (int)(((unsigned long long)(unsigned)row * per_head) >> 35); }
   __device__ __forceinline__ long long before(const LatSeq& s, long long u) const {
     return u * (s.ctx + kTileCost) + ((u * (u + 1) * slope) >> 8);
   }
@@ -167,7 +201,7 @@ struct LatPlan {
   }
   // stages of the keys that rows up to `row` see
   __device__ __forceinline__ int stages(const LatSeq& s, int row) const {
-    return (s.ctx + row / heads + 1 + kLatKeys - 1) / kLatKeys;
+    return (s.ctx + token(row) + kLatKeys) >> kLatKeysShift;
   }
   // the stage at which cost `at` of a tile that starts at 0 is cut
   __device__ __forceinline__ static int stage_at(long long at, int stages) {
@@ -278,17 +312,13 @@ struct LatWork {
   }
 };
 
-// Finds the workgroup's share; false: it has none.  Workgroups with one number modulo `group` take the same member of the tiles, and shares
-// of an XCD's workgroups follow one another.
+// Finds the workgroup's share; false: it has none.  Workgroups with one number modulo `group` (a power of two) take the same member of the
+// tiles, and shares of an XCD's workgroups follow one another.
 template <int M, int kWaves> __device__ __forceinline__ bool lat_find(const LatentArgs& a, LatFind& lds, LatWork& work) {
   constexpr int kThreads = 64 * kWaves;
   const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6);
   const int group = a.group;
-  const int per_xcd = (int)gridDim.x / kNumXcd;
-  work.index = (int)(blockIdx.x % kNumXcd) * per_xcd + (int)(blockIdx.x / kNumXcd);
-  work.share = work.index / group;
-  work.member = work.index - work.share * group;
-  work.plan = LatPlan{group * M, __builtin_ctz(group * M), a.slope, a.heads};
+  work.plan = LatPlan{group * M, __builtin_ctz(group * M), a.slope, a.heads, a.per_head};
   work.job = int4{0, 0, 0, 0};
   if (tid == 0) lds.bad = 0;
   __syncthreads();
@@ -322,6 +352,11 @@ template <int M, int kWaves> __device__ __forceinline__ bool lat_find(const Late
   }
   int shares = (int)gridDim.x / group;
   if (total < (long long)shares << a.min_share_shift) shares = (int)max(1ll, total >> a.min_share_shift);
+  // the workgroups that have a share are spread over the XCDs; the others have the numbers behind theirs
+  const int x = (int)(blockIdx.x % kNumXcd), i = (int)(blockIdx.x / kNumXcd), n = (shares + kNumXcd - 1) / kNumXcd * group;
+  work.index = i < n ? x * n + i : kNumXcd * n + x * ((int)gridDim.x / kNumXcd - n) + i - n;
+  work.share = work.index >> __builtin_ctz(group);
+  work.member = work.index & (group - 1);
   if (uni(lds.bad) || total == 0 || work.share >= shares) {
     if (tid == 0) a.jobs[work.index] = work.job;
     return false;

@@ -252,6 +252,7 @@ struct LatentArgs {
   float* part_ml;            // [2 kLatentGrid][tile][2] running max (log2 units) and sum
   int bt_stride, num_pages, batch, total_q, max_q_len, max_kv_len;
   int heads;
+  unsigned long long per_head;  // 2^35 / heads, rounded up
   int group;                 // workgroups that take neighbouring tiles of one share
   int slope;                 // 128 group * tile / heads
   int min_share_shift;       // a share has 2^this keys, at least
