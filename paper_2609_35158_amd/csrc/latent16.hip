@@ -249,23 +249,51 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
   if (tid == 0) args_anew()->jobs[work.index] = work.job;
 }
 
-// Joins the partials of a cut tile: job (first row, rows, index of the first piece's workgroup, shares).  Its first piece is in slot
+// Joins the partials of cut tiles: job (first row, rows, index of the first piece's workgroup, shares).  A tile's first piece is in slot
 // 1 of that workgroup, the others in slot 0 of the shares that follow, in order (kLatentGrid pieces at most).  A lane takes DC / 64 channels of a
-// row.  Few pieces: a wave a row.  Many: the waves take a fourth of them each, row by row.  Where all workgroups had a share, these run on the XCD that wrote the first piece.
+// row.  Work is counted in turns of a workgroup: four rows of few pieces, a wave each, or one row of many, of which each wave takes a fourth
+// (one wave with 62 pieces in a row waited for 16 times its first loads).
 template <int DC, int M>
 __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a) {
-  static_assert(kLatentGrid <= 64 * kLatWaves, "a lane a piece");
-  constexpr int kRows = M / 16, kC = DC / 64;       // rows of a workgroup
-  const int4 job = a.jobs[blockIdx.x % kNumXcd * (kLatentGrid / kNumXcd) + blockIdx.x / kNumXcd];
-  const int r0 = blockIdx.y * kRows;
-  if (r0 >= job.y) return;
+  static_assert(kLatentGrid == kLatThreads, "a thread a job; a lane a piece");
+  constexpr int kC = DC / 64, kFew = 8;
   __shared__ float s_top[kLatWaves], s_sum[kLatWaves];
+  __shared__ int s_turns[kLatWaves];
+  __shared__ __attribute__((aligned(16))) int s_end[kLatentGrid];    // turns of the jobs up to each one
+  __shared__ __attribute__((aligned(16))) int4 s_job[kLatentGrid];
   __shared__ __attribute__((aligned(16))) float s_o[kLatWaves][DC];
-  const int lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6), n = job.w, end = min(r0 + kRows, job.y);
-  const bool few = n <= (M == 16 ? 16 : 64);
-  const int first = few ? 0 : w, step = few ? 1 : kLatWaves, mine = n > first ? (n - first + step - 1) / step : 0;   // this wave's pieces
-  auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * job.z + 1 : 2 * (job.z + i * a.group)) * M; };
-  for (int r = few ? r0 + w : r0; r < end; r += few ? kLatWaves : 1) {
+  const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6);
+  int total = 0;
+  {
+    const int4 job = a.jobs[tid];
+    int end = job.w <= kFew ? (job.y + kLatWaves - 1) / kLatWaves : job.y;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(end, d);
+      if (lane >= d) end += y;
+    }
+    if (lane == 63) s_turns[w] = end;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < kLatWaves; ++v) {
+      if (v == w) end += total;
+      total += s_turns[v];
+    }
+    s_end[tid] = end;
+    s_job[tid] = job;
+    __syncthreads();
+  }
+  for (int turn = blockIdx.x; turn < total; turn += gridDim.x) {
+    const int4 ends = *reinterpret_cast<const int4*>(&s_end[4 * lane]);
+    const int j = __popcll(__ballot(ends.x <= turn)) + __popcll(__ballot(ends.y <= turn)) + __popcll(__ballot(ends.z <= turn)) +
+                  __popcll(__ballot(ends.w <= turn));
+    const int4 job = s_job[j];
+    const int n = uni(job.w), rows = uni(job.y), at = turn - (j ? uni(s_end[j - 1]) : 0);
+    const bool few = n <= kFew;
+    const int first = few ? 0 : w, step = few ? 1 : kLatWaves, mine = (n - first + step - 1) / step;   // this wave's pieces
+    const int r = few ? kLatWaves * at + w : at;
+    if (r >= rows) continue;                        // only where no other wave waits for this one
+    auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * job.z + 1 : 2 * (job.z + i * a.group)) * M; };
     // lane k holds the maximum and sum of the wave's piece k; a piece that saw nothing counts nothing, its outputs may be unwritten
     const float2 ml = lane < mine ? reinterpret_cast<const float2*>(a.part_ml)[slot(step * lane + first) + r] : float2{-FLT_MAX, 0.f};
     const bool seen = ml.y != 0.f;
@@ -322,13 +350,13 @@ __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a)
             bf16x4{(__bf16)(o[c] * inv), (__bf16)(o[c + 1] * inv), (__bf16)(o[c + 2] * inv), (__bf16)(o[c + 3] * inv)};
       if (a.lse && lane == 0) a.lse[row] = (top + flog2(l)) * kLn2;
     }
-    if (!few) __syncthreads();                      // the next row's sums
+    if (!few) __syncthreads();                      // the next turn's sums
   }
 }
 
 namespace {
 template <int DC, int DR> hipError_t launch_dims(const LatentArgs& a, int tile, bool merge, hipStream_t stream) {
-  const dim3 grid(kLatentGrid), threads(kLatThreads), merge_grid(kLatentGrid, 16);
+  const dim3 grid(kLatentGrid), threads(kLatThreads), merge_grid(8 * kLatentGrid);   // as many as the card holds at once
   if (merge && tile == 16) hipLaunchKernelGGL((latent_merge_kernel<DC, 16>), merge_grid, threads, 0, stream, a);
   else if (merge) hipLaunchKernelGGL((latent_merge_kernel<DC, 64>), merge_grid, threads, 0, stream, a);
   else hipLaunchKernelGGL((latent16_kernel<DC, DR>), grid, threads, 0, stream, a);
