@@ -606,16 +606,18 @@ class Rope:
                     raise ValueError("%s must be one row on inv_freq's device" % n)
         self.inv_freq, self.q_weight, self.k_weight = inv_freq, q_weight, k_weight
         self.dev = inv_freq.get_device()
+        self.q_channels = None if q_weight is None else q_weight.shape[0]
+        self.k_channels = None if k_weight is None else k_weight.shape[0]
         self.desc = RopeDesc(inv_freq.data_ptr(), 2 * inv_freq.shape[0], int(bool(interleaved)), float(factor), float(eps),
                              _ptr(q_weight), _ptr(k_weight))
         self.ref = ctypes.byref(self.desc)
 
     def weights(self, q: Optional[int], k: int) -> None:
         """That the norms' weights are of so many channels (q None: queries have none)."""
-        if self.q_weight is not None and self.q_weight.shape[0] != q:
-            raise ValueError("q_weight has %d channels, %s" % (self.q_weight.shape[0], "the call takes none" if q is None else "a head %d" % q))
-        if self.k_weight is not None and self.k_weight.shape[0] != k:
-            raise ValueError("k_weight has %d channels, not %d" % (self.k_weight.shape[0], k))
+        if self.q_channels is not None and self.q_channels != q:
+            raise ValueError("q_weight has %d channels, %s" % (self.q_channels, "the call takes none" if q is None else "a head %d" % q))
+        if self.k_channels is not None and self.k_channels != k:
+            raise ValueError("k_weight has %d channels, not %d" % (self.k_channels, k))
 
 
 def _on(dev: int):
@@ -630,18 +632,41 @@ def _on(dev: int):
     return need
 
 
-def _rows(t: torch.Tensor, name: str, dev: int, shape: Tuple[Optional[int], ...]) -> int:
-    """The elements from a token to the next one of bf16 rows [tokens][heads][channels], of which a token's are contiguous."""
+def _bf16_on(t: torch.Tensor, name: str, dev: int) -> None:
     if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.get_device() != dev:
         _need(t, name, torch.bfloat16)
         raise ValueError("%s must be on cuda:%d, got %s" % (name, dev, t.device))
+
+
+def _rows(t: torch.Tensor, name: str, dev: int, tokens: Optional[int] = None, heads: Optional[int] = None,
+          channels: Optional[int] = None):
+    """Of bf16 rows [tokens][heads][channels], of which a token's are contiguous: the sizes, and the elements from a token to the
+    next one."""
+    _bf16_on(t, name, dev)
     size = t.shape
-    if len(size) != 3 or any(w is not None and w != n for w, n in zip(shape, size)):
-        raise ValueError("%s must be [%s]" % (name, "][".join("any" if w is None else str(w) for w in shape)))
-    stride = t.stride()
-    if (size[2] > 1 and stride[2] != 1) or (size[1] > 1 and stride[1] != size[2]):
+    if len(size) != 3 or (tokens is not None and size[0] != tokens) or (heads is not None and size[1] != heads) or \
+            (channels is not None and size[2] != channels):
+        raise ValueError("%s must be [%s]" % (name, "][".join("any" if w is None else str(w) for w in (tokens, heads, channels))))
+    n0, n1, n2 = size
+    s0, s1, s2 = t.stride()
+    if (n2 > 1 and s2 != 1) or (n1 > 1 and s1 != n2):
         raise ValueError("a token's rows of %s must be contiguous" % name)
-    return stride[0] if size[0] > 1 else size[1] * size[2]
+    return size, s0 if n0 > 1 else n1 * n2
+
+
+# A shape argument of a call, which the library only reads: building one takes 1 us, as long as a tenth of a small call.
+@functools.lru_cache(maxsize=512)
+def _kv_shape_ref(*sizes: int):
+    return ctypes.byref(KvShape(*sizes))
+
+
+@functools.lru_cache(maxsize=512)
+def _latent_shape_ref(*sizes: int):
+    return ctypes.byref(LatentShape(*sizes))
+
+
+def _stream_on(dev: int) -> int:
+    return _stream() if _raw_stream is None else _raw_stream(dev)
 
 
 def rope_rows(q: torch.Tensor, k_new: torch.Tensor, rope: Rope, ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor],
@@ -649,26 +674,27 @@ def rope_rows(q: torch.Tensor, k_new: torch.Tensor, rope: Rope, ctx_lens: torch.
     """Queries [total_q][H_q][d] and keys [total_q][H_kv][d] normalised and rotated at positions ctx_lens[b] + i
     (pearl_rope_rows); both may be parts of wider rows.  q_out / k_out: contiguous, allocated if not given, q and k_new
     themselves where those are contiguous.  Returns (q_out, k_out)."""
-    need = _on(rope.dev)
-    q_stride = _rows(q, "q", rope.dev, (None, None, None))
-    total, H_q, d = q.shape
-    k_stride = _rows(k_new, "k_new", rope.dev, (total, None, d))
-    H_kv = k_new.shape[1]
+    dev = rope.dev
+    need = _on(dev)
+    q_size, q_stride = _rows(q, "q", dev)
+    total, H_q, d = q_size
+    k_size, k_stride = _rows(k_new, "k_new", dev, total, None, d)
     rope.weights(d, d)
-    outs = []
-    for t, x, n in ((q_out, q, "q_out"), (k_out, k_new, "k_out")):
-        if t is None:
-            t = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
-        need(t, n, torch.bfloat16)
-        if t.shape != x.shape:
-            raise ValueError("%s must have shape %s" % (n, tuple(x.shape)))
-        outs.append(t)
+    if q_out is None:
+        q_out = torch.empty(q_size, dtype=torch.bfloat16, device=q.device)
+    if k_out is None:
+        k_out = torch.empty(k_size, dtype=torch.bfloat16, device=q.device)
+    need(q_out, "q_out", torch.bfloat16)
+    need(k_out, "k_out", torch.bfloat16)
+    if q_out.shape != q_size:
+        raise ValueError("q_out must have shape %s" % (tuple(q_size),))
+    if k_out.shape != k_size:
+        raise ValueError("k_out must have shape %s" % (tuple(k_size),))
     desc = _lens_desc(ctx_lens, cu_q_lens, total, max_q_len, need)
-    shape = KvShape(H_q, H_kv, d, PAGE_SIZE, 1)
-    st = load().pearl_rope_rows(ctypes.byref(shape), ctypes.byref(desc), rope.ref, q.data_ptr(), q_stride, k_new.data_ptr(),
-                                k_stride, outs[0].data_ptr(), outs[1].data_ptr(), _stream())
+    st = load().pearl_rope_rows(_kv_shape_ref(H_q, k_size[1], d, PAGE_SIZE, 1), ctypes.byref(desc), rope.ref, q.data_ptr(), q_stride,
+                                k_new.data_ptr(), k_stride, q_out.data_ptr(), k_out.data_ptr(), _stream_on(dev))
     _check(st, "pearl_rope_rows")
-    return outs[0], outs[1]
+    return q_out, k_out
 
 
 def _lens_desc(ctx_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor], total_q: int, max_q_len: int, need) -> SeqDesc:
@@ -687,27 +713,30 @@ def kv_append_rope(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, ro
                    cu_q_lens: Optional[torch.Tensor], max_q_len: int, max_kv_len: int,
                    q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """rope_rows with k_new (rotated) and v_new going into the pools (pearl_kv_append_rope); returns q_out."""
-    need = _on(rope.dev)
-    for t, n in ((k_pool, "k_pool"), (v_pool, "v_pool")):
-        need(t, n, torch.bfloat16)
-    shape = make_shape(q.shape[1] if q.dim() == 3 else 0, k_pool)
-    if v_pool.shape != k_pool.shape:
+    dev = rope.dev
+    need = _on(dev)
+    need(k_pool, "k_pool", torch.bfloat16)
+    need(v_pool, "v_pool", torch.bfloat16)
+    pool = k_pool.shape
+    if len(pool) != 4:
+        raise ValueError("pools must be [num_pages][num_kv_heads][page_size][head_dim]")
+    if v_pool.shape != pool:
         raise ValueError("k_pool and v_pool must have one shape")
-    H_kv, d = k_pool.shape[1], k_pool.shape[3]
-    q_stride = _rows(q, "q", rope.dev, (None, None, d))
-    total = q.shape[0]
-    k_stride = _rows(k_new, "k_new", rope.dev, (total, H_kv, d))
-    v_stride = _rows(v_new, "v_new", rope.dev, (total, H_kv, d))
+    pages, H_kv, page_size, d = pool
+    q_size, q_stride = _rows(q, "q", dev, None, None, d)
+    total = q_size[0]
+    _, k_stride = _rows(k_new, "k_new", dev, total, H_kv, d)
+    _, v_stride = _rows(v_new, "v_new", dev, total, H_kv, d)
     rope.weights(d, d)
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        q_out = torch.empty(q_size, dtype=torch.bfloat16, device=q.device)
     need(q_out, "q_out", torch.bfloat16)
-    if q_out.shape != q.shape:
-        raise ValueError("q_out must have shape %s" % (tuple(q.shape),))
+    if q_out.shape != q_size:
+        raise ValueError("q_out must have shape %s" % (tuple(q_size),))
     desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, need)
-    st = load().pearl_kv_append_rope(ctypes.byref(shape), ctypes.byref(desc), rope.ref, q.data_ptr(), q_stride,
-                                     k_new.data_ptr(), k_stride, v_new.data_ptr(), v_stride, q_out.data_ptr(),
-                                     k_pool.data_ptr(), v_pool.data_ptr(), _stream())
+    st = load().pearl_kv_append_rope(_kv_shape_ref(q_size[1], H_kv, d, page_size, pages), ctypes.byref(desc), rope.ref, q.data_ptr(),
+                                     q_stride, k_new.data_ptr(), k_stride, v_new.data_ptr(), v_stride, q_out.data_ptr(),
+                                     k_pool.data_ptr(), v_pool.data_ptr(), _stream_on(dev))
     _check(st, "pearl_kv_append_rope")
     return q_out
 
@@ -727,11 +756,12 @@ def latent_cache(num_pages: int, latent_dim: int, rope_dim: int, device="cuda") 
     return torch.zeros((num_pages, PAGE_SIZE, latent_dim + rope_dim), dtype=torch.bfloat16, device=device)
 
 
-def _latent_shape(num_q_heads: int, cache: torch.Tensor) -> LatentShape:
-    if cache.dim() != 3 or cache.shape[1] != PAGE_SIZE or cache.shape[2] not in _LATENT_DIMS:
+def _latent_sizes(num_q_heads: int, cache: torch.Tensor) -> Tuple[int, int, int, int, int]:
+    size = cache.shape
+    if len(size) != 3 or size[1] != PAGE_SIZE or size[2] not in _LATENT_DIMS:
         raise ValueError("cache must be [num_pages][16][latent_dim + rope_dim], (512, 64) or (256, 32)")
-    dc, dr = _LATENT_DIMS[cache.shape[2]]
-    return LatentShape(num_q_heads, dc, dr, PAGE_SIZE, cache.shape[0])
+    dc, dr = _LATENT_DIMS[size[2]]
+    return num_q_heads, dc, dr, PAGE_SIZE, size[0]
 
 
 def latent_append(q_rope: torch.Tensor, rows_new: torch.Tensor, rope: Rope, q: torch.Tensor, cache: torch.Tensor,
@@ -740,40 +770,48 @@ def latent_append(q_rope: torch.Tensor, rows_new: torch.Tensor, rope: Rope, q: t
     """New latent rows [total_q][latent_dim + rope_dim] into the cache, the latent part normalised (rope.k_weight), the
     rest rotated; q_rope [total_q][H][rope_dim], rotated, into the last channels of the absorbed queries q
     [total_q][H][latent_dim + rope_dim] (pearl_latent_append).  rows_new may be a part of wider rows, q_rope of wider heads."""
-    need = _on(rope.dev)
+    dev = rope.dev
+    need = _on(dev)
     need(cache, "cache", torch.bfloat16)
     need(q, "q", torch.bfloat16)
-    if q.dim() != 3:
+    q_size = q.shape
+    if len(q_size) != 3:
         raise ValueError("q must be [total_q][num_q_heads][latent_dim + rope_dim]")
-    total, H, width = q.shape
-    shape = _latent_shape(H, cache)
-    if width != cache.shape[2]:
-        raise ValueError("q has %d channels, the cache %d" % (width, cache.shape[2]))
-    if rows_new.dim() != 2:
-        raise ValueError("rows_new must be [total_q][latent_dim + rope_dim]")
-    rows_stride = _rows(rows_new[:, None], "rows_new", rope.dev, (total, 1, width))
-    if q_rope.dim() != 3 or tuple(q_rope.shape) != (total, H, shape.rope_dim):
-        raise ValueError("q_rope must be [%d][%d][%d]" % (total, H, shape.rope_dim))
-    by_token, by_head, _ = q_rope.stride()
+    total, H, width = q_size
+    sizes = _latent_sizes(H, cache)
+    _, dc, dr, _, _ = sizes
+    if width != dc + dr:
+        raise ValueError("q has %d channels, the cache %d" % (width, dc + dr))
+    _bf16_on(rows_new, "rows_new", dev)
+    if rows_new.shape != (total, width):
+        raise ValueError("rows_new must be [%d][%d]" % (total, width))
+    rows_stride, by_channel = rows_new.stride()
+    if by_channel != 1:
+        raise ValueError("the rows of rows_new must be contiguous")
+    if total <= 1:
+        rows_stride = width
+    _bf16_on(q_rope, "q_rope", dev)
+    if q_rope.shape != (total, H, dr):
+        raise ValueError("q_rope must be [%d][%d][%d]" % (total, H, dr))
+    by_token, by_head, by_channel = q_rope.stride()
+    if by_channel != 1:
+        raise ValueError("the heads of q_rope must be contiguous")
     if H == 1:
         by_head = by_token
     elif total > 1 and by_token != H * by_head:
         raise ValueError("q_rope's heads must be evenly spaced, a token's last to the next one's first alike")
     if total * H <= 1:
-        by_head = shape.rope_dim
-    _rows(q_rope.as_strided((total * H, 1, shape.rope_dim), (by_head, shape.rope_dim, q_rope.stride(2))), "q_rope", rope.dev,
-          (total * H, 1, shape.rope_dim))
-    rope.weights(None, shape.latent_dim)
+        by_head = dr
+    rope.weights(None, dc)
     desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, need)
-    st = load().pearl_latent_append(ctypes.byref(shape), ctypes.byref(desc), rope.ref, q_rope.data_ptr(), by_head,
-                                    rows_new.data_ptr(), rows_stride, q.data_ptr(), cache.data_ptr(), _stream())
+    st = load().pearl_latent_append(_latent_shape_ref(*sizes), ctypes.byref(desc), rope.ref, q_rope.data_ptr(), by_head,
+                                    rows_new.data_ptr(), rows_stride, q.data_ptr(), cache.data_ptr(), _stream_on(dev))
     _check(st, "pearl_latent_append")
 
 
 def workspace_bytes_latent(num_q_heads: int, cache: torch.Tensor, desc: SeqDesc) -> int:
     """Bytes of workspace that the attention calls over this cache need (pearl_latent_workspace_bytes)."""
-    shape = _latent_shape(int(num_q_heads), cache)
-    n = load().pearl_latent_workspace_bytes(ctypes.byref(shape), ctypes.byref(desc))
+    n = load().pearl_latent_workspace_bytes(_latent_shape_ref(*_latent_sizes(int(num_q_heads), cache)), ctypes.byref(desc))
     if n == 0:
         raise PearlError(1, "pearl_latent_workspace_bytes", last_error())
     return int(n)
@@ -783,16 +821,19 @@ def _attention_latent(fname: str, q: torch.Tensor, cache: torch.Tensor, block_ta
                       cu_q_lens: Optional[torch.Tensor], max_q_len: int, max_kv_len: int, scale: float, return_lse: bool,
                       out: Optional[torch.Tensor], lse: Optional[torch.Tensor], workspace: Optional[torch.Tensor]):
     _need(cache, "cache", torch.bfloat16)
-    need = _on(cache.get_device())
+    dev = cache.get_device()
+    need = _on(dev)
     need(q, "q", torch.bfloat16)
-    if q.dim() != 3:
+    q_size = q.shape
+    if len(q_size) != 3:
         raise ValueError("q must be [total_q][num_q_heads][latent_dim + rope_dim]")
-    total, H, width = q.shape
-    shape = _latent_shape(H, cache)
-    if width != cache.shape[2]:
-        raise ValueError("q has %d channels, the cache %d" % (width, cache.shape[2]))
+    total, H, width = q_size
+    sizes = _latent_sizes(H, cache)
+    _, dc, dr, _, _ = sizes
+    if width != dc + dr:
+        raise ValueError("q has %d channels, the cache %d" % (width, dc + dr))
     desc = make_desc(block_table, ctx_lens, cu_q_lens, total, max_q_len, max_kv_len, need)
-    want = (total, H, shape.latent_dim)
+    want = (total, H, dc)
     if out is None:
         out = torch.empty(want, dtype=torch.bfloat16, device=q.device)
     else:
@@ -809,8 +850,8 @@ def _attention_latent(fname: str, q: torch.Tensor, cache: torch.Tensor, block_ta
         workspace = torch.empty(workspace_bytes_latent(H, cache, desc), dtype=torch.uint8, device=q.device)
     else:
         need(workspace, "workspace", torch.uint8)    # the library checks its size
-    st = getattr(load(), fname)(ctypes.byref(shape), ctypes.byref(desc), q.data_ptr(), cache.data_ptr(), float(scale),
-                                out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream())
+    st = getattr(load(), fname)(_latent_shape_ref(*sizes), ctypes.byref(desc), q.data_ptr(), cache.data_ptr(), float(scale),
+                                out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream_on(dev))
     _check(st, fname)
     return (out, lse) if lse is not None else out
 
