@@ -77,16 +77,16 @@ template <int DC, int DR> struct LatRows16 {
   __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])); }
   // Whether some score is far above its row's maximum so far; the new maximum.
   __device__ __forceinline__ bool above(float scale) const { return __ballot(fmaf(largest(), scale, -m) > kLag) != 0; }
-  __device__ __forceinline__ void raise(float scale) {
-    const float x = fmaxf(m, xor32_max(xor16_max(largest() * scale)));
-    scale_to(x);
-  }
-  __device__ __forceinline__ void scale_to(float x) {
+  __device__ __forceinline__ void raise(float to_log2) {
+    const float x = fmaxf(m, xor32_max(xor16_max(largest() * to_log2)));
     const float alpha = fexp2(m - x);
     m = x;
     l *= alpha;
+    scale(alpha);
+  }
+  __device__ __forceinline__ void scale(float f) {
 #pragma unroll
-    for (int d = 0; d < kBlocks; ++d) o[d] *= alpha;
+    for (int d = 0; d < kBlocks; ++d) o[d] *= f;
   }
   __device__ __forceinline__ void add_values(const char* page, float scale) {
     // The weights of the lane's row and keys 4 g16 .. + 3 are where the product (16x16x16: A row l%16, k 4(l/16)+e; B column l%16, k
@@ -201,8 +201,17 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
     }
     barrier_lds();
     const bool odd = uni(lds.notes.any_odd) != 0;
+    const bool whole = work.starts && work.ends;
+    const LatArgsPtr args = args_anew();
     const float top = fmaxf(fmaxf(lds.max[0][x.l16], lds.max[1][x.l16]), fmaxf(lds.max[2][x.l16], lds.max[3][x.l16]));
-    x.scale_to(top);
+    float l = 0.f;
+#pragma unroll
+    for (int v = 0; v < kLatWaves; ++v) l = fmaf(lds.sum[v][x.l16], fexp2(lds.max[v][x.l16] - top), l);
+    if (tid < M) {
+      if (!whole) reinterpret_cast<float2*>(args->part_ml)[(size_t)work.slot * M + tid] = float2{top, l};
+      else if (args->lse && tid < n_rows) args->lse[work.row0 + tid] = (top + flog2(l)) * kLn2;
+    }
+    x.scale(fexp2(x.m - top) * (whole ? 1.f / l : 1.f));
     // outputs of a wave: rows of DC channels in 32 bits, chunk c of row r in slot c ^ r of its 16
     constexpr int kWaveBytes = M * DC * 4;
     static_assert(kWaveBytes <= 2 * Page::kBytes, "in the wave's own buffers");
@@ -210,13 +219,10 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
     for (int d = 0; d < Rows::kBlocks; ++d)
       *reinterpret_cast<f32x4*>(buffers + x.l16 * DC * 4 + 16 * ((4 * d + x.g16) ^ x.l16)) = x.o[d];
     barrier_lds();
-    const LatArgsPtr args = args_anew();
-    for (int r = w; r < n_rows || (r < M && !(work.starts && work.ends)); r += kLatWaves) {
-      const float t = fmaxf(fmaxf(lds.max[0][r], lds.max[1][r]), fmaxf(lds.max[2][r], lds.max[3][r]));
-      float l = 0.f;
-#pragma unroll
-      for (int v = 0; v < kLatWaves; ++v) l = fmaf(lds.sum[v][r], fexp2(lds.max[v][r] - t), l);
-      const float inv = 1.f / l;
+    // a wave every fourth row
+    const int rows = whole ? n_rows : M;
+#pragma unroll 2
+    for (int r = w; r < rows; r += kLatWaves) {
 #pragma unroll
       for (int c = 0; c < DC; c += 256) {
         const int channel = c + 4 * lane;
@@ -228,16 +234,8 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (lds.notes.odd[channel + e] <= lds.notes.limit[r]) y[e] = __builtin_nanf("");
-        if (work.starts && work.ends) {
-          y *= inv;
-          *reinterpret_cast<bf16x4*>(args->out + (work.row0 + r) * DC + channel) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
-        } else {
-          *reinterpret_cast<f32x4*>(args->part_o + ((size_t)work.slot * M + r) * DC + channel) = y;
-        }
-      }
-      if (lane == 0) {
-        if (!(work.starts && work.ends)) reinterpret_cast<float2*>(args->part_ml)[(size_t)work.slot * M + r] = float2{t, l};
-        else if (args->lse) args->lse[work.row0 + r] = (t + flog2(l)) * kLn2;
+        if (whole) *reinterpret_cast<bf16x4*>(args->out + (work.row0 + r) * DC + channel) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+        else *reinterpret_cast<f32x4*>(args->part_o + ((size_t)work.slot * M + r) * DC + channel) = y;
       }
     }
     barrier_lds();                                  // the next tile writes all of it
