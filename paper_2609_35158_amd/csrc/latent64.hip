@@ -1,14 +1,14 @@
 // gfx950 kernel of attention over a paged cache of latent vectors (what it computes: latent16.hip) for sequences of more than 16 rows:
 // tiles of 64 rows.
 //
-// A workgroup has 8 waves, two on each SIMD: four take the scores and their weights, four the values, a stage (32 keys, 2 pages) behind, so that
-// the one's products run while the other weighs, waits or copies.
-//   S^T (keys x rows) = K . Q^T: score wave w has the keys of page w % 2 and rows 32 (w / 2) .., Q in registers (16x16x32 MFMA: A row l%16,
+// A workgroup has 8 waves, two on each SIMD: four take the scores and their weights, four the values, a stage (32 keys, 2 pages; at 256 channels
+// 64 keys, 4 pages) behind, so that the one's products run while the other weighs, waits or copies.
+//   S^T (keys x rows) = K . Q^T: score wave w has the keys of every second page from w % 2 on and rows 32 (w / 2) .., Q in registers (16x16x32 MFMA: A row l%16,
 //                       k 8(l/16)+e; B column l%16, k 8(l/16)+e; D column l%16, row 4(l/16)+r);
 //   O^T (channels x rows) += V^T . P^T: value wave w has a quarter of the channels and all rows, V^T by transposing reads of the same LDS
 //                       rows (32x32x16 MFMA: A row l%32, k 8(l/32)+e; B column l%32, k 8(l/32)+e; D column l%32, row r%4 + 8(r/4) + 4(l/32)).
 // Step t between two barriers: scores of stage t, values of stage t - 1, and the copies of stage t + 2 go out (four stages in LDS: t - 1 and t in
-// use, t + 1 on its way or there).
+// use, t + 1 on its way or there; at 256 channels three, of twice the keys, and the copies of stage t + 1).
 // A row's maximum is common to all.  It may lag the true one by kLag (log2 units), so most stages go on with the old one.  Where some score
 // is further above, a score wave weighs with a maximum of its own, rounded up to a whole number, and behind the next barrier all waves take up the
 // largest; what was weighed with another is scaled by a power of two.
@@ -18,25 +18,34 @@
 namespace pearl {
 namespace {
 
-constexpr int kWaves64 = 8, kStageKeys = 32, kStageShift = 5, kStages = 4;
+constexpr int kWaves64 = 8;
+
+template <int DC> struct LatStage {
+  static constexpr int kPages = DC == 512 ? 2 : 4, kKeys = kPage * kPages, kShift = DC == 512 ? 5 : 6;
+  static constexpr int kStages = DC == 512 ? 4 : 3, kLead = kStages - 2;   // kLead: stages on their way
+  static constexpr int kRowBytes = 2 * kKeys;       // of a row's weights; chunk c of row r is in slot c ^ f(r)
+  __device__ static __forceinline__ constexpr int f(int r) { return DC == 512 ? (r >> 2) & 3 : (r >> 1) & 7; }
+};
 
 template <int DC, int DR> struct LatLds64 {
   using Page = LatPage<DC, DR, true>;
-  char page[kStages][2][Page::kBytes];
-  char p[2][64 * kStageKeys * 2];                   // weights of a stage: rows of 64 bytes, chunk c of row r in slot c ^ (r / 4)
+  using Stage = LatStage<DC>;
+  char page[Stage::kStages][Stage::kPages][Page::kBytes];
+  char p[2][64 * Stage::kRowBytes];                 // weights of a stage
   LatNotes<DC, 64> notes;
   int limit2[64];                                   // notes.limit of every other tile
-  float max[2][2][64];                              // of a stage, of each page: the rows' maxima that its weights were taken with
+  float max[2][2][64];                              // of a stage, of every second page: the rows' maxima that their weights were taken with
   float sum[2][64];                                 // at the end of a tile: the rows' sums, in parts
   int flag[2];                                      // the last step with some score far above its row's maximum, of even and odd ones
   LatFind find;
 };
 
-// The copies of half a page (8 rows) by a wave, 1 KiB an instruction.
-template <int DC, int DR> struct LatHalfCopies {
+// A value wave's copies in a stage, 1 KiB an instruction: half a page (8 rows) or (256 channels) a page.
+template <int DC, int DR> struct LatMyCopies {
   using Page = LatPage<DC, DR, true>;
-  static constexpr int kRows = 1024 / Page::kRowBytes, kLatent = 8 / kRows, kCopies = kLatent + 1;
-  static constexpr bool kRotAtOnce = 8 * Page::kRotBytes < 1024;   // one instruction takes the page's rotated parts: both waves bring all of them
+  static constexpr int kMine = DC == 512 ? 8 : 16;  // rows
+  static constexpr int kRows = 1024 / Page::kRowBytes, kLatent = kMine / kRows, kCopies = kLatent + 1;
+  static_assert(kMine * Page::kRotBytes == 1024, "one instruction takes the rotated parts");
   int off[kCopies];                                 // the lane's source offsets in the page
   __device__ __forceinline__ void start(int half) {
     const int l = threadIdx.x & 63;
@@ -46,7 +55,7 @@ template <int DC, int DR> struct LatHalfCopies {
       off[i] = r * Page::kWidth + 16 * (slot ^ Page::f(r)) - 1024 * (i & 1);   // the second of a pair has 1 KiB as its immediate
     }
     constexpr int kChunks = Page::kRotBytes / 16;
-    const int r = l / kChunks + (kRotAtOnce ? 0 : 8 * half);
+    const int r = l / kChunks + 8 * half;
     off[kLatent] = r * Page::kWidth + Page::kRowBytes + 16 * ((l % kChunks) ^ Page::rot_f(r));
   }
   // Copies i and i + 1 (the last one, of the rotated parts, by itself) to the page at the LDS address lds, if `go`.
@@ -65,7 +74,7 @@ template <int DC, int DR> struct LatHalfCopies {
           : "v"(off[i]), "v"(off[i + 1]), "s"(src), "s"(to), "s"(uni(go))
           : "memory", "scc", "m0");
     } else {
-      const unsigned to = uni((int)lds + Page::kRot + (kRotAtOnce ? 0 : 1024 * half));
+      const unsigned to = uni((int)lds + Page::kRot + 1024 * half);
       __asm__ volatile(
           "s_cmp_eq_u32 %3, 0\n\t"
           "s_cbranch_scc1 .Lno_copy%=\n\t"
@@ -78,42 +87,46 @@ template <int DC, int DR> struct LatHalfCopies {
           : "memory", "scc", "m0");
     }
   }
-  // Zeros in place of the half's latent parts from row `valid` of the page on (of rotated parts scores alone are made, which are masked).
+  // Zeros in place of its latent parts from row `valid` of the page on (of rotated parts scores alone are made, which are masked).
   __device__ static __forceinline__ void clear(char* page, int half, int valid) {
-    for (int i = max(valid, 8 * half) * Page::kRowBytes + 16 * (threadIdx.x & 63); i < 8 * (half + 1) * Page::kRowBytes; i += 1024)
+    for (int i = max(valid, 8 * half) * Page::kRowBytes + 16 * (threadIdx.x & 63); i < (8 * half + kMine) * Page::kRowBytes; i += 1024)
       *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
   }
 };
 
-// A score wave: page `page` of a stage, rows 32 half ...
+// A score wave: pages `page`, page + 2, .. of a stage, rows row0 ..
 template <int DC, int DR> struct LatScores {
   using Page = LatPage<DC, DR, true>;
   using Lds = LatLds64<DC, DR>;
-  static constexpr int kSteps = DC / 32, kAll = kSteps + DR / 32;
+  using Stage = LatStage<DC>;
+  static constexpr int kAll = (DC + DR) / 32, kMine = Stage::kPages / 2;
   static constexpr int kAhead = 4;                  // LDS reads of the product's operands, ahead of it
   bf16x8 q[2][kAll];
-  f32x4 s[2];
+  f32x4 s[kMine][2];
   float m[2], l[2], sum[2], ref[2];
   LatOperand<Page> operand;
-  int page, row0, g16, l16, place;                  // place: of the lane's weights among a stage's
+  int page, row0, g16, l16, place;                  // place: of the lane's weights among a stage's (the next page's: ^ 64)
 
-  // The queries come as pages through the last two stages; wave 2 h + p brings rows 32 h + 16 p ..
+  // The queries come as pages through the stages that are not on their way yet; wave 2 h + p brings rows 32 h + 16 p ..
+  __device__ static __forceinline__ const char* queries(const Lds& lds, int i) {
+    return lds.page[Stage::kLead + i / Stage::kPages][i % Stage::kPages];
+  }
   __device__ __forceinline__ void start(Lds& lds, int wave, const uint16_t* rows, int n_rows) {
     page = wave & 1;
     const int h = wave >> 1;
     row0 = 32 * h;
     const int first = min(row0 + 16 * page, n_rows - 1);
-    lat_queries<Page>(rows + first * (DC + DR), min(n_rows - first, kPage), lds.page[2 + h][page]);
+    lat_queries<Page>(rows + first * (DC + DR), min(n_rows - first, kPage), queries(lds, 2 * h + page));
     g16 = (threadIdx.x & 63) >> 4;
     l16 = threadIdx.x & 15;
     operand.start(l16, g16);
-    place = (row0 + l16) * 64 + 16 * ((2 * page + (g16 >> 1)) ^ (l16 >> 2)) + 8 * (g16 & 1);
+    place = (row0 + l16) * Stage::kRowBytes + 16 * ((2 * page + (g16 >> 1)) ^ Stage::f(l16)) + 8 * (g16 & 1);
     wait_copies();
     barrier_lds();
 #pragma unroll
     for (int rg = 0; rg < 2; ++rg) {
 #pragma unroll
-      for (int k = 0; k < kAll; ++k) q[rg][k] = operand.get(lds.page[2 + h][rg], k);
+      for (int k = 0; k < kAll; ++k) q[rg][k] = operand.get(queries(lds, 2 * h + rg), k);
       m[rg] = -FLT_MAX;
       l[rg] = sum[rg] = 0.f;
       ref[rg] = -FLT_MAX;
@@ -124,62 +137,76 @@ template <int DC, int DR> struct LatScores {
   __device__ __forceinline__ int scores(const Lds& lds, const char* stage, int step) {
     const int flag = lds.flag[(step - 1) & 1];
     const char* const at_page = stage + page * Page::kBytes;
-    auto key_of = [&](int k) { return operand.get(at_page, k); };
+    auto key_of = [&](int i) { return operand.get(at_page + i / kAll * 2 * Page::kBytes, i % kAll); };
     bf16x8 key[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) key[k] = key_of(k);
-    s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < kAhead; ++i) key[i] = key_of(i);
 #pragma unroll
-    for (int k = 0; k < kAll; ++k) {
-      const bf16x8 x = key[k % kAhead];
-      s[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[0][k], s[0], 0, 0, 0);
-      s[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[1][k], s[1], 0, 0, 0);
-      if (k + kAhead < kAll) key[k % kAhead] = key_of(k + kAhead);
+    for (int i = 0; i < kMine * kAll; ++i) {
+      const int h = i / kAll, k = i % kAll;
+      const bf16x8 x = key[i % kAhead];
+      if (k == 0) s[h][0] = s[h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      s[h][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[0][k], s[h][0], 0, 0, 0);
+      s[h][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[1][k], s[h][1], 0, 0, 0);
+      if (i + kAhead < kMine * kAll) key[i % kAhead] = key_of(i + kAhead);
       __builtin_amdgcn_sched_barrier(0);
     }
     return uni(flag);
   }
   __device__ __forceinline__ void mask(const int* limits, int key0) {
-    const int key = key0 + kPage * page + 4 * g16;
 #pragma unroll
     for (int rg = 0; rg < 2; ++rg) {
-      const int limit = limits[row0 + 16 * rg + l16];
+      const int limit = limits[row0 + 16 * rg + l16] - key0 - kPage * page - 4 * g16;
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (key + r > limit) s[rg][r] = -__builtin_inff();
+      for (int h = 0; h < kMine; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (2 * kPage * h + r > limit) s[h][rg][r] = -__builtin_inff();
     }
   }
+  __device__ __forceinline__ float largest(int rg) const {
+    float x = fmaxf(fmaxf(s[0][rg][0], s[0][rg][1]), fmaxf(s[0][rg][2], s[0][rg][3]));
+#pragma unroll
+    for (int h = 1; h < kMine; ++h) x = fmaxf(x, fmaxf(fmaxf(s[h][rg][0], s[h][rg][1]), fmaxf(s[h][rg][2], s[h][rg][3])));
+    return x;
+  }
   __device__ __forceinline__ void weigh(Lds& lds, int step, float scale) {
-    float p[2][4], top = -FLT_MAX;
+    float p[kMine][2][4], top = -FLT_MAX;
     auto weights = [&](int rg) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) p[rg][r] = fexp2(fmaf(s[rg][r], scale, -ref[rg]));
+      for (int h = 0; h < kMine; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[h][rg][r] = fexp2(fmaf(s[h][rg][r], scale, -ref[rg]));
     };
 #pragma unroll
     for (int rg = 0; rg < 2; ++rg) {
       ref[rg] = m[rg];
       weights(rg);
-      top = fmaxf(top, fmaf(fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])), scale, -m[rg]));
+      top = fmaxf(top, fmaf(largest(rg), scale, -m[rg]));
     }
     if (__ballot(top > kLag)) {
 #pragma unroll
       for (int rg = 0; rg < 2; ++rg) {
-        const float x = fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3])) * scale;
-        ref[rg] = fmaxf(m[rg], ceilf(xor32_max(xor16_max(x))));
+        ref[rg] = fmaxf(m[rg], ceilf(xor32_max(xor16_max(largest(rg) * scale))));
         weights(rg);
         if (g16 == 0) lds.max[step & 1][page][row0 + 16 * rg + l16] = ref[rg];
       }
       lds.flag[step & 1] = step;
     }
-    char* const to = lds.p[step & 1] + place;
+    char* const to = lds.p[step & 1];
 #pragma unroll
     for (int rg = 0; rg < 2; ++rg) {
-      sum[rg] = (p[rg][0] + p[rg][1]) + (p[rg][2] + p[rg][3]);
-      *reinterpret_cast<bf16x4*>(to + 1024 * rg) = bf16x4{(__bf16)p[rg][0], (__bf16)p[rg][1], (__bf16)p[rg][2], (__bf16)p[rg][3]};
+      sum[rg] = 0.f;
+#pragma unroll
+      for (int h = 0; h < kMine; ++h) {
+        const float* const x = p[h][rg];
+        sum[rg] += (x[0] + x[1]) + (x[2] + x[3]);
+        *reinterpret_cast<bf16x4*>(to + (place ^ (64 * h)) + kPage * Stage::kRowBytes * rg) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+      }
     }
   }
   // Behind the barrier after weigh(step): the stage's sums, and new maxima if there are any (flag == step), with the weights in LDS scaled to
-  // them.  A page's maxima in LDS are older ones, no larger, where its own scores are near them.
+  // them.  A wave's maxima in LDS are older ones, no larger, where its own scores are near them.
   __device__ __forceinline__ void take_up(Lds& lds, int step, int flag) {
     if (flag == step) {
 #pragma unroll
@@ -189,8 +216,11 @@ template <int DC, int DR> struct LatScores {
         l[rg] *= fexp2(m[rg] - x);
         sum[rg] *= f;
         m[rg] = x;
-        bf16x4& p = *reinterpret_cast<bf16x4*>(lds.p[step & 1] + place + 1024 * rg);
-        p = bf16x4{(__bf16)((float)p[0] * f), (__bf16)((float)p[1] * f), (__bf16)((float)p[2] * f), (__bf16)((float)p[3] * f)};
+#pragma unroll
+        for (int h = 0; h < kMine; ++h) {
+          bf16x4& p = *reinterpret_cast<bf16x4*>(lds.p[step & 1] + (place ^ (64 * h)) + kPage * Stage::kRowBytes * rg);
+          p = bf16x4{(__bf16)((float)p[0] * f), (__bf16)((float)p[1] * f), (__bf16)((float)p[2] * f), (__bf16)((float)p[3] * f)};
+        }
       }
       barrier_lds();
     }
@@ -210,11 +240,12 @@ template <int DC, int DR> struct LatScores {
 template <int DC, int DR> struct LatValues {
   using Page = LatPage<DC, DR, true>;
   using Lds = LatLds64<DC, DR>;
-  static constexpr int kTiles = DC / 4 / 32;        // of 32 channels
+  using Stage = LatStage<DC>;
+  static constexpr int kTiles = DC / 4 / 32, kAll = Stage::kPages * kTiles;   // of 32 channels
   static constexpr int kAhead = 4;
   f32x16 o[kTiles][2];
   float m[2];                                       // of rows l32 and 32 + l32
-  bf16x8 p[2][2], value[kAhead];
+  bf16x8 p[Stage::kPages][2], value[kAhead];
   int channel0, half, l32, at;
 
   __device__ __forceinline__ void start(int wave) {
@@ -283,22 +314,22 @@ template <int DC, int DR> struct LatValues {
     for (int i = 0; i < kAhead; ++i) value[i] = value_of(stage, i);
   }
   __device__ __forceinline__ void weights(const Lds& lds, int step) {
-    const char* const from = lds.p[step & 1] + l32 * 64;
+    const char* const from = lds.p[step & 1] + l32 * Stage::kRowBytes;
 #pragma unroll
-    for (int page = 0; page < 2; ++page)
+    for (int page = 0; page < Stage::kPages; ++page)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        p[page][t] = as_bf16x8(*reinterpret_cast<const u32x4*>(from + 2048 * t + 16 * ((2 * page + half) ^ ((l32 >> 2) & 3))));
+        p[page][t] = as_bf16x8(*reinterpret_cast<const u32x4*>(from + 32 * Stage::kRowBytes * t + 16 * ((2 * page + half) ^ Stage::f(l32))));
   }
   // The stage's products, behind first() and weights().
   __device__ __forceinline__ void add(const char* stage) {
 #pragma unroll
-    for (int i = 0; i < 2 * kTiles; ++i) {
+    for (int i = 0; i < kAll; ++i) {
       const int page = i / kTiles, d = i % kTiles;
       const bf16x8 x = value[i % kAhead];
       o[d][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[page][0], o[d][0], 0, 0, 0);
       o[d][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[page][1], o[d][1], 0, 0, 0);
-      if (i + kAhead < 2 * kTiles) value[i % kAhead] = value_of(stage, i + kAhead);
+      if (i + kAhead < kAll) value[i % kAhead] = value_of(stage, i + kAhead);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -309,16 +340,21 @@ template <int DC, int DR> struct LatValues {
 template <int DC, int DR>
 __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a) {
   using Page = LatPage<DC, DR, true>;
-  using Copies = LatHalfCopies<DC, DR>;
+  using Copies = LatMyCopies<DC, DR>;
+  using Stage = LatStage<DC>;
   using Lds = LatLds64<DC, DR>;
-  constexpr int M = 64;
+  // 512 channels, of 64, 128, 192 and 256: two prompts of 300 tokens and 128 heads 102, 88, 84, 80 us; 256 channels, of 64, 256, 512 and 768: six
+  // prompts of up to 2000 tokens 288, 218, 182, 186 us
+  constexpr int kTileCost = DC == 512 ? 256 : 512;
+  constexpr int M = 64, kStages = Stage::kStages, kLead = Stage::kLead, kStageShift = Stage::kShift, kStageKeys = Stage::kKeys;
   __shared__ __attribute__((aligned(256))) Lds lds;
   const int tid = threadIdx.x, w = uni(tid >> 6);
-  clear_notes(lds.notes);
+  clear_notes(lds.notes, tid);
   if (tid == 0) lds.flag[0] = lds.flag[1] = -1;
   LatWork work;
-  if (!lat_find<M, kWaves64>(a, lds.find, work)) return;
+  if (!lat_find<M, kWaves64, kTileCost>(a, lds.find, work)) return;
   int step = 0;                                     // of the workgroup, over all tiles
+  bool odd_before = false;                          // the value waves': the tile before left notes
   int* limits = lds.notes.limit;                    // in turn with limit2: the value waves may still read the tile's before
   do {
     work.tile<M>();
@@ -326,7 +362,8 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
     const LatSeq seq = work.seq;
     const int r0 = work.r0, n_rows = work.n_rows, last = seq.ctx + work.plan.token(r0 + n_rows - 1);   // the last key
     const int first_limit = seq.ctx + work.plan.token(r0);   // keys behind it are not all rows'
-    const int i0 = 2 * work.j0, n = min(2 * work.j1, (last >> kStageShift) + 1) - i0;   // stages
+    constexpr int kCut = kLatKeys / kStageKeys;
+    const int i0 = kCut * work.j0, n = min(kCut * work.j1, (last >> kStageShift) + 1) - i0;   // stages
     const bool in_part = last != first_limit;
     auto look = [&](int i) { return in_part && ((i0 + i) << kStageShift) + kStageKeys - 1 > first_limit; };   // keys that rows see in part
     if (tid < M) limits[tid] = seq.ctx + work.plan.token(r0 + min(tid, n_rows - 1));
@@ -350,13 +387,13 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
       x.sums(lds);
       barrier_lds();
     } else {
-      const int part = w & 1, page = (w >> 1) & 1;  // half `part` of page `page` of a stage is this wave's to bring
+      const int part = DC == 512 ? w & 1 : 0, page = DC == 512 ? (w >> 1) & 1 : w & 3;   // this wave brings rows from 8 part on of a stage's page `page`
       const int kv = seq.ctx + seq.q_len, pages = (kv + kPage - 1) / kPage;
       const int32_t* const bt = a.block_table + (size_t)work.b * a.bt_stride;
       // Ids of 64 stages' pages at once (the sequence's last one where there is none; zeros take its place).  They are waited for here: the
       // compiler, which does not know of the copies, would wait in every step, for these too.
       auto ids_from = [&](int i) {
-        int ids = bt[min(2 * (i0 + i + (tid & 63)) + page, pages - 1)];
+        int ids = bt[min(Stage::kPages * (i0 + i + (tid & 63)) + page, pages - 1)];
         __asm__ volatile("" : "+v"(ids));
         return ids;
       };
@@ -366,7 +403,7 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
         return reinterpret_cast<const char*>(a.cache) + (size_t)clamp_page(id, a.num_pages) * Page::kBytes;
       };
       const unsigned pages_at = lds_address(lds.page[0][page]);
-      constexpr int kStageBytes = 2 * Page::kBytes;
+      constexpr int kStageBytes = Stage::kPages * Page::kBytes;
       Copies copies;
       copies.start(part);
       LatValues<DC, DR> x;
@@ -376,29 +413,31 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
         for (int c = 0; c < Copies::kCopies; c += 2) copies.copy2(c, part, src, pages_at + i % kStages * kStageBytes, 1);
       };
       bring(0);
-      if (n > 1) bring(1);
+      if (kLead > 1 && n > 1) bring(1);
       x.start(w - 4);
       barrier_lds();                                // the queries are there
+      if (odd_before) clear_notes(lds.notes, tid - 256);   // all have left the tile before
+      odd_before = false;
       // Behind it a stage of this wave's is there for all, and the one after it on its way.
       auto arrive = [&](int i) {
-        if (i + 1 < n) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");
+        if (kLead > 1 && i + 1 < n) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");
         else wait_copies();
         const int valid = kv - ((i0 + i) << kStageShift) - kPage * page;
         if (i < n && valid < kPage) Copies::clear(lds.page[i % kStages][page], part, max(valid, 0));
         barrier_lds();
       };
       arrive(0);
-      if (n > 2) bring(2);
+      if (n > kLead) bring(kLead);
       ++step;
 #pragma unroll 1
       for (int i = 1; i <= n; ++i, ++step) {
         const char* const stage = lds.page[(i - 1) % kStages][0];
         x.first(stage);                             // before the weights are there
-        if (((i + 2) & 63) == 0) ids = ids_from(i + 2);
-        const char* const src = source(i + 2);
+        if (((i + kLead) & 63) == 0) ids = ids_from(i + kLead);
+        const char* const src = source(i + kLead);
         arrive(i);
         if (look(i - 1)) {
-          note_odd<Page>(lds.page[(i - 1) % kStages][page], ((i0 + i - 1) << kStageShift) + kPage * page, lds.notes, 8 * part, 8 * part + 8);
+          note_odd<Page>(lds.page[(i - 1) % kStages][page], ((i0 + i - 1) << kStageShift) + kPage * page, lds.notes, 8 * part, 8 * part + Copies::kMine);
           barrier_lds();
           x.first(stage);
         }
@@ -410,21 +449,23 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
           x.weights(lds, step - 1);
         }
         // All copies at once, while the score waves have the matrix units; these waves' products are made while the others weigh.
-        const int more = i + 2 < n;
+        const int more = i + kLead < n;
 #pragma unroll
-        for (int c = 0; c < Copies::kCopies; c += 2) copies.copy2(c, part, src, pages_at + (i + 2) % kStages * kStageBytes, more);
+        for (int c = 0; c < Copies::kCopies; c += 2) copies.copy2(c, part, src, pages_at + (i + kLead) % kStages * kStageBytes, more);
         x.add(stage);
       }
       // ---- the output or the partial
       barrier_lds();
       const LatArgsPtr args = args_anew();
-      const bool odd = uni(lds.notes.any_odd) != 0, whole = work.starts && work.ends;
-      // Through LDS, so that rows are stored in whole lines (half a row's share by the lane that has it: 10 times as long): 32 rows at once, in the
-      // places of the half pages that this wave brings, chunk c of row r in slot c ^ r.
+      const bool odd = uni(lds.notes.any_odd) != 0;
+      odd_before = odd;
+      const bool whole = work.starts && work.ends;
+      // Through LDS, so that rows are stored in whole lines (half a row's share by the lane that has it: 10 times as long): 32 rows at once, in
+      // places that this wave brings (the first stages', the others may take the next tile's queries), chunk c of row r in slot c ^ r.
       constexpr int kShare = DC / 4, kChunks = kShare / 4;    // of a row: the wave's channels, in chunks of 4
-      static_assert(kPage * kShare * 4 == 8 * Page::kRowBytes, "16 rows are a half page's");
+      static_assert(kPage * kShare * 4 == 8 * Page::kRowBytes, "16 rows are half a page's");
       auto place = [&](int r, int c) {
-        return lds.page[r >> 4][page] + part * 8 * Page::kRowBytes + (r & 15) * kShare * 4 + 16 * (c ^ (r & 15));
+        return lds.page[DC == 512 ? r >> 4 : 0][page] + (DC == 512 ? part : r >> 4) * 8 * Page::kRowBytes + (r & 15) * kShare * 4 + 16 * (c ^ (r & 15));
       };
       int lane = tid & 63;
       __asm__ volatile("" : "+v"(lane));            // else the addresses are made before the first tile, and kept in scratch memory
@@ -463,14 +504,6 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
             if (32 * t + r + r0 < n_rows) *reinterpret_cast<bf16x4*>(to + r * DC) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
           }
         }
-      }
-    }
-    // The notes are cleared by all, behind a barrier; else the score waves go on to the next tile's queries.
-    if (in_part) {
-      barrier_lds();
-      if (uni(lds.notes.any_odd) != 0) {
-        barrier_lds();
-        clear_notes(lds.notes);
       }
     }
     limits = limits == lds.limit2 ? lds.notes.limit : lds.limit2;

@@ -179,10 +179,9 @@ template <int DC, int M> struct LatNotes {
 };
 
 // ---- the plan --------------------------------------------------------------------------------------------------------
-// A sequence's rows are cut into tiles of `tile_rows` (group * M).  Work is measured in keys: tile u costs its keys, kTileCost and
-// what its rows add, such that the cost of tiles 0 .. u - 1 is u (ctx + kTileCost) + (u (u + 1) slope >> 8), slope
-// being 256 times half the tokens of a tile.
-constexpr int kTileCost = 64;
+// A sequence's rows are cut into tiles of `tile_rows` (group * M).  Work is measured in keys: tile u costs its keys, tile_cost (its
+// start, join and stores, in the time of so many keys) and what its rows add, such that the cost of tiles 0 .. u - 1 is u (ctx + tile_cost) +
+// (u (u + 1) slope >> 8), slope being 256 times half the tokens of a tile.
 
 struct LatSeq {
   int q_start, q_len, ctx;
@@ -190,11 +189,12 @@ struct LatSeq {
 
 struct LatPlan {
   int tile_rows, tile_shift, slope, heads;          // tile_rows = 1 << tile_shift
+  int tile_cost;
   unsigned long long per_head;                      // 2^35 / heads, rounded up
   // row / heads: exact, as rows are below 2^28 and heads 128 at most
   __device__ __forceinline__ int token(int row) const { return (int)(((unsigned long long)(unsigned)row * per_head) >> 35); }
   __device__ __forceinline__ long long before(const LatSeq& s, long long u) const {
-    return u * (s.ctx + kTileCost) + ((u * (u + 1) * slope) >> 8);
+    return u * (s.ctx + tile_cost) + ((u * (u + 1) * slope) >> 8);
   }
   __device__ __forceinline__ int tiles(const LatSeq& s) const {
     return (s.q_len * heads + tile_rows - 1) >> tile_shift;   // at most 2^21 tokens of 128 heads
@@ -204,8 +204,8 @@ struct LatPlan {
     return (s.ctx + token(row) + kLatKeys) >> kLatKeysShift;
   }
   // the stage at which cost `at` of a tile that starts at 0 is cut
-  __device__ __forceinline__ static int stage_at(long long at, int stages) {
-    const long long j = (at - kTileCost) >> kLatKeysShift;
+  __device__ __forceinline__ int stage_at(long long at, int stages) const {
+    const long long j = (at - tile_cost) >> kLatKeysShift;
     return j < 0 ? 0 : j > stages ? stages : (int)j;
   }
   // the tile that cost `at` of a sequence falls into
@@ -292,8 +292,8 @@ struct LatWork {
     j0 = j1 = 0;
     if (n_rows <= 0) return;
     const int stages = plan.stages(seq, r0 + n_rows - 1);
-    j0 = starts ? 0 : min(LatPlan::stage_at(lo - t0, all_stages), stages);
-    j1 = ends ? stages : min(LatPlan::stage_at(hi - t0, all_stages), stages);
+    j0 = starts ? 0 : min(plan.stage_at(lo - t0, all_stages), stages);
+    j1 = ends ? stages : min(plan.stage_at(hi - t0, all_stages), stages);
     if (starts && !ends) job = int4{(int)row0, n_rows, index, cut.of(t1 - 1) - share + 1};
     // a piece of a cut tile without keys
     if (j0 >= j1 && !(starts && ends) && threadIdx.x < M)
@@ -314,11 +314,11 @@ struct LatWork {
 
 // Finds the workgroup's share; false: it has none.  Workgroups with one number modulo `group` (a power of two) take the same member of the
 // tiles, and shares of an XCD's workgroups follow one another.
-template <int M, int kWaves> __device__ __forceinline__ bool lat_find(const LatentArgs& a, LatFind& lds, LatWork& work) {
+template <int M, int kWaves, int kTileCost> __device__ __forceinline__ bool lat_find(const LatentArgs& a, LatFind& lds, LatWork& work) {
   constexpr int kThreads = 64 * kWaves;
   const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6);
   const int group = a.group;
-  work.plan = LatPlan{group * M, __builtin_ctz(group * M), a.slope, a.heads, a.per_head};
+  work.plan = LatPlan{group * M, __builtin_ctz(group * M), a.slope, a.heads, kTileCost, a.per_head};
   work.job = int4{0, 0, 0, 0};
   if (tid == 0) lds.bad = 0;
   __syncthreads();
@@ -408,9 +408,11 @@ template <typename Page, int DC, int M> __device__ __forceinline__ void note_odd
   }
 }
 
-template <int DC, int M> __device__ __forceinline__ void clear_notes(LatNotes<DC, M>& notes) {
-  for (int i = threadIdx.x; i < DC; i += blockDim.x) notes.odd[i] = INT32_MAX;
-  if (threadIdx.x == 0) notes.any_odd = 0;
+// By the first 256 of the threads that call it.
+template <int DC, int M> __device__ __forceinline__ void clear_notes(LatNotes<DC, M>& notes, int thread) {
+  if (thread >= 256) return;
+  for (int i = thread; i < DC; i += 256) notes.odd[i] = INT32_MAX;
+  if (thread == 0) notes.any_odd = 0;
 }
 
 }  // namespace
