@@ -114,6 +114,9 @@ template <int DC, int DR> struct LatRows16 {
 
 // Up to 16 rows a sequence: every wave takes pages of its own, two in LDS, and no barrier until the tile ends, where the four waves'
 // outputs are joined in LDS.  The products are far from their limit here, what counts is that copies never pause.
+// 64 sequences of 2K to 16K tokens and 16 heads, 666 MB: 110 us (6.0 TB/s; read past the caches the same bytes take 94), of which 98 in the pages;
+// 5 us until the first page is asked for (lengths, cut, page ids) and 6 for the join.  One sequence of 2731 tokens: 12 us, and 6 to 7
+// for the join of its 42 pieces.  Four waves that share stages of 64 keys: 143 and 31 us for both cases with their joins.
 template <int DC, int DR>
 __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) {
   using Rows = LatRows16<DC, DR>;
@@ -250,11 +253,14 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
 
 // Joins the partials of cut tiles: job (first row, rows, index of the first piece's workgroup, shares).  A tile's first piece is in slot
 // 1 of that workgroup, the others in slot 0 of the shares that follow, in order (kLatentGrid pieces at most).  A lane takes DC / 64 channels of a
-// row.  Work is counted in turns of a workgroup: four rows of few pieces, a wave each, or one row of many, of which each wave takes a fourth
+// row.  Bound by the latency of job, maxima and partials (5 to 7 us), where all workgroups cut 64-row tiles by the partials' 67 MB (15 us, 4.5 TB/s).
+// Work is counted in turns of a workgroup: four rows of few pieces, a wave each, or one row of many, of which each wave takes a fourth
 // (one wave with 62 pieces in a row waited for 16 times its first loads).
 template <int DC, int M>
 __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a) {
   static_assert(kLatentGrid == kLatThreads, "a thread a job; a lane a piece");
+  // at most 0, 3, 8 and 64 pieces are few: one sequence of 42 pieces 18.8, 18.8, 18.8, 30.1 us with its attention, of 8000 tokens and 128 heads 28.4,
+  // 28.3, 28.3, 45.8, two prompts of 300 tokens and 128 heads 90.5, 80.8, 81.1, 80.4
   constexpr int kC = DC / 64, kFew = 8;
   __shared__ float s_top[kLatWaves], s_sum[kLatWaves];
   __shared__ int s_turns[kLatWaves];

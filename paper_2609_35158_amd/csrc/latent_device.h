@@ -12,6 +12,7 @@ namespace {
 constexpr int kLatWaves = 4;
 constexpr int kLatThreads = 64 * kLatWaves;
 constexpr int kLatKeysShift = 6, kLatKeys = 1 << kLatKeysShift;   // of a stage: where work is cut
+// A row's maximum may lag the true one by so much (log2 units): weights are below 2^8, sums of 2^25 keys below 2^33.
 constexpr float kLag = 8.f;
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
