@@ -1,0 +1,87 @@
+"""Attention over a paged cache of latent rows where workgroups have much to do: shares of many tiles, tiles of more pages than the ids
+that a wave holds at once, many sequences, and values that are not finite among them."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_35158_amd as pa
+from latent_helpers import torch_latent
+from rope_helpers import dev
+
+pytestmark = pytest.mark.gpu
+
+SCALE = 192.0 ** -0.5
+
+
+def _batch(heads, dc, ctx, new, seed):
+    width = dc + {512: 64, 256: 32}[dc]
+    kv = np.add(ctx, new)
+    pages = (kv + 15) // 16
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    cache = torch.empty((int(pages.sum()) + 2, 16, width), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    perm = np.random.default_rng(seed).permutation(len(cache))
+    bt = np.full((len(kv), int(pages.max())), -1)
+    at = 0
+    for b, n in enumerate(pages):
+        bt[b, :n] = perm[at:at + n]
+        at += n
+    cu = np.concatenate([[0], np.cumsum(new)])
+    q = (torch.randn((int(cu[-1]), heads, width), generator=gen, device="cuda") * 1.15).to(torch.bfloat16)
+    return q, cache, bt, cu, kv
+
+
+def _check(q, cache, bt, kv, dc, out, lse):
+    """One sequence, within the roundings: weights to bf16 (2^-8 of themselves: `size` times that), the result to bf16, and sums over
+    the keys in 32 bits (below 2^-10 of `size`)."""
+    rows = cache[dev(bt, np.int64)[:(kv + 15) // 16]].flatten(0, 1)[:kv]
+    ref, ref_lse, size = torch_latent(q, rows, dc, SCALE)
+    off = (out.double() - ref).abs()
+    assert float((off - 2.0 ** -8 * ref.abs() - (2.0 ** -8 + 2.0 ** -10) * size).max()) <= 0
+    assert float(off.norm() / ref.norm()) < 2.0 ** -8
+    assert float((lse.double() - ref_lse).abs().max()) < 3e-5
+
+
+@pytest.mark.parametrize("heads,dc,ctx,new", [(64, 512, [5000, 30], [500, 90]), (16, 512, [40, 700, 0], [230, 200, 261]), (20, 256, [3000, 0], [600, 900]),
+                                              (128, 256, [100], [257])])
+def test_many_tiles(heads, dc, ctx, new):
+    q, cache, bt, cu, kv = _batch(heads, dc, ctx, new, seed=heads + dc)
+    out, lse = pa.latent_prefill_append(q, cache, dev(bt), dev(ctx), dev(cu), max(new), int(kv.max()), SCALE, return_lse=True)
+    for b, n in enumerate(kv):
+        sl = slice(int(cu[b]), int(cu[b + 1]))
+        _check(q[sl], cache, bt[b], int(n), dc, out[sl], lse[sl])
+
+
+@pytest.mark.parametrize("heads,dc", [(16, 512), (32, 512), (128, 512), (16, 256), (48, 256)])
+def test_shares_of_many_pages(heads, dc):
+    """More than 64 pages a wave (16 rows a sequence) or 64 stages a share (more rows)."""
+    ctx = np.random.default_rng(heads).integers(14000, 15000, size=90)
+    q, cache, bt, cu, kv = _batch(heads, dc, ctx, np.ones(90, int), seed=heads)
+    out, lse = pa.latent_decode(q, cache, dev(bt), dev(ctx), int(kv.max()), SCALE, return_lse=True)
+    for b in (0, 17, 44, 45, 89):
+        _check(q[b:b + 1], cache, bt[b], int(kv[b]), dc, out[b:b + 1], lse[b:b + 1])
+
+
+@pytest.mark.parametrize("heads,dc", [(20, 256), (16, 512)])
+def test_not_finite_among_many_tiles(heads, dc):
+    """A new token's NaN reaches the tokens from it on, in every channel (its scores are NaN); its infinite channel of a score of minus
+    infinity reaches theirs alone.  Tokens before it, and the other sequence, are what they are without."""
+    new = [900, 700]
+    q, cache, bt, cu, kv = _batch(heads, dc, [0, 11], new, seed=7)
+    q[:, :, 5] = q[:, :, 5].abs() + 0.25                       # so that scores of a channel of minus infinity are minus infinity
+    args = (dev(bt), dev([0, 11]), dev(cu), max(new), int(kv.max()), SCALE)
+    clean, clean_lse = pa.latent_prefill_append(q, cache, *args, return_lse=True)
+    for value in (float("nan"), float("-inf")):
+        bad = cache.clone()
+        for t in (13, 410, 411, 777):
+            bad[int(bt[0, t // 16]), t % 16, 5] = value
+        out, lse = pa.latent_prefill_append(q, bad, *args, return_lse=True)
+        assert torch.equal(out[:13], clean[:13]) and torch.equal(out[900:], clean[900:])
+        assert torch.equal(lse[:13], clean_lse[:13]) and torch.equal(lse[900:], clean_lse[900:])
+        hit = out[13:900]
+        if value != value:
+            assert bool(torch.isnan(hit).all())
+        else:
+            assert bool(torch.isnan(hit[:, :, 5]).all())
+            rest = torch.cat([hit[:, :, :5], hit[:, :, 6:]], -1)
+            assert bool(torch.isfinite(rest).all()) and bool(torch.isfinite(lse[13:900]).all())
