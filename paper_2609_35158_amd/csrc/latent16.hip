@@ -135,7 +135,7 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
     if (work.j0 >= work.j1) continue;
     const LatSeq seq = work.seq;
     const int r0 = work.r0, n_rows = work.n_rows, last = seq.ctx + work.plan.token(r0 + n_rows - 1);   // the last key
-    const int kv = seq.ctx + seq.q_len, p1 = min(work.j1 * kLatWaves, last / kPage + 1);
+    const int p1 = min(work.j1 * kLatWaves, last / kPage + 1);
     const int first_limit = seq.ctx + work.plan.token(r0);   // keys behind it are not all rows'
     const bool in_part = last != first_limit;
     const int32_t* const bt = a.block_table + (size_t)work.b * a.bt_stride;
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
           wait_copies();
         }
         const int key0 = p * kPage;
-        if (kv - key0 < kPage) Copies::clear(page, kv - key0);   // rows behind the sequence's end
+        if (last + 1 - key0 < kPage) Copies::clear(page, last + 1 - key0);   // keys that no row sees are none of the products'
         x.scores(page);
         if (key0 + kPage - 1 > first_limit) {
           x.mask(lds.notes.limit, key0);

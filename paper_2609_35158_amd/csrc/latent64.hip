@@ -409,9 +409,9 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
       barrier_lds();
     } else {
       const int part = DC == 512 ? w & 1 : 0, page = DC == 512 ? (w >> 1) & 1 : w & 3;   // this wave brings rows from 8 part on of a stage's page `page`
-      const int kv = seq.ctx + seq.q_len, pages = (kv + kPage - 1) / kPage;
+      const int pages = last / kPage + 1;
       const int32_t* const bt = a.block_table + (size_t)work.b * a.bt_stride;
-      // Ids of 64 stages' pages at once (the sequence's last one where there is none; zeros take its place).  They are waited for here: the
+      // Ids of 64 stages' pages at once (the last one where there is none; zeros take its place).  They are waited for here: the
       // compiler, which does not know of the copies, would wait in every step, for these too.
       auto ids_from = [&](int i) {
         int ids = bt[min(Stage::kPages * (i0 + i + (tid & 63)) + page, pages - 1)];
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
       auto arrive = [&](int i) {
         if (kLead > 1 && i + 1 < n) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");
         else wait_copies();
-        const int valid = kv - ((i0 + i) << kStageShift) - kPage * page;
+        const int valid = last + 1 - ((i0 + i) << kStageShift) - kPage * page;   // keys that no row sees are none of the products'
         if (i < n && valid < kPage) Copies::clear(lds.page[i % kStages][page], part, max(valid, 0));
         barrier_lds();
       };

@@ -85,3 +85,21 @@ def test_not_finite_among_many_tiles(heads, dc):
             assert bool(torch.isnan(hit[:, :, 5]).all())
             rest = torch.cat([hit[:, :, :5], hit[:, :, 6:]], -1)
             assert bool(torch.isfinite(rest).all()) and bool(torch.isfinite(lse[13:900]).all())
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("heads,dc", [(64, 512), (100, 512), (128, 512), (128, 256), (8, 512)])
+def test_not_finite_in_later_tokens(heads, dc, value):
+    """A tile whose rows are all one token's, in a page with later tokens: what these hold does not reach it."""
+    ctx, new = [5, 40, 0], [20, 3, 2]
+    q, cache, bt, cu, kv = _batch(heads, dc, ctx, new, seed=heads)
+    args = (dev(bt), dev(ctx), dev(cu), max(new), int(kv.max()), SCALE)
+    bad, first = cache.clone(), [9, 1, 1]
+    for b, i in enumerate(first):
+        at = ctx[b] + i
+        bad[int(bt[b, at // 16]), at % 16, 7:dc:3] = value
+    out, lse = pa.latent_prefill_append(q, bad, *args, return_lse=True)
+    for b, i in enumerate(first):
+        lo, at, hi = int(cu[b]), int(cu[b]) + i, int(cu[b + 1])
+        _check(q[lo:at], bad, bt[b], ctx[b] + i, dc, out[lo:at], lse[lo:at])
+        assert not bool(torch.isfinite(out[at:hi, :, 7:dc:3]).any())
