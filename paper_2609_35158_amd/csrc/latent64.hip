@@ -14,10 +14,11 @@
 // largest; what was weighed with another is scaled by a power of two.
 
 // Bound by the score and value waves' chains: a step of 32 keys takes about 1950 cycles, of which the matrix units are busy 1088 (54%).  A value
-// wave's: 150 for weights and flag, 780 for nine copies (four waves' 36 KiB pass at 20 cycles a KiB), 620 for its products, 350 for operands, arrival and
-// barrier; a score wave's: 870 for scores beside the others' products, 430 for weights, 140 for sums, the rest waits.
-// Measured at 512 channels: turns of 500 to 2000 tokens on contexts of 4K to 16K, 16 heads, 2.90 TFLOP, 2.55 ms (1140 TF/s; the library's product of
-// two 8192 x 8192 matrices 1350); of 64 to 400 tokens 0.84 ms (1100 TF/s).  A step of 32 sequences with 128 heads, 282 MB and 66 GFLOP, 84 us: bytes on
+// wave's: 150 for weights and flag, 600 to 780 for seven to nine copies (36 KiB a step pass at 20 cycles a KiB), 620 for its products, 350 for operands,
+// arrival and barrier; a score wave's: 870 for scores beside the others' products, 430 for weights, 140 for sums, the rest waits; at 512 channels it makes
+// two of the copies behind its scores (2.56 -> 2.51 ms for the long turns below; four 2.57, or behind the weights 2.54).
+// Measured at 512 channels: turns of 500 to 2000 tokens on contexts of 4K to 16K, 16 heads, 2.90 TFLOP, 2.51 ms (1155 TF/s; the library's product of
+// two 8192 x 8192 matrices 1350); of 64 to 400 tokens 0.83 ms (1115 TF/s).  A step of 32 sequences with 128 heads, 282 MB and 66 GFLOP, 84 us: bytes on
 // their way, two stages a compute unit.  At 256 channels six prompts of 300 to 2000 tokens, 115 GFLOP, 182 us.
 // Tried: four waves that do both in turn, stages of 64 keys, two in LDS (2.69 ms); eight in lockstep or in two alternating sets (3.4 to 3.5 ms); copies
 // spread among the products (2.78 for 2.66 ms on one card: the copies go out while the score waves have the matrix units); touching the lines of later stages so that they
@@ -50,11 +51,13 @@ template <int DC, int DR> struct LatLds64 {
   LatFind find;
 };
 
-// A value wave's copies in a stage, 1 KiB an instruction: half a page (8 rows) or (256 channels) a page.
+// The copies of a stage, 1 KiB an instruction: half a page (8 rows) a value wave or (256 channels) a page, of which a score wave makes kPairs pairs.
 template <int DC, int DR> struct LatMyCopies {
   using Page = LatPage<DC, DR, true>;
   static constexpr int kMine = DC == 512 ? 8 : 16;  // rows
   static constexpr int kRows = 1024 / Page::kRowBytes, kLatent = kMine / kRows, kCopies = kLatent + 1;
+  static constexpr int kPairs = DC == 512 ? 1 : 0;  // that a score wave makes, the last ones of the latent parts
+  static constexpr int kGiven = kLatent - 2 * kPairs, kGivenRow = kRows * kGiven;
   static_assert(kMine * Page::kRotBytes == 1024, "one instruction takes the rotated parts");
   int off[kCopies];                                 // the lane's source offsets in the page
   __device__ __forceinline__ void start(int half) {
@@ -108,9 +111,9 @@ template <int DC, int DR> struct LatMyCopies {
           : "memory", "scc", "m0");
     }
   }
-  // Zeros in place of its latent parts from row `valid` of the page on (of rotated parts scores alone are made, which are masked).
-  __device__ static __forceinline__ void clear(char* page, int half, int valid) {
-    for (int i = max(valid, 8 * half) * Page::kRowBytes + 16 * (threadIdx.x & 63); i < (8 * half + kMine) * Page::kRowBytes; i += 1024)
+  // Zeros in place of the latent parts of rows r0 .. r1 - 1 from row `valid` of the page on (of rotated parts scores alone are made, which are masked).
+  __device__ static __forceinline__ void clear(char* page, int r0, int r1, int valid) {
+    for (int i = max(valid, r0) * Page::kRowBytes + 16 * (threadIdx.x & 63); i < r1 * Page::kRowBytes; i += 1024)
       *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
   }
 };
@@ -388,16 +391,49 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
     const bool in_part = last != first_limit;
     auto look = [&](int i) { return in_part && ((i0 + i) << kStageShift) + kStageKeys - 1 > first_limit; };   // keys that rows see in part
     if (tid < M) limits[tid] = seq.ctx + work.plan.token(r0 + min(tid, n_rows - 1));
+    const int part = DC == 512 ? w & 1 : 0, page = DC == 512 ? (w >> 1) & 1 : w & 3;   // this wave brings rows from 8 part on of a stage's page `page`
+    const int pages = last / kPage + 1;
+    const int32_t* const bt = a.block_table + (size_t)work.b * a.bt_stride;
+    // Ids of 64 stages' pages at once (the last one where there is none; zeros take its place).  They are waited for here: the
+    // compiler, which does not know of the copies, would wait in every step, for these too.
+    auto ids_from = [&](int i) {
+      int ids = bt[min(Stage::kPages * (i0 + i + (tid & 63)) + page, pages - 1)];
+      __asm__ volatile("" : "+v"(ids));
+      return ids;
+    };
+    auto source = [&](int ids, int i) {             // of stage i
+      const int id = __builtin_amdgcn_readlane(ids, i & 63);
+      return reinterpret_cast<const char*>(a.cache) + (size_t)clamp_page(id, a.num_pages) * Page::kBytes;
+    };
+    const unsigned pages_at = lds_address(lds.page[0][page]);
+    constexpr int kStageBytes = Stage::kPages * Page::kBytes;
+    const int how = a.group == 1 ? 2 : 1;
     if (w < 4) {
       LatScores<DC, DR> x;
       __builtin_amdgcn_s_setprio(3);
       x.start(lds, w, args_anew()->q + work.row0 * (DC + DR), n_rows);
+      Copies copies;
+      copies.start(part);
+      int ids = ids_from(0);
 #pragma unroll 1
       for (int i = 0; i <= n; ++i, ++step) {
+        const char* src = nullptr;
+        if constexpr (Copies::kPairs > 0) {
+          if (((i + kLead) & 63) == 0) ids = ids_from(i + kLead);
+          src = source(ids, i + kLead);
+          if (i + 1 < n) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * Copies::kPairs) : "memory");
+          else wait_copies();
+          const int valid = last + 1 - ((i0 + i) << kStageShift) - kPage * page;
+          if (i > kLead && i < n && valid < kPage)
+            Copies::clear(lds.page[i % kStages][page], 8 * part + Copies::kGivenRow, 8 * part + Copies::kMine, max(valid, 0));
+        }
         barrier_lds();
         const int key0 = (i0 + i) << kStageShift;
         const int flag = i < n ? x.scores(lds, lds.page[i % kStages][0], step) : uni(lds.flag[(step - 1) & 1]);
         if (i > 0) {
+#pragma unroll
+          for (int c = Copies::kGiven; c < Copies::kLatent; c += 2)
+            copies.copy2(c, part, src, pages_at + (i + kLead) % kStages * kStageBytes, i + kLead < n ? how : 0);
           x.take_up(lds, step - 1, flag);
           if (look(i - 1)) barrier_lds();           // while the value waves see to values that are not finite
         }
@@ -408,29 +444,12 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
       x.sums(lds);
       barrier_lds();
     } else {
-      const int part = DC == 512 ? w & 1 : 0, page = DC == 512 ? (w >> 1) & 1 : w & 3;   // this wave brings rows from 8 part on of a stage's page `page`
-      const int pages = last / kPage + 1;
-      const int32_t* const bt = a.block_table + (size_t)work.b * a.bt_stride;
-      // Ids of 64 stages' pages at once (the last one where there is none; zeros take its place).  They are waited for here: the
-      // compiler, which does not know of the copies, would wait in every step, for these too.
-      auto ids_from = [&](int i) {
-        int ids = bt[min(Stage::kPages * (i0 + i + (tid & 63)) + page, pages - 1)];
-        __asm__ volatile("" : "+v"(ids));
-        return ids;
-      };
-      int ids = ids_from(0);
-      auto source = [&](int i) {                    // of stage i
-        const int id = __builtin_amdgcn_readlane(ids, i & 63);
-        return reinterpret_cast<const char*>(a.cache) + (size_t)clamp_page(id, a.num_pages) * Page::kBytes;
-      };
-      const unsigned pages_at = lds_address(lds.page[0][page]);
-      constexpr int kStageBytes = Stage::kPages * Page::kBytes;
-      const int how = a.group == 1 ? 2 : 1;
       Copies copies;
       copies.start(part);
+      int ids = ids_from(0);
       LatValues<DC, DR> x;
       auto bring = [&](int i) {
-        const char* const src = source(i);
+        const char* const src = source(ids, i);
 #pragma unroll
         for (int c = 0; c < Copies::kCopies; c += 2) copies.copy2(c, part, src, pages_at + i % kStages * kStageBytes, how);
       };
@@ -442,10 +461,14 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
       odd_before = false;
       // Behind it a stage of this wave's is there for all, and the one after it on its way.
       auto arrive = [&](int i) {
-        if (kLead > 1 && i + 1 < n) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");
-        else wait_copies();
+        if (kLead > 1 && i + 1 < n) {
+          if (i == 0) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies) : "memory");
+          else __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(Copies::kCopies - 2 * Copies::kPairs) : "memory");
+        } else {
+          wait_copies();
+        }
         const int valid = last + 1 - ((i0 + i) << kStageShift) - kPage * page;   // keys that no row sees are none of the products'
-        if (i < n && valid < kPage) Copies::clear(lds.page[i % kStages][page], part, max(valid, 0));
+        if (i < n && valid < kPage) Copies::clear(lds.page[i % kStages][page], 8 * part, 8 * part + (i > kLead ? Copies::kGivenRow : Copies::kMine), max(valid, 0));
         barrier_lds();
       };
       arrive(0);
@@ -456,7 +479,7 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
         const char* const stage = lds.page[(i - 1) % kStages][0];
         x.first(stage);                             // before the weights are there
         if (((i + kLead) & 63) == 0) ids = ids_from(i + kLead);
-        const char* const src = source(i + kLead);
+        const char* const src = source(ids, i + kLead);
         arrive(i);
         if (look(i - 1)) {
           note_odd<Page>(lds.page[(i - 1) % kStages][page], ((i0 + i - 1) << kStageShift) + kPage * page, lds.notes, 8 * part, 8 * part + Copies::kMine);
@@ -473,7 +496,8 @@ __global__ __launch_bounds__(64 * kWaves64, 2) void latent64_kernel(LatentArgs a
         // All copies at once, while the score waves have the matrix units; these waves' products are made while the others weigh.
         const int more = i + kLead < n ? how : 0;
 #pragma unroll
-        for (int c = 0; c < Copies::kCopies; c += 2) copies.copy2(c, part, src, pages_at + (i + kLead) % kStages * kStageBytes, more);
+        for (int c = 0; c < Copies::kCopies; c += 2)
+          if (c < Copies::kGiven || c == Copies::kLatent) copies.copy2(c, part, src, pages_at + (i + kLead) % kStages * kStageBytes, more);
         x.add(stage);
       }
       // ---- the output or the partial
