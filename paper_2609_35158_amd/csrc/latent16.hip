@@ -115,7 +115,7 @@ template <int DC, int DR> struct LatRows16 {
 // Up to 16 rows a sequence: every wave takes pages of its own, two in LDS, and no barrier until the tile ends, where the four waves'
 // outputs are joined in LDS.  The products are far from their limit here, what counts is that copies never pause.
 // 64 sequences of 2K to 16K tokens and 16 heads, 666 MB: 110 us (6.0 TB/s; read past the caches the same bytes take 94), of which 98 in the pages;
-// 5 us until the first page is asked for (lengths, cut, page ids) and 6 for the join.  One sequence of 2731 tokens: 12 us, and 6 to 7
+// 5 us until the first page is asked for (lengths, cut, page ids) and 6 for the join.  One sequence of 2731 tokens: 11 us, and 5
 // for the join of its 42 pieces.  Four waves that share stages of 64 keys: 143 and 31 us for both cases with their joins.
 template <int DC, int DR>
 __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) {
@@ -253,15 +253,15 @@ __global__ __launch_bounds__(kLatThreads, 1) void latent16_kernel(LatentArgs a) 
 
 // Joins the partials of cut tiles: job (first row, rows, index of the first piece's workgroup, shares).  A tile's first piece is in slot
 // 1 of that workgroup, the others in slot 0 of the shares that follow, in order (kLatentGrid pieces at most).  A lane takes DC / 64 channels of a
-// row.  Bound by the latency of job, maxima and partials (5 to 7 us), where all workgroups cut 64-row tiles by the partials' 67 MB (15 us, 4.5 TB/s).
+// row.  Bound by the latency of job, maxima and partials (5 to 6 us), where all workgroups cut 64-row tiles by the partials' 67 MB (15 us, 4.5 TB/s).
 // Work is counted in turns of a workgroup: four rows of few pieces, a wave each, or one row of many, of which each wave takes a fourth
 // (one wave with 62 pieces in a row waited for 16 times its first loads).
 template <int DC, int M>
 __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a) {
   static_assert(kLatentGrid == kLatThreads, "a thread a job; a lane a piece");
-  // at most 0, 3, 8 and 64 pieces are few: one sequence of 42 pieces 18.8, 18.8, 18.8, 30.1 us with its attention, of 8000 tokens and 128 heads 28.4,
-  // 28.3, 28.3, 45.8, two prompts of 300 tokens and 128 heads 90.5, 80.8, 81.1, 80.4
-  constexpr int kC = DC / 64, kFew = 8;
+  // at most 0, 3, 8 and 64 pieces are few: one sequence of 42 pieces 16.2, 16.4, 16.3, 21.2 us with its attention, of 8000 tokens and 128 heads 25.1,
+  // 25.0, 25.0, 31.3, two prompts of 300 tokens and 128 heads 100.8, 81.9, 81.4, 81.7
+  constexpr int kC = DC / 64, kFew = 8, kChunk = 4;   // kChunk: pieces asked for at once (8: the same or 1 to 4% slower)
   __shared__ float s_top[kLatWaves], s_sum[kLatWaves];
   __shared__ int s_turns[kLatWaves];
   __shared__ __attribute__((aligned(16))) int s_end[kLatentGrid];    // turns of the jobs up to each one
@@ -299,8 +299,19 @@ __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a)
     const int r = few ? kLatWaves * at + w : at;
     if (r >= rows) continue;                        // only where no other wave waits for this one
     auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * job.z + 1 : 2 * (job.z + i * a.group)) * M; };
-    // lane k holds the maximum and sum of the wave's piece k; a piece that saw nothing counts nothing, its outputs may be unwritten
+    // The first pieces are asked for before their weights are known (one sequence of 42 pieces 19.1 -> 16.2 us with its attention).  Lane k holds the maximum and sum of the wave's piece k; a piece that saw
+    // nothing counts nothing, its outputs may be unwritten.
     const float2 ml = lane < mine ? reinterpret_cast<const float2*>(a.part_ml)[slot(step * lane + first) + r] : float2{-FLT_MAX, 0.f};
+    f32x4 x[kChunk][kC / 4];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int j = 0; j < kChunk; ++j) {
+        const float* const src = a.part_o + (slot(step * min(k0 + j, mine - 1) + first) + r) * DC + 4 * lane;
+#pragma unroll
+        for (int c = 0; c < kC; c += 4) x[j][c / 4] = *reinterpret_cast<const f32x4*>(src + 64 * c);
+      }
+    };
+    if (mine > 0) load(0);
     const bool seen = ml.y != 0.f;
     float top = seen ? ml.x : -FLT_MAX;
     top = xor32_max(xor16_max(top));
@@ -320,16 +331,15 @@ __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a)
     float o[kC];
 #pragma unroll
     for (int c = 0; c < kC; ++c) o[c] = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < mine; ++k) {
-      const bool use = all_seen >> k & 1;
-      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), k));
-      const float* const src = a.part_o + (slot(step * k + first) + r) * DC + 4 * lane;
+    for (int k0 = 0; k0 < mine; k0 += kChunk) {
+      if (k0 > 0) load(k0);
 #pragma unroll
-      for (int c = 0; c < kC; c += 4) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(src + 64 * c);
+      for (int j = 0; j < kChunk; ++j) {
+        const int k = min(k0 + j, mine - 1);
+        const bool use = k0 + j < mine && (all_seen >> k & 1);
+        const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), k));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[c + e] = use ? fmaf(f, x[e], o[c + e]) : o[c + e];
+        for (int c = 0; c < kC; ++c) o[c] = use ? fmaf(f, x[j][c / 4][c % 4], o[c]) : o[c];
       }
     }
     if (!few) {
