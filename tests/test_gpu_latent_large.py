@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2609_35158_amd as pa
-from latent_helpers import torch_latent
+from latent_helpers import LatentCase, check, torch_latent
 from rope_helpers import dev
 
 pytestmark = pytest.mark.gpu
@@ -103,3 +103,62 @@ def test_not_finite_in_later_tokens(heads, dc, value):
         lo, at, hi = int(cu[b]), int(cu[b]) + i, int(cu[b + 1])
         _check(q[lo:at], bad, bt[b], ctx[b] + i, dc, out[lo:at], lse[lo:at])
         assert not bool(torch.isfinite(out[at:hi, :, 7:dc:3]).any())
+
+
+@pytest.mark.parametrize("batch", [63, 64, 65, 129])
+@pytest.mark.parametrize("heads", [4, 20])
+def test_batches_around_a_wave(batch, heads):
+    """The cut is found in a wave's lanes up to 64 sequences; sequences without new tokens at both ends."""
+    rng = np.random.default_rng(batch)
+    new = rng.choice([0, 1, 2, 4], size=batch)
+    new[0] = new[-1] = 0
+    c = LatentCase(heads, 256, rng.integers(0, 70, size=batch), new, seed=batch)
+    check(c, *c.prefill())
+    c = LatentCase(heads, 256, rng.integers(0, 70, size=batch), np.ones(batch, int), seed=batch)
+    check(c, *c.decode())
+
+
+@pytest.mark.parametrize("batch", [64, 70])
+@pytest.mark.parametrize("heads", [16, 32])
+def test_one_length_that_cannot_be(batch, heads):
+    """Of many sequences the last one's: nothing is written."""
+    c = LatentCase(heads, 512, [40] * batch, [1] * batch, seed=batch)
+    q, cache, bt, ctx, _ = c.args()
+    out = torch.full((batch, heads, 512), 7.0, dtype=torch.bfloat16, device="cuda")
+    ctx[-1] = 4000
+    pa.latent_decode(q, cache, bt, ctx, c.max_kv, c.scale, out=out)
+    assert bool((out == 7).all())
+    ctx[-1] = 40
+    check(c, *pa.latent_decode(q, cache, bt, ctx, c.max_kv, c.scale, return_lse=True))
+
+
+def test_two_graphs_share_a_workspace():
+    """Captured calls of different shapes and kernels on one workspace, replayed in turn with eager calls between."""
+    cases = [LatentCase(16, 512, [3000, 7], [1, 1], seed=1), LatentCase(64, 512, [900, 0], [1, 30], seed=2)]
+    args = [c.args() for c in cases]
+    ws = torch.empty(80 << 20, dtype=torch.uint8, device="cuda")
+    outs = [(torch.empty((c.total, c.heads, 512), dtype=torch.bfloat16, device="cuda"), torch.empty((c.total, c.heads), device="cuda")) for c in cases]
+
+    def call(i, out, lse, work):
+        c, (q, cache, bt, ctx, cu) = cases[i], args[i]
+        pa.latent_prefill_append(q, cache, bt, ctx, cu, c.max_q, c.max_kv, c.scale, out=out, lse=lse, workspace=work)
+
+    for i in (0, 1):
+        call(i, *outs[i], ws)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for i, g in enumerate(graphs):
+        with torch.cuda.graph(g):
+            call(i, *outs[i], ws)
+    for r in range(3):
+        for i in (0, 1):
+            args[i][0].normal_()
+            outs[i][0].zero_()
+        graphs[r % 2].replay()
+        graphs[1 - r % 2].replay()
+        graphs[r % 2].replay()
+        for i in (0, 1):
+            out, lse = torch.empty_like(outs[i][0]), torch.empty_like(outs[i][1])
+            call(i, out, lse, ws)
+            torch.cuda.synchronize()
+            assert torch.equal(out, outs[i][0]) and torch.equal(lse, outs[i][1]), (r, i)
