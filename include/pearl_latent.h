@@ -45,7 +45,8 @@ typedef struct {
  *   rows_new: bf16 [total_q][latent_dim + rope_dim] (read): c, then r; rows_stride elements from a token to the next (a multiple
  *           of 8, >= latent_dim + rope_dim);
  *   q: the last rope_dim channels of every head are written, the others left as they are; cache: written.
- * q_rope and rows_new must not overlap q or the cache.  No other byte of the cache changes; rows whose page id is outside [0, num_pages) or
+ * q_rope may be the tails of q themselves (their rows are then rotated in place); otherwise it and rows_new must not overlap q or
+ * the cache.  No other byte of the cache changes; rows whose page id is outside [0, num_pages) or
  * whose logical page is beyond bt_stride are skipped (their queries are written all the same).
  */
 pearl_status pearl_latent_append(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const pearl_rope* rope,
@@ -63,6 +64,7 @@ size_t pearl_latent_workspace_bytes(const pearl_latent_shape* shape, const pearl
  * Batched single-token decode: seqs->cu_q_lens must be NULL; row b of q and out is sequence b's new token at position
  * ctx_lens[b], whose row the cache already holds (pearl_latent_append first, on the same stream).
  * Contexts are cut into shares that run in parallel and are joined by log-sum-exp.  Weights enter the second product in bf16.
+ * out must not overlap q or the cache.
  */
 pearl_status pearl_attn_latent_decode(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const void* q,
                                       const void* cache, float softmax_scale, void* out, float* lse, void* workspace,

@@ -769,7 +769,8 @@ def latent_append(q_rope: torch.Tensor, rows_new: torch.Tensor, rope: Rope, q: t
                   max_kv_len: int) -> None:
     """New latent rows [total_q][latent_dim + rope_dim] into the cache, the latent part normalised (rope.k_weight), the
     rest rotated; q_rope [total_q][H][rope_dim], rotated, into the last channels of the absorbed queries q
-    [total_q][H][latent_dim + rope_dim] (pearl_latent_append).  rows_new may be a part of wider rows, q_rope of wider heads."""
+    [total_q][H][latent_dim + rope_dim] (pearl_latent_append).  rows_new may be a part of wider rows, q_rope of wider heads, or the
+    tails of q themselves."""
     dev = rope.dev
     need = _on(dev)
     need(cache, "cache", torch.bfloat16)

@@ -6,7 +6,7 @@ import torch
 
 import paper_2609_35158_amd as pa
 from latent_helpers import LatentCase, check, torch_latent
-from rope_helpers import dev
+from rope_helpers import dev, inv_freq
 
 pytestmark = pytest.mark.gpu
 
@@ -162,3 +162,22 @@ def test_two_graphs_share_a_workspace():
             call(i, out, lse, ws)
             torch.cuda.synchronize()
             assert torch.equal(out, outs[i][0]) and torch.equal(lse, outs[i][1]), (r, i)
+
+
+@pytest.mark.parametrize("heads,dc,tokens", [(16, 512, 40), (128, 512, 3), (5, 256, 9000)])
+def test_append_into_the_rows_it_reads(heads, dc, tokens):
+    """The queries' part rotated in place, in the tails of q: what it is from a buffer of its own."""
+    dr = {512: 64, 256: 32}[dc]
+    gen = torch.Generator(device="cuda").manual_seed(heads)
+    rows = torch.randn((tokens, dc + dr), generator=gen, device="cuda").to(torch.bfloat16)
+    q = torch.randn((tokens, heads, dc + dr), generator=gen, device="cuda").to(torch.bfloat16)
+    rope = pa.Rope(dev(inv_freq(dr), np.float32), interleaved=heads == 5)
+    pages = (tokens + 15) // 16
+    bt, ctx, cu = dev(np.arange(pages)[None]), dev([0]), dev([0, tokens])
+    got = []
+    for own in (False, True):
+        out, cache = q.clone(), pa.latent_cache(pages, dc, dr)
+        pa.latent_append(out[..., dc:].clone() if own else out[..., dc:], rows, rope, out, cache, bt, ctx, cu, tokens, tokens)
+        got.append((out, cache))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert not torch.equal(got[0][0][1:, :, dc:], q[1:, :, dc:])
