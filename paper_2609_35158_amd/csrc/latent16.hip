@@ -19,6 +19,58 @@
 namespace pearl {
 namespace {
 
+// The copies of a page by a wave, 1 KiB an instruction, kRows rows' latent parts each, and then the rotated parts.
+// A key is read by one workgroup here: the copies go past the caches (nt).
+template <int DC, int DR> struct LatCopies {
+  using Page = LatPage<DC, DR, false>;
+  static constexpr int kRows = 1024 / Page::kRowBytes;
+  static constexpr int kLatent = kPage / kRows, kCopies = kLatent + kPage * Page::kRotBytes / 1024;
+  static_assert(kLatent % 2 == 0 && Page::kWidth % 32 == 0 && (DR == 32 || Page::kWidth % 128 == 0), "copies in pairs; the swizzle's bits");
+
+  // The lane's source offset in the page, of copy i.
+  __device__ static __forceinline__ int offset(int i) {
+    const int l = threadIdx.x & 63;
+    if (i < kLatent) {
+      const int r = kRows * i + (kRows == 2 ? l >> 5 : 0), slot = kRows == 2 ? l & 31 : l;
+      return r * Page::kWidth + 16 * (slot ^ Page::f(r));
+    }
+    constexpr int kChunks = Page::kRotBytes / 16;
+    const int r = (64 * (i - kLatent) + l) / kChunks;
+    return r * Page::kWidth + Page::kRowBytes + 16 * ((l % kChunks) ^ Page::rot_f(r));
+  }
+
+  // The page at src to the one at the LDS address lds, two copies an asm.  An instruction's immediate offset advances both addresses.
+  __device__ static __forceinline__ void page(const char* src, unsigned lds) {
+#pragma unroll
+    for (int i = 0; i < kCopies; i += 2) {
+      const unsigned to = uni((int)lds + 1024 * i);
+      if (i + 1 < kCopies)
+        __asm__ volatile("s_mov_b32 m0, %3\n\t"
+                         "s_nop 0\n\t"
+                         "global_load_lds_dwordx4 %0, %2 nt\n\t"
+                         "global_load_lds_dwordx4 %1, %2 offset:1024 nt"
+                         :
+                         : "v"(offset(i)), "v"(offset(i + 1) - 1024), "s"(src), "s"(to)
+                         : "memory", "m0");
+      else
+        __asm__ volatile("s_mov_b32 m0, %2\n\t"
+                         "s_nop 0\n\t"
+                         "global_load_lds_dwordx4 %0, %1 nt"
+                         :
+                         : "v"(offset(i)), "s"(src), "s"(to)
+                         : "memory", "m0");
+    }
+  }
+
+  // Zeros in place of the rows from `valid` on.
+  __device__ static __forceinline__ void clear(char* page, int valid) {
+    const int l = threadIdx.x & 63;
+    for (int i = valid * Page::kRowBytes + 16 * l; i < Page::kRot; i += 1024) *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+    for (int i = Page::kRot + valid * Page::kRotBytes + 16 * l; i < Page::kBytes; i += 1024)
+      *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
+  }
+};
+
 template <int DC, int DR> struct LatLds16 {
   char page[kLatWaves][2][LatPage<DC, DR, false>::kBytes];   // at the end of a tile: the waves' outputs
   LatNotes<DC, 16> notes;
@@ -30,7 +82,7 @@ template <int DC, int DR> struct LatLds16 {
 template <int DC, int DR> struct LatRows16 {
   static constexpr int M = 16;
   using Page = LatPage<DC, DR, false>;
-  using Copies = LatCopies<DC, DR, false>;
+  using Copies = LatCopies<DC, DR>;
   static constexpr int kSteps = DC / 32, kAll = kSteps + DR / 32;
   static constexpr int kBlocks = DC / 16;           // of 16 channels
   static constexpr int kAhead = 4;                  // LDS reads of the products' operands, ahead of them

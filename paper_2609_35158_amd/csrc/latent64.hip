@@ -71,7 +71,8 @@ template <int DC, int DR> struct LatMyCopies {
     const int r = l / kChunks + 8 * half;
     off[kLatent] = r * Page::kWidth + Page::kRowBytes + 16 * ((l % kChunks) ^ Page::rot_f(r));
   }
-  // Copies i and i + 1 (the last one, of the rotated parts, by itself) to the page at the LDS address lds, if `go`; past the caches (nt) if it is 2,
+  // Copies i and i + 1 (the last one, of the rotated parts, by itself) to the page at the LDS address lds, if `go` (the branches are the
+  // instructions' own: ones that the compiler sees split the products' code, with moves of all outputs between the parts); past the caches (nt) if it is 2,
   // where no other workgroup reads the keys (64 sequences of 64 heads: 140 instead of 160 us; with two workgroups to the keys of 128 heads
   // 216 instead of 209, with eight 3190 instead of 2590).
   __device__ __forceinline__ void copy2(int i, int half, const char* src, unsigned lds, int go) const {

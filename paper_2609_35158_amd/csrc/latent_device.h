@@ -108,64 +108,6 @@ template <typename Page> struct LatOperand {
   }
 };
 
-// The copies of a page by a wave, 1 KiB an instruction, kRows rows' latent parts each, and then the rotated parts.
-// kWide: as LatPage's; without it, where a key is read by one workgroup, the copies go past the caches (nt).
-template <int DC, int DR, bool kWide> struct LatCopies {
-  using Page = LatPage<DC, DR, kWide>;
-  static constexpr int kRows = 1024 / Page::kRowBytes;
-  static constexpr int kLatent = kPage / kRows, kCopies = kLatent + kPage * Page::kRotBytes / 1024;
-  static_assert(kLatent % 2 == 0 && Page::kWidth % 32 == 0 && (DR == 32 || Page::kWidth % 128 == 0), "copies in pairs; the swizzle's bits");
-
-  // The lane's source offset in the page, of copy i.
-  __device__ static __forceinline__ int offset(int i) {
-    const int l = threadIdx.x & 63;
-    if (i < kLatent) {
-      const int r = kRows * i + (kRows == 2 ? l >> 5 : 0), slot = kRows == 2 ? l & 31 : l;
-      return r * Page::kWidth + 16 * (slot ^ Page::f(r));
-    }
-    constexpr int kChunks = Page::kRotBytes / 16;
-    const int r = (64 * (i - kLatent) + l) / kChunks;
-    return r * Page::kWidth + Page::kRowBytes + 16 * ((l % kChunks) ^ Page::rot_f(r));
-  }
-
-  // Copies i and (if there is one) i + 1 of the page at src to the page at the LDS address lds, if `go`.  The branch is the
-  // instructions' own: one that the compiler sees splits the products' code in two, with moves of all outputs between them.  An
-  // instruction's immediate offset advances both addresses.  (i is a constant where this is inlined.)
-  __device__ static __forceinline__ void copy2(int i, const char* src, unsigned lds, int go) {
-    const unsigned to = uni((int)lds + 1024 * i);
-#define PEARL_LATENT_COPY(SECOND, NT)                                                                                          \
-  __asm__ volatile("s_cmp_eq_u32 %4, 0\n\t"                                                                                    \
-                   "s_cbranch_scc1 .Lno_copy%=\n\t"                                                                            \
-                   "s_mov_b32 m0, %3\n\t"                                                                                      \
-                   "s_nop 0\n\t"                                                                                               \
-                   "global_load_lds_dwordx4 %0, %2" NT "\n\t" SECOND ".Lno_copy%=:"                                           \
-                   :                                                                                                           \
-                   : "v"(offset(i)), "v"(offset(i + 1) - 1024), "s"(src), "s"(to), "s"(uni(go))                                \
-                   : "memory", "scc", "m0")
-    if (kWide) {
-      if (i + 1 < kCopies) PEARL_LATENT_COPY("global_load_lds_dwordx4 %1, %2 offset:1024\n", "");
-      else PEARL_LATENT_COPY("", "");
-    } else {
-      if (i + 1 < kCopies) PEARL_LATENT_COPY("global_load_lds_dwordx4 %1, %2 offset:1024 nt\n", " nt");
-      else PEARL_LATENT_COPY("", " nt");
-    }
-#undef PEARL_LATENT_COPY
-  }
-
-  __device__ static __forceinline__ void page(const char* src, unsigned lds) {
-#pragma unroll
-    for (int i = 0; i < kCopies; i += 2) copy2(i, src, lds, 1);
-  }
-
-  // Zeros in place of the rows from `valid` on.
-  __device__ static __forceinline__ void clear(char* page, int valid) {
-    const int l = threadIdx.x & 63;
-    for (int i = valid * Page::kRowBytes + 16 * l; i < Page::kRot; i += 1024) *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
-    for (int i = Page::kRot + valid * Page::kRotBytes + 16 * l; i < Page::kBytes; i += 1024)
-      *reinterpret_cast<u32x4*>(page + i) = u32x4{0u, 0u, 0u, 0u};
-  }
-};
-
 // What finding a workgroup's share takes.
 struct LatFind {
   long long sum[8], before;                         // a wave each
