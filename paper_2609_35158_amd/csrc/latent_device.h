@@ -71,6 +71,8 @@ template <int DC, int DR, bool kWide> struct LatPage {
   __device__ static __forceinline__ constexpr int rot_f(int r) { return DR == 64 ? (r >> 1) & 7 : 0x78 >> (2 * (r >> 2)) & 3; }
 };
 
+// Copies into LDS take their address from m0, which nothing else in these kernels uses (the compiler does not keep it across an asm).
+//
 // Queries: 16 rows of a cached row's width to a page in LDS, by a wave.  The last of `valid` rows stands for those behind it.
 template <typename Page> __device__ __forceinline__ void lat_queries(const uint16_t* rows, int valid, const char* page) {
   const int l = threadIdx.x & 63;
