@@ -5,6 +5,7 @@
 #include "../../include/pearl_attn.h"
 #include "../../include/pearl_latent.h"
 #include "pearl_internal.h"
+#include "rope_latent.h"
 
 #include <hip/hip_runtime.h>
 

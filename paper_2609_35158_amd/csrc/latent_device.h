@@ -3,6 +3,7 @@
 #pragma once
 
 #include "attn_device.h"
+#include "rope_latent.h"
 
 #include <float.h>
 

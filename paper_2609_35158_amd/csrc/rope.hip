@@ -17,7 +17,7 @@
 // id and rows one after the other: 64 tokens 4.1 to 4.4 us, 32 latent rows 3.8.  Tried: the rows' loads before the place is looked up
 // (registers for fewer waves: 83 -> 110 us).
 
-#include "pearl_internal.h"
+#include "rope_latent.h"
 
 namespace pearl {
 namespace {

@@ -60,6 +60,19 @@ def test_counter_records_are_tied_to_the_kernel_source():
     assert not bench._record_current(e)
 
 
+@pytest.mark.parametrize("name", ["hbm_traffic.json", "kernel_counters.json"])
+def test_committed_records_are_of_the_committed_kernels(name):
+    """A change of a file that the counters are tied to drops them from the benchmark's line: declarations that those kernels do not
+    read belong into another file, and a change of the kernels needs the counters taken again."""
+    entries = json.load(open(os.path.join(ROOT, "profiles", name)))["entries"]
+    assert entries
+    stale = [(e["kernel"], e["workload"]) for e in entries if not bench._record_current(e)]
+    assert not stale, stale
+    for kernel, workload in (("decode_kernel<128>", "qwen3-8b-decode-b64"), ("attn_kernel<128, 1>", "qwen3-8b-prefill-append"),
+                             ("attn_kernel<128, 3>", "mixed-colocated")):
+        assert (bench.measured_traffic if name == "hbm_traffic.json" else bench.kernel_counters)(kernel, workload) is not None
+
+
 def test_oracle_pool_baseline_and_parity():
     pool = bench.OraclePool(2)
     try:
