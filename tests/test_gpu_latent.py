@@ -260,6 +260,29 @@ def test_append(heads, dc, interleaved, norm):
     assert np.array_equal(bits(cache2), keep)
 
 
+@pytest.mark.parametrize("dc", [512, 256])
+def test_append_of_values_that_are_not_finite(dc):
+    """In a normalised latent part an infinity makes the other channels 0 and its own NaN, a NaN all of them; the rotated part and other tokens are
+    what they are without."""
+    dr = {512: 64, 256: 32}[dc]
+    rng = np.random.default_rng(dc)
+    rows = bf16(rng.standard_normal((4, dc + dr))).cuda()
+    q_rope, rope = bf16(rng.standard_normal((4, 3, dr))).cuda(), pa.Rope(dev(inv_freq(dr), np.float32), k_weight=bf16(1 + 0.25 * rng.standard_normal(dc)).cuda())
+    got = []
+    for odd in (False, True):
+        x = rows.clone()
+        if odd:
+            x[1, 77], x[2, 200] = float("-inf"), float("nan")
+        cache, q = pa.latent_cache(1, dc, dr), torch.zeros((4, 3, dc + dr), dtype=torch.bfloat16, device="cuda")
+        pa.latent_append(q_rope, x, rope, q, cache, dev([[0]]), dev([7]), dev([0, 4]), 4, 11)
+        got.append((cache[0], q))
+    want = got[0][0].clone()
+    want[8, :dc], want[9, :dc] = 0, float("nan")
+    want[8, 77] = float("nan")
+    same = torch.eq(got[1][0], want) | (torch.isnan(got[1][0]) & torch.isnan(want))
+    assert bool(same.all()) and torch.equal(got[0][1], got[1][1])
+
+
 def test_turns_and_steps_equal_one_prompt():
     """A prompt in one call, or in turns and single tokens (append, then attention), gives the same cache and the same outputs."""
     rng = np.random.default_rng(2)

@@ -1,0 +1,69 @@
+"""Attention over a paged cache of latent rows: values that are not finite at up to 16 rows a sequence."""
+import numpy as np
+import pytest
+
+import oracle
+from gpu_helpers import bits
+from latent_helpers import LatentCase
+from rope_helpers import bf16
+
+pytestmark = pytest.mark.gpu
+
+
+def put(c, b, key, channels, value):
+    c.cache[int(c.bt[b, key // 16]), key % 16, channels] = bits(bf16([value]))[0]
+
+
+def positive(c, channels):
+    """Queries that make an infinity of these channels one of the same sign in their scores."""
+    q = oracle.bf16_bits_to_f64(bits(c.q))
+    q[..., channels] = np.abs(q[..., channels]) + 0.25
+    c.q = bf16(q)
+
+
+def check_odd(c, out, lse):
+    """Elements are finite where the oracle's are, and within its bounds there."""
+    ref, ref_lse, tol, tol_lse = c.oracle()
+    n = c.owned
+    got, got_lse = oracle.bf16_bits_to_f64(bits(out))[:n], lse.cpu().numpy().astype(np.float64)[:n]
+    for g, r, t in ((got, ref[:n], tol[:n]), (got_lse, ref_lse[:n], tol_lse[:n])):
+        finite = np.isfinite(r)
+        assert np.array_equal(np.isfinite(g), finite), np.argwhere(np.isfinite(g) != finite)[:4]
+        assert (np.abs(g - r)[finite] <= t[finite]).all()
+    return ref[:n]
+
+
+NEW = {4: [4, 3, 1, 4], 1: [16, 9, 2], 16: [1, 1], 5: [3, 2, 0, 3]}
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dc", [512, 256])
+@pytest.mark.parametrize("heads", [4, 1, 5])
+def test_not_finite_at_16_rows(heads, dc, value):
+    """Several channels of several new tokens; tokens before them in the same page, and other sequences, see nothing of it, also where the
+    tile is cut (a context of 2000)."""
+    new = NEW[heads]
+    ctx = [30, 2000, 15, 64][:len(new)]
+    c = LatentCase(heads, dc, ctx, new, seed=heads + dc)
+    channels = [0, 7, 8, 15, 100, 129, dc - 1]
+    positive(c, channels)
+    for b, n in enumerate(new):
+        for i in range(1, n):
+            put(c, b, ctx[b] + i, channels[i % 3::3], value)
+    ref = check_odd(c, *c.prefill())
+    rows = int(np.isnan(ref).any((1, 2)).sum())
+    assert rows == sum(max(n - 1, 0) for n in new)             # as the case is meant
+
+
+@pytest.mark.parametrize("dc", [512, 256])
+def test_notes_of_a_tile_end_with_it(dc):
+    """Many short sequences, several tiles a workgroup, every third with values that are not finite."""
+    rng = np.random.default_rng(dc)
+    new = rng.integers(1, 5, size=700)
+    ctx = rng.integers(0, 60, size=700)
+    c = LatentCase(4, dc, ctx, new, seed=dc)
+    positive(c, list(range(dc)))
+    for b in range(0, 700, 3):
+        if new[b] > 1:
+            put(c, b, int(ctx[b] + new[b]) - 1, [b % dc, (7 * b + 8) % dc], (float("-inf"), float("nan"))[b % 2])
+    check_odd(c, *c.prefill())

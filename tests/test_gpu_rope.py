@@ -143,6 +143,27 @@ def test_values_that_are_not_finite():
     assert float(q[1, 0, 100]) == float("inf")
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_values_that_are_not_finite_in_a_normalised_head(interleaved):
+    """An infinity makes the mean square infinite: the head's other channels are 0, its own NaN, and the one it is paired with if it is rotated; a NaN
+    makes the whole head NaN.  Other heads and tokens are what they are without."""
+    c = RopeCase(4, 2, 128, 64, [5], [3], seed=15, interleaved=interleaved, norm=True)
+    want = run_rows(c)
+    x = c.fused.clone()
+    x[1, 0, 100], x[1, 1, 3], x[1, 2, 9], x[2, 4, 40] = float("inf"), float("-inf"), float("nan"), float("inf")
+    q, k = pa.rope_rows(x[:, :4], x[:, 4:6], c.rope(), dev(c.ctx), dev(c.cu), 3)
+    other = (lambda n: n ^ 1) if interleaved else (lambda n: n + 32 if n < 32 else n - 32)
+    for got, ref, odd in ((q, want[0], {(1, 0): [100], (1, 1): [3, other(3)], (1, 2): list(range(128))}), (k, want[1], {(2, 0): [40, other(40)]})):
+        for t in range(3):
+            for h in range(got.shape[1]):
+                if (t, h) not in odd:
+                    assert torch.equal(got[t, h], ref[t, h])
+                    continue
+                nan = torch.zeros(128, dtype=torch.bool, device="cuda")
+                nan[odd[t, h]] = True
+                assert torch.equal(torch.isnan(got[t, h]), nan) and bool((got[t, h][~nan] == 0).all()), (t, h)
+
+
 def test_step_by_step_equals_prompt():
     """A prompt in one call, in turns and token by token gives the same pools, bit for bit, and decode_append after
     rope_rows the same as kv_append_rope and decode."""
