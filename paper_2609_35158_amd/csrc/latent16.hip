@@ -351,9 +351,9 @@ __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a)
     const int r = few ? kLatWaves * at + w : at;
     if (r >= rows) continue;                        // only where no other wave waits for this one
     auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * job.z + 1 : 2 * (job.z + i * a.group)) * M; };
-    // The first pieces are asked for before their weights are known (one sequence of 42 pieces 19.1 -> 16.2 us with its attention).  Lane k holds the maximum and sum of the wave's piece k; a piece that saw
-    // nothing counts nothing, its outputs may be unwritten.
-    const float2 ml = lane < mine ? reinterpret_cast<const float2*>(a.part_ml)[slot(step * lane + first) + r] : float2{-FLT_MAX, 0.f};
+    // The first pieces are asked for before their weights are known (one sequence of 42 pieces 19.1 -> 16.2 us with its attention).  Lane k holds the maximum and sum of the wave's piece k; a piece without
+    // keys counts nothing, its outputs are unwritten.
+    const float2 ml = lane < mine ? reinterpret_cast<const float2*>(a.part_ml)[slot(step * lane + first) + r] : float2{-FLT_MAX, kNoKeys};
     f32x4 x[kChunk][kC / 4];
     auto load = [&](int k0) {
 #pragma unroll
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(kLatThreads) void latent_merge_kernel(LatentArgs a)
       }
     };
     if (mine > 0) load(0);
-    const bool seen = ml.y != 0.f;
+    const bool seen = ml.y != kNoKeys;
     float top = seen ? ml.x : -FLT_MAX;
     top = xor32_max(xor16_max(top));
 #pragma unroll

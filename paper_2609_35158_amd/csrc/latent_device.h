@@ -16,6 +16,10 @@ constexpr int kLatKeysShift = 6, kLatKeys = 1 << kLatKeysShift;   // of a stage:
 // A row's maximum may lag the true one by so much (log2 units): weights are below 2^8, sums of 2^25 keys below 2^33.
 constexpr float kLag = 8.f;
 
+// In place of a row's sum in a piece of a cut tile that has no keys.  (The sum of a piece whose scores are all minus infinity is 0, its outputs are 0 or, in
+// channels with values that are not finite, NaN.)
+constexpr float kNoKeys = -1.f;
+
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ void barrier_lds() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -246,9 +250,9 @@ struct LatWork {
     j0 = starts ? 0 : min(plan.stage_at(lo - t0, all_stages), stages);
     j1 = ends ? stages : min(plan.stage_at(hi - t0, all_stages), stages);
     if (starts && !ends) job = int4{(int)row0, n_rows, index, cut.of(t1 - 1) - share + 1};
-    // a piece of a cut tile without keys
+    // a piece of a cut tile without keys, whose outputs stay unwritten
     if (j0 >= j1 && !(starts && ends) && threadIdx.x < M)
-      reinterpret_cast<float2*>(args_anew()->part_ml)[(size_t)slot * M + threadIdx.x] = float2{-FLT_MAX, 0.f};
+      reinterpret_cast<float2*>(args_anew()->part_ml)[(size_t)slot * M + threadIdx.x] = float2{-FLT_MAX, kNoKeys};
   }
   // Whether there is a tile after this one.
   __device__ __forceinline__ bool next(const LatentArgs& a) {

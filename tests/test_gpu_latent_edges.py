@@ -1,4 +1,5 @@
-"""Attention over a paged cache of latent rows: values that are not finite at up to 16 rows a sequence."""
+"""Attention over a paged cache of latent rows: values that are not finite at up to 16 rows a sequence and where all scores of a cut tile's
+piece are minus infinity."""
 import numpy as np
 import pytest
 
@@ -67,3 +68,17 @@ def test_notes_of_a_tile_end_with_it(dc):
         if new[b] > 1:
             put(c, b, int(ctx[b] + new[b]) - 1, [b % dc, (7 * b + 8) % dc], (float("-inf"), float("nan"))[b % 2])
     check_odd(c, *c.prefill())
+
+
+@pytest.mark.parametrize("heads,dc", [(16, 512), (16, 256), (64, 512), (64, 256)])
+def test_pieces_of_scores_of_minus_infinity(heads, dc):
+    """A cut tile's piece whose scores are all minus infinity has weight 0, and its channels that are not finite are NaN in the output
+    (0 times infinity), as in a tile that is not cut."""
+    c = LatentCase(heads, dc, [4000, 200], [1, 1], seed=heads)
+    positive(c, [5, 40, dc])
+    for key in range(1500):
+        put(c, 0, key, dc, float("-inf"))                      # of the rotated part
+    put(c, 0, 100, 5, float("-inf"))
+    put(c, 0, 1100, 40, float("-inf"))
+    ref = check_odd(c, *c.decode())
+    assert np.isnan(ref[0][:, [5, 40]]).all() and np.isnan(ref).sum() == 2 * heads
