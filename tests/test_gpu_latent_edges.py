@@ -1,11 +1,13 @@
 """Attention over a paged cache of latent rows: values that are not finite at up to 16 rows a sequence and where all scores of a cut tile's
-piece are minus infinity."""
+piece are minus infinity, and batches with rows behind the last sequence."""
 import numpy as np
 import pytest
+import torch
 
 import oracle
+import paper_2609_35158_amd as pa
 from gpu_helpers import bits
-from latent_helpers import LatentCase
+from latent_helpers import LatentCase, check
 from rope_helpers import bf16
 
 pytestmark = pytest.mark.gpu
@@ -82,3 +84,16 @@ def test_pieces_of_scores_of_minus_infinity(heads, dc):
     put(c, 0, 1100, 40, float("-inf"))
     ref = check_odd(c, *c.decode())
     assert np.isnan(ref[0][:, [5, 40]]).all() and np.isnan(ref).sum() == 2 * heads
+
+
+@pytest.mark.parametrize("heads,dc,ctx,new,spare", [(16, 512, [3000, 40], [1, 1], 62), (4, 512, [900, 17, 5], [4, 1, 3], 200),
+                                                    (1, 256, [5000], [16], 1000), (16, 512, [700, 1200], [4, 3], 500),
+                                                    (128, 512, [2000, 30, 77], [1, 1, 1], 61)])
+def test_rows_behind_the_last_sequence(heads, dc, ctx, new, spare):
+    """They take no part: the call's outputs are those without them, bit for bit."""
+    c = LatentCase(heads, dc, ctx, new, seed=heads, spare=spare)
+    out, lse = c.prefill()
+    check(c, out, lse)
+    q, cache, bt, ctx_d, cu = c.args()
+    alone = pa.latent_prefill_append(q[:c.owned].contiguous(), cache, bt, ctx_d, cu, c.max_q, c.max_kv, c.scale, return_lse=True)
+    assert torch.equal(out[:c.owned], alone[0]) and torch.equal(lse[:c.owned], alone[1])
