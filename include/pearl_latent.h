@@ -16,6 +16,11 @@
  *          block_table[b*bt_stride + p/page_size].  Any bytes are valid in rows that no attended position owns.
  *   q: bf16 [total_q][num_q_heads][latent_dim + rope_dim]; out: bf16 [total_q][num_q_heads][latent_dim];
  *   lse: fp32 [total_q][num_q_heads] or NULL.
+ * Scores, softmax state and sums are held in 32 bits; weights enter the second product in bf16, outputs are rounded to bf16.
+ * A row of the cache with infinite or NaN channels reaches only the tokens that attend to it.  A token whose score of the row is NaN or
+ * plus infinity has NaN in all channels and in lse.  Where the score is minus infinity the row has weight 0: the output is NaN in those latent channels
+ * that are infinite in the row (in none, if all of them are in its rotated part) and lse is without it.  Where all of a token's scores are minus
+ * infinity its output is NaN and lse minus infinity.
  * Supported: (latent_dim, rope_dim) (512, 64) and (256, 32); page_size 16; 1 .. 128 query heads;
  * max_q_len <= 2^21, max_kv_len <= 2^25.
  */
@@ -63,7 +68,7 @@ size_t pearl_latent_workspace_bytes(const pearl_latent_shape* shape, const pearl
 /*
  * Batched single-token decode: seqs->cu_q_lens must be NULL; row b of q and out is sequence b's new token at position
  * ctx_lens[b], whose row the cache already holds (pearl_latent_append first, on the same stream).
- * Contexts are cut into shares that run in parallel and are joined by log-sum-exp.  Weights enter the second product in bf16.
+ * Contexts are cut into shares that run in parallel and are joined by log-sum-exp.
  * out must not overlap q or the cache.
  */
 pearl_status pearl_attn_latent_decode(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const void* q,
@@ -73,8 +78,10 @@ pearl_status pearl_attn_latent_decode(const pearl_latent_shape* shape, const pea
 /*
  * Prefill-append: every new token of every sequence attends to its context and causally to the new ones, whose rows the
  * cache already holds.  Sequences without new tokens are skipped; rows behind the last sequence are left as they
- * were.  A batch of single tokens, or of a few each (drafted tokens that are verified), can take this call too.
- * A row of the cache with an infinite or NaN channel makes outputs infinite or NaN in the tokens that attend to it only.
+ * were.  A batch of single tokens, or of a few each (drafted tokens that are verified), can take this call too.  A colocated batch, of large turns
+ * and of single tokens on long contexts, is better served by two calls, pearl_attn_latent_decode for the latter: the cut goes by the batch's longest
+ * and average turn (63 single tokens on 2K to 16K and a turn of 2000 on 9K, 16 heads: 901 us in one call, 746 in two; 56 single tokens and 8 turns of 1000: 1840
+ * and 1504; with 128 heads 3% apart).
  */
 pearl_status pearl_attn_latent_prefill_append(const pearl_latent_shape* shape, const pearl_seq_desc* seqs, const void* q,
                                               const void* cache, float softmax_scale, void* out, float* lse, void* workspace,

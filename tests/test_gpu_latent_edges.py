@@ -58,6 +58,35 @@ def test_not_finite_at_16_rows(heads, dc, value):
     assert rows == sum(max(n - 1, 0) for n in new)             # as the case is meant
 
 
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("heads,dc", [(16, 512), (40, 512), (128, 512), (20, 256), (7, 256)])
+def test_not_finite_at_64_rows(heads, dc, value):
+    ctx, new = [30, 1500, 5, 64], [20, 7, 0, 40]
+    c = LatentCase(heads, dc, ctx, new, seed=heads + dc)
+    channels = [1, 8, 17, 64, 130, dc - 1]
+    positive(c, channels)
+    for b, n in enumerate(new):
+        for i in range(3, n, 5):
+            put(c, b, ctx[b] + i, channels[i % 3::3], value)
+    ref = check_odd(c, *c.prefill())
+    assert int(np.isnan(ref).any((1, 2)).sum()) == sum(max(n - 3, 0) for n in new)
+
+
+@pytest.mark.parametrize("ctx", [20, 5000])
+@pytest.mark.parametrize("heads,dc", [(16, 512), (64, 512), (4, 256), (30, 256)])
+def test_all_scores_minus_infinity(heads, dc, ctx):
+    """NaN, as 0 / 0 is, and the logarithm of 0; in that sequence alone."""
+    c = LatentCase(heads, dc, [ctx, 100], [1, 1], seed=heads)
+    positive(c, [dc + 3])
+    for key in range(ctx + 1):
+        put(c, 0, key, dc + 3, float("-inf"))
+    out, lse = c.decode()
+    assert bool(torch.isnan(out[0]).all()) and bool((lse[0] == float("-inf")).all())
+    ref, ref_lse, tol, tol_lse = c.oracle()
+    got = oracle.bf16_bits_to_f64(bits(out))
+    assert (np.abs(got - ref) <= tol)[1].all() and (np.abs(lse.cpu().numpy() - ref_lse) <= tol_lse)[1].all()
+
+
 @pytest.mark.parametrize("dc", [512, 256])
 def test_notes_of_a_tile_end_with_it(dc):
     """Many short sequences, several tiles a workgroup, every third with values that are not finite."""
