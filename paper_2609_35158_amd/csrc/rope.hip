@@ -193,8 +193,8 @@ template <int D> struct RopeLane {
 template <int D, bool kToPool>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs r, RopeSeqs seqs, RopeRows a, int waves) {
   using Lane = RopeLane<D>;
-  // groups asked for at once: 2 leave registers for more waves (64 channels: 14.5K tokens of 16 + 8 heads 20.3 us, with 4 21.1; 128 channels: 19.4K
-  // tokens of 32 + 4 + 4 heads 89.4, with 4 88.4)
+  // groups asked for at once: 2 leave registers for more waves (64 channels, in a graph: 14.5K tokens of 16 + 8 heads 22.4 us, with 4 23.7; 128 channels: 19.4K
+  // tokens of 32 + 4 + 4 heads 85.7, with 4 85.2)
   constexpr int kUnroll = D == 64 ? 2 : 4;
   const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * kRopeWaves + (int)(threadIdx.x >> 6));
   const int row = id / waves, w = id - row * waves;
